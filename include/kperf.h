@@ -416,6 +416,111 @@ kp_status kp_attn_instrumented(const void* Q, const void* K, const void* V, void
                                int D, int causal, float scale, uint32_t region_mask, void* trace_buf,
                                size_t trace_cap, void* stream);
 
+/* ---- attention with windows, caches and gradients ----------------------------------------------
+ *
+ * The attentions that models train and serve with, as further targets.  Everywhere below, query token
+ * i of n_q stands over n_k keys at position p = n_k - n_q + i and sees key j where
+ *     j <= p  and  (window == 0  or  p - j < window  or  j < sinks)
+ * (window 0: all keys up to p; sinks: first keys that stay visible).  With Hq query heads and Hkv heads
+ * of keys and values, Hq a multiple of Hkv, query head h reads head h / (Hq / Hkv).  Softmax, its sums
+ * and all accumulation are in fp32; results are rounded once, to the inputs' type.  A token that sees no
+ * key (p < 0), or only scores of -inf, gives o = 0 and lse = -inf.  What a token does not see has no
+ * influence on its result, not even as an infinity or a NaN.
+ *
+ * kp_heads names a tensor [sequence, head, token, D] by its first element and three strides, in
+ * elements; the D values of a row are contiguous and 16-byte aligned (so are all strides: multiples of 8).
+ * Strides of inputs may be 0 (broadcast); rows of an output must not overlap.
+ *   type        KP_BF16 or KP_FP16: the type of q, k, v, o and of all gradients
+ *   D           64 or 128
+ *   scale       positive and finite
+ *   lse         log of the sum of exp(score) per row, natural, fp32, contiguous; may be NULL
+ *   workspace   device, 16-byte aligned, at least the bytes that the operator's _bytes call names for the
+ *               same sizes (which may be 0: then workspace may be NULL); its contents need not be kept
+ * KP_ERR_UNSUPPORTED_SHAPE: D, strides of 2^24 elements or more between tokens, 2^30 or more tokens,
+ * more workgroups than a launch takes.  All calls are asynchronous on `stream` and can be captured.
+ */
+enum { KP_BF16 = 0, KP_FP16 = 1 };
+
+typedef struct {
+  void* at;        /* device, element [0][0][0][0] */
+  int64_t seq;     /* strides in elements */
+  int64_t head;
+  int64_t token;
+} kp_heads;
+
+/*
+ * o = softmax(scale q k^T, visible keys) v for B sequences of Sq query tokens over Sk keys (any lengths from
+ * 1 on, Sq > Sk included); lse [B, Hq, Sq].
+ */
+size_t kp_attn_window_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks);
+kp_status kp_attn_window(const kp_heads* q, const kp_heads* k, const kp_heads* v, const kp_heads* o, float* lse,
+                         int B, int Hq, int Hkv, int Sq, int Sk, int D, int type, int window, int sinks,
+                         float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of kp_attn_window: from its o and lse and the gradient d_o of o, with
+ *   delta_i = d_o_i . o_i,  P_ij = exp(scale q_i . k_j - lse_i),  dS_ij = P_ij (d_o_i . v_j - delta_i):
+ *   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij d_o_i,
+ * the latter two summed over the query heads that read the head.  Sums are taken in a fixed order: the same
+ * inputs give the same bits.  lse as kp_attn_window wrote it (not NULL).  All of dq, dk, dv are written.
+ */
+size_t kp_attn_window_grad_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks);
+kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, const kp_heads* v, const kp_heads* o,
+                              const float* lse, const kp_heads* d_o, const kp_heads* dq, const kp_heads* dk,
+                              const kp_heads* dv, int B, int Hq, int Hkv, int Sq, int Sk, int D, int type,
+                              int window, int sinks, float scale, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/*
+ * A cache of keys and values in pages: either half is [n_pages, Hkv, page, D], contiguous, page a power of two.
+ * Slot s of the cache is token s % page of page s / page.  cache_type:
+ *   KP_CACHE_SAME  values of `type`
+ *   KP_CACHE_E4M3  8-bit codes (4 exponent bits of bias 7, 3 mantissa bits, no infinities) and, in
+ *                  k_exp / v_exp [n_pages, Hkv, page], one exponent byte E per row of D: a code c stands for
+ *                  c 2^(E - 127).  A row is written with the least E for which its largest finite magnitude is
+ *                  at most 448 2^(E - 127) (E = 127 for a row of zeros, never below 1), each value rounded to
+ *                  nearest even; what is not finite becomes the code of NaN.  A power of two costs a
+ *                  floating-point code no precision, and makes writing and reading back exact but for that rounding.
+ */
+enum { KP_CACHE_SAME = 0, KP_CACHE_E4M3 = 1 };
+
+typedef struct {
+  void* k;         /* device, 16-byte aligned */
+  void* v;
+  uint8_t* k_exp;  /* device; NULL with KP_CACHE_SAME */
+  uint8_t* v_exp;
+  int n_pages, Hkv, page, D, type, cache_type;
+} kp_cache;
+
+/*
+ * Writes T new tokens' keys and values (kp_heads with seq ignored: [head, token, D]) to the slots
+ * slots[T] (device, int64).  Slots below 0 are skipped, and so are slots past the cache's end.  If a slot is named
+ * twice, one of the tokens' rows is left in it, unspecified which.  T = 0 is allowed.
+ */
+kp_status kp_cache_write(const kp_heads* k, const kp_heads* v, const int64_t* slots, int T, const kp_cache* cache,
+                         void* stream);
+
+/*
+ * Reads sequences back in the cache's `type`: key number t of sequence s lies in page block_table[s][t / page] and goes
+ * to token starts[s] + t of k and v, for starts[s] + t < starts[s + 1] (starts: device, n_seqs + 1 non-decreasing numbers
+ * from 0 to T; block_table: device, [n_seqs, table_width]).  Where the table is too narrow or names no page of the cache
+ * the row is zeros; nothing is read outside the cache or written outside the T tokens.
+ */
+kp_status kp_cache_read(const kp_cache* cache, const int32_t* block_table, int table_width, const int32_t* starts,
+                        int n_seqs, int T, const kp_heads* k, const kp_heads* v, void* stream);
+
+/*
+ * Attention of T new tokens over a cache that already holds them: sequence s has the query tokens starts[s] ..
+ * starts[s + 1] - 1 (device, n_seqs + 1 non-decreasing numbers from 0 to T; none, one or many per sequence) and lens[s] keys
+ * (device, the new ones included; at most table_width * page count).  q, o: kp_heads with seq ignored; lse [Hq, T].  Keys whose
+ * block_table entry names no page of the cache are not visible; table entries past a sequence's keys are not read.
+ */
+size_t kp_attn_paged_bytes(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int window, int sinks);
+kp_status kp_attn_paged(const kp_heads* q, const kp_cache* cache, const int32_t* block_table, int table_width,
+                        const int32_t* lens, const int32_t* starts, const kp_heads* o, float* lse, int T, int n_seqs,
+                        int Hq, int window, int sinks, float scale, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
 /*
  * Timer calibration (Sec. 5.4 "Cycle-level Overhead": cost of one record; Sec. 4.3: that
  * constant is subtracted at replay).  Launches n_wg workgroups of `waves` waves, one workgroup

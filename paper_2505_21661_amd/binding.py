@@ -29,6 +29,8 @@ KP_MASK_COLLAB = 1 << 27      # all lanes store a record; hardware ids of the wa
 KP_MASK_UNFENCED = 1 << 26    # with KP_MASK_PHASES and no region: the staged K step without scheduling fences
 KP_FLAG_REALTIME = 2
 KP_FLAG_HW_IDS = 4
+KP_BF16, KP_FP16 = 0, 1
+KP_CACHE_SAME, KP_CACHE_E4M3 = 0, 1
 
 
 class KperfError(RuntimeError):
@@ -43,6 +45,16 @@ class kp_trace_hdr(ctypes.Structure):
         ("waves_per_wg", ctypes.c_uint32), ("n_regions", ctypes.c_uint32), ("cap_wave", ctypes.c_uint32),
         ("rec_cost", ctypes.c_uint32), ("flags", ctypes.c_uint32), ("pad", ctypes.c_uint32 * 8),
     ]
+
+
+class kp_heads(ctypes.Structure):
+    _fields_ = [("at", ctypes.c_void_p), ("seq", ctypes.c_int64), ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
+
+
+class kp_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int), ("Hkv", ctypes.c_int), ("page", ctypes.c_int), ("D", ctypes.c_int),
+                ("type", ctypes.c_int), ("cache_type", ctypes.c_int)]
 
 
 _lib = None
@@ -112,7 +124,13 @@ def lib() -> ctypes.CDLL:
 def _optional(L):
     vp, sz, ci, u32, fl = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_uint32, ctypes.c_float
     ip = ctypes.POINTER(ctypes.c_int)
+    hp, cp = ctypes.POINTER(kp_heads), ctypes.POINTER(kp_cache)
     sigs = {
+        "kp_attn_window": [hp, hp, hp, hp, vp, ci, ci, ci, ci, ci, ci, ci, ci, ci, fl, vp, sz, vp],
+        "kp_attn_window_grad": [hp, hp, hp, hp, vp, hp, hp, hp, hp, ci, ci, ci, ci, ci, ci, ci, ci, ci, fl, vp, sz, vp],
+        "kp_cache_write": [hp, hp, vp, ci, cp, vp],
+        "kp_cache_read": [cp, vp, ci, vp, ci, ci, hp, hp, vp],
+        "kp_attn_paged": [hp, cp, vp, ci, vp, vp, hp, vp, ci, ci, ci, ci, ci, fl, vp, sz, vp],
         "kp_gemm_launch_shape": [ci, ci, ci, ip, ip, ip],
         "kp_gemm_instrumented": [vp, vp, vp, ci, ci, ci, u32, vp, sz, vp],
         "kp_attn_launch_shape": [ci, ci, ci, ci, ip, ip, ip],
@@ -124,6 +142,10 @@ def _optional(L):
             f = getattr(L, name)
             f.restype = ci
             f.argtypes = args
+    for name, n in (("kp_attn_window_bytes", 8), ("kp_attn_window_grad_bytes", 8), ("kp_attn_paged_bytes", 9)):
+        if hasattr(L, name):
+            getattr(L, name).restype = sz
+            getattr(L, name).argtypes = [ci] * n
 
 
 def _check(status: int):
@@ -357,6 +379,141 @@ def kp_attn_instrumented(Q, K, V, O, B: int, H: int, S: int, D: int, causal: boo
 def kp_calibrate(cycles, n_wg: int, waves: int, mode: int, trace_buf, trace_cap: int, stream=None) -> None:
     arr = (ctypes.c_uint32 * len(cycles))(*[int(c) for c in cycles])
     _check(lib().kp_calibrate(arr, len(cycles), n_wg, waves, mode, _ptr(trace_buf), trace_cap, _stream(stream)))
+
+
+# ---- attention with windows, caches and gradients --------------------------------------------------
+# Tensors of heads keep their strides: [B, H, S, D] in any order in memory with D innermost (a transposed view of
+# [B, S, H, D], a slice of a fused projection), or [T, H, D] where there is no batch.
+
+
+def _type_code(dtype) -> int:
+    name = str(dtype)
+    if name == "torch.bfloat16":
+        return KP_BF16
+    if name == "torch.float16":
+        return KP_FP16
+    raise ValueError(f"tensors must be bfloat16 or float16, not {name}")
+
+
+def _heads(name: str, t, shape, dtype):
+    """kp_heads of a [B, H, S, D] or (three sizes in `shape`) [T, H, D] tensor."""
+    if not t.is_cuda:
+        raise ValueError("libkperf takes device memory: tensor must be on the GPU")
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} must be {list(shape)} of {dtype}, not {list(t.shape)} of {t.dtype}")
+    st = t.stride()
+    if st[-1] != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    if len(st) == 4:
+        return ctypes.byref(kp_heads(t.data_ptr(), st[0], st[1], st[2]))
+    return ctypes.byref(kp_heads(t.data_ptr(), 0, st[1], st[0]))
+
+
+def _flat(name: str, t, dtype: str, shape=None):
+    """Device pointer of a contiguous tensor of a type and (where given) a shape."""
+    if str(t.dtype) != dtype or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must be {'' if shape is None else str(list(shape)) + ' '}of {dtype}, not {list(t.shape)} of {t.dtype}")
+    return _ptr(t)
+
+
+def _workspace(workspace) -> tuple[int, int]:
+    return (0, 0) if workspace is None else (_ptr(workspace), workspace.numel() * workspace.element_size())
+
+
+def _window_sizes(q, k):
+    B, Hq, Sq, D = q.shape
+    return B, Hq, k.shape[1], Sq, k.shape[2], D
+
+
+def kp_attn_window_bytes(q, k, window: int, sinks: int) -> int:
+    """Bytes of workspace that kp_attn_window takes for q [B, Hq, Sq, D] and k [B, Hkv, Sk, D]."""
+    return int(lib().kp_attn_window_bytes(*_window_sizes(q, k), window, sinks))
+
+
+def kp_attn_window(q, k, v, o, lse, window: int, sinks: int, scale: float, workspace=None, stream=None) -> None:
+    """o = softmax(scale q k^T over the visible keys) v; q, o [B, Hq, Sq, D], k, v [B, Hkv, Sk, D] (any strides with D
+    innermost), lse [B, Hq, Sq] float32 or None.  A token at position p = Sk - Sq + i sees keys j <= p with p - j < window
+    (window 0: all) or j < sinks."""
+    dtype, kv = q.dtype, k.shape
+    B, Hq, Hkv, Sq, Sk, D = _window_sizes(q, k)
+    ws, n = _workspace(workspace)
+    _check(lib().kp_attn_window(
+        _heads("q", q, q.shape, dtype), _heads("k", k, (B, Hkv, Sk, D), dtype), _heads("v", v, kv, dtype),
+        _heads("o", o, q.shape, dtype), 0 if lse is None else _flat("lse", lse, "torch.float32", (B, Hq, Sq)),
+        B, Hq, Hkv, Sq, Sk, D, _type_code(dtype), window, sinks, scale, ws, n, _stream(stream)))
+
+
+def kp_attn_window_grad_bytes(q, k, window: int, sinks: int) -> int:
+    return int(lib().kp_attn_window_grad_bytes(*_window_sizes(q, k), window, sinks))
+
+
+def kp_attn_window_grad(q, k, v, o, lse, d_o, dq, dk, dv, window: int, sinks: int, scale: float, workspace,
+                        stream=None) -> None:
+    """Gradients dq, dk, dv of kp_attn_window from its o and lse and the gradient d_o of o."""
+    dtype, qs, ks = q.dtype, q.shape, k.shape
+    B, Hq, Hkv, Sq, Sk, D = _window_sizes(q, k)
+    ws, n = _workspace(workspace)
+    _check(lib().kp_attn_window_grad(
+        _heads("q", q, qs, dtype), _heads("k", k, (B, Hkv, Sk, D), dtype), _heads("v", v, ks, dtype),
+        _heads("o", o, qs, dtype), _flat("lse", lse, "torch.float32", (B, Hq, Sq)), _heads("d_o", d_o, qs, dtype),
+        _heads("dq", dq, qs, dtype), _heads("dk", dk, ks, dtype), _heads("dv", dv, ks, dtype),
+        B, Hq, Hkv, Sq, Sk, D, _type_code(dtype), window, sinks, scale, ws, n, _stream(stream)))
+
+
+def _cache_of(k_cache, v_cache, k_exp, v_exp, dtype):
+    """kp_cache of two halves [n_pages, Hkv, page, D]: of `dtype`, or float8_e4m3fn with exponent bytes."""
+    n_pages, Hkv, page, D = k_cache.shape
+    e4m3 = str(k_cache.dtype) == "torch.float8_e4m3fn"
+    kind = str(k_cache.dtype) if e4m3 else str(dtype)
+    exps = [0, 0]
+    if e4m3:
+        exps = [_flat(n, e, "torch.uint8", (n_pages, Hkv, page)) for n, e in (("k_exp", k_exp), ("v_exp", v_exp))]
+    return ctypes.byref(kp_cache(_flat("k_cache", k_cache, kind), _flat("v_cache", v_cache, kind, k_cache.shape), *exps,
+                                 n_pages, Hkv, page, D, _type_code(dtype), int(e4m3)))
+
+
+def kp_cache_write(k, v, slots, k_cache, v_cache, k_exp=None, v_exp=None, stream=None) -> None:
+    """New rows k, v [T, Hkv, D] into slots [T] int64 (negative: skipped) of the cache [n_pages, Hkv, page, D], as they are
+    or, into a float8_e4m3fn cache with exponents [n_pages, Hkv, page] uint8, quantised row by row."""
+    T, (_, Hkv, _, D) = k.shape[0], k_cache.shape
+    _check(lib().kp_cache_write(_heads("k", k, (T, Hkv, D), k.dtype), _heads("v", v, (T, Hkv, D), k.dtype),
+                                _flat("slots", slots, "torch.int64", (T,)), T,
+                                _cache_of(k_cache, v_cache, k_exp, v_exp, k.dtype), _stream(stream)))
+
+
+def kp_cache_read(k_cache, v_cache, k_exp, v_exp, block_table, starts, k, v, stream=None) -> None:
+    """Whole sequences out of the cache: key t of sequence s (block_table [n, width] int32) goes to row starts[s] + t of
+    k, v [T, Hkv, D], up to starts[s + 1] (starts [n + 1] int32)."""
+    T, (_, Hkv, _, D) = k.shape[0], k_cache.shape
+    n, width = block_table.shape
+    _check(lib().kp_cache_read(_cache_of(k_cache, v_cache, k_exp, v_exp, k.dtype),
+                               _flat("block_table", block_table, "torch.int32"), width,
+                               _flat("starts", starts, "torch.int32", (n + 1,)), n, T,
+                               _heads("k", k, (T, Hkv, D), k.dtype), _heads("v", v, (T, Hkv, D), k.dtype), _stream(stream)))
+
+
+def kp_attn_paged_bytes(q, k_cache, block_table, window: int, sinks: int) -> int:
+    """Bytes of workspace that kp_attn_paged takes for q [T, Hq, D]."""
+    T, Hq, D = q.shape
+    n, width = block_table.shape
+    return int(lib().kp_attn_paged_bytes(T, n, Hq, k_cache.shape[1], D, width, k_cache.shape[2], window, sinks))
+
+
+def kp_attn_paged(q, k_cache, v_cache, k_exp, v_exp, block_table, lens, starts, o, lse, window: int, sinks: int,
+                  scale: float, workspace=None, stream=None) -> None:
+    """Attention of new tokens q [T, Hq, D] over a cache that holds them: sequence s has the tokens starts[s] ..
+    starts[s + 1] - 1 and lens[s] keys, found through block_table [n, width] int32; o [T, Hq, D], lse [Hq, T] or None."""
+    T, Hq, D = q.shape
+    n, width = block_table.shape
+    if D != k_cache.shape[3]:
+        raise ValueError("q and the cache must have the same D")
+    ws, nbytes = _workspace(workspace)
+    _check(lib().kp_attn_paged(
+        _heads("q", q, q.shape, q.dtype), _cache_of(k_cache, v_cache, k_exp, v_exp, q.dtype),
+        _flat("block_table", block_table, "torch.int32"), width, _flat("lens", lens, "torch.int32", (n,)),
+        _flat("starts", starts, "torch.int32", (n + 1,)), _heads("o", o, q.shape, q.dtype),
+        0 if lse is None else _flat("lse", lse, "torch.float32", (Hq, T)), T, n, Hq, window, sinks, scale, ws, nbytes,
+        _stream(stream)))
 
 
 # ---- views of the statistics block (layout documented in include/kperf.h) ------------------------

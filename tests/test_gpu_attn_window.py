@@ -1,0 +1,216 @@
+"""Attention with a sliding window and sinks, forward and gradient, against its definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from tests.attn_util import assert_lse, assert_within, forward, gradients, o_bound
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.bfloat16, torch.float16]
+
+
+@pytest.fixture(scope="module")
+def kp():
+    import paper_2505_21661_amd as kp
+
+    return kp
+
+
+def heads(gen, b, h, n, d, dtype, layout="bhsd"):
+    if layout == "bhsd":
+        return torch.randn(b, h, n, d, device="cuda", generator=gen).to(dtype)
+    return torch.randn(b, n, h, d, device="cuda", generator=gen).to(dtype).transpose(1, 2)
+
+
+def attend(kp, q, k, v, window, sinks, scale, o=None):
+    o = torch.full_like(q, math.nan) if o is None else o
+    lse = torch.full(q.shape[:3], math.nan, device="cuda")
+    ws = torch.full((kp.kp_attn_window_bytes(q, k, window, sinks),), 0xFF, dtype=torch.uint8, device="cuda")
+    kp.kp_attn_window(q, k, v, o, lse, window, sinks, scale, ws if ws.numel() else None)
+    return o, lse
+
+
+def grads(kp, q, k, v, o, lse, d_o, window, sinks, scale):
+    out = [torch.full(x.shape, math.nan, dtype=x.dtype, device="cuda") for x in (q, k, v)]
+    ws = torch.full((kp.kp_attn_window_grad_bytes(q, k, window, sinks),), 0xFF, dtype=torch.uint8, device="cuda")
+    kp.kp_attn_window_grad(q, k, v, o, lse, d_o, *out, window, sinks, scale, ws)
+    return out
+
+
+# (B, Hq, Hkv, Sq, Sk, window, sinks): one token, odd lengths around the tiles, more queries than keys (rows that see
+# nothing), windows of one key and of more than there are, sinks inside, at and past the window's edge
+SIZES = [
+    (1, 1, 1, 1, 1, 0, 0), (1, 2, 1, 1, 65, 0, 0), (2, 4, 2, 1, 700, 100, 4), (1, 8, 1, 1, 3001, 0, 0), (3, 16, 1, 1, 257, 64, 70),
+    (1, 17, 1, 1, 130, 0, 0), (1, 3, 3, 63, 63, 0, 0), (2, 6, 2, 64, 64, 1, 0), (1, 4, 2, 65, 65, 1, 1), (1, 7, 1, 129, 129, 33, 3),
+    (1, 2, 2, 200, 200, 64, 0), (1, 4, 1, 257, 257, 100, 64), (1, 4, 4, 300, 300, 50, 130), (1, 2, 1, 100, 37, 0, 0), (2, 4, 2, 90, 20, 5, 2),
+    (1, 4, 2, 33, 500, 0, 0), (1, 4, 2, 33, 500, 70, 9), (1, 6, 2, 5, 1025, 300, 5), (1, 2, 1, 511, 640, 4096, 3), (1, 1, 1, 1000, 1000, 128, 500),
+    (1, 2, 2, 2, 2, 0, 0), (2, 2, 1, 384, 384, 0, 0), (1, 8, 8, 128, 128, 0, 7),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", SIZES)
+def test_forward_and_gradient(kp, size, d, dtype):
+    b, hq, hkv, n_q, n_k, window, sinks = size
+    gen = torch.Generator(device="cuda").manual_seed(hash(size) % 1000 + d)
+    layout = "bshd" if n_q % 2 else "bhsd"
+    q, k, v, d_o = (heads(gen, b, h, n, d, dtype, layout) for h, n in ((hq, n_q), (hkv, n_k), (hkv, n_k), (hq, n_q)))
+    scale = 1.5 / math.sqrt(d)
+    o, lse = attend(kp, q, k, v, window, sinks, scale)
+    p, want, want_lse = forward(q, k, v, window, sinks, scale)
+    assert_within(o, want, o_bound(p, v, dtype), "o")
+    assert_lse(lse, want_lse)
+    for name, got, (want, bound) in zip(("dq", "dk", "dv"), grads(kp, q, k, v, o, lse, d_o, window, sinks, scale),
+                                        gradients(q, k, v, d_o, window, sinks, scale, dtype)):
+        assert_within(got, want, bound, name)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shift", [-14, -4, 6])
+def test_gradients_of_other_magnitudes(kp, dtype, shift):
+    """Losses scaled by a power of two scale the gradients, down to what the type's own range leaves of them."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    q, k, v, d_o = (heads(gen, 1, h, 300, 64, dtype) for h in (4, 2, 2, 4))
+    d_o = (d_o.float() * 2.0 ** shift).to(dtype)
+    o, lse = attend(kp, q, k, v, 90, 3, 0.125)
+    tiny = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps  # half a step of the smallest results, twice
+    for got, (want, bound) in zip(grads(kp, q, k, v, o, lse, d_o, 90, 3, 0.125), gradients(q, k, v, d_o, 90, 3, 0.125, dtype)):
+        assert_within(got, want, bound + tiny)
+
+
+def test_peaked_scores(kp):
+    """Scores that grow along the keys move the softmax's reference in every tile; large scores leave one key."""
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    q, k, v = (heads(gen, 1, 2, 400, 64, torch.bfloat16) for _ in range(3))
+    q = q.abs()
+    k = (k.abs() * torch.linspace(-3, 3, 400, device="cuda")[:, None]).to(torch.bfloat16)
+    for scale in (0.02, 0.3):
+        for window in (0, 77):
+            o, lse = attend(kp, q, k, v, window, 2, scale)
+            p, want, want_lse = forward(q, k, v, window, 2, scale)
+            s = torch.matmul(q.double().abs(), k.double().abs().transpose(2, 3)).amax() * scale
+            bound = o_bound(p, v, torch.bfloat16) + 2 * float(s) * 2.0 ** -20 * torch.matmul(p, v.double().abs())
+            assert_within(o, want, bound)
+            assert bool(((lse.double() - want_lse).abs() <= 2.0 ** -18 * float(s)).all())
+
+
+def test_gradient_against_differences(kp):
+    """The gradient along random directions against central differences of the definition in 64 bits."""
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    dtype, window, sinks, scale = torch.float16, 20, 3, 0.2
+    q, k, v, d_o = (heads(gen, 1, h, 70, 64, dtype) for h in (4, 2, 2, 4))
+    o, lse = attend(kp, q, k, v, window, sinks, scale)
+    got = grads(kp, q, k, v, o, lse, d_o, window, sinks, scale)
+    bounds = gradients(q, k, v, d_o, window, sinks, scale, dtype)
+    loss = lambda *x: float((forward(*x, window, sinks, scale)[1] * d_o.double()).sum())  # noqa: E731
+    x = [t.double() for t in (q, k, v)]
+    for i in range(3):
+        way = torch.randn(x[i].shape, dtype=torch.float64, device="cuda", generator=gen)
+        h = 1e-5
+        up, down = list(x), list(x)
+        up[i], down[i] = x[i] + h * way, x[i] - h * way
+        slope = (loss(*up) - loss(*down)) / (2 * h)
+        allowed = float((bounds[i][1] * way.abs()).sum()) + 1e-5 * abs(slope) + 1e-5
+        assert abs(float((got[i].double() * way).sum()) - slope) <= allowed
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_what_is_not_seen_has_no_influence(kp, bad):
+    """A key or a token that is not finite reaches those that see it (or are seen by it), and nobody else."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    n, at, window, sinks, scale = 200, 70, 40, 2, 0.125
+    q, k, v, d_o = (heads(gen, 1, h, n, 64, torch.bfloat16) for h in (4, 2, 2, 4))
+    see = forward(q, k, v, window, sinks, scale)[0][0, 0] > 0
+    clean = attend(kp, q, k, v, window, sinks, scale)
+    clean_grad = grads(kp, q, k, v, *clean, d_o, window, sinks, scale)
+    bound = gradients(q, k, v, d_o, window, sinks, scale, torch.bfloat16)
+    k2, v2 = k.clone(), v.clone()
+    k2[0, 0, at, 3], v2[0, 0, at, 5] = bad, bad
+    hit = see[:, at]  # tokens that see it
+    for kk, vv in ((k2, v), (k, v2)):
+        o, lse = attend(kp, q, kk, vv, window, sinks, scale)
+        p, want, _ = forward(q, k, v, window, sinks, scale)
+        far = ~hit
+        assert_within(o[:, :2, far], want[:, :2, far], o_bound(p, v, torch.bfloat16)[:, :2, far])
+        assert torch.equal(o[:, 2:], clean[0][:, 2:])
+        if bad != bad:
+            assert torch.isnan(o[:, :2, hit].float()).any(-1).all()
+    # a token whose own gradient is not finite: the keys it does not see, and all other tokens, keep their gradients
+    d_o2 = d_o.clone()
+    d_o2[0, 0, at, 7] = bad
+    dq, dk, dv = grads(kp, q, k, v, *clean, d_o2, window, sinks, scale)
+    others = torch.arange(n, device="cuda") != at
+    assert_within(dq[:, 0, others], bound[0][0][:, 0, others], bound[0][1][:, 0, others])
+    unseen = ~see[at]
+    assert_within(dk[:, 0, unseen], bound[1][0][:, 0, unseen], bound[1][1][:, 0, unseen])
+    assert_within(dv[:, 0, unseen], bound[2][0][:, 0, unseen], bound[2][1][:, 0, unseen])
+    for got, ref in zip((dq[:, 1:], dk[:, 1:], dv[:, 1:]), (clean_grad[0][:, 1:], clean_grad[1][:, 1:], clean_grad[2][:, 1:])):
+        assert torch.equal(got, ref)
+
+
+def test_strides(kp):
+    """Slices of one projection, a head broadcast to all sequences, outputs inside larger tensors: same values as contiguous."""
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    b, hq, hkv, n, d, dtype = 2, 4, 2, 150, 128, torch.bfloat16
+    fused = torch.randn(b, n, hq + 2 * hkv, d, device="cuda", generator=gen).to(dtype)
+    q, k, v = (x.transpose(1, 2) for x in (fused[:, :, :hq], fused[:, :, hq:hq + hkv], fused[:, :, hq + hkv:]))
+    big = torch.zeros(b, hq, n, 2 * d, dtype=dtype, device="cuda")
+    o, lse = attend(kp, q, k, v, 60, 1, 0.1, o=big[..., :d])
+    o2, lse2 = attend(kp, q.contiguous(), k.contiguous(), v.contiguous(), 60, 1, 0.1)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2) and not big[..., d:].any()
+    d_o = heads(gen, 1, 1, n, d, dtype).expand(b, hq, n, d)  # a broadcast gradient
+    got = grads(kp, q, k, v, o, lse, d_o, 60, 1, 0.1)
+    want = grads(kp, q.contiguous(), k.contiguous(), v.contiguous(), o2, lse2, d_o.contiguous(), 60, 1, 0.1)
+    assert all(torch.equal(a, c) for a, c in zip(got, want))
+    kb, vb = k[:1].expand(b, hkv, n, d), v[:1].expand(b, hkv, n, d)
+    o3, _ = attend(kp, q, kb, vb, 60, 1, 0.1)
+    o4, _ = attend(kp, q, kb.contiguous(), vb.contiguous(), 60, 1, 0.1)
+    assert torch.equal(o3, o4)
+
+
+def test_offsets_past_32_bits(kp):
+    """Keys whose places in memory lie more than 2^32 elements apart."""
+    gen = torch.Generator(device="cuda").manual_seed(10)
+    n, d, step = 4200, 64, 1 << 20
+    room = torch.empty(n * step, dtype=torch.bfloat16, device="cuda")
+    k = room.as_strided((1, 1, n, d), (0, 0, step, 1))
+    v = room[d:].as_strided((1, 1, n, d), (0, 0, step, 1))
+    k.copy_(heads(gen, 1, 1, n, d, torch.bfloat16))
+    v.copy_(heads(gen, 1, 1, n, d, torch.bfloat16))
+    for n_q, window in ((1, 0), (200, 64)):
+        q = heads(gen, 1, 2, n_q, d, torch.bfloat16)
+        o, lse = attend(kp, q, k, v, window, 4, 0.125)
+        o2, lse2 = attend(kp, q, k.contiguous(), v.contiguous(), window, 4, 0.125)
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+def test_same_inputs_same_bits_on_any_stream_and_in_a_graph(kp):
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    q, k, v, d_o = (heads(gen, 2, h, 333, 64, torch.float16) for h in (6, 2, 2, 6))
+    window, sinks, scale = 70, 5, 0.125
+    o, lse = attend(kp, q, k, v, window, sinks, scale)
+    first = [o, lse, *grads(kp, q, k, v, o, lse, d_o, window, sinks, scale)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        o, lse = attend(kp, q, k, v, window, sinks, scale)
+        second = [o, lse, *grads(kp, q, k, v, o, lse, d_o, window, sinks, scale)]
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(first, second))
+    out = [torch.zeros_like(x) for x in first]
+    n = max(kp.kp_attn_window_bytes(q, k, window, sinks), kp.kp_attn_window_grad_bytes(q, k, window, sinks))
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        kp.kp_attn_window(q, k, v, out[0], out[1], window, sinks, scale, ws)
+        kp.kp_attn_window_grad(q, k, v, out[0], out[1], d_o, *out[2:], window, sinks, scale, ws)
+    for step in range(4):
+        q.copy_(heads(gen, 2, 6, 333, 64, torch.float16))
+        graph.replay()
+        torch.cuda.synchronize()
+        o, lse = attend(kp, q, k, v, window, sinks, scale)
+        eager = [o, lse, *grads(kp, q, k, v, o, lse, d_o, window, sinks, scale)]
+        assert all(torch.equal(a, b) for a, b in zip(out, eager)), step
