@@ -22,7 +22,7 @@ __device__ __forceinline__ const uint16_t* row_at(const Heads& t, uint32_t seq, 
   return t.at + t.seq * (int64_t)seq + t.head * (int64_t)head + t.token * (int64_t)token;
 }
 __device__ __forceinline__ bool sees(int32_t p, uint32_t j, uint32_t window, uint32_t sinks) {
-  return (int32_t)j <= p && (window == 0u || (uint32_t)p - j < window || j < sinks);
+  return ((int32_t)j <= p) & ((window == 0u) | ((uint32_t)p - j < window) | (j < sinks));
 }
 template <class T, int E>
 __device__ __forceinline__ void load_row(const uint16_t* at, float (&out)[E]) {

@@ -1,6 +1,6 @@
 // Attention with a sliding window and sinks over keys that lie in one piece (kp_attn_window).
 #include "kp_attn_host.h"
-#include "kp_attn_rows.h"
+#include "kp_attn_launch.h"
 
 using namespace kp::attn;
 
@@ -13,7 +13,15 @@ kp_status check_sizes(int B, int Hq, int Hkv, int Sq, int Sk, int D) {
 }
 }  // namespace
 
-extern "C" size_t kp_attn_window_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks) { return 0; }
+static Plan plan_window(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks) {
+  const long long rows = (long long)(Hq / Hkv) * Sq;
+  return plan_of(B, rows * B, most_keys_of(Sk, Sq < kTileRows ? Sq : kTileRows, window, sinks), Hkv, D, true);
+}
+
+extern "C" size_t kp_attn_window_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks) {
+  if (Hq < 1 || Hkv < 1 || Hq % Hkv || (D != 64 && D != 128) || window < 0 || sinks < 0 || check_sizes(B, Hq, Hkv, Sq, Sk, D)) return 0;
+  return plan_window(B, Hq, Hkv, Sq, Sk, D, window, sinks).bytes;
+}
 
 extern "C" kp_status kp_attn_window(const kp_heads* q, const kp_heads* k, const kp_heads* v, const kp_heads* o, float* lse,
                                     int B, int Hq, int Hkv, int Sq, int Sk, int D, int type, int window, int sinks,
@@ -26,21 +34,16 @@ extern "C" kp_status kp_attn_window(const kp_heads* q, const kp_heads* k, const 
   if (kp_status s = check_heads("v", v, B, Hkv, Sk, D, false)) return s;
   if (kp_status s = check_heads("o", o, B, Hq, Sq, D, true)) return s;
   if ((uintptr_t)lse & 3u) return kp::fail(KP_ERR_INVALID_ARG, "lse must be 4-byte aligned");
-  if (kp_status s = check_workspace(workspace, workspace_bytes, kp_attn_window_bytes(B, Hq, Hkv, Sq, Sk, D, window, sinks))) return s;
+  const Plan plan = plan_window(B, Hq, Hkv, Sq, Sk, D, window, sinks);
+  if (kp_status s = check_workspace(workspace, workspace_bytes, plan.bytes)) return s;
   Args g{};
   g.q = heads_of(q, B, Hq, Sq); g.o = heads_of(o, B, Hq, Sq);
   g.k = heads_of(k, B, Hkv, Sk); g.v = heads_of(v, B, Hkv, Sk);
   g.lse = lse; g.lse_seq = (int64_t)Hq * Sq; g.lse_head = Sq;
   g.seqs = (uint32_t)B; g.hkv = (uint32_t)Hkv; g.group = (uint32_t)(Hq / Hkv); g.n_q = (uint32_t)Sq; g.n_k = (uint32_t)Sk;
   g.window = (uint32_t)window; g.sinks = (uint32_t)sinks; g.scale_log2 = scale * kLog2e;
-  const long long per_seq = ((long long)g.group * Sq + 15) / 16, grid = per_seq * B * Hkv;
-  if (grid >= (1ll << 31)) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^31 or more workgroups");
-  g.tiles = (uint32_t)(per_seq * B);
+  g.part = static_cast<float*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
-#define KP_LAUNCH(T, D) hipLaunchKernelGGL((kp_attn_row_by_row<T, D, kPlain>), dim3((uint32_t)grid), dim3(kThreads), 0, st, g)
-  if (type == KP_BF16) { if (D == 64) KP_LAUNCH(Bf16, 64); else KP_LAUNCH(Bf16, 128); }
-  else { if (D == 64) KP_LAUNCH(Fp16, 64); else KP_LAUNCH(Fp16, 128); }
-#undef KP_LAUNCH
-  KP_HIP_TRY(hipGetLastError());
-  return KP_OK;
+  if (type == KP_FP16) return D == 64 ? launch<Fp16, 64, kPlain>(g, plan, st) : launch<Fp16, 128, kPlain>(g, plan, st);
+  return D == 64 ? launch<Bf16, 64, kPlain>(g, plan, st) : launch<Bf16, 128, kPlain>(g, plan, st);
 }

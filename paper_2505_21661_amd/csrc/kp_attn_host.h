@@ -78,6 +78,34 @@ inline kp_status check_cache(const kp_cache* c) {
   return KP_OK;
 }
 
+// Which kernel takes a call, on how many row tiles, and into how many runs the keys of a tile are split.
+struct Plan {
+  bool few;
+  long long tiles, splits, units;  // units: heads of keys (of all sequences where a tile belongs to one)
+  size_t bytes;                    // workspace
+};
+// rows: query rows of a head of keys, of all `seqs` sequences; most_keys: keys that a row tile may have to go over;
+// even: every sequence has rows / seqs of them.
+inline Plan plan_of(long long seqs, long long rows, long long most_keys, int Hkv, int D, bool even) {
+  Plan p{};
+  p.few = rows <= 16 * seqs;
+  const long long per_tile = p.few ? 16 : 128;
+  p.tiles = even ? (rows / seqs + per_tile - 1) / per_tile * seqs : rows / per_tile + seqs;
+  p.units = p.tiles * Hkv;
+  // as many workgroups as the chip holds at a time, as long as a run has 256 keys
+  const long long want = p.few ? 1024 : 512, runs = (most_keys + 255) / 256;
+  p.splits = p.units * 2 > want ? 1 : want / p.units;
+  if (p.splits > runs) p.splits = runs;
+  if (p.splits < 1) p.splits = 1;
+  p.bytes = p.splits > 1 ? (size_t)p.splits * (size_t)(p.units * per_tile) * (size_t)(D + 2) * 4 : 0;
+  return p;
+}
+// Keys that the rows of a tile may see: all there are, or the window of its tokens and the sinks.
+inline long long most_keys_of(long long n_k, long long tokens, int window, int sinks) {
+  const long long w = (long long)window + sinks + tokens;
+  return window > 0 && w < n_k ? w : n_k;
+}
+
 inline uint32_t log2_of(int pow2) { return (uint32_t)__builtin_ctz((unsigned)pow2); }
 
 }  // namespace attn

@@ -1,13 +1,31 @@
-// Attention of a tile of query rows over the keys they see (the kernels behind kp_attn_window and kp_attn_paged).
+// Attention of a tile of 128 query rows over the keys they see (the kernel behind kp_attn_window and kp_attn_paged
+// wherever there are more than a few rows), and the join of partial results.
+//
+// The rows of a tile are (token, query head of a group) pairs, token by token: heads that share keys share the tile, so
+// that 16 tokens of 8 heads read a key once, and a window costs its keys once per tile.  4 waves of 32 rows; products
+// are formed transposed (S^T = K Q^T, O^T = V^T P^T), so that a lane holds all scores of one row: maximum and sum are
+// in-lane but for one exchange, P needs no movement between the products, O is rescaled per lane.  K and V tiles of 64
+// keys are shared through LDS (K one buffer, V two): 16-bit keys go there directly from global memory, every lane
+// fetching the chunk that belongs at its place; e4m3 codes come through registers and are widened on the way.
+// A tile begins at the first key that a row of the tile sees, not at a multiple of 64, and past the last one the last is
+// read again: nothing outside the visible ranges is touched, whatever the cache holds there.
 #pragma once
+#include <type_traits>
+
 #include "kp_attn.h"
+#include "kp_record.h"
 
 namespace kp {
 namespace attn {
 
 constexpr int kThreads = 256;
+constexpr int kTileRows = 128, kTileKeys = 64;
+constexpr float kSlack = 8.0f;  // log2 of how far a score may exceed the softmax's reference before that moves
 
-// Where row `flat` (token by token, query heads of a group within a token) of a tile's sequence lies.
+template <int D>
+constexpr uint32_t tile_lds_bytes() { return 3u * kTileKeys * 2u * D; }
+
+// Where row `flat` of a tile's sequence lies.
 struct RowPlace {
   uint32_t token, in_group;
 };
@@ -18,26 +36,496 @@ __device__ __forceinline__ RowPlace place_of(uint32_t flat, uint32_t group) {
   return r;
 }
 
-template <class T, int D, int SRC>
-__global__ __launch_bounds__(kThreads) void kp_attn_row_by_row(Args g) {
-  constexpr int kRows = 16;
-  const uint32_t h = blockIdx.x % g.hkv, lane = threadIdx.x & 63u;
-  Tile tile;
-  if (!find_tile<kRows, SRC != kPlain>(g, blockIdx.x / g.hkv, &tile)) return;
-  const Source<D, SRC> src(g, tile.seq, h);
-  for (uint32_t r = threadIdx.x >> 6; r < kRows; r += kThreads / 64) {
-    const uint32_t flat = tile.first + r;
-    if (flat >= tile.rows) break;
-    const RowPlace at = place_of(flat, g.group);
-    const uint32_t head = h * g.group + at.in_group, seq = SRC == kPlain ? tile.seq : 0u;
-    const int64_t token = (int64_t)tile.q0 + at.token;
-    float q[D / 64];
-    row_elements<T, D / 64>(reinterpret_cast<const uint8_t*>(g.q.at + g.q.seq * seq + g.q.head * head + g.q.token * token), lane, q);
-    Row<D / 64> row;
-    row_over_keys<T, D, SRC>(row, q, src, (int32_t)tile.n_k - (int32_t)tile.n_q + (int32_t)at.token, g.window, g.sinks, g.scale_log2, 0u, tile.n_k);
-    store_row<T, D / 64>(row, const_cast<uint16_t*>(g.o.at) + g.o.seq * seq + g.o.head * head + g.o.token * token,
-                         g.lse ? g.lse + g.lse_seq * seq + g.lse_head * head + token : nullptr);
+// The larger of a lane's value and that of the lane 32 away.
+__device__ __forceinline__ float either_half_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+
+// Workgroup `id` of units x per items: which unit (a head of keys, of one sequence or of all), which of its items.
+// Workgroups are dealt round-robin to the 8 XCDs, each with its own L2.  All items of a unit go to one XCD where the units
+// can be dealt out evenly; as many units as have places at a time (two workgroups per CU) are taken together, the first
+// items of all of them first, which are the longest.
+__device__ __forceinline__ void unit_of(uint32_t id, uint32_t units, uint32_t per, uint32_t* unit, uint32_t* item) {
+  const uint32_t even = (units & 7u) == 0u ? 1u : 0u;
+  const uint32_t xcd = even ? id & 7u : 0u, j = even ? id >> 3 : id;
+  const uint32_t mine = even ? units >> 3 : units, places = even ? 64u : 512u;
+  const uint32_t together = places > per ? places / per : 1u;
+  const uint32_t group = j / (together * per), in = j - group * (together * per);
+  const uint32_t left = mine - group * together, n = left < together ? left : together;
+  const uint32_t block = in / n, u = group * together + in - block * n;
+  *unit = even ? u * 8u + xcd : u;
+  *item = block;
+}
+
+// Index of a row in the partial results, which hold [splits][rows](maximum, sum) and then [splits][rows][D].
+template <int ROWS>
+__device__ __forceinline__ size_t part_row(const Args& g, uint32_t tile, uint32_t h, uint32_t r) {
+  return ((size_t)tile * g.hkv + h) * ROWS + r;
+}
+
+#define KP_BOUNDARY(ring, end_r, start_r) do { if constexpr (INSTR != 0) kp::site<INSTR>(ring, end_r, start_r); } while (0)
+
+template <class T, int D, int SRC, int INSTR>
+__global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
+  constexpr uint32_t kRow = 2u * D, kChunks = kRow / 16u, kTile = kTileKeys * kRow;
+  constexpr uint32_t kBlockRows = 1024u / kRow;  // rows of the 1 KiB that a wave's load fills
+  constexpr int NS = D / 16, ND = D / 32, NL = (int)(kTile / 4096u);
+  constexpr bool E4M3 = SRC == kPagedE4m3;
+  extern __shared__ __align__(16) unsigned char smem[];  // [K tile][V tile, two buffers][ring]
+
+  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = wave_uniform(tid >> 6);
+  const uint32_t h32 = lane >> 5, l32 = lane & 31u;
+
+  uint32_t unit, item;
+  const uint32_t units = SRC == kPlain ? g.seqs * g.hkv : g.hkv;
+  const uint32_t tiles_per = SRC == kPlain ? g.tiles / g.seqs : g.tiles, per = tiles_per * g.splits;
+  unit_of(blockIdx.x, units, per, &unit, &item);
+  const uint32_t split = item % g.splits;
+  uint32_t tile_id = item / g.splits, h = unit;
+  if constexpr (SRC == kPlain) {  // the last rows see the most keys
+    const uint32_t seq = unit / g.hkv;
+    h = unit - seq * g.hkv;
+    tile_id = seq * tiles_per + (tiles_per - 1u - tile_id);
   }
+  Tile tl;
+  const bool there = find_tile<kTileRows, SRC != kPlain>(g, tile_id, &tl);
+
+  kp::Ring ring{};
+  if constexpr (INSTR != 0) {
+    ring = kp::ring_init<true>(reinterpret_cast<uint32_t*>(smem + 3u * kTile), reinterpret_cast<uint64_t*>(smem), g.cap_lds, g.region_mask, g.flush,
+                               g.cap_hbm, g.trace, g.n_wg, 4u >> g.group_log2, unit * per + item, g.group_log2);
+    ring.collab = g.collab;
+    if constexpr (INSTR == 3) kp::ring_use_realtime(ring);
+  }
+  if (there) {
+    const Source<D, SRC> src(g, tl.seq, h);
+    const uint32_t last_row = tl.rows - 1u;
+    auto position = [&](uint32_t flat) __attribute__((always_inline)) {
+      return (int32_t)tl.n_k - (int32_t)tl.n_q + (int32_t)place_of(flat < last_row ? flat : last_row, g.group).token;
+    };
+    const uint32_t wave_first = tl.first + 32u * wave, flat = wave_first + l32;
+    const bool mine = flat <= last_row;
+    const RowPlace at = place_of(mine ? flat : last_row, g.group);
+    const int32_t p = (int32_t)tl.n_k - (int32_t)tl.n_q + (int32_t)at.token;
+    const int32_t p_min = position(wave_first), p_max = position(wave_first + 31u);
+    const Span span = span_of(position(tl.first), position(tl.first + kTileRows - 1u), g.window, g.sinks);
+    const uint32_t sink_tiles = (span.sink_end + kTileKeys - 1u) / kTileKeys;
+    const uint32_t all_tiles = sink_tiles + (span.end > span.lo ? (span.end - span.lo + kTileKeys - 1u) / kTileKeys : 0u);
+    const uint32_t t_begin = (uint32_t)((uint64_t)all_tiles * split / g.splits), t_end = (uint32_t)((uint64_t)all_tiles * (split + 1u) / g.splits);
+
+    const uint32_t q_seq = SRC == kPlain ? tl.seq : 0u, head = h * g.group + at.in_group;
+    const int64_t token = (int64_t)tl.q0 + at.token;
+    u32x4 qf[NS];  // this lane's row: d = 16 s + 8 h32 .. + 7
+    {
+      const uint16_t* q = g.q.at + g.q.seq * (int64_t)q_seq + g.q.head * (int64_t)head + g.q.token * token;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const u32x4*>(q + 16 * s + 8 * h32);
+    }
+
+    // ---- the tile that is requested next ----------------------------------------------------------------------
+    const uint32_t lds0 = wave_uniform((uint32_t)(uintptr_t)smem + 1024u * wave);
+    const uint32_t ld_row = kBlockRows * wave + lane / kChunks, pos = lane % kChunks;
+    // chunk c of row r lies at position c ^ swizzle(r): 16 neighbouring rows' 16-byte reads (K), and the four rows of a
+    // transposing read (V), cover all banks once
+    const uint32_t k_sw = D == 128 ? ld_row & 15u : (ld_row >> 1) & 7u, v_sw = D == 128 ? 4u * (ld_row & 3u) : 4u * ((ld_row >> 1) & 1u);
+    const uint32_t k_in = (pos ^ k_sw) << 4, v_in = (pos ^ v_sw) << 4;
+    uint32_t k_ofs[NL], v_ofs[NL];        // kPlain: from the tile's first key, bytes
+    const uint8_t *k_base = nullptr, *v_base = nullptr;
+    uint64_t k_ptr[NL], v_ptr[NL];        // kPaged
+    uint32_t ofs_last = 0;                // last row that the offsets were made for
+    int32_t page_id = 0;                  // paged: block-table entry of the next tile's key number `lane`
+    uint64_t valid = ~0ull, valid_next = ~0ull;  // paged: keys of this and the next tile whose page exists
+    u32x4 k8[E4M3 ? D / 64 : 1], v8[E4M3 ? D / 64 : 1];
+    float ke[E4M3 ? D / 64 : 1], ve[E4M3 ? D / 64 : 1];
+    uint32_t v_into = kTile;              // LDS offset of the V buffer that the next tile goes to
+
+    auto tile_start = [&](uint32_t t, uint32_t* limit) __attribute__((always_inline)) {
+      *limit = t < sink_tiles ? span.sink_end : span.end;
+      return t < sink_tiles ? t * kTileKeys : span.lo + (t - sink_tiles) * kTileKeys;
+    };
+    auto load_page_ids = [&](uint32_t t) __attribute__((always_inline)) {
+      if constexpr (SRC != kPlain) {
+        if (t < t_end) {
+          uint32_t limit;
+          const uint32_t start = tile_start(t, &limit), last = limit - 1u - start;
+          page_id = src.table[(start + (lane < last ? lane : last)) >> src.page_log2];
+        }
+      }
+    };
+    // Where tile t's rows are; its page ids have been asked for before.
+    auto locate = [&](uint32_t t) __attribute__((always_inline)) {
+      uint32_t limit;
+      const uint32_t start = tile_start(t, &limit), left = limit - 1u - start, last = left < kTileKeys - 1u ? left : kTileKeys - 1u;
+      if constexpr (SRC == kPlain) {
+        k_base = src.k + src.k_step * (int64_t)start;
+        v_base = src.v + src.v_step * (int64_t)start;
+        if (last != ofs_last) {
+          ofs_last = last;
+#pragma unroll
+          for (int i = 0; i < NL; ++i) {
+            const uint32_t row = ld_row + 4u * kBlockRows * (uint32_t)i, r = row < last ? row : last;
+            k_ofs[i] = r * (uint32_t)src.k_step + k_in;
+            v_ofs[i] = r * (uint32_t)src.v_step + v_in;
+          }
+        }
+      } else {
+        uint32_t row_no = src.row_of_page(page_id, start + (lane < last ? lane : last));
+        valid_next = __builtin_amdgcn_ballot_w64(row_no != ~0u);
+        if (row_no == ~0u) row_no = 0u;  // (some row of the cache: its scores are masked)
+        if constexpr (!E4M3) {
+#pragma unroll
+          for (int i = 0; i < NL; ++i) {
+            const uint32_t r = __shfl(row_no, (int)(ld_row + 4u * kBlockRows * (uint32_t)i), 64);
+            k_ptr[i] = (uint64_t)(uintptr_t)src.k + (uint64_t)r * kRow + k_in;
+            v_ptr[i] = (uint64_t)(uintptr_t)src.v + (uint64_t)r * kRow + v_in;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < D / 64; ++i) {
+            constexpr uint32_t kPer = D / 16;  // 16-byte chunks of a row of codes
+            const uint32_t r = __shfl(row_no, (int)((tid + kThreads * (uint32_t)i) / kPer), 64);
+            k8[i] = *reinterpret_cast<const u32x4*>(src.k + (size_t)r * D + 16u * (tid % kPer));
+            v8[i] = *reinterpret_cast<const u32x4*>(src.v + (size_t)r * D + 16u * (tid % kPer));
+            ke[i] = power_of(src.k_exp[r]);
+            ve[i] = power_of(src.v_exp[r]);
+          }
+        }
+        load_page_ids(t + 1u);
+      }
+    };
+    // One load straight to LDS: M0 (the LDS base) is put back afterwards.  From inline assembly because the compiler would
+    // make the next LDS access of any kind wait for such a load; the loads complete in order, and the kernel waits for them
+    // itself in front of the barrier that precedes the tile's use.
+    auto load_from = [&](const uint8_t* base, uint32_t ofs, uint32_t dst) __attribute__((always_inline)) {
+      uint32_t saved_m0;
+      asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+                   : "=&s"(saved_m0) : "v"(ofs), "s"(base), "s"(dst) : "memory");
+    };
+    auto load_at = [&](uint64_t ptr, uint32_t dst) __attribute__((always_inline)) {
+      uint32_t saved_m0;
+      asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
+                   : "=&s"(saved_m0) : "v"(ptr), "s"(dst) : "memory");
+    };
+    auto load_k = [&](int i) __attribute__((always_inline)) {
+      const uint32_t dst = lds0 + 4096u * (uint32_t)i;
+      if constexpr (SRC == kPlain) load_from(k_base, k_ofs[i], dst);
+      else if constexpr (!E4M3) load_at(k_ptr[i], dst);
+    };
+    auto load_v = [&](int i) __attribute__((always_inline)) {
+      const uint32_t dst = lds0 + v_into + 4096u * (uint32_t)i;
+      if constexpr (SRC == kPlain) load_from(v_base, v_ofs[i], dst);
+      else if constexpr (!E4M3) load_at(v_ptr[i], dst);
+    };
+    // e4m3: the codes in registers become 16-bit rows in LDS
+    auto widen = [&](const u32x4& codes, float scale, uint32_t base, uint32_t row, uint32_t c, uint32_t sw) __attribute__((always_inline)) {
+      u32x4 lo, hi;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        u32x4& to = w < 2 ? lo : hi;
+        to[2 * (w & 1)] = T::template from_e4m3<false>(codes[w], scale);
+        to[2 * (w & 1) + 1] = T::template from_e4m3<true>(codes[w], scale);
+      }
+      *reinterpret_cast<u32x4*>(smem + base + row * kRow + (((2u * c) ^ sw) << 4)) = lo;
+      *reinterpret_cast<u32x4*>(smem + base + row * kRow + (((2u * c + 1u) ^ sw) << 4)) = hi;
+    };
+    auto store_codes = [&](bool keys) __attribute__((always_inline)) {
+      if constexpr (E4M3) {
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+          const uint32_t j = tid + kThreads * (uint32_t)i, row = j / (D / 16), c = j % (D / 16);
+          if (keys) widen(k8[i], ke[i], 0u, row, c, D == 128 ? row & 15u : (row >> 1) & 7u);
+          else widen(v8[i], ve[i], v_into, row, c, D == 128 ? 4u * (row & 3u) : 4u * ((row >> 1) & 1u));
+        }
+      }
+    };
+    auto requested = [&]() __attribute__((always_inline)) {
+      v_into ^= kTile ^ (2u * kTile);
+    };
+
+    // ---- operand reads: K row 32 tk + l32, chunk 2 s + h32; V for the keys of step (16 keys) and the d of dt --------
+    uint32_t k_rd[NS], v_rd[ND];
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+      k_rd[s] = (uint32_t)(uintptr_t)smem + l32 * kRow + (((2u * (uint32_t)s + h32) ^ (D == 128 ? l32 & 15u : (l32 >> 1) & 7u)) << 4);
+    {
+      const uint32_t i = lane & 15u, grp = lane >> 4, row = 4u * (grp >> 1) + (i >> 2);
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) {
+        const uint32_t d = 32u * (uint32_t)dt + 16u * (grp & 1u) + 4u * (i & 3u), sw = D == 128 ? 4u * (row & 3u) : 4u * ((row >> 1) & 1u);
+        v_rd[dt] = (uint32_t)(uintptr_t)smem + kTile + row * kRow + (((d >> 3) ^ sw) << 4) + 8u * ((d >> 2) & 1u);
+      }
+    }
+    uint32_t v_other = kTile;  // from the V buffer in use to the other one
+    auto read_k = [&](int s, int tk) __attribute__((always_inline)) -> u32x4 {
+      typedef const __attribute__((address_space(3))) u32x4* lds_u32x4;
+      return *(lds_u32x4)(uintptr_t)(k_rd[s] + (uint32_t)tk * 32u * kRow);
+    };
+    auto read_v = [&](uint32_t step, int dt) __attribute__((always_inline)) -> u32x4 {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef short s16x8 __attribute__((ext_vector_type(8)));
+      typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+      const uint32_t a = v_rd[dt] + step * (16u * kRow);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(a));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(a + 8u * kRow));
+      const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      return __builtin_bit_cast(u32x4, v);
+    };
+
+    f32x16 oacc[ND];  // O^T: rows d = 32 dt + 8 j + 4 h32 + i, column = row l32
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) oacc[dt] = f32x16{0};
+    float m_run = kNoKey, l_run = 0.f;
+
+    u32x4 kf[NS];  // operands of K Q^T, NS MFMAs ahead
+    auto request_k_operands = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int n = 0; n < NS; ++n) kf[n] = read_k(n, 0);
+    };
+    auto tile = [&](uint32_t t, auto more_c) __attribute__((always_inline)) {
+      constexpr bool MORE = decltype(more_c)::value;
+      uint32_t limit;
+      const uint32_t start = tile_start(t, &limit);
+      const int32_t end = (int32_t)(start + kTileKeys);  // one past the tile's last key
+      bool masked = end > (int32_t)limit || end - 1 > p_min;
+      if (g.window != 0u) masked = masked || (p_max - (int32_t)start >= (int32_t)g.window && end > (int32_t)g.sinks);
+      if constexpr (SRC != kPlain) masked = masked || valid != ~0ull;
+      f32x16 sacc[2];
+      sacc[0] = f32x16{0}; sacc[1] = f32x16{0};
+      float mx = -INFINITY, psum = 0.f;
+      u32x4 pw[4];  // P, in accumulator order: one entry per MFMA step of V^T P^T (16 keys)
+      auto mask = [&](int tk) __attribute__((always_inline)) {
+        if (!masked) return;
+        // key of element c: start + 4 h32 + c
+        const int32_t base = (int32_t)(start + 4u * h32), hi = (p < (int32_t)limit ? p : (int32_t)limit - 1) - base;
+        const int32_t lo = g.window != 0u ? p - (int32_t)g.window + 1 - base : -base, sk = (int32_t)g.sinks - base;
+        const uint64_t there = SRC != kPlain ? valid >> (4u * h32) : 0ull;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int32_t c = 32 * tk + 8 * (v >> 2) + (v & 3);
+          bool seen = (c <= hi) & ((c >= lo) | (c < sk));  // (no short cuts: they become branches)
+          if constexpr (SRC != kPlain) seen = seen & (((there >> c) & 1ull) != 0ull);
+          sacc[tk][v] = seen ? sacc[tk][v] : -INFINITY;
+        }
+      };
+      auto exps = [&](int pair) __attribute__((always_inline)) {
+        const int tk = pair >> 3, v = 2 * (pair & 7);
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[tk][v], g.scale_log2, -m_run));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[tk][v + 1], g.scale_log2, -m_run));
+        psum += p0 + p1;  // the sum is of the unrounded probabilities
+        pw[pair >> 2][pair & 3] = T::pack(p0, p1);
+      };
+
+      // ---- region 0: S^T = K Q^T ------------------------------------------------------------------------------
+      if constexpr (MORE) locate(t + 1u);
+      __builtin_amdgcn_s_setprio(2);
+      constexpr int kBarrier = NS + 1, kLoads = NS == 8 ? 11 : 6;
+#pragma unroll
+      for (int n = 0; n < 2 * NS; ++n) {  // the lower 32 keys, then the upper ones, whose operands are requested meanwhile
+        const int s = n % NS, tk = n / NS;
+        sacc[tk] = T::mfma32(kf[s], qf[s], sacc[tk]);
+        if (tk == 0) kf[s] = read_k(s, 1);
+        if (MORE && tk == 0 && (s & 1)) load_v(s >> 1);
+        if (MORE && n >= kLoads && n < kLoads + NL) load_k(n - kLoads);
+        if (tk == 1) {  // the maximum of the lower half
+          if (s == 0) mask(0);
+#pragma unroll
+          for (int v = s * (16 / NS); v < (s + 1) * (16 / NS); v += 2) mx = fmaxf(fmaxf(mx, sacc[0][v]), sacc[0][v + 1]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        // every wave has read this K tile
+        if (MORE && n == kBarrier) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      }
+      __builtin_amdgcn_s_setprio(0);
+      KP_BOUNDARY(ring, 0, 1);
+
+      // ---- region 1: online softmax (this lane: 32 of the tile's 64 keys) -----------------------------------------
+      u32x4 vf[4];  // operands of V^T P^T, four MFMAs ahead
+#pragma unroll
+      for (int m = 0; m < 4; ++m) vf[m] = read_v((uint32_t)(m / ND), m % ND);
+      mask(1);
+#pragma unroll
+      for (int v = 0; v < 16; v += 2) mx = fmaxf(fmaxf(mx, sacc[1][v]), sacc[1][v + 1]);
+      mx = either_half_max(mx);
+      // The reference of the exponentials only has to keep them in range: it moves (and O and l are rescaled) when some
+      // row of the wave exceeds it by more than 2^kSlack.
+      const float mx_s = mx * g.scale_log2;
+      if (__builtin_amdgcn_ballot_w64(mx_s > m_run + kSlack) != 0ull) {
+        const float m_new = fmaxf(m_run, mx_s);
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+        l_run *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) oacc[dt][v] *= alpha;
+        m_run = m_new;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) exps(i);
+      l_run += psum;
+      KP_BOUNDARY(ring, 1, 2);
+      if constexpr (MORE && E4M3) { store_codes(true); store_codes(false); }
+      __builtin_amdgcn_s_setprio(1);
+
+      // ---- region 2: O^T += V^T P^T ---------------------------------------------------------------------------------
+      // The key order inside a step follows the accumulator layout of S^T, so P needs no movement; V is read to match.
+      auto pv = [&](int m) __attribute__((always_inline)) {
+        oacc[m % ND] = T::mfma32(vf[m & 3], pw[m / ND], oacc[m % ND]);
+      };
+#pragma unroll
+      for (int m = 0; m < 4 * ND - 4; ++m) {
+        pv(m);
+        vf[m & 3] = read_v((uint32_t)((m + 4) / ND), (m + 4) % ND);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      // Every wave has read this V tile, and the next K and V tiles have landed.  The last four MFMAs come behind the
+      // barrier, under the first operand reads of the next tile.
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if constexpr (MORE) request_k_operands();
+#pragma unroll
+      for (int m = 4 * ND - 4; m < 4 * ND; ++m) pv(m);
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) v_rd[dt] += v_other;
+      v_other = 0u - v_other;
+      if constexpr (MORE) { requested(); valid = valid_next; }
+      __builtin_amdgcn_s_setprio(0);
+      if constexpr (MORE) KP_BOUNDARY(ring, 2, 0); else KP_BOUNDARY(ring, 2, kp::kNoRegion);
+    };
+    if (t_begin < t_end) {
+      load_page_ids(t_begin);
+      ofs_last = ~0u;
+      locate(t_begin);
+#pragma unroll
+      for (int i = 0; i < NL; ++i) { load_k(i); load_v(i); }
+      store_codes(true);
+      store_codes(false);
+      requested();
+      valid = valid_next;
+      __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own count of outstanding loads)
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      constexpr std::true_type yes{};
+      constexpr std::false_type no{};
+      KP_BOUNDARY(ring, kp::kNoRegion, 0);
+      request_k_operands();
+      for (uint32_t t = t_begin; t + 1u < t_end; ++t) tile(t, yes);
+      tile(t_end - 1u, no);
+    }
+
+    // ---- the rows leave -----------------------------------------------------------------------------------------------
+    const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+    const int64_t o_at = g.o.seq * (int64_t)q_seq + g.o.head * (int64_t)head + g.o.token * token;
+    const int64_t lse_at = g.lse_seq * (int64_t)q_seq + g.lse_head * (int64_t)head + token;
+    // 0 where all values are finite, else a NaN
+    float odd = l_tot * 0.f;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) odd = __builtin_fmaf(oacc[dt][v], 0.f, odd);
+    uint64_t again = __builtin_amdgcn_ballot_w64(odd != odd && mine);
+    again = (again | again >> 32) & 0xFFFFFFFFull;
+    float* const part_ml = g.part;
+    const size_t part_rows = (size_t)g.tiles * g.hkv * kTileRows;
+    if (g.splits > 1u) {
+      const size_t row = split * part_rows + part_row<kTileRows>(g, tile_id, h, 32u * wave + l32);
+      if (mine) {
+        if (h32 == 0) *reinterpret_cast<f32x2*>(part_ml + 2 * row) = f32x2{m_run, l_tot};
+        float* o = g.part + 2 * g.splits * part_rows + row * D;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<f32x4*>(o + 32 * dt + 8 * j + 4 * h32) = f32x4{oacc[dt][4 * j], oacc[dt][4 * j + 1], oacc[dt][4 * j + 2], oacc[dt][4 * j + 3]};
+      }
+    } else {
+      if (g.lse && mine && h32 == 0) g.lse[lse_at] = l_tot == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_tot)) * kLn2;
+      const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
+      // Through LDS (32 rows of a wave: every wave is past its last operand read), whole rows leave.  Chunk c of row r at
+      // position c ^ r % 8, its halves swapped where r / 8 is odd: 16 lanes of an 8-byte write hit all banks once.
+      unsigned char* const sO = smem + 32u * kRow * wave;
+      const uint32_t half = h32 ^ ((l32 >> 3) & 1u);
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          u32x2 two;
+          two.x = T::pack(oacc[dt][4 * j + 0] * inv, oacc[dt][4 * j + 1] * inv);
+          two.y = T::pack(oacc[dt][4 * j + 2] * inv, oacc[dt][4 * j + 3] * inv);
+          *reinterpret_cast<u32x2*>(sO + l32 * kRow + (((uint32_t)(4 * dt + j) ^ (l32 & 7u)) << 4) + 8u * half) = two;
+        }
+      uint16_t* const o = const_cast<uint16_t*>(g.o.at);
+#pragma unroll
+      for (int i = 0; i < (int)(32u / kBlockRows); ++i) {
+        const uint32_t r = kBlockRows * (uint32_t)i + lane / kChunks, chunk = (lane % kChunks) ^ (r & 7u);
+        const u32x4 v = *reinterpret_cast<const u32x4*>(sO + 1024u * (uint32_t)i + 16u * lane);
+        const int64_t to = (int64_t)(((uint64_t)(uint32_t)__shfl((int)(o_at >> 32), (int)r, 64) << 32) | (uint32_t)__shfl((int)o_at, (int)r, 64));
+        if (wave_first + r <= last_row) *reinterpret_cast<u32x4*>(o + to + 8u * chunk) = (r & 8u) ? u32x4{v.z, v.w, v.x, v.y} : v;
+      }
+    }
+    // Rows with a value that is not finite, taken again (see kp_attn.h).
+    if (again != 0ull) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // their first results have left
+      for (; again != 0ull; again &= again - 1ull) {
+        const uint32_t r = (uint32_t)__builtin_ctzll(again);
+        const RowPlace a = place_of(wave_first + r, g.group);
+        const uint32_t hd = h * g.group + a.in_group;
+        const int64_t tok = (int64_t)tl.q0 + a.token;
+        float q[D / 64];
+        row_elements<T, D / 64>(reinterpret_cast<const uint8_t*>(g.q.at + g.q.seq * (int64_t)q_seq + g.q.head * (int64_t)hd + g.q.token * tok), lane, q);
+        Row<D / 64> row;
+        for (uint32_t t = t_begin; t < t_end; ++t) {
+          uint32_t limit;
+          const uint32_t start = tile_start(t, &limit), to = start + kTileKeys;
+          row_over_keys<T, D, SRC>(row, q, src, (int32_t)tl.n_k - (int32_t)tl.n_q + (int32_t)a.token, g.window, g.sinks, g.scale_log2, start, to < limit ? to : limit);
+        }
+        if (g.splits > 1u) {
+          const size_t to = split * part_rows + part_row<kTileRows>(g, tile_id, h, 32u * wave + r);
+          if (lane == 0) *reinterpret_cast<f32x2*>(part_ml + 2 * to) = f32x2{row.m, row.l};
+#pragma unroll
+          for (int e = 0; e < D / 64; ++e) g.part[2 * g.splits * part_rows + to * D + lane * (D / 64) + e] = row.o[e];
+        } else {
+          store_row<T, D / 64>(row, const_cast<uint16_t*>(g.o.at) + g.o.seq * (int64_t)q_seq + g.o.head * (int64_t)hd + g.o.token * tok,
+                               g.lse ? g.lse + g.lse_seq * (int64_t)q_seq + g.lse_head * (int64_t)hd + tok : nullptr);
+        }
+      }
+    }
+  }
+  if constexpr (INSTR != 0) {
+    kp::TraceGeom tg{g.n_wg, 4u >> g.group_log2, 3, g.cap_hbm, g.flags};
+    kp::ring_finish<INSTR == 3>(ring, g.cap_lds, g.trace, tg, unit * per + item, g.rec_cost);
+  }
+}
+
+// Joins the partial results of a row: D / 4 lanes to a row, 4 elements to a lane.  ROWS: of a tile of the kernel that made them.
+template <class T, int D, int ROWS, bool PAGED>
+__global__ __launch_bounds__(kThreads) void kp_attn_join(Args g) {
+  constexpr uint32_t kLanes = D / 4, kPer = kThreads / kLanes;  // rows of a workgroup
+  const uint32_t blocks = ROWS / kPer, unit = blockIdx.x / blocks, block = blockIdx.x - unit * blocks;
+  const uint32_t tile_id = unit / g.hkv, h = unit - tile_id * g.hkv, r = block * kPer + threadIdx.x / kLanes, c = threadIdx.x % kLanes;
+  Tile tl;
+  if (!find_tile<ROWS, PAGED>(g, tile_id, &tl)) return;
+  const uint32_t flat = tl.first + r;
+  if (flat >= tl.rows) return;
+  const size_t rows = (size_t)g.tiles * g.hkv * ROWS, row = part_row<ROWS>(g, tile_id, h, r);
+  float m = kNoKey;
+  for (uint32_t s = 0; s < g.splits; ++s) m = fmaxf(m, g.part[2 * (s * rows + row)]);
+  float l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (uint32_t s = 0; s < g.splits; ++s) {
+    const f32x2 ml = *reinterpret_cast<const f32x2*>(g.part + 2 * (s * rows + row));
+    if (ml.y == 0.f) continue;
+    const float w = __builtin_amdgcn_exp2f(ml.x - m);
+    l = __builtin_fmaf(ml.y, w, l);
+    const f32x4 part = *reinterpret_cast<const f32x4*>(g.part + 2 * g.splits * rows + (s * rows + row) * D + 4u * c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(part[i], w, o[i]);
+  }
+  const RowPlace at = place_of(flat, g.group);
+  const uint32_t head = h * g.group + at.in_group, seq = PAGED ? 0u : tl.seq;
+  const int64_t token = (int64_t)tl.q0 + at.token;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  uint16_t* to = const_cast<uint16_t*>(g.o.at) + g.o.seq * (int64_t)seq + g.o.head * (int64_t)head + g.o.token * token + 4u * c;
+  *reinterpret_cast<u32x2*>(to) = u32x2{T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv)};
+  if (g.lse && c == 0) g.lse[g.lse_seq * (int64_t)seq + g.lse_head * (int64_t)head + token] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 }  // namespace attn
