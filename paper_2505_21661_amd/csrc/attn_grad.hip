@@ -2,19 +2,35 @@
 //
 // With P_ij = exp2(scale log2(e) q_i.k_j - lse_i log2(e)) and delta_i = d_o_i . o_i (= sum_j P_ij d_o_i . v_j):
 //   dS_ij = P_ij (d_o_i . v_j - delta_i),  dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij d_o_i.
+// Two kernels, both of which form S and d_o v^T for themselves: one goes over the keys of a tile of query rows (dq), the
+// other over the query rows that see a tile of keys (dk, dv).  That is seven products instead of the five that one kernel
+// would need, which would have to add up dq with atomics, in an order that changes from run to run.
 #include "kp_attn_host.h"
+#include "kp_attn_rows.h"
 
 using namespace kp::attn;
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kGradKeys = 128;   // keys of a workgroup of the dk, dv kernel
+
+// fp16 holds little below 2^-14, and P and dS are often smaller: they are rounded to it times a power of two that their
+// factors leave room for.  P <= 1 times 2^kShiftP; dS, of the order of |d_o|, times 2^kShiftS over the power of two of the
+// largest |d_o| of the row (dq) or of all rows of the key's heads (dk).  What overflows all the same is not finite and is
+// taken again in fp32.  bf16 has the exponents of fp32 and needs none of it.
+template <class T> constexpr float kShiftP = 0.f;
+template <> constexpr float kShiftP<Fp16> = 14.f;
+constexpr int kShiftS = 5;
 
 struct GradArgs {
   Heads q, k, v, o, d_o, dq, dk, dv;
   const float* lse;
-  float *lse2, *delta;  // workspace, [B, Hq, Sq]: lse * log2(e) and d_o . o
+  float *neg, *delta;  // workspace, [B, Hq, Sq]: kShiftP - lse log2(e), and d_o . o
+  float* most;         // fp16: largest finite |d_o| of every row tile, [B, Hkv, row tiles]
+  float* part;         // partial dk, dv: [slot][dk, dv][kGradKeys][D]
   uint32_t seqs, hkv, group, n_q, n_k, window, sinks;
+  uint32_t row_tiles, key_tiles;            // of one head of keys
+  uint32_t sink_tiles, sink_runs, runs;     // key tiles with sinks, into how many runs of query rows they and the others are split
   float scale, scale_log2;
 };
 
@@ -42,9 +58,10 @@ __device__ __forceinline__ void put_row(uint16_t* at, const float (&x)[E], float
   else reinterpret_cast<uint32_t*>(at)[lane] = T::pack(x[0] * by, x[1] * by);
 }
 
-// One query row's gradient in fp32, by a wave; only keys that the row sees are touched.
+// One query row's gradient in fp32, by a wave; only keys that the row sees are touched.  For rows whose sums on the matrix
+// instructions are not finite (as in kp_attn.h).
 template <class T, int D>
-__device__ void query_row(const GradArgs& g, uint32_t seq, uint32_t head, uint32_t token, float lse2, float delta, float (&dq)[D / 64]) {
+__device__ __forceinline__ void query_row(const GradArgs& g, uint32_t seq, uint32_t head, uint32_t token, float neg, float delta, float (&dq)[D / 64]) {
   constexpr int E = D / 64;
   const uint32_t hk = head / g.group;
   float q[E], d_o[E];
@@ -58,64 +75,636 @@ __device__ void query_row(const GradArgs& g, uint32_t seq, uint32_t head, uint32
     float k[E], v[E];
     load_row<T, E>(row_at(g.k, seq, hk, (uint32_t)j), k);
     load_row<T, E>(row_at(g.v, seq, hk, (uint32_t)j), v);
-    const float w = __builtin_amdgcn_exp2f(dot<E>(q, k) * g.scale_log2 - lse2), ds = w * (dot<E>(d_o, v) - delta);
+    const float w = __builtin_amdgcn_exp2f(dot<E>(q, k) * g.scale_log2 + (neg - kShiftP<T>)), ds = w * (dot<E>(d_o, v) - delta);
 #pragma unroll
     for (int e = 0; e < E; ++e) dq[e] = __builtin_fmaf(ds, k[e], dq[e]);
   }
 }
 
-// One key's gradients from the query tokens from .. to - 1 of every head of its group.
+// Adds one key's gradients from the query tokens from .. to - 1 of one head.
 template <class T, int D>
-__device__ void key_row(const GradArgs& g, uint32_t seq, uint32_t hk, uint32_t j, uint32_t head_from, uint32_t head_to, uint32_t from, uint32_t to,
-                        float (&dk)[D / 64], float (&dv)[D / 64]) {
+__device__ __forceinline__ void key_row(const GradArgs& g, uint32_t seq, uint32_t head, uint32_t j, uint32_t from, uint32_t to,
+                                        const float (&k)[D / 64], const float (&v)[D / 64], float (&dk)[D / 64], float (&dv)[D / 64]) {
   constexpr int E = D / 64;
-  float k[E], v[E];
-  load_row<T, E>(row_at(g.k, seq, hk, j), k);
-  load_row<T, E>(row_at(g.v, seq, hk, j), v);
+  for (uint32_t i = from; i < to; ++i) {
+    if (!sees((int32_t)g.n_k - (int32_t)g.n_q + (int32_t)i, j, g.window, g.sinks)) continue;
+    float q[E], d_o[E];
+    load_row<T, E>(row_at(g.q, seq, head, i), q);
+    load_row<T, E>(row_at(g.d_o, seq, head, i), d_o);
+    const size_t at = ((size_t)seq * g.hkv * g.group + head) * g.n_q + i;
+    const float w = __builtin_amdgcn_exp2f(dot<E>(q, k) * g.scale_log2 + (g.neg[at] - kShiftP<T>)), ds = w * (dot<E>(d_o, v) - g.delta[at]);
 #pragma unroll
-  for (int e = 0; e < E; ++e) dk[e] = dv[e] = 0.f;
-  for (uint32_t head = head_from; head < head_to; ++head)
-    for (uint32_t i = from; i < to; ++i) {
-      const int32_t p = (int32_t)g.n_k - (int32_t)g.n_q + (int32_t)i;
-      if (!sees(p, j, g.window, g.sinks)) continue;
-      float q[E], d_o[E];
-      load_row<T, E>(row_at(g.q, seq, head, i), q);
-      load_row<T, E>(row_at(g.d_o, seq, head, i), d_o);
-      const size_t at = ((size_t)seq * g.hkv * g.group + head) * g.n_q + i;
-      const float w = __builtin_amdgcn_exp2f(dot<E>(q, k) * g.scale_log2 - g.lse2[at]), ds = w * (dot<E>(d_o, v) - g.delta[at]);
+    for (int e = 0; e < E; ++e) {
+      dk[e] = __builtin_fmaf(ds, q[e], dk[e]);
+      dv[e] = __builtin_fmaf(w, d_o[e], dv[e]);
+    }
+  }
+}
+
+// ---- tiles of 64 rows in LDS that are read both ways ---------------------------------------------------------------
+// A row's 16-byte chunk c lies at position c ^ swizzle(row).  Read as it lies (32 rows x 16 bytes to a half wave) the 16
+// rows of a pass take all banks; read transposed (four rows x 32 bytes to 16 lanes, two such pieces to a pass) so do they.
+template <int D>
+__device__ __forceinline__ uint32_t swizzle(uint32_t row) {
+  if constexpr (D == 128) return ((row & 3u) << 2) | ((row >> 2) & 3u);
+  else return (((row >> 1) & 1u) << 2) | ((row >> 2) & 3u);
+}
+template <int D>
+struct TileReader {
+  static constexpr uint32_t kRow = 2u * D;
+  static constexpr int NS = D / 16, ND = D / 32;
+  uint32_t row_ofs[NS], col_ofs[ND];  // LDS byte addresses
+  __device__ __forceinline__ TileReader(uint32_t base) {
+    const uint32_t lane = threadIdx.x & 63u, h32 = lane >> 5, l32 = lane & 31u, i = lane & 15u, grp = lane >> 4;
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        dk[e] = __builtin_fmaf(ds, q[e], dk[e]);
-        dv[e] = __builtin_fmaf(w, d_o[e], dv[e]);
+    for (int s = 0; s < NS; ++s) row_ofs[s] = base + l32 * kRow + (((2u * (uint32_t)s + h32) ^ swizzle<D>(l32)) << 4);
+    const uint32_t row = 4u * (grp >> 1) + (i >> 2);
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) {
+      const uint32_t d = 32u * (uint32_t)dt + 16u * (grp & 1u) + 4u * (i & 3u);
+      col_ofs[dt] = base + row * kRow + (((d >> 3) ^ swizzle<D>(row)) << 4) + 8u * ((d >> 2) & 1u);
+    }
+  }
+  __device__ __forceinline__ void move(uint32_t by) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s) row_ofs[s] += by;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) col_ofs[dt] += by;
+  }
+  // rows `from` + l32 (from: a multiple of 32), d = 16 s + 8 h32 .. + 7
+  __device__ __forceinline__ u32x4 rows(int s, uint32_t from) const {
+    typedef const __attribute__((address_space(3))) u32x4* lds_u32x4;
+    return *(lds_u32x4)(uintptr_t)(row_ofs[s] + from * kRow);
+  }
+  // d = 32 dt + l32 of the 16 rows from `from` on, in the order of an accumulator's rows.  The tile has to begin at a
+  // multiple of 64 bytes: kernels that use this have no LDS but the dynamic, which begins at 0.
+  __device__ __forceinline__ u32x4 cols(int dt, uint32_t from) const {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+    const uint32_t a = col_ofs[dt] + from * kRow;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(a));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)((a ^ 32u) + 8u * kRow));  // (swizzle(row + 8) = swizzle(row) ^ 2)
+    const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    return __builtin_bit_cast(u32x4, v);
+  }
+};
+
+// 64 rows from global memory straight to such a tile: 1 KiB to a wave's load.
+template <int D>
+struct TileLoader {
+  static constexpr uint32_t kRow = 2u * D, kChunks = kRow / 16u, kBlockRows = 1024u / kRow;
+  static constexpr int NL = (int)(64u * kRow / 4096u);
+  uint32_t ofs[NL], step, in;  // bytes
+  __device__ __forceinline__ TileLoader(int64_t token_step) {
+    const uint32_t lane = threadIdx.x & 63u, row = first_row();
+    step = (uint32_t)(2 * token_step);
+    in = ((lane % kChunks) ^ swizzle<D>(row)) << 4;
+  }
+  static __device__ __forceinline__ uint32_t first_row() {
+    return kBlockRows * (threadIdx.x >> 6) + (threadIdx.x & 63u) / kChunks;
+  }
+  // rows past `last` are that row again
+  __device__ __forceinline__ void upto(uint32_t last) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const uint32_t row = first_row() + 4u * kBlockRows * (uint32_t)i;
+      ofs[i] = (row < last ? row : last) * step + in;
+    }
+  }
+  // M0 (the LDS base) is put back; the loads are waited for by hand (see kp_attn_tile)
+  __device__ __forceinline__ void load(const uint16_t* base, uint32_t dst) const {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      uint32_t saved_m0;
+      asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+                   : "=&s"(saved_m0) : "v"(ofs[i]), "s"(base), "s"(dst + 4096u * (uint32_t)i) : "memory");
+    }
+  }
+};
+
+// A wave's 32 rows of D accumulators (row l32, d = 32 dt + 8 j + 4 h32 + i), times `by`, through LDS and out as whole rows.
+template <class T, int D>
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float by, unsigned char* lds, uint16_t* to, int64_t at, uint64_t rows_out) {
+  constexpr uint32_t kRow = 2u * D, kChunks = kRow / 16u, kBlockRows = 1024u / kRow;
+  const uint32_t lane = threadIdx.x & 63u, h32 = lane >> 5, l32 = lane & 31u, half = h32 ^ ((l32 >> 3) & 1u);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const u32x2 two = {T::pack(acc[dt][4 * j] * by, acc[dt][4 * j + 1] * by), T::pack(acc[dt][4 * j + 2] * by, acc[dt][4 * j + 3] * by)};
+      *reinterpret_cast<u32x2*>(lds + l32 * kRow + (((uint32_t)(4 * dt + j) ^ (l32 & 7u)) << 4) + 8u * half) = two;
+    }
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < (int)(32u / kBlockRows); ++i) {
+    const uint32_t r = kBlockRows * (uint32_t)i + lane / kChunks, chunk = (lane % kChunks) ^ (r & 7u);
+    const u32x4 v = *reinterpret_cast<const u32x4*>(lds + 1024u * (uint32_t)i + 16u * lane);
+    const int64_t row = (int64_t)(((uint64_t)(uint32_t)__shfl((int)(at >> 32), (int)r, 64) << 32) | (uint32_t)__shfl((int)at, (int)r, 64));
+    if ((rows_out >> r) & 1ull) *reinterpret_cast<u32x4*>(to + row + 8u * chunk) = (r & 8u) ? u32x4{v.z, v.w, v.x, v.y} : v;
+  }
+  asm volatile("" ::: "memory");
+}
+// A NaN where a value of a lane is not finite, else 0.
+template <int N>
+__device__ __forceinline__ float odd_of(const f32x16 (&acc)[N]) {
+  float odd = 0.f;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) odd = __builtin_fmaf(acc[n][v], 0.f, odd);
+  return odd;
+}
+__device__ __forceinline__ float power_of_two_in(float x) {  // the largest power of two <= x (1 for 0), as a number
+  const uint32_t e = __builtin_bit_cast(uint32_t, x) >> 23;
+  return x == 0.f ? 1.f : __builtin_bit_cast(float, (e < 1u ? 1u : e) << 23);
+}
+
+// dq of a tile of 128 rows, and delta and lse for the kernel after it.  Tiles, rows and keys as in kp_attn_tile; K and V
+// tiles in two buffers each.  Per 32 keys: S^T = K Q^T, dP^T = V dO^T, dS^T in place, dq^T += K^T dS^T.  The operands of
+// the three products go through one set of NS registers that is refilled as it is used up, a product ahead.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
+  constexpr uint32_t kTile = 64u * 2u * D;
+  constexpr int NS = D / 16, ND = D / 32;
+  constexpr bool kScaled = std::is_same<T, Fp16>::value;
+  extern __shared__ __align__(16) unsigned char smem[];  // two buffers of [K tile][V tile]
+  const uint32_t lane = threadIdx.x & 63u, wave = kp::wave_uniform(threadIdx.x >> 6), h32 = lane >> 5, l32 = lane & 31u;
+  uint32_t unit, item;
+  unit_of(blockIdx.x, g.seqs * g.hkv, g.row_tiles, &unit, &item);
+  const uint32_t seq = unit / g.hkv, hk = unit - seq * g.hkv, first = (g.row_tiles - 1u - item) * kTileRows;
+  const uint32_t last_row = g.n_q * g.group - 1u, wave_first = first + 32u * wave, flat = wave_first + l32;
+  const bool mine = flat <= last_row;
+  const int32_t off = (int32_t)g.n_k - (int32_t)g.n_q;
+  auto position = [&](uint32_t f) __attribute__((always_inline)) { return off + (int32_t)place_of(f < last_row ? f : last_row, g.group).token; };
+  const RowPlace at = place_of(mine ? flat : last_row, g.group);
+  const uint32_t head = hk * g.group + at.in_group;
+  const int32_t p = off + (int32_t)at.token, p_min = position(wave_first), p_max = position(wave_first + 31u);
+  const Span span = span_of(position(first), position(first + kTileRows - 1u), g.window, g.sinks);
+  const uint32_t sink_tiles = (span.sink_end + 63u) / 64u, tiles = sink_tiles + (span.end > span.lo ? (span.end - span.lo + 63u) / 64u : 0u);
+
+  u32x4 qf[NS], dof[NS];
+  float delta = 0.f, most = 0.f;
+  {
+    const uint16_t *q = row_at(g.q, seq, head, at.token), *d_o = row_at(g.d_o, seq, head, at.token), *o = row_at(g.o, seq, head, at.token);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      qf[s] = *reinterpret_cast<const u32x4*>(q + 16 * s + 8 * h32);
+      dof[s] = *reinterpret_cast<const u32x4*>(d_o + 16 * s + 8 * h32);
+      const u32x4 of = *reinterpret_cast<const u32x4*>(o + 16 * s + 8 * h32);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float a = T::to_float(dof[s][w] & 0xFFFFu), b = T::to_float(dof[s][w] >> 16);
+        delta = __builtin_fmaf(a, T::to_float(of[w] & 0xFFFFu), __builtin_fmaf(b, T::to_float(of[w] >> 16), delta));
+        if constexpr (kScaled) {
+          most = fmaxf(most, __builtin_fabsf(a) < INFINITY ? __builtin_fabsf(a) : 0.f);
+          most = fmaxf(most, __builtin_fabsf(b) < INFINITY ? __builtin_fabsf(b) : 0.f);
+        }
       }
     }
+  }
+  delta += __shfl_xor(delta, 32, 64);
+  const size_t row_no = ((size_t)seq * g.hkv * g.group + head) * g.n_q + at.token;
+  // (a row that sees nothing: any finite number, so that its scores of -inf give 0)
+  const float lse = g.lse[row_no], neg = lse == -INFINITY ? 0.f : kShiftP<T> - lse * kLog2e;
+  if (mine && h32 == 0) g.neg[row_no] = neg;
+  float row_scale = 1.f;  // dS is rounded times this
+  if constexpr (kScaled) {
+    most = either_half_max(most);
+    row_scale = __builtin_ldexpf(1.0f, kShiftS) / power_of_two_in(most);
+    float all = mine ? most : 0.f;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) all = fmaxf(all, __shfl_xor(all, d, 64));
+    float* const most_of = reinterpret_cast<float*>(smem);
+    if (lane == 0) most_of[wave] = all;
+    __syncthreads();
+    if (threadIdx.x == 0) g.most[(size_t)unit * g.row_tiles + (g.row_tiles - 1u - item)] = fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3]));
+    __syncthreads();  // (the tiles go there)
+  }
+  const float neg_p = kScaled ? neg - kShiftP<T> : neg;
+
+  TileReader<D> rd((uint32_t)(uintptr_t)smem);
+  TileLoader<D> lk(g.k.token), lv(g.v.token);
+  const uint32_t lds0 = kp::wave_uniform((uint32_t)(uintptr_t)smem + 1024u * wave);
+  const uint16_t *k_head = row_at(g.k, seq, hk, 0), *v_head = row_at(g.v, seq, hk, 0);
+  uint32_t loaded_last = ~0u, into = 0u;  // `into`: LDS offset of the buffer that the next tiles go to
+  auto tile_start = [&](uint32_t t, uint32_t* limit) __attribute__((always_inline)) {
+    *limit = t < sink_tiles ? span.sink_end : span.end;
+    return t < sink_tiles ? t * 64u : span.lo + (t - sink_tiles) * 64u;
+  };
+  auto request = [&](uint32_t t) __attribute__((always_inline)) {
+    uint32_t limit;
+    const uint32_t start = tile_start(t, &limit), left = limit - 1u - start, last = left < 63u ? left : 63u;
+    if (last != loaded_last) { loaded_last = last; lk.upto(last); lv.upto(last); }
+    lk.load(k_head + g.k.token * (int64_t)start, lds0 + into);
+    lv.load(v_head + g.v.token * (int64_t)start, lds0 + into + kTile);
+    into ^= 2u * kTile;
+  };
+
+  f32x16 acc[ND];  // dq^T: rows d, column = row l32
+#pragma unroll
+  for (int dt = 0; dt < ND; ++dt) acc[dt] = f32x16{0};  // (for rows that see nothing)
+  u32x4 ra[NS];
+  uint32_t other = 2u * kTile;
+  // delta comes from an o that was rounded; the exact one makes sum_j dS_ij = 0, so the sum of a row's dS is what it lacks.
+  // The kernel after this one gets it.  Here it counts for rows that see a few keys (it enters dq by half a step of the
+  // type over the square root of their number): tiles of up to 128 keys are gone over twice.
+  float lacks = 0.f;
+  for (uint32_t pass = tiles - 1u < 2u ? 0u : 1u; pass < 2u && tiles > 0u; ++pass) {
+    if (lacks != 0.f) {
+      delta += lacks;
+      lacks = 0.f;
+    }
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) acc[dt] = f32x16{0};
+    request(0u);
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own count of outstanding loads)
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+    for (int s = 0; s < NS; ++s) ra[s] = rd.rows(s, 0u);
+    for (uint32_t t = 0; t < tiles; ++t) {
+      if (t + 1u < tiles) request(t + 1u);
+      uint32_t limit;
+      const uint32_t start = tile_start(t, &limit);
+      const int32_t end = (int32_t)(start + 64u);
+      bool masked = (end > (int32_t)limit) | (end - 1 > p_min);
+      masked = masked | ((g.window != 0u) & (p_max - (int32_t)start >= (int32_t)g.window) & (end > (int32_t)g.sinks));
+#pragma unroll
+      for (int tk = 0; tk < 2; ++tk) {
+        f32x16 sacc = f32x16{0}, dp = f32x16{0};
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          sacc = T::mfma32(ra[s], qf[s], sacc);
+          ra[s] = rd.rows(s, 64u + 32u * (uint32_t)tk);  // V
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          dp = T::mfma32(ra[s], dof[s], dp);
+          ra[s] = rd.cols(s % ND, 32u * (uint32_t)tk + 16u * (uint32_t)(s / ND));  // K^T
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (masked) {
+          const int32_t base = (int32_t)(start + 4u * h32), hi = (p < (int32_t)limit ? p : (int32_t)limit - 1) - base;
+          const int32_t lo = g.window != 0u ? p - (int32_t)g.window + 1 - base : -base, sk = (int32_t)g.sinks - base;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int32_t c = 32 * tk + 8 * (v >> 2) + (v & 3);
+            const bool seen = (c <= hi) & ((c >= lo) | (c < sk));
+            sacc[v] = seen ? sacc[v] : -INFINITY;
+          }
+        }
+        u32x4 ds[2];
+#pragma unroll
+        for (int v = 0; v < 16; v += 2) {
+          float x[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[v + e], g.scale_log2, neg_p));
+            x[e] = w * (dp[v + e] - delta);
+            lacks += x[e];
+            if constexpr (kScaled) x[e] *= row_scale;
+          }
+          ds[v >> 3][(v >> 1) & 3] = T::pack(x[0], x[1]);
+        }
+        // behind the second half's last operand read: every wave has read these tiles, and the next ones have landed
+        if (tk == 1) {
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          rd.move(other);
+          other = 0u - other;
+        }
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          acc[s % ND] = T::mfma32(ra[s], ds[s / ND], acc[s % ND]);
+          ra[s] = rd.rows(s, tk == 0 ? 32u : 0u);  // K: the upper half, or the next tile (the last time: not used)
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    lacks += __shfl_xor(lacks, 32, 64);
+    lacks = __builtin_fabsf(lacks) < INFINITY ? lacks : 0.f;  // (a value that the row does not see may be in it)
+  }
+  if (mine && h32 == 0) g.delta[row_no] = delta + lacks;
+  uint64_t again = __builtin_amdgcn_ballot_w64(odd_of<ND>(acc) != 0.f && mine);
+  again = (again | again >> 32) & 0xFFFFFFFFull;
+  const uint64_t rows_out = __builtin_amdgcn_ballot_w64(mine) & 0xFFFFFFFFull;
+  __syncthreads();  // (the tiles' room is used below)
+  uint16_t* const dq = const_cast<uint16_t*>(g.dq.at);
+  store_rows<T, D>(acc, kScaled ? g.scale / row_scale : g.scale, smem + 64u * D * wave, dq, g.dq.seq * (int64_t)seq + g.dq.head * (int64_t)head + g.dq.token * (int64_t)at.token, rows_out);
+  if (again != 0ull) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // their first results have left
+    for (; again != 0ull; again &= again - 1ull) {
+      const int r = __builtin_ctzll(again);
+      const RowPlace a = place_of(wave_first + (uint32_t)r, g.group);
+      float out[D / 64];
+      query_row<T, D>(g, seq, hk * g.group + a.in_group, a.token, __shfl(neg, r, 64), __shfl(delta, r, 64), out);
+      put_row<T, D / 64>(const_cast<uint16_t*>(row_at(g.dq, seq, hk * g.group + a.in_group, a.token)), out, g.scale);
+    }
+  }
+}
+
+// Query tokens that see keys of key tile `kt`: [from, to).
+struct Tokens {
+  uint32_t from, to;
+};
+__device__ __forceinline__ Tokens tokens_of(const GradArgs& g, uint32_t kt) {
+  const int64_t off = (int64_t)g.n_k - (int64_t)g.n_q, k0 = (int64_t)kt * kGradKeys;
+  const int64_t k1 = k0 + kGradKeys < (int64_t)g.n_k ? k0 + kGradKeys : (int64_t)g.n_k;  // one past the last key
+  int64_t from = k0 - off, to = g.window != 0u && k0 >= (int64_t)g.sinks ? k1 - 1 + (int64_t)g.window - off : (int64_t)g.n_q;
+  from = from < 0 ? 0 : from;
+  to = to > (int64_t)g.n_q ? (int64_t)g.n_q : to;
+  Tokens t;
+  t.from = from < (int64_t)g.n_q ? (uint32_t)from : g.n_q;
+  t.to = to > from ? (uint32_t)to : t.from;
+  return t;
+}
+
+// dk and dv of 128 keys from a run of the query rows that see them.  A wave holds 32 keys: K and V rows and the sums in
+// registers, 32 x 32 products formed so that a lane has one key (S = Q K^T, dP = dO V^T, dv^T += dO^T P, dk^T += Q^T dS).
+// Steps are 64 tokens of one query head; Q and dO tiles are in LDS, two buffers each, with the rows' lse and delta.
+// Key tiles that hold sinks are seen by all later tokens: their rows are split into runs of about an ordinary tile's length,
+// and so are all tiles' where there are few; the runs' sums are added up by kp_grad_join, in order.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradArgs g) {
+  constexpr uint32_t kTile = 64u * 2u * D;
+  constexpr int NS = D / 16, ND = D / 32;
+  constexpr bool kScaled = std::is_same<T, Fp16>::value;
+  extern __shared__ __align__(16) unsigned char smem[];  // two buffers of [Q tile][dO tile], then two of [neg][delta] of 64 rows
+  constexpr uint32_t kStats = 4u * kTile;
+  const uint32_t lane = threadIdx.x & 63u, wave = kp::wave_uniform(threadIdx.x >> 6), h32 = lane >> 5, l32 = lane & 31u;
+  const uint32_t sink_items = g.sink_tiles * g.sink_runs, per = sink_items + (g.key_tiles - g.sink_tiles) * g.runs;
+  uint32_t unit, item;
+  unit_of(blockIdx.x, g.seqs * g.hkv, per, &unit, &item);
+  const uint32_t seq = unit / g.hkv, hk = unit - seq * g.hkv;
+  const uint32_t runs = item < sink_items ? g.sink_runs : g.runs;
+  const uint32_t kt = item < sink_items ? item / g.sink_runs : g.sink_tiles + (item - sink_items) / g.runs;
+  const uint32_t run = item < sink_items ? item % g.sink_runs : (item - sink_items) % g.runs;
+  const Tokens tok = tokens_of(g, kt);
+  const uint32_t steps_per_head = (tok.to - tok.from + 63u) / 64u, steps = steps_per_head * g.group;
+  const uint32_t s_begin = (uint32_t)((uint64_t)steps * run / runs), s_end = (uint32_t)((uint64_t)steps * (run + 1u) / runs);
+
+  const uint32_t j0 = kt * kGradKeys + 32u * wave, j_last = g.n_k - 1u;
+  const uint32_t j = j0 + l32, j_in = j < j_last ? j : j_last;
+  const int32_t off = (int32_t)g.n_k - (int32_t)g.n_q;
+  u32x4 kf[NS], vf[NS];
+  {
+    const uint16_t *k = row_at(g.k, seq, hk, j_in), *v = row_at(g.v, seq, hk, j_in);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      kf[s] = *reinterpret_cast<const u32x4*>(k + 16 * s + 8 * h32);
+      vf[s] = *reinterpret_cast<const u32x4*>(v + 16 * s + 8 * h32);
+    }
+  }
+  float ds_scale = 1.f;  // dS is rounded times this (and 2^kShiftP, which is in P)
+  if constexpr (kScaled) {
+    float most = 0.f;
+    for (uint32_t i = lane; i < g.row_tiles; i += 64u) most = fmaxf(most, g.most[(size_t)unit * g.row_tiles + i]);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+    ds_scale = __builtin_ldexpf(1.0f, kShiftS - (int)kShiftP<T>) / power_of_two_in(most);
+  }
+
+  TileReader<D> rd((uint32_t)(uintptr_t)smem);
+  TileLoader<D> lq(g.q.token), ld(g.d_o.token);
+  const uint32_t lds0 = kp::wave_uniform((uint32_t)(uintptr_t)smem + 1024u * wave);
+  uint32_t loaded_last = ~0u, into = 0u;
+  auto request = [&](uint32_t step) __attribute__((always_inline)) {
+    const uint32_t in_group = step / steps_per_head, start = tok.from + (step - in_group * steps_per_head) * 64u, head = hk * g.group + in_group;
+    const uint32_t left = tok.to - 1u - start, last = left < 63u ? left : 63u;
+    if (last != loaded_last) { loaded_last = last; lq.upto(last); ld.upto(last); }
+    lq.load(row_at(g.q, seq, head, start), lds0 + into);
+    ld.load(row_at(g.d_o, seq, head, start), lds0 + into + kTile);
+    if (wave < 2u) {  // the rows' neg (wave 0) and delta (wave 1): 4 bytes to a lane
+      const float* from = (wave == 0u ? g.neg : g.delta) + ((size_t)seq * g.hkv * g.group + head) * g.n_q + start;
+      const uint32_t ofs = 4u * (lane < last ? lane : last), dst = kp::wave_uniform((uint32_t)(uintptr_t)smem + kStats + (into != 0u ? 512u : 0u) + 256u * wave);
+      uint32_t saved_m0;
+      asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0"
+                   : "=&s"(saved_m0) : "v"(ofs), "s"(from), "s"(dst) : "memory");
+    }
+    into ^= 2u * kTile;
+  };
+
+  f32x16 dk[ND], dv[ND];  // transposed: rows d, column = key l32
+#pragma unroll
+  for (int dt = 0; dt < ND; ++dt) { dk[dt] = f32x16{0}; dv[dt] = f32x16{0}; }
+  u32x4 ra[NS];
+  if (s_begin < s_end) {
+    request(s_begin);
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own count of outstanding loads)
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+    for (int s = 0; s < NS; ++s) ra[s] = rd.rows(s, 0u);
+    uint32_t other = 2u * kTile, stats = kStats;
+    for (uint32_t step = s_begin; step < s_end; ++step) {
+      if (step + 1u < s_end) request(step + 1u);
+      const uint32_t start = tok.from + (step % steps_per_head) * 64u;
+      auto next_buffer = [&]() __attribute__((always_inline)) {
+        // every wave has read these tiles, and the next ones have landed
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        rd.move(other);
+        other = 0u - other;
+      };
+#pragma unroll
+      for (int rt = 0; rt < 2; ++rt) {
+        // rows of this half: tokens first .. last, positions p0 .. p1; this wave's keys: j0 .. j1
+        const int32_t first = (int32_t)start + 32 * rt, last = first + 31, p0 = off + first, p1 = off + (last < (int32_t)tok.to ? last : (int32_t)tok.to - 1);
+        const int32_t k0 = (int32_t)j0, k1 = (int32_t)(j0 + 31u < j_last ? j0 + 31u : j_last);
+        const bool windowed = (g.window != 0u) & (k1 >= (int32_t)g.sinks);
+        const bool none = (first >= (int32_t)tok.to) | (k0 > (int32_t)j_last) | (p1 < k0) | ((g.window != 0u) & (k0 >= (int32_t)g.sinks) & (p0 - k1 >= (int32_t)g.window));
+        const bool masked = (last >= (int32_t)tok.to) | (p0 < k1) | (windowed & (p1 - k0 >= (int32_t)g.window));
+        if (none) {
+          if (rt == 1) next_buffer();
+#pragma unroll
+          for (int s = 0; s < NS; ++s) ra[s] = rd.rows(s, rt == 0 ? 32u : 0u);
+          continue;
+        }
+        f32x16 sacc = f32x16{0}, dp = f32x16{0};
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          sacc = T::mfma32(ra[s], kf[s], sacc);
+          ra[s] = rd.rows(s, 64u + 32u * (uint32_t)rt);  // dO
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        f32x4 neg[4], delta[4];  // of rows 8 i + 4 h32 .. + 3
+        const unsigned char* const st = smem + stats + 128u * (uint32_t)rt + 16u * h32;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          neg[i] = *reinterpret_cast<const f32x4*>(st + 32 * i);
+          delta[i] = *reinterpret_cast<const f32x4*>(st + 256 + 32 * i);
+        }
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          dp = T::mfma32(ra[s], vf[s], dp);
+          ra[s] = rd.cols(s % ND, 64u + 32u * (uint32_t)rt + 16u * (uint32_t)(s / ND));  // dO^T
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (masked) {
+          const int32_t base = first + 4 * (int32_t)h32;  // token of element c: base + c
+          const int32_t lo = (int32_t)j - off - base;
+          int32_t hi = (int32_t)tok.to - 1 - base;
+          const int32_t w = (int32_t)j + (int32_t)g.window - 1 - off - base;
+          hi = ((g.window != 0u) & (j >= g.sinks) & (w < hi)) ? w : hi;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int32_t c = 8 * (v >> 2) + (v & 3);
+            const bool seen = (c >= lo) & (c <= hi);
+            sacc[v] = seen ? sacc[v] : -INFINITY;
+          }
+        }
+        u32x4 pw[2], ds[2];
+#pragma unroll
+        for (int v = 0; v < 16; v += 2) {
+          float w[2], x[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[v + e], g.scale_log2, neg[v >> 2][(v & 3) + e]));
+            x[e] = w[e] * (dp[v + e] - delta[v >> 2][(v & 3) + e]);
+            if constexpr (kScaled) x[e] *= ds_scale;
+          }
+          pw[v >> 3][(v >> 1) & 3] = T::pack(w[0], w[1]);
+          ds[v >> 3][(v >> 1) & 3] = T::pack(x[0], x[1]);
+        }
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          dv[s % ND] = T::mfma32(ra[s], pw[s / ND], dv[s % ND]);
+          ra[s] = rd.cols(s % ND, 32u * (uint32_t)rt + 16u * (uint32_t)(s / ND));  // Q^T
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (rt == 1) next_buffer();
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          dk[s % ND] = T::mfma32(ra[s], ds[s / ND], dk[s % ND]);
+          ra[s] = rd.rows(s, rt == 0 ? 32u : 0u);  // Q: the other half, or the next step's (the last time: not used)
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      stats ^= kStats ^ (kStats + 512u);
+    }
+  }
+
+  const float by_k = kScaled ? g.scale / (ds_scale * __builtin_ldexpf(1.0f, (int)kShiftP<T>)) : g.scale;
+  const float by_v = kScaled ? __builtin_ldexpf(1.0f, -(int)kShiftP<T>) : 1.f;
+  const bool mine = j <= j_last;
+  uint64_t again = __builtin_amdgcn_ballot_w64((odd_of<ND>(dk) != 0.f || odd_of<ND>(dv) != 0.f) && mine);
+  again = (again | again >> 32) & 0xFFFFFFFFull;
+  const uint64_t rows_out = __builtin_amdgcn_ballot_w64(mine) & 0xFFFFFFFFull;
+  // run `run` of this tile among the partial sums: the sink tiles' first
+  const uint32_t sink_slots = g.sink_runs > 1u ? sink_items : 0u, slots = sink_slots + (g.runs > 1u ? per - sink_items : 0u);
+  const size_t slot = (size_t)unit * slots + (item < sink_items ? item : sink_slots + (item - sink_items));
+  float* const part = g.part + slot * (2u * kGradKeys * D) + (size_t)(32u * wave) * D;
+  __syncthreads();  // (the tiles' room is used below)
+  if (runs > 1u) {
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float* to = part + l32 * D + 32 * dt + 8 * i + 4 * h32;
+        *reinterpret_cast<f32x4*>(to) = f32x4{dk[dt][4 * i] * by_k, dk[dt][4 * i + 1] * by_k, dk[dt][4 * i + 2] * by_k, dk[dt][4 * i + 3] * by_k};
+        *reinterpret_cast<f32x4*>(to + kGradKeys * D) = f32x4{dv[dt][4 * i] * by_v, dv[dt][4 * i + 1] * by_v, dv[dt][4 * i + 2] * by_v, dv[dt][4 * i + 3] * by_v};
+      }
+  } else {
+    store_rows<T, D>(dk, by_k, smem + 64u * D * wave, const_cast<uint16_t*>(g.dk.at), g.dk.seq * (int64_t)seq + g.dk.head * (int64_t)hk + g.dk.token * (int64_t)j_in, rows_out);
+    store_rows<T, D>(dv, by_v, smem + 64u * D * wave, const_cast<uint16_t*>(g.dv.at), g.dv.seq * (int64_t)seq + g.dv.head * (int64_t)hk + g.dv.token * (int64_t)j_in, rows_out);
+  }
+  if (again != 0ull) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // their first results have left
+    for (; again != 0ull; again &= again - 1ull) {
+      const uint32_t r = (uint32_t)__builtin_ctzll(again), key = j0 + r;
+      constexpr int E = D / 64;
+      float k[E], v[E], out_k[E] = {}, out_v[E] = {};
+      load_row<T, E>(row_at(g.k, seq, hk, key), k);
+      load_row<T, E>(row_at(g.v, seq, hk, key), v);
+      for (uint32_t step = s_begin; step < s_end; ++step) {
+        const uint32_t in_group = step / steps_per_head, start = tok.from + (step - in_group * steps_per_head) * 64u;
+        key_row<T, D>(g, seq, hk * g.group + in_group, key, start, start + 64u < tok.to ? start + 64u : tok.to, k, v, out_k, out_v);
+      }
+      if (runs > 1u) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          part[r * D + lane * E + e] = out_k[e] * g.scale;
+          part[kGradKeys * D + r * D + lane * E + e] = out_v[e];
+        }
+      } else {
+        put_row<T, E>(const_cast<uint16_t*>(row_at(g.dk, seq, hk, key)), out_k, g.scale);
+        put_row<T, E>(const_cast<uint16_t*>(row_at(g.dv, seq, hk, key)), out_v, 1.f);
+      }
+    }
+  }
+}
+
+// Adds up the runs' sums of the key tiles that were split: D / 4 lanes to a row, four elements to a lane; blockIdx.y: dk or dv.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void kp_grad_join(GradArgs g) {
+  constexpr uint32_t kLanes = D / 4, kPer = kThreads / kLanes, kBlocks = kGradKeys / kPer;
+  const uint32_t sink_items = g.sink_tiles * g.sink_runs, per = sink_items + (g.key_tiles - g.sink_tiles) * g.runs;
+  const uint32_t sink_split = g.sink_runs > 1u ? g.sink_tiles : 0u, split = sink_split + (g.runs > 1u ? g.key_tiles - g.sink_tiles : 0u);
+  const uint32_t tile = blockIdx.x / kBlocks, unit = tile / split, n = tile - unit * split;
+  const bool sink = n < sink_split;
+  const uint32_t kt = sink ? n : g.sink_tiles + (n - sink_split), runs = sink ? g.sink_runs : g.runs;
+  const uint32_t r = (blockIdx.x % kBlocks) * kPer + threadIdx.x / kLanes, c = threadIdx.x % kLanes, j = kt * kGradKeys + r;
+  if (j >= g.n_k) return;
+  const uint32_t sink_slots = g.sink_runs > 1u ? sink_items : 0u, slots = sink_slots + (g.runs > 1u ? per - sink_items : 0u);
+  const size_t slot = (size_t)unit * slots + (sink ? n * g.sink_runs : sink_slots + (n - sink_split) * g.runs);
+  const float* from = g.part + slot * (2u * kGradKeys * D) + (size_t)blockIdx.y * (kGradKeys * D) + (size_t)r * D + 4u * c;
+  f32x4 sum = *reinterpret_cast<const f32x4*>(from);
+  for (uint32_t i = 1; i < runs; ++i) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(from + (size_t)i * (2u * kGradKeys * D));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += x[e];
+  }
+  const uint32_t seq = unit / g.hkv, hk = unit - seq * g.hkv;
+  const Heads& out = blockIdx.y ? g.dv : g.dk;
+  *reinterpret_cast<u32x2*>(const_cast<uint16_t*>(row_at(out, seq, hk, j)) + 4u * c) = u32x2{T::pack(sum[0], sum[1]), T::pack(sum[2], sum[3])};
+}
+
+// Tiles of a call and how they are split.
+struct GradPlan {
+  long long units, row_tiles, key_tiles, sink_tiles, sink_runs, runs, items, split;  // items: workgroups of kp_grad_keys per unit
+  size_t rows, part_at, most_at, bytes;  // rows: query rows; byte offsets into the workspace
+};
+GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks) {
+  GradPlan p{};
+  const long long group = Hq / Hkv, head_steps = (Sq + 63) / 64;
+  p.units = (long long)B * Hkv;
+  p.row_tiles = (group * Sq + kTileRows - 1) / kTileRows;
+  p.key_tiles = (Sk + kGradKeys - 1) / kGradKeys;
+  // steps of 64 tokens of an ordinary key tile, and of one that all tokens see
+  long long steps = window > 0 ? ((long long)window + kGradKeys + 62) / 64 + 1 : head_steps;
+  steps = (steps < head_steps ? steps : head_steps) * group;
+  const long long sink_steps = head_steps * group;
+  p.sink_tiles = window > 0 ? (sinks + (long long)kGradKeys - 1) / kGradKeys : 0;
+  if (p.sink_tiles > p.key_tiles) p.sink_tiles = p.key_tiles;
+  // enough workgroups for the chip (two per CU for D = 64, one for 128), as long as a run has four steps
+  const long long want = D == 64 ? 512 : 256, tiles = p.units * p.key_tiles;
+  p.runs = tiles * 2 > want ? 1 : want / tiles;
+  if (p.runs > steps / 4) p.runs = steps / 4;
+  if (p.runs < 1) p.runs = 1;
+  p.sink_runs = p.sink_tiles > 0 ? (sink_steps * p.runs + steps - 1) / steps : 1;
+  if (p.sink_runs > 256) p.sink_runs = 256;
+  if (p.sink_tiles == 0) p.sink_runs = 1;
+  p.items = p.sink_tiles * p.sink_runs + (p.key_tiles - p.sink_tiles) * p.runs;
+  p.split = (p.sink_runs > 1 ? p.sink_tiles : 0) + (p.runs > 1 ? p.key_tiles - p.sink_tiles : 0);
+  const long long slots = (p.sink_runs > 1 ? p.sink_tiles * p.sink_runs : 0) + (p.runs > 1 ? (p.key_tiles - p.sink_tiles) * p.runs : 0);
+  p.rows = (size_t)B * (size_t)Hq * (size_t)Sq;
+  const auto up = [](size_t n) { return (n + 15) & ~(size_t)15; };
+  p.most_at = up(8 * p.rows);
+  p.part_at = up(p.most_at + 4 * (size_t)(p.units * p.row_tiles));
+  p.bytes = p.part_at + (size_t)(p.units * slots) * (2u * kGradKeys * 4u) * (size_t)D;
+  return p;
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(kThreads) void kp_grad_query_rows(GradArgs g) {
-  constexpr int E = D / 64;
-  const uint64_t row = (uint64_t)blockIdx.x * 4u + (threadIdx.x >> 6);
-  if (row >= (uint64_t)g.seqs * g.hkv * g.group * g.n_q) return;
-  const uint32_t token = (uint32_t)(row % g.n_q), bh = (uint32_t)(row / g.n_q), seq = bh / (g.hkv * g.group), head = bh % (g.hkv * g.group);
-  float o[E], d_o[E], dq[E];
-  load_row<T, E>(row_at(g.o, seq, head, token), o);
-  load_row<T, E>(row_at(g.d_o, seq, head, token), d_o);
-  const float delta = dot<E>(o, d_o), lse2 = g.lse[row] * kLog2e;
-  if ((threadIdx.x & 63u) == 0) { g.lse2[row] = lse2; g.delta[row] = delta; }
-  query_row<T, D>(g, seq, head, token, lse2, delta, dq);
-  put_row<T, E>(const_cast<uint16_t*>(row_at(g.dq, seq, head, token)), dq, g.scale);
-}
-
-template <class T, int D>
-__global__ __launch_bounds__(kThreads) void kp_grad_key_rows(GradArgs g) {
-  constexpr int E = D / 64;
-  const uint64_t row = (uint64_t)blockIdx.x * 4u + (threadIdx.x >> 6);
-  if (row >= (uint64_t)g.seqs * g.hkv * g.n_k) return;
-  const uint32_t j = (uint32_t)(row % g.n_k), bh = (uint32_t)(row / g.n_k), seq = bh / g.hkv, hk = bh % g.hkv;
-  float dk[E], dv[E];
-  key_row<T, D>(g, seq, hk, j, hk * g.group, (hk + 1u) * g.group, 0u, g.n_q, dk, dv);
-  put_row<T, E>(const_cast<uint16_t*>(row_at(g.dk, seq, hk, j)), dk, g.scale);
-  put_row<T, E>(const_cast<uint16_t*>(row_at(g.dv, seq, hk, j)), dv, 1.f);
+kp_status launch_grad(GradArgs& g, const GradPlan& p, hipStream_t st) {
+  constexpr uint32_t kTiles = 4u * 64u * 2u * D;
+  hipLaunchKernelGGL((kp_grad_query<T, D>), dim3((uint32_t)(p.units * p.row_tiles)), dim3(kThreads), kTiles, st, g);
+  KP_HIP_TRY(hipGetLastError());
+  hipLaunchKernelGGL((kp_grad_keys<T, D>), dim3((uint32_t)(p.units * p.items)), dim3(kThreads), kTiles + 1024u, st, g);
+  KP_HIP_TRY(hipGetLastError());
+  if (p.split > 0) {
+    hipLaunchKernelGGL((kp_grad_join<T, D>), dim3((uint32_t)(p.units * p.split * (kGradKeys / (kThreads / (D / 4)))), 2), dim3(kThreads), 0, st, g);
+    KP_HIP_TRY(hipGetLastError());
+  }
+  return KP_OK;
 }
 
 bool sizes_ok(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks) {
@@ -127,7 +716,7 @@ bool sizes_ok(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sin
 
 extern "C" size_t kp_attn_window_grad_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks) {
   if (!sizes_ok(B, Hq, Hkv, Sq, Sk, D, window, sinks)) return 0;
-  return (size_t)B * (size_t)Hq * (size_t)Sq * 8;
+  return plan_grad(B, Hq, Hkv, Sq, Sk, D, window, sinks).bytes;
 }
 
 extern "C" kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, const kp_heads* v, const kp_heads* o,
@@ -144,26 +733,21 @@ extern "C" kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, c
   for (const auto& a : all)
     if (kp_status s = check_heads(a.name, a.t, B, a.query ? Hq : Hkv, a.query ? Sq : Sk, D, a.written)) return s;
   if (!lse || ((uintptr_t)lse & 3u)) return kp::fail(KP_ERR_INVALID_ARG, "lse must be device memory, 4-byte aligned");
-  if (kp_status s = check_workspace(workspace, workspace_bytes, kp_attn_window_grad_bytes(B, Hq, Hkv, Sq, Sk, D, window, sinks))) return s;
+  const GradPlan p = plan_grad(B, Hq, Hkv, Sq, Sk, D, window, sinks);
+  if (p.units * p.row_tiles >= (1ll << 31) || p.units * p.items >= (1ll << 31) || p.units * p.split * 16 >= (1ll << 31)) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^31 or more workgroups");
+  if (kp_status s = check_workspace(workspace, workspace_bytes, p.bytes)) return s;
   GradArgs g{};
   g.q = heads_of(q, B, Hq, Sq); g.o = heads_of(o, B, Hq, Sq); g.d_o = heads_of(d_o, B, Hq, Sq); g.dq = heads_of(dq, B, Hq, Sq);
   g.k = heads_of(k, B, Hkv, Sk); g.v = heads_of(v, B, Hkv, Sk); g.dk = heads_of(dk, B, Hkv, Sk); g.dv = heads_of(dv, B, Hkv, Sk);
   g.lse = lse;
-  const size_t rows = (size_t)B * (size_t)Hq * (size_t)Sq;
-  g.lse2 = static_cast<float*>(workspace); g.delta = g.lse2 + rows;
+  char* const ws = static_cast<char*>(workspace);
+  g.neg = reinterpret_cast<float*>(ws); g.delta = g.neg + p.rows;
+  g.most = reinterpret_cast<float*>(ws + p.most_at); g.part = reinterpret_cast<float*>(ws + p.part_at);
+  g.row_tiles = (uint32_t)p.row_tiles; g.key_tiles = (uint32_t)p.key_tiles; g.sink_tiles = (uint32_t)p.sink_tiles;
+  g.sink_runs = (uint32_t)p.sink_runs; g.runs = (uint32_t)p.runs;
   g.seqs = (uint32_t)B; g.hkv = (uint32_t)Hkv; g.group = (uint32_t)(Hq / Hkv); g.n_q = (uint32_t)Sq; g.n_k = (uint32_t)Sk;
   g.window = (uint32_t)window; g.sinks = (uint32_t)sinks; g.scale = scale; g.scale_log2 = scale * kLog2e;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const size_t keys = (size_t)B * (size_t)Hkv * (size_t)Sk;
-  if ((rows + 3) / 4 >= (1ull << 31) || (keys + 3) / 4 >= (1ull << 31)) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^31 or more workgroups");
-#define KP_LAUNCH(T, D)                                                                                              \
-  do {                                                                                                               \
-    hipLaunchKernelGGL((kp_grad_query_rows<T, D>), dim3((uint32_t)((rows + 3) / 4)), dim3(kThreads), 0, st, g);      \
-    hipLaunchKernelGGL((kp_grad_key_rows<T, D>), dim3((uint32_t)((keys + 3) / 4)), dim3(kThreads), 0, st, g);        \
-  } while (0)
-  if (type == KP_BF16) { if (D == 64) KP_LAUNCH(Bf16, 64); else KP_LAUNCH(Bf16, 128); }
-  else { if (D == 64) KP_LAUNCH(Fp16, 64); else KP_LAUNCH(Fp16, 128); }
-#undef KP_LAUNCH
-  KP_HIP_TRY(hipGetLastError());
-  return KP_OK;
+  if (type == KP_FP16) return D == 64 ? launch_grad<Fp16, 64>(g, p, st) : launch_grad<Fp16, 128>(g, p, st);
+  return D == 64 ? launch_grad<Bf16, 64>(g, p, st) : launch_grad<Bf16, 128>(g, p, st);
 }
