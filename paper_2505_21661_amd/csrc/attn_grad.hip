@@ -112,39 +112,28 @@ __device__ __forceinline__ uint32_t swizzle(uint32_t row) {
 template <int D>
 struct TileReader {
   static constexpr uint32_t kRow = 2u * D;
-  static constexpr int NS = D / 16, ND = D / 32;
-  uint32_t row_ofs[NS], col_ofs[ND];  // LDS byte addresses
+  // LDS byte addresses of row l32's first chunk and of the transposing read's first piece; other chunks are an exclusive or
+  // away (the tile begins at a multiple of 256 bytes: kernels that use this have no LDS but the dynamic, which begins at 0)
+  uint32_t row0, col0;
   __device__ __forceinline__ TileReader(uint32_t base) {
     const uint32_t lane = threadIdx.x & 63u, h32 = lane >> 5, l32 = lane & 31u, i = lane & 15u, grp = lane >> 4;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) row_ofs[s] = base + l32 * kRow + (((2u * (uint32_t)s + h32) ^ swizzle<D>(l32)) << 4);
-    const uint32_t row = 4u * (grp >> 1) + (i >> 2);
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt) {
-      const uint32_t d = 32u * (uint32_t)dt + 16u * (grp & 1u) + 4u * (i & 3u);
-      col_ofs[dt] = base + row * kRow + (((d >> 3) ^ swizzle<D>(row)) << 4) + 8u * ((d >> 2) & 1u);
-    }
+    row0 = base + l32 * kRow + ((h32 ^ swizzle<D>(l32)) << 4);
+    const uint32_t row = 4u * (grp >> 1) + (i >> 2), d = 16u * (grp & 1u) + 4u * (i & 3u);
+    col0 = base + row * kRow + (((d >> 3) ^ swizzle<D>(row)) << 4) + 8u * ((d >> 2) & 1u);
   }
-  __device__ __forceinline__ void move(uint32_t by) {
-#pragma unroll
-    for (int s = 0; s < NS; ++s) row_ofs[s] += by;
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt) col_ofs[dt] += by;
-  }
-  // rows `from` + l32 (from: a multiple of 32), d = 16 s + 8 h32 .. + 7
-  __device__ __forceinline__ u32x4 rows(int s, uint32_t from) const {
+  // rows `from` + l32 (from: a multiple of 32), d = 16 s + 8 h32 .. + 7; buffer: its distance from the first
+  __device__ __forceinline__ u32x4 rows(int s, uint32_t from, uint32_t buffer) const {
     typedef const __attribute__((address_space(3))) u32x4* lds_u32x4;
-    return *(lds_u32x4)(uintptr_t)(row_ofs[s] + from * kRow);
+    return *(lds_u32x4)(uintptr_t)(((row0 ^ (32u * (uint32_t)s)) + buffer) + from * kRow);
   }
-  // d = 32 dt + l32 of the 16 rows from `from` on, in the order of an accumulator's rows.  The tile has to begin at a
-  // multiple of 64 bytes: kernels that use this have no LDS but the dynamic, which begins at 0.
-  __device__ __forceinline__ u32x4 cols(int dt, uint32_t from) const {
+  // d = 32 dt + l32 of the 16 rows from `from` on, in the order of an accumulator's rows
+  __device__ __forceinline__ u32x4 cols(int dt, uint32_t from, uint32_t buffer) const {
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
     typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
-    const uint32_t a = col_ofs[dt] + from * kRow;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(a));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)((a ^ 32u) + 8u * kRow));  // (swizzle(row + 8) = swizzle(row) ^ 2)
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(((col0 ^ (64u * (uint32_t)dt)) + buffer) + from * kRow));
+    // (swizzle(row + 8) = swizzle(row) ^ 2)
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(((col0 ^ (64u * (uint32_t)dt + 32u)) + buffer) + (from + 8u) * kRow));
     const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     return __builtin_bit_cast(u32x4, v);
   }
@@ -221,8 +210,7 @@ __device__ __forceinline__ float power_of_two_in(float x) {  // the largest powe
 }
 
 // dq of a tile of 128 rows, and delta and lse for the kernel after it.  Tiles, rows and keys as in kp_attn_tile; K and V
-// tiles in two buffers each.  Per 32 keys: S^T = K Q^T, dP^T = V dO^T, dS^T in place, dq^T += K^T dS^T.  The operands of
-// the three products go through one set of NS registers that is refilled as it is used up, a product ahead.
+// tiles in two buffers each.  Per 32 keys: S^T = K Q^T, dP^T = V dO^T, dS^T from them, dq^T += K^T dS^T.
 template <class T, int D>
 __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
   constexpr uint32_t kTile = 64u * 2u * D;
@@ -303,25 +291,27 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
 
   f32x16 acc[ND];  // dq^T: rows d, column = row l32
 #pragma unroll
-  for (int dt = 0; dt < ND; ++dt) acc[dt] = f32x16{0};  // (for rows that see nothing)
-  u32x4 ra[NS];
-  uint32_t other = 2u * kTile;
-  // delta comes from an o that was rounded; the exact one makes sum_j dS_ij = 0, so the sum of a row's dS is what it lacks.
-  // The kernel after this one gets it.  Here it counts for rows that see a few keys (it enters dq by half a step of the
-  // type over the square root of their number): tiles of up to 128 keys are gone over twice.
+  for (int dt = 0; dt < ND; ++dt) acc[dt] = f32x16{0};
+  // The operands of the three products come out of LDS LA MFMAs ahead, in one set of registers.
+  constexpr int LA = 4;
+  u32x4 ra[LA];
+  uint32_t buffer = 0u;
+  // operand n of the half tile tk: K rows, V rows, K^T; from 3 NS on the half after it
+  auto fetch = [&](int n, int tk) __attribute__((always_inline)) {
+    if (n >= 3 * NS) { n -= 3 * NS; tk ^= 1; }
+    if (n < NS) return rd.rows(n, 32u * (uint32_t)tk, buffer);
+    if (n < 2 * NS) return rd.rows(n - NS, 64u + 32u * (uint32_t)tk, buffer);
+    return rd.cols((n - 2 * NS) % ND, 32u * (uint32_t)tk + 16u * (uint32_t)((n - 2 * NS) / ND), buffer);
+  };
   float lacks = 0.f;
-  for (uint32_t pass = tiles - 1u < 2u ? 0u : 1u; pass < 2u && tiles > 0u; ++pass) {
-    if (lacks != 0.f) {
-      delta += lacks;
-      lacks = 0.f;
-    }
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt) acc[dt] = f32x16{0};
+  // Over all keys; CHECK: with the sum of dS.
+  auto over_keys = [&](auto check_c) __attribute__((always_inline)) {
+    constexpr bool CHECK = decltype(check_c)::value;
     request(0u);
     __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own count of outstanding loads)
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-    for (int s = 0; s < NS; ++s) ra[s] = rd.rows(s, 0u);
+    for (int n = 0; n < LA; ++n) ra[n] = fetch(n, 0);
     for (uint32_t t = 0; t < tiles; ++t) {
       if (t + 1u < tiles) request(t + 1u);
       uint32_t limit;
@@ -332,18 +322,15 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
 #pragma unroll
       for (int tk = 0; tk < 2; ++tk) {
         f32x16 sacc = f32x16{0}, dp = f32x16{0};
+        __builtin_amdgcn_s_setprio(2);
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          sacc = T::mfma32(ra[s], qf[s], sacc);
-          ra[s] = rd.rows(s, 64u + 32u * (uint32_t)tk);  // V
+        for (int n = 0; n < 2 * NS; ++n) {
+          if (n < NS) sacc = T::mfma32(ra[n % LA], qf[n], sacc);
+          else dp = T::mfma32(ra[n % LA], dof[n - NS], dp);
+          ra[n % LA] = fetch(n + LA, tk);
           __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          dp = T::mfma32(ra[s], dof[s], dp);
-          ra[s] = rd.cols(s % ND, 32u * (uint32_t)tk + 16u * (uint32_t)(s / ND));  // K^T
-          __builtin_amdgcn_sched_barrier(0);
-        }
+        __builtin_amdgcn_s_setprio(0);
         if (masked) {
           const int32_t base = (int32_t)(start + 4u * h32), hi = (p < (int32_t)limit ? p : (int32_t)limit - 1) - base;
           const int32_t lo = g.window != 0u ? p - (int32_t)g.window + 1 - base : -base, sk = (int32_t)g.sinks - base;
@@ -362,29 +349,42 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
           for (int e = 0; e < 2; ++e) {
             const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[v + e], g.scale_log2, neg_p));
             x[e] = w * (dp[v + e] - delta);
-            lacks += x[e];
+            if constexpr (CHECK) lacks += x[e];
             if constexpr (kScaled) x[e] *= row_scale;
           }
           ds[v >> 3][(v >> 1) & 3] = T::pack(x[0], x[1]);
         }
-        // behind the second half's last operand read: every wave has read these tiles, and the next ones have landed
-        if (tk == 1) {
-          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-          rd.move(other);
-          other = 0u - other;
-        }
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          acc[s % ND] = T::mfma32(ra[s], ds[s / ND], acc[s % ND]);
-          ra[s] = rd.rows(s, tk == 0 ? 32u : 0u);  // K: the upper half, or the next tile (the last time: not used)
+        for (int n = 2 * NS; n < 3 * NS; ++n) {
+          const int s = n - 2 * NS;
+          // behind the tile's last operand read: every wave has read these tiles, and the next ones have landed
+          if (tk == 1 && s == NS - LA) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            buffer ^= 2u * kTile;
+          }
+          acc[s % ND] = T::mfma32(ra[n % LA], ds[s / ND], acc[s % ND]);
+          ra[n % LA] = fetch(n + LA, tk);  // (behind the last tile: not used)
           __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
       }
     }
+  };
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  // delta comes from an o that was rounded; the exact one makes sum_j dS_ij = 0, so the sum of a row's dS is what it lacks.
+  // That enters dq as half a step of the type over the square root of the number of keys that count, which shows where a
+  // row sees a few: tiles of up to 128 keys are gone over twice, first for the sum.
+  if (tiles - 1u < 2u) {
+    over_keys(yes);
     lacks += __shfl_xor(lacks, 32, 64);
-    lacks = __builtin_fabsf(lacks) < INFINITY ? lacks : 0.f;  // (a value that the row does not see may be in it)
+    delta += __builtin_fabsf(lacks) < INFINITY ? lacks : 0.f;  // (a value that the row does not see may be in it)
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) acc[dt] = f32x16{0};
   }
-  if (mine && h32 == 0) g.delta[row_no] = delta + lacks;
+  if (tiles != 0u) over_keys(no);
+  if (mine && h32 == 0) g.delta[row_no] = delta;
   uint64_t again = __builtin_amdgcn_ballot_w64(odd_of<ND>(acc) != 0.f && mine);
   again = (again | again >> 32) & 0xFFFFFFFFull;
   const uint64_t rows_out = __builtin_amdgcn_ballot_w64(mine) & 0xFFFFFFFFull;
@@ -421,16 +421,19 @@ __device__ __forceinline__ Tokens tokens_of(const GradArgs& g, uint32_t kt) {
 
 // dk and dv of 128 keys from a run of the query rows that see them.  A wave holds 32 keys: K and V rows and the sums in
 // registers, 32 x 32 products formed so that a lane has one key (S = Q K^T, dP = dO V^T, dv^T += dO^T P, dk^T += Q^T dS).
-// Steps are 64 tokens of one query head; Q and dO tiles are in LDS, two buffers each, with the rows' lse and delta.
+// Steps are 64 tokens of one query head; Q and dO tiles are in LDS, three buffers each, with the rows' lse and delta.
+// For D = 128 these registers leave room for one wave on a SIMD, which has to overlap its own vector and matrix
+// instructions: S and dP of the next 32 rows are formed while those of the current ones become P and dS, element by
+// element between the MFMAs; dv and dk of the current rows follow.
 // Key tiles that hold sinks are seen by all later tokens: their rows are split into runs of about an ordinary tile's length,
 // and so are all tiles' where there are few; the runs' sums are added up by kp_grad_join, in order.
 template <class T, int D>
 __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradArgs g) {
-  constexpr uint32_t kTile = 64u * 2u * D;
+  constexpr uint32_t kTile = 64u * 2u * D, kBuffer = 2u * kTile;
   constexpr int NS = D / 16, ND = D / 32;
   constexpr bool kScaled = std::is_same<T, Fp16>::value;
-  extern __shared__ __align__(16) unsigned char smem[];  // two buffers of [Q tile][dO tile], then two of [neg][delta] of 64 rows
-  constexpr uint32_t kStats = 4u * kTile;
+  extern __shared__ __align__(16) unsigned char smem[];  // three buffers of [Q tile][dO tile], then three of [neg][delta] of 64 rows
+  constexpr uint32_t kStats = 3u * kBuffer;
   const uint32_t lane = threadIdx.x & 63u, wave = kp::wave_uniform(threadIdx.x >> 6), h32 = lane >> 5, l32 = lane & 31u;
   const uint32_t sink_items = g.sink_tiles * g.sink_runs, per = sink_items + (g.key_tiles - g.sink_tiles) * g.runs;
   uint32_t unit, item;
@@ -464,121 +467,141 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradAr
     ds_scale = __builtin_ldexpf(1.0f, kShiftS - (int)kShiftP<T>) / power_of_two_in(most);
   }
 
-  TileReader<D> rd((uint32_t)(uintptr_t)smem);
+  const TileReader<D> rd((uint32_t)(uintptr_t)smem);
   TileLoader<D> lq(g.q.token), ld(g.d_o.token);
   const uint32_t lds0 = kp::wave_uniform((uint32_t)(uintptr_t)smem + 1024u * wave);
-  uint32_t loaded_last = ~0u, into = 0u;
+  uint32_t loaded_last = ~0u, into = 0u;  // `into`: number of the buffer that the next step goes to
+  auto after = [](uint32_t buffer) __attribute__((always_inline)) { return buffer == 2u ? 0u : buffer + 1u; };
   auto request = [&](uint32_t step) __attribute__((always_inline)) {
     const uint32_t in_group = step / steps_per_head, start = tok.from + (step - in_group * steps_per_head) * 64u, head = hk * g.group + in_group;
     const uint32_t left = tok.to - 1u - start, last = left < 63u ? left : 63u;
     if (last != loaded_last) { loaded_last = last; lq.upto(last); ld.upto(last); }
-    lq.load(row_at(g.q, seq, head, start), lds0 + into);
-    ld.load(row_at(g.d_o, seq, head, start), lds0 + into + kTile);
+    lq.load(row_at(g.q, seq, head, start), lds0 + into * kBuffer);
+    ld.load(row_at(g.d_o, seq, head, start), lds0 + into * kBuffer + kTile);
     if (wave < 2u) {  // the rows' neg (wave 0) and delta (wave 1): 4 bytes to a lane
       const float* from = (wave == 0u ? g.neg : g.delta) + ((size_t)seq * g.hkv * g.group + head) * g.n_q + start;
-      const uint32_t ofs = 4u * (lane < last ? lane : last), dst = kp::wave_uniform((uint32_t)(uintptr_t)smem + kStats + (into != 0u ? 512u : 0u) + 256u * wave);
+      const uint32_t ofs = 4u * (lane < last ? lane : last), dst = kp::wave_uniform((uint32_t)(uintptr_t)smem + kStats + into * 512u + 256u * wave);
       uint32_t saved_m0;
       asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0"
                    : "=&s"(saved_m0) : "v"(ofs), "s"(from), "s"(dst) : "memory");
     }
-    into ^= 2u * kTile;
+    into = after(into);
+  };
+  // First token of a half step of 32 rows, and whether it has pairs of a token and a key of this wave that are not visible.
+  // (A wave whose keys none of them sees goes along all the same: the others wait for it at the next barrier anyway.)
+  struct Half {
+    int32_t first;
+    bool masked;
+  };
+  auto half_of = [&](uint32_t step, int rt) __attribute__((always_inline)) {
+    Half h;
+    h.first = (int32_t)(tok.from + (step % steps_per_head) * 64u) + 32 * rt;
+    const int32_t last = h.first + 31, k0 = (int32_t)j0, k1 = (int32_t)j0 + 31;
+    h.masked = (last >= (int32_t)tok.to) | (off + h.first < k1) | ((g.window != 0u) & (k1 >= (int32_t)g.sinks) & (off + last - k0 >= (int32_t)g.window));
+    return h;
   };
 
   f32x16 dk[ND], dv[ND];  // transposed: rows d, column = key l32
 #pragma unroll
   for (int dt = 0; dt < ND; ++dt) { dk[dt] = f32x16{0}; dv[dt] = f32x16{0}; }
-  u32x4 ra[NS];
   if (s_begin < s_end) {
-    request(s_begin);
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own count of outstanding loads)
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    u32x4 ra[NS];        // operands, NS MFMAs ahead
+    f32x16 sacc[2], dp[2];  // of the first and second half of a step
+    uint32_t now = 0u, next = 1u;  // buffers of this step and the next
+    auto fetch_rows = [&](uint32_t from, uint32_t buffer) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < NS; ++s) ra[s] = rd.rows(s, 0u);
-    uint32_t other = 2u * kTile, stats = kStats;
-    for (uint32_t step = s_begin; step < s_end; ++step) {
-      if (step + 1u < s_end) request(step + 1u);
-      const uint32_t start = tok.from + (step % steps_per_head) * 64u;
-      auto next_buffer = [&]() __attribute__((always_inline)) {
-        // every wave has read these tiles, and the next ones have landed
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        rd.move(other);
-        other = 0u - other;
-      };
+      for (int s = 0; s < NS; ++s) ra[s] = rd.rows(s, from, buffer * kBuffer);
+    };
+    auto wait_all = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    // Half RT of `step`, while the half after it gets its S and dP.
+    auto half = [&](auto rt_c, uint32_t step) __attribute__((always_inline)) {
+      constexpr int RT = decltype(rt_c)::value, NX = RT ^ 1;
+      const uint32_t ahead = RT == 0 ? now : next;  // buffer of the half after this one
+      const Half cur = half_of(step, RT);
+      const unsigned char* const st = smem + kStats + now * 512u + 128u * RT + 16u * h32;  // neg and delta of rows 8 i + 4 h32 .. + 3
+      if (cur.masked) {
+        const int32_t base = cur.first + 4 * (int32_t)h32;  // token of element c: base + c
+        const int32_t lo = (int32_t)j - off - base, w = (int32_t)j + (int32_t)g.window - 1 - off - base;
+        int32_t hi = (int32_t)tok.to - 1 - base;
+        hi = ((g.window != 0u) & (j >= g.sinks) & (w < hi)) ? w : hi;
 #pragma unroll
-      for (int rt = 0; rt < 2; ++rt) {
-        // rows of this half: tokens first .. last, positions p0 .. p1; this wave's keys: j0 .. j1
-        const int32_t first = (int32_t)start + 32 * rt, last = first + 31, p0 = off + first, p1 = off + (last < (int32_t)tok.to ? last : (int32_t)tok.to - 1);
-        const int32_t k0 = (int32_t)j0, k1 = (int32_t)(j0 + 31u < j_last ? j0 + 31u : j_last);
-        const bool windowed = (g.window != 0u) & (k1 >= (int32_t)g.sinks);
-        const bool none = (first >= (int32_t)tok.to) | (k0 > (int32_t)j_last) | (p1 < k0) | ((g.window != 0u) & (k0 >= (int32_t)g.sinks) & (p0 - k1 >= (int32_t)g.window));
-        const bool masked = (last >= (int32_t)tok.to) | (p0 < k1) | (windowed & (p1 - k0 >= (int32_t)g.window));
-        if (none) {
-          if (rt == 1) next_buffer();
-#pragma unroll
-          for (int s = 0; s < NS; ++s) ra[s] = rd.rows(s, rt == 0 ? 32u : 0u);
-          continue;
-        }
-        f32x16 sacc = f32x16{0}, dp = f32x16{0};
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          sacc = T::mfma32(ra[s], kf[s], sacc);
-          ra[s] = rd.rows(s, 64u + 32u * (uint32_t)rt);  // dO
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        f32x4 neg[4], delta[4];  // of rows 8 i + 4 h32 .. + 3
-        const unsigned char* const st = smem + stats + 128u * (uint32_t)rt + 16u * h32;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          neg[i] = *reinterpret_cast<const f32x4*>(st + 32 * i);
-          delta[i] = *reinterpret_cast<const f32x4*>(st + 256 + 32 * i);
-        }
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          dp = T::mfma32(ra[s], vf[s], dp);
-          ra[s] = rd.cols(s % ND, 64u + 32u * (uint32_t)rt + 16u * (uint32_t)(s / ND));  // dO^T
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        if (masked) {
-          const int32_t base = first + 4 * (int32_t)h32;  // token of element c: base + c
-          const int32_t lo = (int32_t)j - off - base;
-          int32_t hi = (int32_t)tok.to - 1 - base;
-          const int32_t w = (int32_t)j + (int32_t)g.window - 1 - off - base;
-          hi = ((g.window != 0u) & (j >= g.sinks) & (w < hi)) ? w : hi;
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const int32_t c = 8 * (v >> 2) + (v & 3);
-            const bool seen = (c >= lo) & (c <= hi);
-            sacc[v] = seen ? sacc[v] : -INFINITY;
-          }
-        }
-        u32x4 pw[2], ds[2];
-#pragma unroll
-        for (int v = 0; v < 16; v += 2) {
-          float w[2], x[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[v + e], g.scale_log2, neg[v >> 2][(v & 3) + e]));
-            x[e] = w[e] * (dp[v + e] - delta[v >> 2][(v & 3) + e]);
-            if constexpr (kScaled) x[e] *= ds_scale;
-          }
-          pw[v >> 3][(v >> 1) & 3] = T::pack(w[0], w[1]);
-          ds[v >> 3][(v >> 1) & 3] = T::pack(x[0], x[1]);
-        }
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          dv[s % ND] = T::mfma32(ra[s], pw[s / ND], dv[s % ND]);
-          ra[s] = rd.cols(s % ND, 32u * (uint32_t)rt + 16u * (uint32_t)(s / ND));  // Q^T
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        if (rt == 1) next_buffer();
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          dk[s % ND] = T::mfma32(ra[s], ds[s / ND], dk[s % ND]);
-          ra[s] = rd.rows(s, rt == 0 ? 32u : 0u);  // Q: the other half, or the next step's (the last time: not used)
-          __builtin_amdgcn_sched_barrier(0);
+        for (int v = 0; v < 16; ++v) {
+          const int32_t c = 8 * (v >> 2) + (v & 3);
+          const bool seen = (c >= lo) & (c <= hi);
+          sacc[RT][v] = seen ? sacc[RT][v] : -INFINITY;
         }
       }
-      stats ^= kStats ^ (kStats + 512u);
+      constexpr int kPer = 16 / NS;  // elements between two MFMAs
+      float w[16];
+      u32x4 pw[2], ds[2];
+      f32x4 stat[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) stat[i] = *reinterpret_cast<const f32x4*>(st + 32 * i);
+      sacc[NX] = f32x16{0}; dp[NX] = f32x16{0};
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        sacc[NX] = T::mfma32(ra[s], kf[s], sacc[NX]);
+        ra[s] = rd.rows(s, 64u + 32u * NX, ahead * kBuffer);  // dO
+#pragma unroll
+        for (int v = kPer * s; v < kPer * (s + 1); ++v) w[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[RT][v], g.scale_log2, stat[v >> 2][v & 3]));
+        if ((s + 1) * kPer % 4 == 0) stat[(s + 1) * kPer / 4 - 1] = *reinterpret_cast<const f32x4*>(st + 256 + 32 * ((s + 1) * kPer / 4 - 1));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        dp[NX] = T::mfma32(ra[s], vf[s], dp[NX]);
+        ra[s] = rd.cols(s % ND, 64u + 32u * RT + 16u * (uint32_t)(s / ND), now * kBuffer);  // dO^T
+#pragma unroll
+        for (int v = kPer * s; v < kPer * (s + 1); v += 2) {
+          float x[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            x[e] = w[v + e] * (dp[RT][v + e] - stat[v >> 2][(v & 3) + e]);
+            if constexpr (kScaled) x[e] *= ds_scale;
+          }
+          pw[v >> 3][(v >> 1) & 3] = T::pack(w[v], w[v + 1]);
+          ds[v >> 3][(v >> 1) & 3] = T::pack(x[0], x[1]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        dv[s % ND] = T::mfma32(ra[s], pw[s / ND], dv[s % ND]);
+        ra[s] = rd.cols(s % ND, 32u * RT + 16u * (uint32_t)(s / ND), now * kBuffer);  // Q^T
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (RT == 0) {  // every wave has left the step before, and the next one has landed
+        wait_all();
+        if (step + 2u < s_end) request(step + 2u);
+      }
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        dk[s % ND] = T::mfma32(ra[s], ds[s / ND], dk[s % ND]);
+        ra[s] = rd.rows(s, RT == 0 ? 0u : 32u, next * kBuffer);  // Q rows of the half after the next (past the end: not used)
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    constexpr std::integral_constant<int, 0> first{};
+    constexpr std::integral_constant<int, 1> second{};
+    request(s_begin);
+    if (s_begin + 1u < s_end) request(s_begin + 1u);
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own count of outstanding loads)
+    wait_all();
+    fetch_rows(0u, 0u);
+    sacc[0] = f32x16{0}; dp[0] = f32x16{0};
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      sacc[0] = T::mfma32(ra[s], kf[s], sacc[0]);
+      ra[s] = rd.rows(s, 64u, 0u);
+    }
+#pragma unroll
+    for (int s = 0; s < NS; ++s) dp[0] = T::mfma32(ra[s], vf[s], dp[0]);
+    fetch_rows(32u, 0u);
+    for (uint32_t step = s_begin; step < s_end; ++step) {
+      half(first, step);
+      half(second, step);
+      now = next;
+      next = after(next);
     }
   }
 
@@ -695,10 +718,19 @@ GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, in
 
 template <class T, int D>
 kp_status launch_grad(GradArgs& g, const GradPlan& p, hipStream_t st) {
-  constexpr uint32_t kTiles = 4u * 64u * 2u * D;
-  hipLaunchKernelGGL((kp_grad_query<T, D>), dim3((uint32_t)(p.units * p.row_tiles)), dim3(kThreads), kTiles, st, g);
+  constexpr uint32_t kTile = 64u * 2u * D, kKeysLds = 6u * kTile + 1536u;
+  if constexpr (kKeysLds > 64u * 1024u) {
+    static thread_local int attr_dev = -1;  // the attribute is kept per device
+    int dev = 0;
+    KP_HIP_TRY(hipGetDevice(&dev));
+    if (attr_dev != dev) {
+      KP_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kp_grad_keys<T, D>), hipFuncAttributeMaxDynamicSharedMemorySize, kKeysLds));
+      attr_dev = dev;
+    }
+  }
+  hipLaunchKernelGGL((kp_grad_query<T, D>), dim3((uint32_t)(p.units * p.row_tiles)), dim3(kThreads), 4u * kTile, st, g);
   KP_HIP_TRY(hipGetLastError());
-  hipLaunchKernelGGL((kp_grad_keys<T, D>), dim3((uint32_t)(p.units * p.items)), dim3(kThreads), kTiles + 1024u, st, g);
+  hipLaunchKernelGGL((kp_grad_keys<T, D>), dim3((uint32_t)(p.units * p.items)), dim3(kThreads), kKeysLds, st, g);
   KP_HIP_TRY(hipGetLastError());
   if (p.split > 0) {
     hipLaunchKernelGGL((kp_grad_join<T, D>), dim3((uint32_t)(p.units * p.split * (kGradKeys / (kThreads / (D / 4)))), 2), dim3(kThreads), 0, st, g);
