@@ -27,10 +27,10 @@ struct GradArgs {
   const float* lse;
   float *neg, *delta;  // workspace, [B, Hq, Sq]: kShiftP - lse log2(e), and d_o . o
   float* most;         // fp16: largest finite |d_o| of every row tile, [B, Hkv, row tiles]
-  float* part;         // partial dk, dv: [slot][dk, dv][kGradKeys][D]
+  float* part;         // partial dk, dv: [worker][first, last tile][dk, dv][kGradKeys][D]
   uint32_t seqs, hkv, group, n_q, n_k, window, sinks;
-  uint32_t row_tiles, key_tiles;            // of one head of keys
-  uint32_t sink_tiles, sink_runs, runs;     // key tiles with sinks, into how many runs of query rows they and the others are split
+  uint32_t row_tiles, key_tiles;  // of one head of keys
+  uint32_t workers;               // workgroups of kp_grad_keys; a multiple of 8 where B Hkv is one
   float scale, scale_log2;
 };
 
@@ -123,17 +123,23 @@ struct TileReader {
   }
   // rows `from` + l32 (from: a multiple of 32), d = 16 s + 8 h32 .. + 7; buffer: its distance from the first
   __device__ __forceinline__ u32x4 rows(int s, uint32_t from, uint32_t buffer) const {
-    typedef const __attribute__((address_space(3))) u32x4* lds_u32x4;
-    return *(lds_u32x4)(uintptr_t)(((row0 ^ (32u * (uint32_t)s)) + buffer) + from * kRow);
+    return rows_at((row0 ^ (32u * (uint32_t)s)) + buffer, from);
   }
   // d = 32 dt + l32 of the 16 rows from `from` on, in the order of an accumulator's rows
   __device__ __forceinline__ u32x4 cols(int dt, uint32_t from, uint32_t buffer) const {
+    // (swizzle(row + 8) = swizzle(row) ^ 2)
+    return cols_at((col0 ^ (64u * (uint32_t)dt)) + buffer, (col0 ^ (64u * (uint32_t)dt + 32u)) + buffer, from);
+  }
+  static __device__ __forceinline__ u32x4 rows_at(uint32_t ofs, uint32_t from) {
+    typedef const __attribute__((address_space(3))) u32x4* lds_u32x4;
+    return *(lds_u32x4)(uintptr_t)(ofs + from * kRow);
+  }
+  static __device__ __forceinline__ u32x4 cols_at(uint32_t lo_ofs, uint32_t hi_ofs, uint32_t from) {
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
     typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(((col0 ^ (64u * (uint32_t)dt)) + buffer) + from * kRow));
-    // (swizzle(row + 8) = swizzle(row) ^ 2)
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(((col0 ^ (64u * (uint32_t)dt + 32u)) + buffer) + (from + 8u) * kRow));
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(lo_ofs + from * kRow));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(hi_ofs + (from + 8u) * kRow));
     const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     return __builtin_bit_cast(u32x4, v);
   }
@@ -419,14 +425,74 @@ __device__ __forceinline__ Tokens tokens_of(const GradArgs& g, uint32_t kt) {
   return t;
 }
 
+// The steps (64 tokens of one query head) of all key tiles of all heads of keys stand in one line, a head after the other,
+// and the workers take equal pieces of it, whatever its tiles are: key tiles with sinks are seen by all later tokens, the
+// last keys by few, and a chip of 256 places has no even number of tiles to do.  A tile that lies whole in a worker's
+// piece is written out by it; of the others there is a partial sum for every worker that has a part, first or last in its
+// piece, and kp_grad_join adds them up in order.  Where the heads can be dealt out to the 8 XCDs (and their L2s) evenly,
+// each has a line of its own.
+struct Line {
+  uint32_t lines, mine, units, workers;  // lines, number of this one, its heads and workers
+  uint32_t per_unit;                     // steps of a head
+  uint64_t total;
+  __device__ __forceinline__ uint64_t piece(uint32_t worker) const { return total * worker / workers; }
+};
+__device__ __forceinline__ uint32_t steps_of(const GradArgs& g, uint32_t kt) {
+  const Tokens t = tokens_of(g, kt);
+  return (t.to - t.from + 63u) / 64u * g.group;
+}
+__device__ __forceinline__ Line line_of(const GradArgs& g, uint32_t number, uint32_t lines) {
+  Line l;
+  l.lines = lines; l.mine = number;
+  l.units = g.seqs * g.hkv / lines; l.workers = g.workers / lines;
+  uint32_t sum = 0;
+  for (uint32_t kt = threadIdx.x & 63u; kt < g.key_tiles; kt += 64u) sum += steps_of(g, kt);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) sum += (uint32_t)__shfl_xor((int)sum, d, 64);
+  l.per_unit = kp::wave_uniform(sum);
+  l.total = (uint64_t)l.per_unit * l.units;
+  return l;
+}
+// Steps of the key tiles before tile `kt` of a head.
+__device__ __forceinline__ uint32_t steps_before(const GradArgs& g, uint32_t kt) {
+  uint32_t sum = 0;
+  for (uint32_t t = threadIdx.x & 63u; t < kt; t += 64u) sum += steps_of(g, t);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) sum += (uint32_t)__shfl_xor((int)sum, d, 64);
+  return kp::wave_uniform(sum);
+}
+// The key tile that step number x of a head belongs to, and the step's number in it.
+__device__ __forceinline__ void tile_at(const GradArgs& g, uint32_t x, uint32_t* kt, uint32_t* in) {
+  const uint32_t lane = threadIdx.x & 63u;
+  uint32_t before = 0;
+  for (uint32_t t0 = 0; t0 < g.key_tiles; t0 += 64u) {
+    const uint32_t n = t0 + lane < g.key_tiles ? steps_of(g, t0 + lane) : 0u;
+    uint32_t sum = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t up = __shfl_up(sum, d, 64);
+      if (lane >= (uint32_t)d) sum += up;
+    }
+    const uint64_t past = __builtin_amdgcn_ballot_w64(before + sum > x);
+    if (past != 0ull) {
+      const int l = __builtin_ctzll(past);
+      *kt = t0 + (uint32_t)l;
+      *in = x - (before + __builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(n, l));
+      return;
+    }
+    before += __builtin_amdgcn_readlane(sum, 63);
+  }
+  *kt = g.key_tiles - 1u;  // (not reached: x is a step of the head)
+  *in = 0u;
+}
+__device__ __forceinline__ uint32_t lines_of(const GradArgs& g) { return ((g.seqs * g.hkv) & 7u) == 0u ? 8u : 1u; }
+
 // dk and dv of 128 keys from a run of the query rows that see them.  A wave holds 32 keys: K and V rows and the sums in
 // registers, 32 x 32 products formed so that a lane has one key (S = Q K^T, dP = dO V^T, dv^T += dO^T P, dk^T += Q^T dS).
 // Steps are 64 tokens of one query head; Q and dO tiles are in LDS, three buffers each, with the rows' lse and delta.
 // For D = 128 these registers leave room for one wave on a SIMD, which has to overlap its own vector and matrix
 // instructions: S and dP of the next 32 rows are formed while those of the current ones become P and dS, element by
 // element between the MFMAs; dv and dk of the current rows follow.
-// Key tiles that hold sinks are seen by all later tokens: their rows are split into runs of about an ordinary tile's length,
-// and so are all tiles' where there are few; the runs' sums are added up by kp_grad_join, in order.
 template <class T, int D>
 __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradArgs g) {
   constexpr uint32_t kTile = 64u * 2u * D, kBuffer = 2u * kTile;
@@ -435,20 +501,31 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradAr
   extern __shared__ __align__(16) unsigned char smem[];  // three buffers of [Q tile][dO tile], then three of [neg][delta] of 64 rows
   constexpr uint32_t kStats = 3u * kBuffer;
   const uint32_t lane = threadIdx.x & 63u, wave = kp::wave_uniform(threadIdx.x >> 6), h32 = lane >> 5, l32 = lane & 31u;
-  const uint32_t sink_items = g.sink_tiles * g.sink_runs, per = sink_items + (g.key_tiles - g.sink_tiles) * g.runs;
-  uint32_t unit, item;
-  unit_of(blockIdx.x, g.seqs * g.hkv, per, &unit, &item);
-  const uint32_t seq = unit / g.hkv, hk = unit - seq * g.hkv;
-  const uint32_t runs = item < sink_items ? g.sink_runs : g.runs;
-  const uint32_t kt = item < sink_items ? item / g.sink_runs : g.sink_tiles + (item - sink_items) / g.runs;
-  const uint32_t run = item < sink_items ? item % g.sink_runs : (item - sink_items) % g.runs;
+  const Line line = line_of(g, lines_of(g) == 8u ? blockIdx.x & 7u : 0u, lines_of(g));
+  const uint32_t worker = blockIdx.x / line.lines;
+  const int32_t off = (int32_t)g.n_k - (int32_t)g.n_q;
+  const uint32_t j_last = g.n_k - 1u;
+  uint64_t at = line.piece(worker);
+  const uint64_t to = line.piece(worker + 1u);
+  if (at >= to) return;
+  uint32_t unit_no = (uint32_t)(at / line.per_unit), kt, s_from;
+  tile_at(g, (uint32_t)(at - (uint64_t)unit_no * line.per_unit), &kt, &s_from);
+
+  const TileReader<D> rd((uint32_t)(uintptr_t)smem);
+  TileLoader<D> lq(g.q.token), ld(g.d_o.token);
+  const uint32_t lds0 = kp::wave_uniform((uint32_t)(uintptr_t)smem + 1024u * wave);
+  for (bool first_piece = true; at < to; first_piece = false) {
+  const uint32_t unit = unit_no * line.lines + line.mine, seq = unit / g.hkv, hk = unit - seq * g.hkv;
   const Tokens tok = tokens_of(g, kt);
   const uint32_t steps_per_head = (tok.to - tok.from + 63u) / 64u, steps = steps_per_head * g.group;
-  const uint32_t s_begin = (uint32_t)((uint64_t)steps * run / runs), s_end = (uint32_t)((uint64_t)steps * (run + 1u) / runs);
+  const uint32_t s_begin = s_from, s_end = (uint64_t)(steps - s_from) <= to - at ? steps : s_from + (uint32_t)(to - at);
+  const uint32_t key_tile = kt;
+  at += s_end - s_begin;
+  s_from = 0u;
+  if (++kt == g.key_tiles) { kt = 0u; ++unit_no; }
+  if (s_begin == s_end) continue;  // (a tile that no token sees)
 
-  const uint32_t j0 = kt * kGradKeys + 32u * wave, j_last = g.n_k - 1u;
-  const uint32_t j = j0 + l32, j_in = j < j_last ? j : j_last;
-  const int32_t off = (int32_t)g.n_k - (int32_t)g.n_q;
+  const uint32_t j0 = key_tile * kGradKeys + 32u * wave, j = j0 + l32, j_in = j < j_last ? j : j_last;
   u32x4 kf[NS], vf[NS];
   {
     const uint16_t *k = row_at(g.k, seq, hk, j_in), *v = row_at(g.v, seq, hk, j_in);
@@ -467,25 +544,42 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradAr
     ds_scale = __builtin_ldexpf(1.0f, kShiftS - (int)kShiftP<T>) / power_of_two_in(most);
   }
 
-  const TileReader<D> rd((uint32_t)(uintptr_t)smem);
-  TileLoader<D> lq(g.q.token), ld(g.d_o.token);
-  const uint32_t lds0 = kp::wave_uniform((uint32_t)(uintptr_t)smem + 1024u * wave);
   uint32_t loaded_last = ~0u, into = 0u;  // `into`: number of the buffer that the next step goes to
   auto after = [](uint32_t buffer) __attribute__((always_inline)) { return buffer == 2u ? 0u : buffer + 1u; };
-  auto request = [&](uint32_t step) __attribute__((always_inline)) {
-    const uint32_t in_group = step / steps_per_head, start = tok.from + (step - in_group * steps_per_head) * 64u, head = hk * g.group + in_group;
-    const uint32_t left = tok.to - 1u - start, last = left < 63u ? left : 63u;
+  // The step that is requested next: its head's rows, its first token.
+  uint32_t ask_group = s_begin / steps_per_head, ask_start = tok.from + (s_begin - ask_group * steps_per_head) * 64u;
+  uint32_t start = ask_start;  // of the step at hand
+  const uint16_t *ask_q, *ask_do;
+  const float* ask_stat;
+  auto ask_at = [&]() __attribute__((always_inline)) {
+    const uint32_t head = hk * g.group + ask_group;
+    ask_q = row_at(g.q, seq, head, ask_start);
+    ask_do = row_at(g.d_o, seq, head, ask_start);
+    ask_stat = (wave == 0u ? g.neg : g.delta) + ((size_t)seq * g.hkv * g.group + head) * g.n_q + ask_start;
+  };
+  ask_at();
+  auto request = [&]() __attribute__((always_inline)) {
+    const uint32_t left = tok.to - 1u - ask_start, last = left < 63u ? left : 63u;
     if (last != loaded_last) { loaded_last = last; lq.upto(last); ld.upto(last); }
-    lq.load(row_at(g.q, seq, head, start), lds0 + into * kBuffer);
-    ld.load(row_at(g.d_o, seq, head, start), lds0 + into * kBuffer + kTile);
+    lq.load(ask_q, lds0 + into * kBuffer);
+    ld.load(ask_do, lds0 + into * kBuffer + kTile);
     if (wave < 2u) {  // the rows' neg (wave 0) and delta (wave 1): 4 bytes to a lane
-      const float* from = (wave == 0u ? g.neg : g.delta) + ((size_t)seq * g.hkv * g.group + head) * g.n_q + start;
       const uint32_t ofs = 4u * (lane < last ? lane : last), dst = kp::wave_uniform((uint32_t)(uintptr_t)smem + kStats + into * 512u + 256u * wave);
       uint32_t saved_m0;
       asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0"
-                   : "=&s"(saved_m0) : "v"(ofs), "s"(from), "s"(dst) : "memory");
+                   : "=&s"(saved_m0) : "v"(ofs), "s"(ask_stat), "s"(dst) : "memory");
     }
     into = after(into);
+    ask_start += 64u;
+    if (ask_start < tok.to) {
+      ask_q += 64 * g.q.token;
+      ask_do += 64 * g.d_o.token;
+      ask_stat += 64;
+    } else {  // the next head's first (past the last head: not used)
+      ask_start = tok.from;
+      ++ask_group;
+      ask_at();
+    }
   };
   // First token of a half step of 32 rows, and whether it has pairs of a token and a key of this wave that are not visible.
   // (A wave whose keys none of them sees goes along all the same: the others wait for it at the next barrier anyway.)
@@ -493,9 +587,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradAr
     int32_t first;
     bool masked;
   };
-  auto half_of = [&](uint32_t step, int rt) __attribute__((always_inline)) {
+  auto half_of = [&](int rt) __attribute__((always_inline)) {
     Half h;
-    h.first = (int32_t)(tok.from + (step % steps_per_head) * 64u) + 32 * rt;
+    h.first = (int32_t)start + 32 * rt;
     const int32_t last = h.first + 31, k0 = (int32_t)j0, k1 = (int32_t)j0 + 31;
     h.masked = (last >= (int32_t)tok.to) | (off + h.first < k1) | ((g.window != 0u) & (k1 >= (int32_t)g.sinks) & (off + last - k0 >= (int32_t)g.window));
     return h;
@@ -508,16 +602,27 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradAr
     u32x4 ra[NS];        // operands, NS MFMAs ahead
     f32x16 sacc[2], dp[2];  // of the first and second half of a step
     uint32_t now = 0u, next = 1u;  // buffers of this step and the next
-    auto fetch_rows = [&](uint32_t from, uint32_t buffer) __attribute__((always_inline)) {
+    uint32_t row_ofs[NS], col_lo[ND], col_hi[ND];  // rows: of the buffer of the next operands; columns: of this step's
 #pragma unroll
-      for (int s = 0; s < NS; ++s) ra[s] = rd.rows(s, from, buffer * kBuffer);
+    for (int s = 0; s < NS; ++s) row_ofs[s] = rd.row0 ^ (32u * (uint32_t)s);
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) { col_lo[dt] = rd.col0 ^ (64u * (uint32_t)dt); col_hi[dt] = rd.col0 ^ (64u * (uint32_t)dt + 32u); }
+    auto rows = [&](int s, uint32_t from) __attribute__((always_inline)) { return rd.rows_at(row_ofs[s], from); };
+    auto cols = [&](int dt, uint32_t from) __attribute__((always_inline)) { return rd.cols_at(col_lo[dt], col_hi[dt], from); };
+    auto fetch_rows = [&](uint32_t from) __attribute__((always_inline)) {
+#pragma unroll
+      for (int s = 0; s < NS; ++s) ra[s] = rows(s, from);
     };
     auto wait_all = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    // Keeps a product whose value is not used before the next half where it stands: the compiler would move it there.
+    // (With one wave per SIMD it keeps all sums in accumulation registers.)
+    auto stay = [](f32x16& x) __attribute__((always_inline)) {
+      if constexpr (D == 128) asm volatile("" : "+a"(x)); else asm volatile("" : "+v"(x));
+    };
     // Half RT of `step`, while the half after it gets its S and dP.
     auto half = [&](auto rt_c, uint32_t step) __attribute__((always_inline)) {
       constexpr int RT = decltype(rt_c)::value, NX = RT ^ 1;
-      const uint32_t ahead = RT == 0 ? now : next;  // buffer of the half after this one
-      const Half cur = half_of(step, RT);
+      const Half cur = half_of(RT);
       const unsigned char* const st = smem + kStats + now * 512u + 128u * RT + 16u * h32;  // neg and delta of rows 8 i + 4 h32 .. + 3
       if (cur.masked) {
         const int32_t base = cur.first + 4 * (int32_t)h32;  // token of element c: base + c
@@ -541,7 +646,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradAr
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         sacc[NX] = T::mfma32(ra[s], kf[s], sacc[NX]);
-        ra[s] = rd.rows(s, 64u + 32u * NX, ahead * kBuffer);  // dO
+        stay(sacc[NX]);
+        ra[s] = rows(s, 64u + 32u * NX);  // dO
 #pragma unroll
         for (int v = kPer * s; v < kPer * (s + 1); ++v) w[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[RT][v], g.scale_log2, stat[v >> 2][v & 3]));
         if ((s + 1) * kPer % 4 == 0) stat[(s + 1) * kPer / 4 - 1] = *reinterpret_cast<const f32x4*>(st + 256 + 32 * ((s + 1) * kPer / 4 - 1));
@@ -550,7 +656,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradAr
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         dp[NX] = T::mfma32(ra[s], vf[s], dp[NX]);
-        ra[s] = rd.cols(s % ND, 64u + 32u * RT + 16u * (uint32_t)(s / ND), now * kBuffer);  // dO^T
+        stay(dp[NX]);
+        ra[s] = cols(s % ND, 64u + 32u * RT + 16u * (uint32_t)(s / ND));  // dO^T
 #pragma unroll
         for (int v = kPer * s; v < kPer * (s + 1); v += 2) {
           float x[2];
@@ -567,41 +674,47 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradAr
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         dv[s % ND] = T::mfma32(ra[s], pw[s / ND], dv[s % ND]);
-        ra[s] = rd.cols(s % ND, 32u * RT + 16u * (uint32_t)(s / ND), now * kBuffer);  // Q^T
+        ra[s] = cols(s % ND, 32u * RT + 16u * (uint32_t)(s / ND));  // Q^T
         __builtin_amdgcn_sched_barrier(0);
       }
       if constexpr (RT == 0) {  // every wave has left the step before, and the next one has landed
         wait_all();
-        if (step + 2u < s_end) request(step + 2u);
+        if (step + 2u < s_end) request();
+#pragma unroll
+        for (int s = 0; s < NS; ++s) row_ofs[s] += (next - now) * kBuffer;
       }
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         dk[s % ND] = T::mfma32(ra[s], ds[s / ND], dk[s % ND]);
-        ra[s] = rd.rows(s, RT == 0 ? 0u : 32u, next * kBuffer);  // Q rows of the half after the next (past the end: not used)
+        ra[s] = rows(s, RT == 0 ? 0u : 32u);  // Q rows of the half after the next (past the end: not used)
         __builtin_amdgcn_sched_barrier(0);
       }
     };
     constexpr std::integral_constant<int, 0> first{};
     constexpr std::integral_constant<int, 1> second{};
-    request(s_begin);
-    if (s_begin + 1u < s_end) request(s_begin + 1u);
+    request();
+    if (s_begin + 1u < s_end) request();
     __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own count of outstanding loads)
     wait_all();
-    fetch_rows(0u, 0u);
+    fetch_rows(0u);
     sacc[0] = f32x16{0}; dp[0] = f32x16{0};
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
       sacc[0] = T::mfma32(ra[s], kf[s], sacc[0]);
-      ra[s] = rd.rows(s, 64u, 0u);
+      ra[s] = rows(s, 64u);
     }
 #pragma unroll
     for (int s = 0; s < NS; ++s) dp[0] = T::mfma32(ra[s], vf[s], dp[0]);
-    fetch_rows(32u, 0u);
+    fetch_rows(32u);
     for (uint32_t step = s_begin; step < s_end; ++step) {
       half(first, step);
       half(second, step);
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) { col_lo[dt] += (next - now) * kBuffer; col_hi[dt] += (next - now) * kBuffer; }
       now = next;
       next = after(next);
+      start += 64u;
+      if (start >= tok.to) start = tok.from;
     }
   }
 
@@ -611,12 +724,10 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradAr
   uint64_t again = __builtin_amdgcn_ballot_w64((odd_of<ND>(dk) != 0.f || odd_of<ND>(dv) != 0.f) && mine);
   again = (again | again >> 32) & 0xFFFFFFFFull;
   const uint64_t rows_out = __builtin_amdgcn_ballot_w64(mine) & 0xFFFFFFFFull;
-  // run `run` of this tile among the partial sums: the sink tiles' first
-  const uint32_t sink_slots = g.sink_runs > 1u ? sink_items : 0u, slots = sink_slots + (g.runs > 1u ? per - sink_items : 0u);
-  const size_t slot = (size_t)unit * slots + (item < sink_items ? item : sink_slots + (item - sink_items));
-  float* const part = g.part + slot * (2u * kGradKeys * D) + (size_t)(32u * wave) * D;
+  const bool whole = s_begin == 0u && s_end == steps;
+  float* const part = g.part + (2u * (size_t)(worker * line.lines + line.mine) + (first_piece && s_begin != 0u ? 0u : 1u)) * (2u * kGradKeys * D) + (size_t)(32u * wave) * D;
   __syncthreads();  // (the tiles' room is used below)
-  if (runs > 1u) {
+  if (!whole) {
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
@@ -641,7 +752,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradAr
         const uint32_t in_group = step / steps_per_head, start = tok.from + (step - in_group * steps_per_head) * 64u;
         key_row<T, D>(g, seq, hk * g.group + in_group, key, start, start + 64u < tok.to ? start + 64u : tok.to, k, v, out_k, out_v);
       }
-      if (runs > 1u) {
+      if (!whole) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           part[r * D + lane * E + e] = out_k[e] * g.scale;
@@ -653,66 +764,87 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradAr
       }
     }
   }
+  __syncthreads();  // (the next tile's rows go to the same room)
+  }
 }
 
-// Adds up the runs' sums of the key tiles that were split: D / 4 lanes to a row, four elements to a lane; blockIdx.y: dk or dv.
+// Adds up the parts of the key tiles that do not lie whole in one worker's piece: 32 rows to a workgroup; blockIdx.y: dk or dv.
+constexpr int kJoinRows = 32;
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) void kp_grad_join(GradArgs g) {
-  constexpr uint32_t kLanes = D / 4, kPer = kThreads / kLanes, kBlocks = kGradKeys / kPer;
-  const uint32_t sink_items = g.sink_tiles * g.sink_runs, per = sink_items + (g.key_tiles - g.sink_tiles) * g.runs;
-  const uint32_t sink_split = g.sink_runs > 1u ? g.sink_tiles : 0u, split = sink_split + (g.runs > 1u ? g.key_tiles - g.sink_tiles : 0u);
-  const uint32_t tile = blockIdx.x / kBlocks, unit = tile / split, n = tile - unit * split;
-  const bool sink = n < sink_split;
-  const uint32_t kt = sink ? n : g.sink_tiles + (n - sink_split), runs = sink ? g.sink_runs : g.runs;
-  const uint32_t r = (blockIdx.x % kBlocks) * kPer + threadIdx.x / kLanes, c = threadIdx.x % kLanes, j = kt * kGradKeys + r;
-  if (j >= g.n_k) return;
-  const uint32_t sink_slots = g.sink_runs > 1u ? sink_items : 0u, slots = sink_slots + (g.runs > 1u ? per - sink_items : 0u);
-  const size_t slot = (size_t)unit * slots + (sink ? n * g.sink_runs : sink_slots + (n - sink_split) * g.runs);
-  const float* from = g.part + slot * (2u * kGradKeys * D) + (size_t)blockIdx.y * (kGradKeys * D) + (size_t)r * D + 4u * c;
-  f32x4 sum = *reinterpret_cast<const f32x4*>(from);
-  for (uint32_t i = 1; i < runs; ++i) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(from + (size_t)i * (2u * kGradKeys * D));
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] += x[e];
+  constexpr uint32_t kLanes = D / 4, kPer = kThreads / kLanes, kBlocks = kGradKeys / kJoinRows;
+  __shared__ const float* from[kThreads];  // where the tile's parts are, kThreads at a time
+  const uint32_t tile = blockIdx.x / kBlocks, unit = tile / g.key_tiles, kt = tile - unit * g.key_tiles;
+  const uint32_t lines = lines_of(g);
+  const Line line = line_of(g, unit % lines, lines);
+  const uint32_t n = steps_of(g, kt);
+  const uint64_t begin = (uint64_t)(unit / lines) * line.per_unit + steps_before(g, kt), end = begin + n;
+  uint32_t worker = 0u, parts = 0u;  // the first worker that has a step of the tile, and how many from there on
+  if (n != 0u) {
+    worker = (uint32_t)(begin * line.workers / line.total);
+    while (line.piece(worker + 1u) <= begin) ++worker;
+    if (line.piece(worker + 1u) >= end) return;  // it has all of them
+    parts = (uint32_t)((end - 1u) * line.workers / line.total);
+    while (line.piece(parts + 1u) < end) ++parts;
+    parts += 1u - worker;
   }
   const uint32_t seq = unit / g.hkv, hk = unit - seq * g.hkv;
+  const uint32_t c = threadIdx.x % kLanes, r0 = (blockIdx.x % kBlocks) * kJoinRows + threadIdx.x / kLanes;
+  constexpr int kRows = kJoinRows / (int)kPer;  // of a thread
+  f32x4 sum[kRows];
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) sum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (uint32_t p0 = 0; p0 < parts; p0 += kThreads) {
+    const uint32_t w = worker + p0 + threadIdx.x, left = parts - p0, here = left < (uint32_t)kThreads ? left : (uint32_t)kThreads;
+    __syncthreads();
+    if (threadIdx.x < here) {
+      const uint64_t mine = line.piece(w);
+      const size_t slot = 2u * (size_t)(w * line.lines + line.mine) + (mine > begin ? 0u : 1u);
+      from[threadIdx.x] = line.piece(w + 1u) == mine ? nullptr : g.part + slot * (2u * kGradKeys * D) + (size_t)blockIdx.y * (kGradKeys * D);
+    }
+    __syncthreads();
+    for (uint32_t i = 0; i < here; ++i) {
+      const float* const part = from[i];
+      if (part == nullptr) continue;
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(part + (size_t)(r0 + kPer * (uint32_t)k) * D + 4u * c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[k][e] += x[e];
+      }
+    }
+  }
   const Heads& out = blockIdx.y ? g.dv : g.dk;
-  *reinterpret_cast<u32x2*>(const_cast<uint16_t*>(row_at(out, seq, hk, j)) + 4u * c) = u32x2{T::pack(sum[0], sum[1]), T::pack(sum[2], sum[3])};
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const uint32_t j = kt * kGradKeys + r0 + kPer * (uint32_t)k;
+    if (j < g.n_k)
+      *reinterpret_cast<u32x2*>(const_cast<uint16_t*>(row_at(out, seq, hk, j)) + 4u * c) = u32x2{T::pack(sum[k][0], sum[k][1]), T::pack(sum[k][2], sum[k][3])};
+  }
 }
 
-// Tiles of a call and how they are split.
+// Tiles of a call, its workers and its workspace.
 struct GradPlan {
-  long long units, row_tiles, key_tiles, sink_tiles, sink_runs, runs, items, split;  // items: workgroups of kp_grad_keys per unit
-  size_t rows, part_at, most_at, bytes;  // rows: query rows; byte offsets into the workspace
+  long long units, row_tiles, key_tiles, workers;
+  size_t rows, most_at, part_at, bytes;  // rows: query rows; byte offsets into the workspace
 };
-GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks) {
+GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window) {
   GradPlan p{};
   const long long group = Hq / Hkv, head_steps = (Sq + 63) / 64;
   p.units = (long long)B * Hkv;
   p.row_tiles = (group * Sq + kTileRows - 1) / kTileRows;
   p.key_tiles = (Sk + kGradKeys - 1) / kGradKeys;
-  // steps of 64 tokens of an ordinary key tile, and of one that all tokens see
+  // steps of 64 tokens of an ordinary key tile (an estimate), of which a worker has at least four
   long long steps = window > 0 ? ((long long)window + kGradKeys + 62) / 64 + 1 : head_steps;
-  steps = (steps < head_steps ? steps : head_steps) * group;
-  const long long sink_steps = head_steps * group;
-  p.sink_tiles = window > 0 ? (sinks + (long long)kGradKeys - 1) / kGradKeys : 0;
-  if (p.sink_tiles > p.key_tiles) p.sink_tiles = p.key_tiles;
-  // enough workgroups for the chip (two per CU for D = 64, one for 128), as long as a run has four steps
-  const long long want = D == 64 ? 512 : 256, tiles = p.units * p.key_tiles;
-  p.runs = tiles * 2 > want ? 1 : want / tiles;
-  if (p.runs > steps / 4) p.runs = steps / 4;
-  if (p.runs < 1) p.runs = 1;
-  p.sink_runs = p.sink_tiles > 0 ? (sink_steps * p.runs + steps - 1) / steps : 1;
-  if (p.sink_runs > 256) p.sink_runs = 256;
-  if (p.sink_tiles == 0) p.sink_runs = 1;
-  p.items = p.sink_tiles * p.sink_runs + (p.key_tiles - p.sink_tiles) * p.runs;
-  p.split = (p.sink_runs > 1 ? p.sink_tiles : 0) + (p.runs > 1 ? p.key_tiles - p.sink_tiles : 0);
-  const long long slots = (p.sink_runs > 1 ? p.sink_tiles * p.sink_runs : 0) + (p.runs > 1 ? (p.key_tiles - p.sink_tiles) * p.runs : 0);
+  steps = (steps < head_steps ? steps : head_steps) * group * p.units * p.key_tiles;
+  p.workers = D == 64 ? 512 : 256;  // places: two per CU or one
+  if (steps / 4 < p.workers) p.workers = (steps / 4 + 7) / 8 * 8;
+  if (p.workers < 8) p.workers = 8;
   p.rows = (size_t)B * (size_t)Hq * (size_t)Sq;
   const auto up = [](size_t n) { return (n + 15) & ~(size_t)15; };
   p.most_at = up(8 * p.rows);
   p.part_at = up(p.most_at + 4 * (size_t)(p.units * p.row_tiles));
-  p.bytes = p.part_at + (size_t)(p.units * slots) * (2u * kGradKeys * 4u) * (size_t)D;
+  p.bytes = p.part_at + (size_t)p.workers * (2u * 2u * kGradKeys * 4u) * (size_t)D;
   return p;
 }
 
@@ -730,12 +862,10 @@ kp_status launch_grad(GradArgs& g, const GradPlan& p, hipStream_t st) {
   }
   hipLaunchKernelGGL((kp_grad_query<T, D>), dim3((uint32_t)(p.units * p.row_tiles)), dim3(kThreads), 4u * kTile, st, g);
   KP_HIP_TRY(hipGetLastError());
-  hipLaunchKernelGGL((kp_grad_keys<T, D>), dim3((uint32_t)(p.units * p.items)), dim3(kThreads), kKeysLds, st, g);
+  hipLaunchKernelGGL((kp_grad_keys<T, D>), dim3((uint32_t)p.workers), dim3(kThreads), kKeysLds, st, g);
   KP_HIP_TRY(hipGetLastError());
-  if (p.split > 0) {
-    hipLaunchKernelGGL((kp_grad_join<T, D>), dim3((uint32_t)(p.units * p.split * (kGradKeys / (kThreads / (D / 4)))), 2), dim3(kThreads), 0, st, g);
-    KP_HIP_TRY(hipGetLastError());
-  }
+  hipLaunchKernelGGL((kp_grad_join<T, D>), dim3((uint32_t)(p.units * p.key_tiles * (kGradKeys / kJoinRows)), 2), dim3(kThreads), 0, st, g);
+  KP_HIP_TRY(hipGetLastError());
   return KP_OK;
 }
 
@@ -748,7 +878,7 @@ bool sizes_ok(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sin
 
 extern "C" size_t kp_attn_window_grad_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks) {
   if (!sizes_ok(B, Hq, Hkv, Sq, Sk, D, window, sinks)) return 0;
-  return plan_grad(B, Hq, Hkv, Sq, Sk, D, window, sinks).bytes;
+  return plan_grad(B, Hq, Hkv, Sq, Sk, D, window).bytes;
 }
 
 extern "C" kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, const kp_heads* v, const kp_heads* o,
@@ -765,8 +895,8 @@ extern "C" kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, c
   for (const auto& a : all)
     if (kp_status s = check_heads(a.name, a.t, B, a.query ? Hq : Hkv, a.query ? Sq : Sk, D, a.written)) return s;
   if (!lse || ((uintptr_t)lse & 3u)) return kp::fail(KP_ERR_INVALID_ARG, "lse must be device memory, 4-byte aligned");
-  const GradPlan p = plan_grad(B, Hq, Hkv, Sq, Sk, D, window, sinks);
-  if (p.units * p.row_tiles >= (1ll << 31) || p.units * p.items >= (1ll << 31) || p.units * p.split * 16 >= (1ll << 31)) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^31 or more workgroups");
+  const GradPlan p = plan_grad(B, Hq, Hkv, Sq, Sk, D, window);
+  if (p.units * p.row_tiles >= (1ll << 31) || p.units * p.key_tiles * (kGradKeys / kJoinRows) >= (1ll << 31)) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^31 or more workgroups");
   if (kp_status s = check_workspace(workspace, workspace_bytes, p.bytes)) return s;
   GradArgs g{};
   g.q = heads_of(q, B, Hq, Sq); g.o = heads_of(o, B, Hq, Sq); g.d_o = heads_of(d_o, B, Hq, Sq); g.dq = heads_of(dq, B, Hq, Sq);
@@ -775,8 +905,7 @@ extern "C" kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, c
   char* const ws = static_cast<char*>(workspace);
   g.neg = reinterpret_cast<float*>(ws); g.delta = g.neg + p.rows;
   g.most = reinterpret_cast<float*>(ws + p.most_at); g.part = reinterpret_cast<float*>(ws + p.part_at);
-  g.row_tiles = (uint32_t)p.row_tiles; g.key_tiles = (uint32_t)p.key_tiles; g.sink_tiles = (uint32_t)p.sink_tiles;
-  g.sink_runs = (uint32_t)p.sink_runs; g.runs = (uint32_t)p.runs;
+  g.row_tiles = (uint32_t)p.row_tiles; g.key_tiles = (uint32_t)p.key_tiles; g.workers = (uint32_t)p.workers;
   g.seqs = (uint32_t)B; g.hkv = (uint32_t)Hkv; g.group = (uint32_t)(Hq / Hkv); g.n_q = (uint32_t)Sq; g.n_k = (uint32_t)Sk;
   g.window = (uint32_t)window; g.sinks = (uint32_t)sinks; g.scale = scale; g.scale_log2 = scale * kLog2e;
   hipStream_t st = static_cast<hipStream_t>(stream);
