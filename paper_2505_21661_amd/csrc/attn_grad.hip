@@ -29,7 +29,7 @@ struct GradArgs {
   float* most;         // fp16: largest finite |d_o| of every row tile, [B, Hkv, row tiles]
   float* part;         // partial dk, dv: [worker][first, last tile][dk, dv][kGradKeys][D]
   uint32_t seqs, hkv, group, n_q, n_k, window, sinks;
-  uint32_t row_tiles, key_tiles;  // of one head of keys
+  uint32_t row_tiles, key_tiles, sink_tiles;  // of one head of keys; sink_tiles: key tiles that all later tokens see, for their sinks
   uint32_t workers;               // workgroups of kp_grad_keys; a multiple of 8 where B Hkv is one
   float scale, scale_log2;
 };
@@ -145,11 +145,11 @@ struct TileReader {
   }
 };
 
-// 64 rows from global memory straight to such a tile: 1 KiB to a wave's load.
-template <int D>
+// 64 rows from global memory straight to such a tile: 1 KiB to a load of one of WAVES waves.
+template <int D, int WAVES>
 struct TileLoader {
   static constexpr uint32_t kRow = 2u * D, kChunks = kRow / 16u, kBlockRows = 1024u / kRow;
-  static constexpr int NL = (int)(64u * kRow / 4096u);
+  static constexpr int NL = (int)(64u * kRow / (1024u * WAVES));
   uint32_t ofs[NL], step, in;  // bytes
   __device__ __forceinline__ TileLoader(int64_t token_step) {
     const uint32_t lane = threadIdx.x & 63u, row = first_row();
@@ -163,17 +163,20 @@ struct TileLoader {
   __device__ __forceinline__ void upto(uint32_t last) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const uint32_t row = first_row() + 4u * kBlockRows * (uint32_t)i;
+      const uint32_t row = first_row() + (uint32_t)WAVES * kBlockRows * (uint32_t)i;
       ofs[i] = (row < last ? row : last) * step + in;
     }
   }
   // M0 (the LDS base) is put back; the loads are waited for by hand (see kp_attn_tile)
   __device__ __forceinline__ void load(const uint16_t* base, uint32_t dst) const {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
+    for (int i = 0; i < NL; ++i) load_one(i, base, dst);
+  }
+  __device__ __forceinline__ void load_one(int i, const uint16_t* base, uint32_t dst) const {
+    {
       uint32_t saved_m0;
       asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
-                   : "=&s"(saved_m0) : "v"(ofs[i]), "s"(base), "s"(dst + 4096u * (uint32_t)i) : "memory");
+                   : "=&s"(saved_m0) : "v"(ofs[i]), "s"(base), "s"(dst + 1024u * WAVES * (uint32_t)i) : "memory");
     }
   }
 };
@@ -278,7 +281,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
   const float neg_p = kScaled ? neg - kShiftP<T> : neg;
 
   TileReader<D> rd((uint32_t)(uintptr_t)smem);
-  TileLoader<D> lk(g.k.token), lv(g.v.token);
+  TileLoader<D, 4> lk(g.k.token), lv(g.v.token);
   const uint32_t lds0 = kp::wave_uniform((uint32_t)(uintptr_t)smem + 1024u * wave);
   const uint16_t *k_head = row_at(g.k, seq, hk, 0), *v_head = row_at(g.v, seq, hk, 0);
   uint32_t loaded_last = ~0u, into = 0u;  // `into`: LDS offset of the buffer that the next tiles go to
@@ -425,49 +428,75 @@ __device__ __forceinline__ Tokens tokens_of(const GradArgs& g, uint32_t kt) {
   return t;
 }
 
-// The steps (64 tokens of one query head) of all key tiles of all heads of keys stand in one line, a head after the other,
-// and the workers take equal pieces of it, whatever its tiles are: key tiles with sinks are seen by all later tokens, the
-// last keys by few, and a chip of 256 places has no even number of tiles to do.  A tile that lies whole in a worker's
-// piece is written out by it; of the others there is a partial sum for every worker that has a part, first or last in its
-// piece, and kp_grad_join adds them up in order.  Where the heads can be dealt out to the 8 XCDs (and their L2s) evenly,
-// each has a line of its own.
+// How the key tiles are dealt to the workers (a workgroup per CU).  Where the heads of keys can be dealt out to the 8 XCDs
+// (and their L2s) evenly, each XCD's workers have heads of their own (a line).  Of a line's tiles every worker takes as many
+// whole as there are for all, side by side, so that the rows that neighbouring tiles share are in L2 when they are asked
+// for (every worker a run of tiles of its own: 80 % of the requests missed, and the kernel took 400 us where it takes 270),
+// forwards and backwards in turn, since without a window the first are the longest.  What is left over, and the tiles that
+// hold sinks, which all later tokens see, stand in a line step by step (64 tokens of one query head), of which the workers
+// take equal pieces: a tile that does not lie whole in one of them leaves a partial sum for every worker that has a part,
+// first or last in its piece, and kp_grad_join adds them up in order.
 struct Line {
-  uint32_t lines, mine, units, workers;  // lines, number of this one, its heads and workers
-  uint32_t per_unit;                     // steps of a head
-  uint64_t total;
+  uint32_t lines, number, units, workers;  // lines, this one, its heads and workers
+  uint32_t sink_tiles, per_unit;           // of a head: tiles with sinks, the others
+  uint32_t whole, rest;                    // tiles that are taken whole, tiles that are split
+  uint64_t total;                          // steps of the latter
   __device__ __forceinline__ uint64_t piece(uint32_t worker) const { return total * worker / workers; }
+  // the n-th of the tiles that are not sinks'; the n-th that is split
+  __device__ __forceinline__ void plain_tile(uint32_t n, uint32_t* unit, uint32_t* kt) const {
+    const uint32_t u = n / per_unit;
+    *unit = u * lines + number;
+    *kt = sink_tiles + (n - u * per_unit);
+  }
+  __device__ __forceinline__ void split_tile(uint32_t n, uint32_t* unit, uint32_t* kt) const {
+    if (n < units * sink_tiles) {
+      const uint32_t u = n / sink_tiles;
+      *unit = u * lines + number;
+      *kt = n - u * sink_tiles;
+    } else {
+      plain_tile(whole + (n - units * sink_tiles), unit, kt);
+    }
+  }
 };
 __device__ __forceinline__ uint32_t steps_of(const GradArgs& g, uint32_t kt) {
   const Tokens t = tokens_of(g, kt);
   return (t.to - t.from + 63u) / 64u * g.group;
 }
+__device__ __forceinline__ uint32_t split_steps(const GradArgs& g, const Line& l, uint32_t n) {
+  uint32_t unit, kt;
+  l.split_tile(n, &unit, &kt);
+  return steps_of(g, kt);
+}
+// Steps of the split tiles before number n, by a wave.
+__device__ __forceinline__ uint64_t steps_before(const GradArgs& g, const Line& l, uint32_t n) {
+  uint64_t sum = 0;
+  for (uint32_t t0 = 0; t0 < n; t0 += 64u) {
+    const uint32_t t = t0 + (threadIdx.x & 63u);
+    uint32_t here = t < n ? split_steps(g, l, t) : 0u;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) here += (uint32_t)__shfl_xor((int)here, d, 64);
+    sum += kp::wave_uniform(here);
+  }
+  return sum;
+}
 __device__ __forceinline__ Line line_of(const GradArgs& g, uint32_t number, uint32_t lines) {
   Line l;
-  l.lines = lines; l.mine = number;
+  l.lines = lines; l.number = number;
   l.units = g.seqs * g.hkv / lines; l.workers = g.workers / lines;
-  uint32_t sum = 0;
-  for (uint32_t kt = threadIdx.x & 63u; kt < g.key_tiles; kt += 64u) sum += steps_of(g, kt);
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) sum += (uint32_t)__shfl_xor((int)sum, d, 64);
-  l.per_unit = kp::wave_uniform(sum);
-  l.total = (uint64_t)l.per_unit * l.units;
+  l.sink_tiles = g.sink_tiles; l.per_unit = g.key_tiles - g.sink_tiles;
+  const uint32_t plain = l.units * l.per_unit;
+  l.whole = plain / l.workers * l.workers;
+  l.rest = l.units * l.sink_tiles + (plain - l.whole);
+  l.total = steps_before(g, l, l.rest);
   return l;
 }
-// Steps of the key tiles before tile `kt` of a head.
-__device__ __forceinline__ uint32_t steps_before(const GradArgs& g, uint32_t kt) {
-  uint32_t sum = 0;
-  for (uint32_t t = threadIdx.x & 63u; t < kt; t += 64u) sum += steps_of(g, t);
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) sum += (uint32_t)__shfl_xor((int)sum, d, 64);
-  return kp::wave_uniform(sum);
-}
-// The key tile that step number x of a head belongs to, and the step's number in it.
-__device__ __forceinline__ void tile_at(const GradArgs& g, uint32_t x, uint32_t* kt, uint32_t* in) {
+// The split tile that step number x of the line belongs to, and the step's number in it.
+__device__ __forceinline__ void split_at(const GradArgs& g, const Line& line, uint64_t x, uint32_t* n, uint32_t* in) {
   const uint32_t lane = threadIdx.x & 63u;
-  uint32_t before = 0;
-  for (uint32_t t0 = 0; t0 < g.key_tiles; t0 += 64u) {
-    const uint32_t n = t0 + lane < g.key_tiles ? steps_of(g, t0 + lane) : 0u;
-    uint32_t sum = n;
+  uint64_t before = 0;
+  for (uint32_t t0 = 0; t0 < line.rest; t0 += 64u) {
+    const uint32_t steps = t0 + lane < line.rest ? split_steps(g, line, t0 + lane) : 0u;
+    uint32_t sum = steps;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const uint32_t up = __shfl_up(sum, d, 64);
@@ -476,272 +505,344 @@ __device__ __forceinline__ void tile_at(const GradArgs& g, uint32_t x, uint32_t*
     const uint64_t past = __builtin_amdgcn_ballot_w64(before + sum > x);
     if (past != 0ull) {
       const int l = __builtin_ctzll(past);
-      *kt = t0 + (uint32_t)l;
-      *in = x - (before + __builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(n, l));
+      *n = t0 + (uint32_t)l;
+      *in = (uint32_t)(x - before) - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(steps, l));
       return;
     }
     before += __builtin_amdgcn_readlane(sum, 63);
   }
-  *kt = g.key_tiles - 1u;  // (not reached: x is a step of the head)
+  *n = line.rest;  // (not reached: x is a step of the line)
   *in = 0u;
 }
 __device__ __forceinline__ uint32_t lines_of(const GradArgs& g) { return ((g.seqs * g.hkv) & 7u) == 0u ? 8u : 1u; }
 
-// dk and dv of 128 keys from a run of the query rows that see them.  A wave holds 32 keys: K and V rows and the sums in
-// registers, 32 x 32 products formed so that a lane has one key (S = Q K^T, dP = dO V^T, dv^T += dO^T P, dk^T += Q^T dS).
-// Steps are 64 tokens of one query head; Q and dO tiles are in LDS, three buffers each, with the rows' lse and delta.
-// For D = 128 these registers leave room for one wave on a SIMD, which has to overlap its own vector and matrix
-// instructions: S and dP of the next 32 rows are formed while those of the current ones become P and dS, element by
-// element between the MFMAs; dv and dk of the current rows follow.
+// dk and dv of 128 keys from a run of the query rows that see them.  32 x 32 products are formed so that a lane has one key
+// (S = Q K^T, dP = dO V^T, dv^T += dO^T P, dk^T += Q^T dS); a step is 64 tokens of one query head, whose Q and dO tiles are
+// in LDS, three buffers each, with the rows' lse and delta.
+// 8 waves, two to a group of 32 keys.  K and V rows, dk and dv of 32 keys of D = 128 would fill the registers of a wave that
+// has a SIMD for itself (which issues too slowly: 2200 cycles for 32 rows, of which the matrix pipes need 1024); so the two
+// waves of a group share the rows in the first two products, 32 each, give each other P and dS through LDS, and share d in
+// the last two.  S and dP are formed a step ahead: the exponentials stand between the MFMAs of dP, the rest of the vector
+// work between those of dv.
+constexpr int kKeysThreads = 512;
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradArgs g) {
-  constexpr uint32_t kTile = 64u * 2u * D, kBuffer = 2u * kTile;
-  constexpr int NS = D / 16, ND = D / 32;
+__global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
+  constexpr uint32_t kRow = 2u * D, kTile = 64u * kRow, kBuffer = 2u * kTile;
+  constexpr int NS = D / 16, NH = D / 64;  // NH: tiles of 32 d of a wave
+  constexpr int LA = 4;                    // operands come out of LDS this many MFMAs ahead
   constexpr bool kScaled = std::is_same<T, Fp16>::value;
-  extern __shared__ __align__(16) unsigned char smem[];  // three buffers of [Q tile][dO tile], then three of [neg][delta] of 64 rows
-  constexpr uint32_t kStats = 3u * kBuffer;
-  const uint32_t lane = threadIdx.x & 63u, wave = kp::wave_uniform(threadIdx.x >> 6), h32 = lane >> 5, l32 = lane & 31u;
+  extern __shared__ __align__(16) unsigned char smem[];
+  // [three buffers of Q tile, dO tile][P of every wave: 2 KiB][dS, twice][three times neg, delta of 64 rows]
+  constexpr uint32_t kShared = 3u * kBuffer, kSharedDs = kShared + 8u * 2048u, kStats = kSharedDs + 16u * 2048u;
+  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = kp::wave_uniform(tid >> 6), h32 = lane >> 5, l32 = lane & 31u;
+  const uint32_t group_no = wave & 3u, hf = wave >> 2;  // of 32 keys; the wave's half of the rows and of d
   const Line line = line_of(g, lines_of(g) == 8u ? blockIdx.x & 7u : 0u, lines_of(g));
   const uint32_t worker = blockIdx.x / line.lines;
   const int32_t off = (int32_t)g.n_k - (int32_t)g.n_q;
   const uint32_t j_last = g.n_k - 1u;
   uint64_t at = line.piece(worker);
   const uint64_t to = line.piece(worker + 1u);
-  if (at >= to) return;
-  uint32_t unit_no = (uint32_t)(at / line.per_unit), kt, s_from;
-  tile_at(g, (uint32_t)(at - (uint64_t)unit_no * line.per_unit), &kt, &s_from);
+  uint32_t round = 0u, split_no = 0u, s_from = 0u;
+  if (at < to) split_at(g, line, at, &split_no, &s_from);
+  bool first_piece = true;
 
   const TileReader<D> rd((uint32_t)(uintptr_t)smem);
-  TileLoader<D> lq(g.q.token), ld(g.d_o.token);
+  TileLoader<D, 8> lq(g.q.token), ld(g.d_o.token);
   const uint32_t lds0 = kp::wave_uniform((uint32_t)(uintptr_t)smem + 1024u * wave);
-  for (bool first_piece = true; at < to; first_piece = false) {
-  const uint32_t unit = unit_no * line.lines + line.mine, seq = unit / g.hkv, hk = unit - seq * g.hkv;
-  const Tokens tok = tokens_of(g, kt);
-  const uint32_t steps_per_head = (tok.to - tok.from + 63u) / 64u, steps = steps_per_head * g.group;
-  const uint32_t s_begin = s_from, s_end = (uint64_t)(steps - s_from) <= to - at ? steps : s_from + (uint32_t)(to - at);
-  const uint32_t key_tile = kt;
-  at += s_end - s_begin;
-  s_from = 0u;
-  if (++kt == g.key_tiles) { kt = 0u; ++unit_no; }
-  if (s_begin == s_end) continue;  // (a tile that no token sees)
-
-  const uint32_t j0 = key_tile * kGradKeys + 32u * wave, j = j0 + l32, j_in = j < j_last ? j : j_last;
-  u32x4 kf[NS], vf[NS];
-  {
-    const uint16_t *k = row_at(g.k, seq, hk, j_in), *v = row_at(g.v, seq, hk, j_in);
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      kf[s] = *reinterpret_cast<const u32x4*>(k + 16 * s + 8 * h32);
-      vf[s] = *reinterpret_cast<const u32x4*>(v + 16 * s + 8 * h32);
+  const uint32_t mine_at = 2048u * wave + 16u * lane, other_at = 2048u * (wave ^ 4u) + 16u * lane;  // what this wave and its other share
+  while (round * line.workers < line.whole || at < to) {
+    uint32_t unit, key_tile;
+    const bool rounds = round * line.workers < line.whole;  // first the whole tiles
+    if (rounds) line.plain_tile(round * line.workers + ((round & 1u) ? line.workers - 1u - worker : worker), &unit, &key_tile);
+    else line.split_tile(split_no, &unit, &key_tile);
+    const uint32_t seq = unit / g.hkv, hk = unit - seq * g.hkv;
+    const Tokens tok = tokens_of(g, key_tile);
+    const uint32_t steps_per_head = (tok.to - tok.from + 63u) / 64u, steps = steps_per_head * g.group;
+    const uint32_t s_begin = rounds ? 0u : s_from, s_end = rounds || (uint64_t)(steps - s_begin) <= to - at ? steps : s_begin + (uint32_t)(to - at);
+    const uint32_t slot = first_piece && s_begin != 0u ? 0u : 1u;
+    if (rounds) {
+      ++round;
+    } else {
+      at += s_end - s_begin;
+      s_from = 0u;
+      ++split_no;
+      first_piece = false;
+      if (s_begin == s_end) continue;  // (a tile that no token sees: kp_grad_join's)
     }
-  }
-  float ds_scale = 1.f;  // dS is rounded times this (and 2^kShiftP, which is in P)
-  if constexpr (kScaled) {
-    float most = 0.f;
-    for (uint32_t i = lane; i < g.row_tiles; i += 64u) most = fmaxf(most, g.most[(size_t)unit * g.row_tiles + i]);
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
-    ds_scale = __builtin_ldexpf(1.0f, kShiftS - (int)kShiftP<T>) / power_of_two_in(most);
-  }
+    const bool whole = s_begin == 0u && s_end == steps;
 
-  uint32_t loaded_last = ~0u, into = 0u;  // `into`: number of the buffer that the next step goes to
-  auto after = [](uint32_t buffer) __attribute__((always_inline)) { return buffer == 2u ? 0u : buffer + 1u; };
-  // The step that is requested next: its head's rows, its first token.
-  uint32_t ask_group = s_begin / steps_per_head, ask_start = tok.from + (s_begin - ask_group * steps_per_head) * 64u;
-  uint32_t start = ask_start;  // of the step at hand
-  const uint16_t *ask_q, *ask_do;
-  const float* ask_stat;
-  auto ask_at = [&]() __attribute__((always_inline)) {
-    const uint32_t head = hk * g.group + ask_group;
-    ask_q = row_at(g.q, seq, head, ask_start);
-    ask_do = row_at(g.d_o, seq, head, ask_start);
-    ask_stat = (wave == 0u ? g.neg : g.delta) + ((size_t)seq * g.hkv * g.group + head) * g.n_q + ask_start;
-  };
-  ask_at();
-  auto request = [&]() __attribute__((always_inline)) {
-    const uint32_t left = tok.to - 1u - ask_start, last = left < 63u ? left : 63u;
-    if (last != loaded_last) { loaded_last = last; lq.upto(last); ld.upto(last); }
-    lq.load(ask_q, lds0 + into * kBuffer);
-    ld.load(ask_do, lds0 + into * kBuffer + kTile);
-    if (wave < 2u) {  // the rows' neg (wave 0) and delta (wave 1): 4 bytes to a lane
-      const uint32_t ofs = 4u * (lane < last ? lane : last), dst = kp::wave_uniform((uint32_t)(uintptr_t)smem + kStats + into * 512u + 256u * wave);
-      uint32_t saved_m0;
-      asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0"
-                   : "=&s"(saved_m0) : "v"(ofs), "s"(ask_stat), "s"(dst) : "memory");
+    const uint32_t j0 = key_tile * kGradKeys + 32u * group_no, j = j0 + l32, j_in = j < j_last ? j : j_last;
+    u32x4 kf[NS], vf[NS];
+    {
+      const uint16_t *k = row_at(g.k, seq, hk, j_in), *v = row_at(g.v, seq, hk, j_in);
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        kf[s] = *reinterpret_cast<const u32x4*>(k + 16 * s + 8 * h32);
+        vf[s] = *reinterpret_cast<const u32x4*>(v + 16 * s + 8 * h32);
+      }
     }
-    into = after(into);
-    ask_start += 64u;
-    if (ask_start < tok.to) {
-      ask_q += 64 * g.q.token;
-      ask_do += 64 * g.d_o.token;
-      ask_stat += 64;
-    } else {  // the next head's first (past the last head: not used)
-      ask_start = tok.from;
-      ++ask_group;
-      ask_at();
+    float ds_scale = 1.f;  // dS is rounded times this (and 2^kShiftP, which is in P)
+    if constexpr (kScaled) {
+      float most = 0.f;
+      for (uint32_t i = lane; i < g.row_tiles; i += 64u) most = fmaxf(most, g.most[(size_t)unit * g.row_tiles + i]);
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+      ds_scale = __builtin_ldexpf(1.0f, kShiftS - (int)kShiftP<T>) / power_of_two_in(most);
     }
-  };
-  // First token of a half step of 32 rows, and whether it has pairs of a token and a key of this wave that are not visible.
-  // (A wave whose keys none of them sees goes along all the same: the others wait for it at the next barrier anyway.)
-  struct Half {
-    int32_t first;
-    bool masked;
-  };
-  auto half_of = [&](int rt) __attribute__((always_inline)) {
-    Half h;
-    h.first = (int32_t)start + 32 * rt;
-    const int32_t last = h.first + 31, k0 = (int32_t)j0, k1 = (int32_t)j0 + 31;
-    h.masked = (last >= (int32_t)tok.to) | (off + h.first < k1) | ((g.window != 0u) & (k1 >= (int32_t)g.sinks) & (off + last - k0 >= (int32_t)g.window));
-    return h;
-  };
 
-  f32x16 dk[ND], dv[ND];  // transposed: rows d, column = key l32
+    // ---- requests: the next step's head, first token, place ---------------------------------------------------------
+    uint32_t loaded_last = ~0u, into = 0u;  // `into`: buffer that it goes to
+    auto after = [](uint32_t buffer) __attribute__((always_inline)) { return buffer == 2u ? 0u : buffer + 1u; };
+    const uint32_t head_steps = steps_per_head == 0u ? 1u : steps_per_head;
+    uint32_t ask_group = s_begin / head_steps, ask_start = tok.from + (s_begin - ask_group * head_steps) * 64u;
+    uint32_t start = ask_start;  // first token of the step whose S and dP are formed
+    const uint16_t *ask_q, *ask_do;
+    const float* ask_stat;
+    auto ask_at = [&]() __attribute__((always_inline)) {
+      const uint32_t head = hk * g.group + ask_group;
+      ask_q = row_at(g.q, seq, head, ask_start);
+      ask_do = row_at(g.d_o, seq, head, ask_start);
+      ask_stat = (wave == 0u ? g.neg : g.delta) + ((size_t)seq * g.hkv * g.group + head) * g.n_q + ask_start;
+    };
+    ask_at();
+    constexpr int NL = TileLoader<D, 8>::NL, kAsks = 2 * NL + 2;
+    // The request in kAsks parts, to stand between MFMAs.
+    auto ask = [&](int part) __attribute__((always_inline)) {
+      if (part == 0) {
+        const uint32_t left = tok.to - 1u - ask_start, last = left < 63u ? left : 63u;
+        if (last != loaded_last) { loaded_last = last; lq.upto(last); ld.upto(last); }
+      }
+      if (part >= kAsks) return;
+      if (part < NL) {
+        lq.load_one(part, ask_q, lds0 + into * kBuffer);
+      } else if (part < 2 * NL) {
+        ld.load_one(part - NL, ask_do, lds0 + into * kBuffer + kTile);
+      } else if (part == 2 * NL) {
+        if (wave < 2u) {  // the rows' neg (wave 0) and delta (wave 1): 4 bytes to a lane
+          const uint32_t ofs = 4u * (lane < loaded_last ? lane : loaded_last), dst = kp::wave_uniform((uint32_t)(uintptr_t)smem + kStats + into * 512u + 256u * wave);
+          uint32_t saved_m0;
+          asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0"
+                       : "=&s"(saved_m0) : "v"(ofs), "s"(ask_stat), "s"(dst) : "memory");
+        }
+      } else {
+        into = after(into);
+        ask_start += 64u;
+        if (ask_start < tok.to) {
+          ask_q += 64 * g.q.token;
+          ask_do += 64 * g.d_o.token;
+          ask_stat += 64;
+        } else {  // the next head's first (past the last head: not used)
+          ask_start = tok.from;
+          ++ask_group;
+          ask_at();
+        }
+      }
+    };
+    auto request = [&]() __attribute__((always_inline)) {
 #pragma unroll
-  for (int dt = 0; dt < ND; ++dt) { dk[dt] = f32x16{0}; dv[dt] = f32x16{0}; }
-  if (s_begin < s_end) {
-    u32x4 ra[NS];        // operands, NS MFMAs ahead
-    f32x16 sacc[2], dp[2];  // of the first and second half of a step
-    uint32_t now = 0u, next = 1u;  // buffers of this step and the next
-    uint32_t row_ofs[NS], col_lo[ND], col_hi[ND];  // rows: of the buffer of the next operands; columns: of this step's
-#pragma unroll
-    for (int s = 0; s < NS; ++s) row_ofs[s] = rd.row0 ^ (32u * (uint32_t)s);
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt) { col_lo[dt] = rd.col0 ^ (64u * (uint32_t)dt); col_hi[dt] = rd.col0 ^ (64u * (uint32_t)dt + 32u); }
-    auto rows = [&](int s, uint32_t from) __attribute__((always_inline)) { return rd.rows_at(row_ofs[s], from); };
-    auto cols = [&](int dt, uint32_t from) __attribute__((always_inline)) { return rd.cols_at(col_lo[dt], col_hi[dt], from); };
-    auto fetch_rows = [&](uint32_t from) __attribute__((always_inline)) {
-#pragma unroll
-      for (int s = 0; s < NS; ++s) ra[s] = rows(s, from);
+      for (int part = 0; part < kAsks; ++part) ask(part);
     };
     auto wait_all = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-    // Keeps a product whose value is not used before the next half where it stands: the compiler would move it there.
-    // (With one wave per SIMD it keeps all sums in accumulation registers.)
-    auto stay = [](f32x16& x) __attribute__((always_inline)) {
-      if constexpr (D == 128) asm volatile("" : "+a"(x)); else asm volatile("" : "+v"(x));
+
+    f32x16 dk[NH], dv[NH];  // transposed: rows d = 32 (NH hf + dt) + .., column = key l32
+#pragma unroll
+    for (int dt = 0; dt < NH; ++dt) { dk[dt] = f32x16{0}; dv[dt] = f32x16{0}; }
+    u32x4 ra[LA];
+    f32x16 sacc, dp;
+    float w[16];
+    u32x4 pw[2], ds[2];  // P and dS of the next step's rows of this wave: two operands each
+    uint32_t ds_now = 0u;  // which of the two dS in LDS is this step's
+    uint32_t now = 0u, next = 0u;  // buffers of the step at hand and of the one whose S and dP are formed
+    // Keeps a value that is not used before the next block of code where it is made: the compiler would move it there.
+    auto stay = [](auto& x) __attribute__((always_inline)) { asm volatile("" : "+v"(x)); };
+    // operands in the order of their use: Q and dO rows of the next step (this wave's half), dO^T and then Q^T of this one
+    // (first of this wave's rows, then of the other's); behind them the next step's
+    const uint32_t row_own = rd.row0 + 32u * hf * kRow, col_own = (rd.col0 ^ (64u * NH * hf)) + 32u * hf * kRow;
+    const uint32_t col_other = (rd.col0 ^ (64u * NH * hf)) + 32u * (hf ^ 1u) * kRow;
+    auto fetch = [&](int n) __attribute__((always_inline)) -> u32x4 {
+      if (n >= 4 * NS) n -= 4 * NS;
+      if (n < NS) return rd.rows_at((row_own ^ (32u * (uint32_t)n)) + next * kBuffer, 0u);
+      if (n < 2 * NS) return rd.rows_at((row_own ^ (32u * (uint32_t)(n - NS))) + next * kBuffer, 64u);
+      const int m = (n - 2 * NS) % NS, ks = m / NH, dt = m % NH;
+      const uint32_t c = ks < 2 ? col_own : col_other, from = (n < 3 * NS ? 64u : 0u) + 16u * (uint32_t)(ks & 1);
+      return rd.cols_at((c ^ (64u * (uint32_t)dt)) + now * kBuffer, (c ^ (64u * (uint32_t)dt + 32u)) + now * kBuffer, from);
     };
-    // Half RT of `step`, while the half after it gets its S and dP.
-    auto half = [&](auto rt_c, uint32_t step) __attribute__((always_inline)) {
-      constexpr int RT = decltype(rt_c)::value, NX = RT ^ 1;
-      const Half cur = half_of(RT);
-      const unsigned char* const st = smem + kStats + now * 512u + 128u * RT + 16u * h32;  // neg and delta of rows 8 i + 4 h32 .. + 3
-      if (cur.masked) {
-        const int32_t base = cur.first + 4 * (int32_t)h32;  // token of element c: base + c
-        const int32_t lo = (int32_t)j - off - base, w = (int32_t)j + (int32_t)g.window - 1 - off - base;
+    // S of the wave's 32 rows of the step that starts at `start`: what is not visible becomes -inf
+    auto hide = [&]() __attribute__((always_inline)) {
+      const int32_t first = (int32_t)(start + 32u * hf), last = first + 31, k0 = (int32_t)j0, k1 = k0 + 31;
+      if ((last >= (int32_t)tok.to) | (off + first < k1) | ((g.window != 0u) & (k1 >= (int32_t)g.sinks) & (off + last - k0 >= (int32_t)g.window))) {
+        const int32_t base = first + 4 * (int32_t)h32;  // token of element c: base + c
+        const int32_t lo = (int32_t)j - off - base, wnd = (int32_t)j + (int32_t)g.window - 1 - off - base;
         int32_t hi = (int32_t)tok.to - 1 - base;
-        hi = ((g.window != 0u) & (j >= g.sinks) & (w < hi)) ? w : hi;
+        hi = ((g.window != 0u) & (j >= g.sinks) & (wnd < hi)) ? wnd : hi;
+        const uint32_t from = hi < lo ? 64u : (uint32_t)lo, count = hi < lo ? 0u : (uint32_t)(hi - lo);  // visible: c - from <= count, unsigned
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int32_t c = 8 * (v >> 2) + (v & 3);
-          const bool seen = (c >= lo) & (c <= hi);
-          sacc[RT][v] = seen ? sacc[RT][v] : -INFINITY;
-        }
-      }
-      constexpr int kPer = 16 / NS;  // elements between two MFMAs
-      float w[16];
-      u32x4 pw[2], ds[2];
-      f32x4 stat[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) stat[i] = *reinterpret_cast<const f32x4*>(st + 32 * i);
-      sacc[NX] = f32x16{0}; dp[NX] = f32x16{0};
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        sacc[NX] = T::mfma32(ra[s], kf[s], sacc[NX]);
-        stay(sacc[NX]);
-        ra[s] = rows(s, 64u + 32u * NX);  // dO
-#pragma unroll
-        for (int v = kPer * s; v < kPer * (s + 1); ++v) w[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[RT][v], g.scale_log2, stat[v >> 2][v & 3]));
-        if ((s + 1) * kPer % 4 == 0) stat[(s + 1) * kPer / 4 - 1] = *reinterpret_cast<const f32x4*>(st + 256 + 32 * ((s + 1) * kPer / 4 - 1));
-        __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        dp[NX] = T::mfma32(ra[s], vf[s], dp[NX]);
-        stay(dp[NX]);
-        ra[s] = cols(s % ND, 64u + 32u * RT + 16u * (uint32_t)(s / ND));  // dO^T
-#pragma unroll
-        for (int v = kPer * s; v < kPer * (s + 1); v += 2) {
-          float x[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            x[e] = w[v + e] * (dp[RT][v + e] - stat[v >> 2][(v & 3) + e]);
-            if constexpr (kScaled) x[e] *= ds_scale;
-          }
-          pw[v >> 3][(v >> 1) & 3] = T::pack(w[v], w[v + 1]);
-          ds[v >> 3][(v >> 1) & 3] = T::pack(x[0], x[1]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        dv[s % ND] = T::mfma32(ra[s], pw[s / ND], dv[s % ND]);
-        ra[s] = cols(s % ND, 32u * RT + 16u * (uint32_t)(s / ND));  // Q^T
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if constexpr (RT == 0) {  // every wave has left the step before, and the next one has landed
-        wait_all();
-        if (step + 2u < s_end) request();
-#pragma unroll
-        for (int s = 0; s < NS; ++s) row_ofs[s] += (next - now) * kBuffer;
-      }
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        dk[s % ND] = T::mfma32(ra[s], ds[s / ND], dk[s % ND]);
-        ra[s] = rows(s, RT == 0 ? 0u : 32u);  // Q rows of the half after the next (past the end: not used)
-        __builtin_amdgcn_sched_barrier(0);
+        for (int v = 0; v < 16; ++v) sacc[v] = (uint32_t)(8 * (v >> 2) + (v & 3)) - from <= count ? sacc[v] : -INFINITY;
       }
     };
-    constexpr std::integral_constant<int, 0> first{};
-    constexpr std::integral_constant<int, 1> second{};
+    // neg (which: 0) or delta (1) of rows 8 i + 4 h32 .. + 3 of the wave's half, in buffer `next`
+    auto stat = [&](int which, int i) __attribute__((always_inline)) {
+      return *reinterpret_cast<const f32x4*>(smem + kStats + next * 512u + 256u * (uint32_t)which + 128u * hf + 32u * (uint32_t)i + 16u * h32);
+    };
+    auto exponential = [&](int v, float neg) __attribute__((always_inline)) {
+      w[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[v], g.scale_log2, neg));
+      stay(w[v]);
+    };
+    auto finish = [&](int v, float delta0, float delta1) __attribute__((always_inline)) {  // elements v, v + 1
+      float x0 = w[v] * (dp[v] - delta0), x1 = w[v + 1] * (dp[v + 1] - delta1);
+      if constexpr (kScaled) { x0 *= ds_scale; x1 *= ds_scale; }
+      pw[v >> 3][(v >> 1) & 3] = T::pack(w[v], w[v + 1]);
+      ds[v >> 3][(v >> 1) & 3] = T::pack(x0, x1);
+    };
+    auto share_p = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) *reinterpret_cast<u32x4*>(smem + kShared + mine_at + 1024 * i) = pw[i];
+    };
+    auto share_ds = [&](uint32_t which, int i) __attribute__((always_inline)) {
+      *reinterpret_cast<u32x4*>(smem + kSharedDs + which * 16384u + mine_at + 1024 * i) = ds[i];
+    };
+    // operand ks of the last products: 16 rows each, two of this wave's and two of the other's
+    auto shared_p = [&](int ks) __attribute__((always_inline)) {
+      return *reinterpret_cast<const u32x4*>(smem + kShared + (ks < 2 ? mine_at : other_at) + 1024 * (ks & 1));
+    };
+    auto shared_ds = [&](int ks) __attribute__((always_inline)) {
+      return *reinterpret_cast<const u32x4*>(smem + kSharedDs + ds_now * 16384u + (ks < 2 ? mine_at : other_at) + 1024 * (ks & 1));
+    };
+    constexpr int kPer = 16 / NS;  // elements between two MFMAs
+
+    if (s_begin < s_end) {
     request();
     if (s_begin + 1u < s_end) request();
     __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own count of outstanding loads)
     wait_all();
-    fetch_rows(0u);
-    sacc[0] = f32x16{0}; dp[0] = f32x16{0};
+    sacc = f32x16{0}; dp = f32x16{0};
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      sacc[0] = T::mfma32(ra[s], kf[s], sacc[0]);
-      ra[s] = rows(s, 64u);
+    for (int n = 0; n < LA; ++n) ra[n] = fetch(n);
+#pragma unroll
+    for (int n = 0; n < 2 * NS; ++n) {
+      if (n < NS) sacc = T::mfma32(ra[n % LA], kf[n], sacc); else dp = T::mfma32(ra[n % LA], vf[n - NS], dp);
+      if (n + LA < 2 * NS) ra[n % LA] = fetch(n + LA);
     }
+    hide();
 #pragma unroll
-    for (int s = 0; s < NS; ++s) dp[0] = T::mfma32(ra[s], vf[s], dp[0]);
-    fetch_rows(32u);
+    for (int v = 0; v < 16; v += 4) {
+      const f32x4 neg = stat(0, v >> 2), delta = stat(1, v >> 2);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) exponential(v + e, neg[e]);
+      finish(v, delta[0], delta[1]);
+      finish(v + 2, delta[2], delta[3]);
+    }
+    share_p();
+    share_ds(0u, 0);
+    share_ds(0u, 1);
+    wait_all();
+    next = 1u;
+#pragma unroll
+    for (int n = 0; n < LA; ++n) ra[n] = fetch(n);
     for (uint32_t step = s_begin; step < s_end; ++step) {
-      half(first, step);
-      half(second, step);
-#pragma unroll
-      for (int dt = 0; dt < ND; ++dt) { col_lo[dt] += (next - now) * kBuffer; col_hi[dt] += (next - now) * kBuffer; }
-      now = next;
-      next = after(next);
       start += 64u;
       if (start >= tok.to) start = tok.from;
-    }
-  }
-
-  const float by_k = kScaled ? g.scale / (ds_scale * __builtin_ldexpf(1.0f, (int)kShiftP<T>)) : g.scale;
-  const float by_v = kScaled ? __builtin_ldexpf(1.0f, -(int)kShiftP<T>) : 1.f;
-  const bool mine = j <= j_last;
-  uint64_t again = __builtin_amdgcn_ballot_w64((odd_of<ND>(dk) != 0.f || odd_of<ND>(dv) != 0.f) && mine);
-  again = (again | again >> 32) & 0xFFFFFFFFull;
-  const uint64_t rows_out = __builtin_amdgcn_ballot_w64(mine) & 0xFFFFFFFFull;
-  const bool whole = s_begin == 0u && s_end == steps;
-  float* const part = g.part + (2u * (size_t)(worker * line.lines + line.mine) + (first_piece && s_begin != 0u ? 0u : 1u)) * (2u * kGradKeys * D) + (size_t)(32u * wave) * D;
-  __syncthreads();  // (the tiles' room is used below)
-  if (!whole) {
+      const bool more = step + 2u < s_end;
+      f32x4 st[2];
+      u32x4 rb[2];  // operands of P and dS, one ahead
+      // S and dP of the next step (behind the last: of no use), its exponentials
+      sacc = f32x16{0}; dp = f32x16{0};
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
+      for (int n = 0; n < NS; ++n) {
+        sacc = T::mfma32(ra[n % LA], kf[n], sacc);
+        ra[n % LA] = fetch(n + LA);
+        if (n == NS - 1) st[0] = stat(0, 0);
+        if (more) {  // (the buffer of the step before this one is free)
+          ask(n);
+          if (n == NS - 1)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float* to = part + l32 * D + 32 * dt + 8 * i + 4 * h32;
-        *reinterpret_cast<f32x4*>(to) = f32x4{dk[dt][4 * i] * by_k, dk[dt][4 * i + 1] * by_k, dk[dt][4 * i + 2] * by_k, dk[dt][4 * i + 3] * by_k};
-        *reinterpret_cast<f32x4*>(to + kGradKeys * D) = f32x4{dv[dt][4 * i] * by_v, dv[dt][4 * i + 1] * by_v, dv[dt][4 * i + 2] * by_v, dv[dt][4 * i + 3] * by_v};
+            for (int part = NS; part < kAsks; ++part) ask(part);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
-  } else {
-    store_rows<T, D>(dk, by_k, smem + 64u * D * wave, const_cast<uint16_t*>(g.dk.at), g.dk.seq * (int64_t)seq + g.dk.head * (int64_t)hk + g.dk.token * (int64_t)j_in, rows_out);
-    store_rows<T, D>(dv, by_v, smem + 64u * D * wave, const_cast<uint16_t*>(g.dv.at), g.dv.seq * (int64_t)seq + g.dv.head * (int64_t)hk + g.dv.token * (int64_t)j_in, rows_out);
-  }
-  if (again != 0ull) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // their first results have left
+      hide();
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        dp = T::mfma32(ra[n % LA], vf[n], dp);
+        stay(dp);
+        ra[n % LA] = fetch(NS + n + LA);
+        if (kPer * n % 4 == 0) st[(kPer * n / 4 + 1) & 1] = kPer * n < 12 ? stat(0, kPer * n / 4 + 1) : stat(1, 0);
+#pragma unroll
+        for (int v = kPer * n; v < kPer * (n + 1); ++v) exponential(v, st[(v >> 2) & 1][v & 3]);
+        if (n == NS - 1) rb[0] = shared_p(0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        const int ks = n / NH;
+        if (n % NH == 0) rb[(ks + 1) & 1] = ks < 3 ? shared_p(ks + 1) : shared_ds(0);
+        dv[n % NH] = T::mfma32(ra[n % LA], rb[ks & 1], dv[n % NH]);
+        ra[n % LA] = fetch(2 * NS + n + LA);
+        if (kPer * n % 4 == 0 && kPer * n < 12) st[(kPer * n / 4 + 1) & 1] = stat(1, kPer * n / 4 + 1);
+#pragma unroll
+        for (int v = kPer * n; v < kPer * (n + 1); v += 2) finish(v, st[(v >> 2) & 1][v & 3], st[(v >> 2) & 1][(v & 3) + 1]);
+        if (kPer * (n + 1) % 8 == 0) share_ds(ds_now ^ 1u, kPer * (n + 1) / 8 - 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // every wave has read this step's P
+      share_p();
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        const int ks = n / NH;
+        if (n % NH == 0 && ks < 3) rb[(ks + 1) & 1] = shared_ds(ks + 1);
+        // behind the last operand of this step: P and dS of the next are there, so are its successor's tiles
+        if (n == NS - LA) {
+          wait_all();
+          now = now == 2u ? 0u : now + 1u;
+          next = next == 2u ? 0u : next + 1u;
+        }
+        dk[n % NH] = T::mfma32(ra[n % LA], rb[ks & 1], dk[n % NH]);
+        ra[n % LA] = fetch(3 * NS + n + LA);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      ds_now ^= 1u;
+    }
+    }
+
+    const float by_k = kScaled ? g.scale / (ds_scale * __builtin_ldexpf(1.0f, (int)kShiftP<T>)) : g.scale;
+    const float by_v = kScaled ? __builtin_ldexpf(1.0f, -(int)kShiftP<T>) : 1.f;
+    uint64_t again = __builtin_amdgcn_ballot_w64((odd_of<NH>(dk) != 0.f || odd_of<NH>(dv) != 0.f) && j <= j_last);
+    again = (again | again >> 32) & 0xFFFFFFFFull;
+    float* const part = g.part + (2u * (size_t)(worker * line.lines + line.number) + slot) * (2u * kGradKeys * D) + (size_t)(32u * group_no) * D;
+    __syncthreads();  // (the tiles' room is used below)
+    if (!whole) {
+#pragma unroll
+      for (int dt = 0; dt < NH; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float* const out = part + l32 * D + 32u * (NH * hf + (uint32_t)dt) + 8 * i + 4 * h32;
+          *reinterpret_cast<f32x4*>(out) = f32x4{dk[dt][4 * i] * by_k, dk[dt][4 * i + 1] * by_k, dk[dt][4 * i + 2] * by_k, dk[dt][4 * i + 3] * by_k};
+          *reinterpret_cast<f32x4*>(out + kGradKeys * D) = f32x4{dv[dt][4 * i] * by_v, dv[dt][4 * i + 1] * by_v, dv[dt][4 * i + 2] * by_v, dv[dt][4 * i + 3] * by_v};
+        }
+    } else {
+      // Through LDS as in store_rows, the dk tile and behind it the dv tile: [128 keys][D]
+      unsigned char* const to_lds = smem + 32u * group_no * kRow + l32 * kRow;
+      const uint32_t half = h32 ^ ((l32 >> 3) & 1u);
+#pragma unroll
+      for (int dt = 0; dt < NH; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t at_lds = (((4u * (NH * hf + (uint32_t)dt) + (uint32_t)i) ^ (l32 & 7u)) << 4) + 8u * half;
+          *reinterpret_cast<u32x2*>(to_lds + at_lds) = u32x2{T::pack(dk[dt][4 * i] * by_k, dk[dt][4 * i + 1] * by_k), T::pack(dk[dt][4 * i + 2] * by_k, dk[dt][4 * i + 3] * by_k)};
+          *reinterpret_cast<u32x2*>(to_lds + kGradKeys * kRow + at_lds) = u32x2{T::pack(dv[dt][4 * i] * by_v, dv[dt][4 * i + 1] * by_v), T::pack(dv[dt][4 * i + 2] * by_v, dv[dt][4 * i + 3] * by_v)};
+        }
+      __syncthreads();
+      constexpr uint32_t kChunks = kRow / 16u;
+#pragma unroll
+      for (uint32_t i = 0; i < 2u * kGradKeys * kChunks / kKeysThreads; ++i) {
+        const uint32_t n = tid + i * kKeysThreads, r = n / kChunks % kGradKeys, chunk = (n % kChunks) ^ (r & 7u), key = key_tile * kGradKeys + r;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(smem + 16u * n);
+        const Heads& out = n < kGradKeys * kChunks ? g.dk : g.dv;
+        if (key <= j_last) *reinterpret_cast<u32x4*>(const_cast<uint16_t*>(row_at(out, seq, hk, key)) + 8u * chunk) = (r & 8u) ? u32x4{v.z, v.w, v.x, v.y} : v;
+      }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the results have left, before some are put right
+    __syncthreads();  // (and the next tile's rows go to the same room)
     for (; again != 0ull; again &= again - 1ull) {
       const uint32_t r = (uint32_t)__builtin_ctzll(again), key = j0 + r;
       constexpr int E = D / 64;
@@ -749,8 +850,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradAr
       load_row<T, E>(row_at(g.k, seq, hk, key), k);
       load_row<T, E>(row_at(g.v, seq, hk, key), v);
       for (uint32_t step = s_begin; step < s_end; ++step) {
-        const uint32_t in_group = step / steps_per_head, start = tok.from + (step - in_group * steps_per_head) * 64u;
-        key_row<T, D>(g, seq, hk * g.group + in_group, key, start, start + 64u < tok.to ? start + 64u : tok.to, k, v, out_k, out_v);
+        const uint32_t in_group = step / steps_per_head, first = tok.from + (step - in_group * steps_per_head) * 64u;
+        key_row<T, D>(g, seq, hk * g.group + in_group, key, first, first + 64u < tok.to ? first + 64u : tok.to, k, v, out_k, out_v);
       }
       if (!whole) {
 #pragma unroll
@@ -764,21 +865,20 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void kp_grad_keys(GradAr
       }
     }
   }
-  __syncthreads();  // (the next tile's rows go to the same room)
-  }
 }
 
-// Adds up the parts of the key tiles that do not lie whole in one worker's piece: 32 rows to a workgroup; blockIdx.y: dk or dv.
+// Adds up the parts of the split key tiles that do not lie whole in one worker's piece: 32 rows to a workgroup; blockIdx.y: dk or dv.
 constexpr int kJoinRows = 32;
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) void kp_grad_join(GradArgs g) {
   constexpr uint32_t kLanes = D / 4, kPer = kThreads / kLanes, kBlocks = kGradKeys / kJoinRows;
   __shared__ const float* from[kThreads];  // where the tile's parts are, kThreads at a time
-  const uint32_t tile = blockIdx.x / kBlocks, unit = tile / g.key_tiles, kt = tile - unit * g.key_tiles;
-  const uint32_t lines = lines_of(g);
-  const Line line = line_of(g, unit % lines, lines);
+  const uint32_t lines = lines_of(g), tile = blockIdx.x / kBlocks;
+  const Line line = line_of(g, tile % lines, lines);
+  uint32_t unit, kt;
+  line.split_tile(tile / lines, &unit, &kt);
   const uint32_t n = steps_of(g, kt);
-  const uint64_t begin = (uint64_t)(unit / lines) * line.per_unit + steps_before(g, kt), end = begin + n;
+  const uint64_t begin = steps_before(g, line, tile / lines), end = begin + n;
   uint32_t worker = 0u, parts = 0u;  // the first worker that has a step of the tile, and how many from there on
   if (n != 0u) {
     worker = (uint32_t)(begin * line.workers / line.total);
@@ -799,7 +899,7 @@ __global__ __launch_bounds__(kThreads) void kp_grad_join(GradArgs g) {
     __syncthreads();
     if (threadIdx.x < here) {
       const uint64_t mine = line.piece(w);
-      const size_t slot = 2u * (size_t)(w * line.lines + line.mine) + (mine > begin ? 0u : 1u);
+      const size_t slot = 2u * (size_t)(w * line.lines + line.number) + (mine > begin ? 0u : 1u);
       from[threadIdx.x] = line.piece(w + 1u) == mine ? nullptr : g.part + slot * (2u * kGradKeys * D) + (size_t)blockIdx.y * (kGradKeys * D);
     }
     __syncthreads();
@@ -825,10 +925,10 @@ __global__ __launch_bounds__(kThreads) void kp_grad_join(GradArgs g) {
 
 // Tiles of a call, its workers and its workspace.
 struct GradPlan {
-  long long units, row_tiles, key_tiles, workers;
+  long long units, row_tiles, key_tiles, sink_tiles, workers, split;  // split: key tiles that kp_grad_join looks at
   size_t rows, most_at, part_at, bytes;  // rows: query rows; byte offsets into the workspace
 };
-GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window) {
+GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks) {
   GradPlan p{};
   const long long group = Hq / Hkv, head_steps = (Sq + 63) / 64;
   p.units = (long long)B * Hkv;
@@ -837,9 +937,13 @@ GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window) {
   // steps of 64 tokens of an ordinary key tile (an estimate), of which a worker has at least four
   long long steps = window > 0 ? ((long long)window + kGradKeys + 62) / 64 + 1 : head_steps;
   steps = (steps < head_steps ? steps : head_steps) * group * p.units * p.key_tiles;
-  p.workers = D == 64 ? 512 : 256;  // places: two per CU or one
+  p.workers = 256;  // one per CU
   if (steps / 4 < p.workers) p.workers = (steps / 4 + 7) / 8 * 8;
   if (p.workers < 8) p.workers = 8;
+  p.sink_tiles = window > 0 ? ((long long)sinks + kGradKeys - 1) / kGradKeys : 0;
+  if (p.sink_tiles > p.key_tiles) p.sink_tiles = p.key_tiles;
+  const long long lines = p.units % 8 == 0 ? 8 : 1, plain = p.units / lines * (p.key_tiles - p.sink_tiles);
+  p.split = p.units * p.sink_tiles + lines * (plain % (p.workers / lines));
   p.rows = (size_t)B * (size_t)Hq * (size_t)Sq;
   const auto up = [](size_t n) { return (n + 15) & ~(size_t)15; };
   p.most_at = up(8 * p.rows);
@@ -850,7 +954,7 @@ GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window) {
 
 template <class T, int D>
 kp_status launch_grad(GradArgs& g, const GradPlan& p, hipStream_t st) {
-  constexpr uint32_t kTile = 64u * 2u * D, kKeysLds = 6u * kTile + 1536u;
+  constexpr uint32_t kTile = 64u * 2u * D, kKeysLds = 6u * kTile + 24u * 2048u + 1536u;
   if constexpr (kKeysLds > 64u * 1024u) {
     static thread_local int attr_dev = -1;  // the attribute is kept per device
     int dev = 0;
@@ -862,10 +966,12 @@ kp_status launch_grad(GradArgs& g, const GradPlan& p, hipStream_t st) {
   }
   hipLaunchKernelGGL((kp_grad_query<T, D>), dim3((uint32_t)(p.units * p.row_tiles)), dim3(kThreads), 4u * kTile, st, g);
   KP_HIP_TRY(hipGetLastError());
-  hipLaunchKernelGGL((kp_grad_keys<T, D>), dim3((uint32_t)p.workers), dim3(kThreads), kKeysLds, st, g);
+  hipLaunchKernelGGL((kp_grad_keys<T, D>), dim3((uint32_t)p.workers), dim3(kKeysThreads), kKeysLds, st, g);
   KP_HIP_TRY(hipGetLastError());
-  hipLaunchKernelGGL((kp_grad_join<T, D>), dim3((uint32_t)(p.units * p.key_tiles * (kGradKeys / kJoinRows)), 2), dim3(kThreads), 0, st, g);
-  KP_HIP_TRY(hipGetLastError());
+  if (p.split > 0) {
+    hipLaunchKernelGGL((kp_grad_join<T, D>), dim3((uint32_t)(p.split * (kGradKeys / kJoinRows)), 2), dim3(kThreads), 0, st, g);
+    KP_HIP_TRY(hipGetLastError());
+  }
   return KP_OK;
 }
 
@@ -878,7 +984,7 @@ bool sizes_ok(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sin
 
 extern "C" size_t kp_attn_window_grad_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks) {
   if (!sizes_ok(B, Hq, Hkv, Sq, Sk, D, window, sinks)) return 0;
-  return plan_grad(B, Hq, Hkv, Sq, Sk, D, window).bytes;
+  return plan_grad(B, Hq, Hkv, Sq, Sk, D, window, sinks).bytes;
 }
 
 extern "C" kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, const kp_heads* v, const kp_heads* o,
@@ -895,7 +1001,7 @@ extern "C" kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, c
   for (const auto& a : all)
     if (kp_status s = check_heads(a.name, a.t, B, a.query ? Hq : Hkv, a.query ? Sq : Sk, D, a.written)) return s;
   if (!lse || ((uintptr_t)lse & 3u)) return kp::fail(KP_ERR_INVALID_ARG, "lse must be device memory, 4-byte aligned");
-  const GradPlan p = plan_grad(B, Hq, Hkv, Sq, Sk, D, window);
+  const GradPlan p = plan_grad(B, Hq, Hkv, Sq, Sk, D, window, sinks);
   if (p.units * p.row_tiles >= (1ll << 31) || p.units * p.key_tiles * (kGradKeys / kJoinRows) >= (1ll << 31)) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^31 or more workgroups");
   if (kp_status s = check_workspace(workspace, workspace_bytes, p.bytes)) return s;
   GradArgs g{};
@@ -905,7 +1011,7 @@ extern "C" kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, c
   char* const ws = static_cast<char*>(workspace);
   g.neg = reinterpret_cast<float*>(ws); g.delta = g.neg + p.rows;
   g.most = reinterpret_cast<float*>(ws + p.most_at); g.part = reinterpret_cast<float*>(ws + p.part_at);
-  g.row_tiles = (uint32_t)p.row_tiles; g.key_tiles = (uint32_t)p.key_tiles; g.workers = (uint32_t)p.workers;
+  g.row_tiles = (uint32_t)p.row_tiles; g.key_tiles = (uint32_t)p.key_tiles; g.sink_tiles = (uint32_t)p.sink_tiles; g.workers = (uint32_t)p.workers;
   g.seqs = (uint32_t)B; g.hkv = (uint32_t)Hkv; g.group = (uint32_t)(Hq / Hkv); g.n_q = (uint32_t)Sq; g.n_k = (uint32_t)Sk;
   g.window = (uint32_t)window; g.sinks = (uint32_t)sinks; g.scale = scale; g.scale_log2 = scale * kLog2e;
   hipStream_t st = static_cast<hipStream_t>(stream);
