@@ -386,13 +386,23 @@ def kp_calibrate(cycles, n_wg: int, waves: int, mode: int, trace_buf, trace_cap:
 # [B, S, H, D], a slice of a fused projection), or [T, H, D] where there is no batch.
 
 
+_names = {}  # torch's types by the names below, filled in by the first call
+
+
+def _dtype(name: str):
+    if not _names:
+        import torch
+
+        _names.update({n: getattr(torch, n) for n in ("float32", "uint8", "int32", "int64", "float8_e4m3fn")})
+        _names.update({torch.bfloat16: KP_BF16, torch.float16: KP_FP16})
+    return _names.get(name)
+
+
 def _type_code(dtype) -> int:
-    name = str(dtype)
-    if name == "torch.bfloat16":
-        return KP_BF16
-    if name == "torch.float16":
-        return KP_FP16
-    raise ValueError(f"tensors must be bfloat16 or float16, not {name}")
+    code = _dtype(dtype)
+    if code is None:
+        raise ValueError(f"tensors must be bfloat16 or float16, not {dtype}")
+    return code
 
 
 def _heads(name: str, t, shape, dtype):
@@ -405,13 +415,13 @@ def _heads(name: str, t, shape, dtype):
     if st[-1] != 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
     if len(st) == 4:
-        return ctypes.byref(kp_heads(t.data_ptr(), st[0], st[1], st[2]))
-    return ctypes.byref(kp_heads(t.data_ptr(), 0, st[1], st[0]))
+        return kp_heads(t.data_ptr(), st[0], st[1], st[2])
+    return kp_heads(t.data_ptr(), 0, st[1], st[0])
 
 
-def _flat(name: str, t, dtype: str, shape=None):
+def _flat(name: str, t, dtype, shape=None):
     """Device pointer of a contiguous tensor of a type and (where given) a shape."""
-    if str(t.dtype) != dtype or (shape is not None and tuple(t.shape) != tuple(shape)):
+    if t.dtype != dtype or (shape is not None and t.shape != shape):
         raise ValueError(f"{name} must be {'' if shape is None else str(list(shape)) + ' '}of {dtype}, not {list(t.shape)} of {t.dtype}")
     return _ptr(t)
 
@@ -439,7 +449,7 @@ def kp_attn_window(q, k, v, o, lse, window: int, sinks: int, scale: float, works
     ws, n = _workspace(workspace)
     _check(lib().kp_attn_window(
         _heads("q", q, q.shape, dtype), _heads("k", k, (B, Hkv, Sk, D), dtype), _heads("v", v, kv, dtype),
-        _heads("o", o, q.shape, dtype), 0 if lse is None else _flat("lse", lse, "torch.float32", (B, Hq, Sq)),
+        _heads("o", o, q.shape, dtype), 0 if lse is None else _flat("lse", lse, _dtype("float32"), (B, Hq, Sq)),
         B, Hq, Hkv, Sq, Sk, D, _type_code(dtype), window, sinks, scale, ws, n, _stream(stream)))
 
 
@@ -455,7 +465,7 @@ def kp_attn_window_grad(q, k, v, o, lse, d_o, dq, dk, dv, window: int, sinks: in
     ws, n = _workspace(workspace)
     _check(lib().kp_attn_window_grad(
         _heads("q", q, qs, dtype), _heads("k", k, (B, Hkv, Sk, D), dtype), _heads("v", v, ks, dtype),
-        _heads("o", o, qs, dtype), _flat("lse", lse, "torch.float32", (B, Hq, Sq)), _heads("d_o", d_o, qs, dtype),
+        _heads("o", o, qs, dtype), _flat("lse", lse, _dtype("float32"), (B, Hq, Sq)), _heads("d_o", d_o, qs, dtype),
         _heads("dq", dq, qs, dtype), _heads("dk", dk, ks, dtype), _heads("dv", dv, ks, dtype),
         B, Hq, Hkv, Sq, Sk, D, _type_code(dtype), window, sinks, scale, ws, n, _stream(stream)))
 
@@ -463,13 +473,13 @@ def kp_attn_window_grad(q, k, v, o, lse, d_o, dq, dk, dv, window: int, sinks: in
 def _cache_of(k_cache, v_cache, k_exp, v_exp, dtype):
     """kp_cache of two halves [n_pages, Hkv, page, D]: of `dtype`, or float8_e4m3fn with exponent bytes."""
     n_pages, Hkv, page, D = k_cache.shape
-    e4m3 = str(k_cache.dtype) == "torch.float8_e4m3fn"
-    kind = str(k_cache.dtype) if e4m3 else str(dtype)
-    exps = [0, 0]
+    kind, ke, ve = dtype, 0, 0
+    e4m3 = k_cache.dtype == _dtype("float8_e4m3fn")
     if e4m3:
-        exps = [_flat(n, e, "torch.uint8", (n_pages, Hkv, page)) for n, e in (("k_exp", k_exp), ("v_exp", v_exp))]
-    return ctypes.byref(kp_cache(_flat("k_cache", k_cache, kind), _flat("v_cache", v_cache, kind, k_cache.shape), *exps,
-                                 n_pages, Hkv, page, D, _type_code(dtype), int(e4m3)))
+        kind, rows = k_cache.dtype, (n_pages, Hkv, page)
+        ke, ve = _flat("k_exp", k_exp, _dtype("uint8"), rows), _flat("v_exp", v_exp, _dtype("uint8"), rows)
+    return kp_cache(_flat("k_cache", k_cache, kind), _flat("v_cache", v_cache, kind, k_cache.shape), ke, ve,
+                    n_pages, Hkv, page, D, _type_code(dtype), int(e4m3))
 
 
 def kp_cache_write(k, v, slots, k_cache, v_cache, k_exp=None, v_exp=None, stream=None) -> None:
@@ -477,7 +487,7 @@ def kp_cache_write(k, v, slots, k_cache, v_cache, k_exp=None, v_exp=None, stream
     or, into a float8_e4m3fn cache with exponents [n_pages, Hkv, page] uint8, quantised row by row."""
     T, (_, Hkv, _, D) = k.shape[0], k_cache.shape
     _check(lib().kp_cache_write(_heads("k", k, (T, Hkv, D), k.dtype), _heads("v", v, (T, Hkv, D), k.dtype),
-                                _flat("slots", slots, "torch.int64", (T,)), T,
+                                _flat("slots", slots, _dtype("int64"), (T,)), T,
                                 _cache_of(k_cache, v_cache, k_exp, v_exp, k.dtype), _stream(stream)))
 
 
@@ -487,8 +497,8 @@ def kp_cache_read(k_cache, v_cache, k_exp, v_exp, block_table, starts, k, v, str
     T, (_, Hkv, _, D) = k.shape[0], k_cache.shape
     n, width = block_table.shape
     _check(lib().kp_cache_read(_cache_of(k_cache, v_cache, k_exp, v_exp, k.dtype),
-                               _flat("block_table", block_table, "torch.int32"), width,
-                               _flat("starts", starts, "torch.int32", (n + 1,)), n, T,
+                               _flat("block_table", block_table, _dtype("int32")), width,
+                               _flat("starts", starts, _dtype("int32"), (n + 1,)), n, T,
                                _heads("k", k, (T, Hkv, D), k.dtype), _heads("v", v, (T, Hkv, D), k.dtype), _stream(stream)))
 
 
@@ -510,9 +520,9 @@ def kp_attn_paged(q, k_cache, v_cache, k_exp, v_exp, block_table, lens, starts, 
     ws, nbytes = _workspace(workspace)
     _check(lib().kp_attn_paged(
         _heads("q", q, q.shape, q.dtype), _cache_of(k_cache, v_cache, k_exp, v_exp, q.dtype),
-        _flat("block_table", block_table, "torch.int32"), width, _flat("lens", lens, "torch.int32", (n,)),
-        _flat("starts", starts, "torch.int32", (n + 1,)), _heads("o", o, q.shape, q.dtype),
-        0 if lse is None else _flat("lse", lse, "torch.float32", (Hq, T)), T, n, Hq, window, sinks, scale, ws, nbytes,
+        _flat("block_table", block_table, _dtype("int32")), width, _flat("lens", lens, _dtype("int32"), (n,)),
+        _flat("starts", starts, _dtype("int32"), (n + 1,)), _heads("o", o, q.shape, q.dtype),
+        0 if lse is None else _flat("lse", lse, _dtype("float32"), (Hq, T)), T, n, Hq, window, sinks, scale, ws, nbytes,
         _stream(stream)))
 
 

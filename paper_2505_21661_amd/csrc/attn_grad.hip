@@ -135,11 +135,14 @@ struct TileReader {
     return *(lds_u32x4)(uintptr_t)(ofs + from * kRow);
   }
   static __device__ __forceinline__ u32x4 cols_at(uint32_t lo_ofs, uint32_t hi_ofs, uint32_t from) {
+    return cols_from(lo_ofs + from * kRow, hi_ofs + (from + 8u) * kRow);
+  }
+  static __device__ __forceinline__ u32x4 cols_from(uint32_t lo_at, uint32_t hi_at) {
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
     typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(lo_ofs + from * kRow));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(hi_ofs + (from + 8u) * kRow));
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)lo_at);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)hi_at);
     const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     return __builtin_bit_cast(u32x4, v);
   }
@@ -431,8 +434,7 @@ __device__ __forceinline__ Tokens tokens_of(const GradArgs& g, uint32_t kt) {
 // How the key tiles are dealt to the workers (a workgroup per CU).  Where the heads of keys can be dealt out to the 8 XCDs
 // (and their L2s) evenly, each XCD's workers have heads of their own (a line).  Of a line's tiles every worker takes as many
 // whole as there are for all, side by side, so that the rows that neighbouring tiles share are in L2 when they are asked
-// for (every worker a run of tiles of its own: 80 % of the requests missed, and the kernel took 400 us where it takes 270),
-// forwards and backwards in turn, since without a window the first are the longest.  What is left over, and the tiles that
+// for (with a run of tiles of its own for every worker 80 % of the requests missed it, this way 50 %), forwards and backwards in turn, since without a window the first are the longest.  What is left over, and the tiles that
 // hold sinks, which all later tokens see, stand in a line step by step (64 tokens of one query head), of which the workers
 // take equal pieces: a tile that does not lie whole in one of them leaves a partial sum for every worker that has a part,
 // first or last in its piece, and kp_grad_join adds them up in order.
@@ -516,14 +518,15 @@ __device__ __forceinline__ void split_at(const GradArgs& g, const Line& line, ui
 }
 __device__ __forceinline__ uint32_t lines_of(const GradArgs& g) { return ((g.seqs * g.hkv) & 7u) == 0u ? 8u : 1u; }
 
-// dk and dv of 128 keys from a run of the query rows that see them.  32 x 32 products are formed so that a lane has one key
-// (S = Q K^T, dP = dO V^T, dv^T += dO^T P, dk^T += Q^T dS); a step is 64 tokens of one query head, whose Q and dO tiles are
-// in LDS, three buffers each, with the rows' lse and delta.
+// dk and dv of 128 keys from a run of the query rows that see them.  A step is 64 tokens of one query head, whose Q and dO
+// tiles are in LDS, three buffers each, with the rows' lse and delta.
 // 8 waves, two to a group of 32 keys.  K and V rows, dk and dv of 32 keys of D = 128 would fill the registers of a wave that
 // has a SIMD for itself (which issues too slowly: 2200 cycles for 32 rows, of which the matrix pipes need 1024); so the two
 // waves of a group share the rows in the first two products, 32 each, give each other P and dS through LDS, and share d in
-// the last two.  S and dP are formed a step ahead: the exponentials stand between the MFMAs of dP, the rest of the vector
-// work between those of dv.
+// the last two.  S^T = K Q^T and dP^T = V dO^T have a row to a lane, with its lse and delta; P and dS go to LDS as
+// [row][key] and are read transposed, for dv^T += dO^T P and dk^T += Q^T dS, which have a key to a lane.
+// S and dP are formed a step ahead: the exponentials stand between the MFMAs of dP, the rest of the vector work between
+// those of dv.
 constexpr int kKeysThreads = 512;
 template <class T, int D>
 __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
@@ -549,7 +552,15 @@ __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
   const TileReader<D> rd((uint32_t)(uintptr_t)smem);
   TileLoader<D, 8> lq(g.q.token), ld(g.d_o.token);
   const uint32_t lds0 = kp::wave_uniform((uint32_t)(uintptr_t)smem + 1024u * wave);
-  const uint32_t mine_at = 2048u * wave + 16u * lane, other_at = 2048u * (wave ^ 4u) + 16u * lane;  // what this wave and its other share
+  // What the waves of a group share, [32 rows][32 keys] each: the 8-byte piece n of row r at n ^ r / 4 % 8, so that 32 rows'
+  // writes and four rows' transposing reads cover all banks once.
+  const uint32_t shared_wr = 2048u * wave + 64u * l32 + ((h32 ^ ((l32 >> 2) & 7u)) << 3);
+  uint32_t shared_own, shared_other;
+  {
+    const uint32_t i = lane & 15u, grp = lane >> 4, row = 4u * (grp >> 1) + (i >> 2), piece = 4u * (grp & 1u) + (i & 3u);
+    shared_own = (uint32_t)(uintptr_t)smem + 2048u * wave + 64u * row + ((piece ^ (row >> 2)) << 3);
+    shared_other = shared_own ^ 8192u;
+  }
   while (round * line.workers < line.whole || at < to) {
     uint32_t unit, key_tile;
     const bool rounds = round * line.workers < line.whole;  // first the whole tiles
@@ -595,6 +606,7 @@ __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
     auto after = [](uint32_t buffer) __attribute__((always_inline)) { return buffer == 2u ? 0u : buffer + 1u; };
     const uint32_t head_steps = steps_per_head == 0u ? 1u : steps_per_head;
     uint32_t ask_group = s_begin / head_steps, ask_start = tok.from + (s_begin - ask_group * head_steps) * 64u;
+    uint32_t asked = s_begin;    // number of the step that is requested next
     uint32_t start = ask_start;  // first token of the step whose S and dP are formed
     const uint16_t *ask_q, *ask_do;
     const float* ask_stat;
@@ -626,12 +638,13 @@ __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
         }
       } else {
         into = after(into);
+        if (++asked >= s_end) return;  // (past the last step: that one again, of no use)
         ask_start += 64u;
         if (ask_start < tok.to) {
           ask_q += 64 * g.q.token;
           ask_do += 64 * g.d_o.token;
           ask_stat += 64;
-        } else {  // the next head's first (past the last head: not used)
+        } else {  // the next head's first
           ask_start = tok.from;
           ++ask_group;
           ask_at();
@@ -649,8 +662,8 @@ __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
     for (int dt = 0; dt < NH; ++dt) { dk[dt] = f32x16{0}; dv[dt] = f32x16{0}; }
     u32x4 ra[LA];
     f32x16 sacc, dp;
-    float w[16];
-    u32x4 pw[2], ds[2];  // P and dS of the next step's rows of this wave: two operands each
+    float w[16], neg, delta;  // of the wave's 32 rows of the next step, row l32
+    u32x2 pw[4], ds[4];  // P and dS: keys 8 i + 4 h32 .. + 3 of row l32
     uint32_t ds_now = 0u;  // which of the two dS in LDS is this step's
     uint32_t now = 0u, next = 0u;  // buffers of the step at hand and of the one whose S and dP are formed
     // Keeps a value that is not used before the next block of code where it is made: the compiler would move it there.
@@ -671,48 +684,64 @@ __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
     auto hide = [&]() __attribute__((always_inline)) {
       const int32_t first = (int32_t)(start + 32u * hf), last = first + 31, k0 = (int32_t)j0, k1 = k0 + 31;
       if ((last >= (int32_t)tok.to) | (off + first < k1) | ((g.window != 0u) & (k1 >= (int32_t)g.sinks) & (off + last - k0 >= (int32_t)g.window))) {
-        const int32_t base = first + 4 * (int32_t)h32;  // token of element c: base + c
-        const int32_t lo = (int32_t)j - off - base, wnd = (int32_t)j + (int32_t)g.window - 1 - off - base;
-        int32_t hi = (int32_t)tok.to - 1 - base;
-        hi = ((g.window != 0u) & (j >= g.sinks) & (wnd < hi)) ? wnd : hi;
-        const uint32_t from = hi < lo ? 64u : (uint32_t)lo, count = hi < lo ? 0u : (uint32_t)(hi - lo);  // visible: c - from <= count, unsigned
+        asm volatile("");  // (a branch, not 16 selects every time)
+        // key of element c: base + c; visible: from hi - count to hi (unsigned: c - from <= count), and below sk
+        const int32_t token = first + (int32_t)l32, p = token < (int32_t)tok.to ? off + token : -1, base = k0 + 4 * (int32_t)h32;
+        const int32_t hi = p - base, lo = (g.window != 0u ? p - (int32_t)g.window + 1 : 0) - base;
+        const uint32_t from = hi < lo ? 64u : (uint32_t)lo, count = hi < lo ? 0u : (uint32_t)(hi - lo);
+        if ((g.window == 0u) | (k0 >= (int32_t)g.sinks)) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) sacc[v] = (uint32_t)(8 * (v >> 2) + (v & 3)) - from <= count ? sacc[v] : -INFINITY;
+          for (int v = 0; v < 16; ++v) sacc[v] = (uint32_t)(8 * (v >> 2) + (v & 3)) - from <= count ? sacc[v] : -INFINITY;
+        } else {
+          const int32_t sk = (hi < (int32_t)g.sinks - 1 - base ? hi : (int32_t)g.sinks - 1 - base);
+          if (off + first - k1 >= (int32_t)g.window) {  // sinks alone are left
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sacc[v] = 8 * (v >> 2) + (v & 3) <= sk ? sacc[v] : -INFINITY;
+          } else {
+            asm volatile("");
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+              const int32_t c = 8 * (v >> 2) + (v & 3);
+              sacc[v] = (((uint32_t)c - from <= count) | (c <= sk)) ? sacc[v] : -INFINITY;
+            }
+          }
+        }
       }
     };
-    // neg (which: 0) or delta (1) of rows 8 i + 4 h32 .. + 3 of the wave's half, in buffer `next`
-    auto stat = [&](int which, int i) __attribute__((always_inline)) {
-      return *reinterpret_cast<const f32x4*>(smem + kStats + next * 512u + 256u * (uint32_t)which + 128u * hf + 32u * (uint32_t)i + 16u * h32);
+    auto load_stats = [&]() __attribute__((always_inline)) {
+      const float* const st = reinterpret_cast<const float*>(smem + kStats + next * 512u + 128u * hf) + l32;
+      neg = st[0];
+      delta = st[64];
     };
-    auto exponential = [&](int v, float neg) __attribute__((always_inline)) {
+    auto exponential = [&](int v) __attribute__((always_inline)) {
       w[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[v], g.scale_log2, neg));
       stay(w[v]);
     };
-    auto finish = [&](int v, float delta0, float delta1) __attribute__((always_inline)) {  // elements v, v + 1
-      float x0 = w[v] * (dp[v] - delta0), x1 = w[v + 1] * (dp[v + 1] - delta1);
+    auto finish = [&](int v) __attribute__((always_inline)) {  // elements v, v + 1
+      float x0 = w[v] * (dp[v] - delta), x1 = w[v + 1] * (dp[v + 1] - delta);
       if constexpr (kScaled) { x0 *= ds_scale; x1 *= ds_scale; }
-      pw[v >> 3][(v >> 1) & 3] = T::pack(w[v], w[v + 1]);
-      ds[v >> 3][(v >> 1) & 3] = T::pack(x0, x1);
+      pw[v >> 2][(v >> 1) & 1] = T::pack(w[v], w[v + 1]);
+      ds[v >> 2][(v >> 1) & 1] = T::pack(x0, x1);
     };
     auto share_p = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) *reinterpret_cast<u32x4*>(smem + kShared + mine_at + 1024 * i) = pw[i];
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x2*>(smem + kShared + (shared_wr ^ (16u * (uint32_t)i))) = pw[i];
     };
     auto share_ds = [&](uint32_t which, int i) __attribute__((always_inline)) {
-      *reinterpret_cast<u32x4*>(smem + kSharedDs + which * 16384u + mine_at + 1024 * i) = ds[i];
+      *reinterpret_cast<u32x2*>(smem + kSharedDs + which * 16384u + (shared_wr ^ (16u * (uint32_t)i))) = ds[i];
     };
-    // operand ks of the last products: 16 rows each, two of this wave's and two of the other's
-    auto shared_p = [&](int ks) __attribute__((always_inline)) {
-      return *reinterpret_cast<const u32x4*>(smem + kShared + (ks < 2 ? mine_at : other_at) + 1024 * (ks & 1));
+    // operand ks of the last products: 16 rows each, two of this wave's and two of the other's; key l32
+    auto shared_at = [&](uint32_t region, int ks) __attribute__((always_inline)) {
+      const uint32_t a = ks < 2 ? shared_own : shared_other, x = 32u * (uint32_t)(ks & 1), rows = 1024u * (uint32_t)(ks & 1);
+      return TileReader<D>::cols_from((a ^ x) + region + rows, (a ^ (x + 16u)) + region + rows + 512u);
     };
-    auto shared_ds = [&](int ks) __attribute__((always_inline)) {
-      return *reinterpret_cast<const u32x4*>(smem + kSharedDs + ds_now * 16384u + (ks < 2 ? mine_at : other_at) + 1024 * (ks & 1));
-    };
+    auto shared_p = [&](int ks) __attribute__((always_inline)) { return shared_at(kShared, ks); };
+    auto shared_ds = [&](int ks) __attribute__((always_inline)) { return shared_at(kSharedDs + ds_now * 16384u, ks); };
     constexpr int kPer = 16 / NS;  // elements between two MFMAs
 
     if (s_begin < s_end) {
     request();
-    if (s_begin + 1u < s_end) request();
+    request();
     __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own count of outstanding loads)
     wait_all();
     sacc = f32x16{0}; dp = f32x16{0};
@@ -720,21 +749,18 @@ __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
     for (int n = 0; n < LA; ++n) ra[n] = fetch(n);
 #pragma unroll
     for (int n = 0; n < 2 * NS; ++n) {
-      if (n < NS) sacc = T::mfma32(ra[n % LA], kf[n], sacc); else dp = T::mfma32(ra[n % LA], vf[n - NS], dp);
+      if (n < NS) sacc = T::mfma32(kf[n], ra[n % LA], sacc); else dp = T::mfma32(vf[n - NS], ra[n % LA], dp);
       if (n + LA < 2 * NS) ra[n % LA] = fetch(n + LA);
     }
     hide();
+    load_stats();
 #pragma unroll
-    for (int v = 0; v < 16; v += 4) {
-      const f32x4 neg = stat(0, v >> 2), delta = stat(1, v >> 2);
+    for (int v = 0; v < 16; ++v) exponential(v);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) exponential(v + e, neg[e]);
-      finish(v, delta[0], delta[1]);
-      finish(v + 2, delta[2], delta[3]);
-    }
+    for (int v = 0; v < 16; v += 2) finish(v);
     share_p();
-    share_ds(0u, 0);
-    share_ds(0u, 1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) share_ds(0u, i);
     wait_all();
     next = 1u;
 #pragma unroll
@@ -742,33 +768,30 @@ __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
     for (uint32_t step = s_begin; step < s_end; ++step) {
       start += 64u;
       if (start >= tok.to) start = tok.from;
-      const bool more = step + 2u < s_end;
-      f32x4 st[2];
       u32x4 rb[2];  // operands of P and dS, one ahead
-      // S and dP of the next step (behind the last: of no use), its exponentials
+      // S and dP of the next step (behind the last: of no use), its exponentials; the one after that is asked for, into the
+      // buffer of the step before this one
       sacc = f32x16{0}; dp = f32x16{0};
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
-        sacc = T::mfma32(ra[n % LA], kf[n], sacc);
+        sacc = T::mfma32(kf[n], ra[n % LA], sacc);
         ra[n % LA] = fetch(n + LA);
-        if (n == NS - 1) st[0] = stat(0, 0);
-        if (more) {  // (the buffer of the step before this one is free)
-          ask(n);
-          if (n == NS - 1)
+        if (n == 0) load_stats();
+        ask(n);
+        if (n == NS - 1) {
 #pragma unroll
-            for (int part = NS; part < kAsks; ++part) ask(part);
+          for (int part = NS; part < kAsks; ++part) ask(part);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
       hide();
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
-        dp = T::mfma32(ra[n % LA], vf[n], dp);
+        dp = T::mfma32(vf[n], ra[n % LA], dp);
         stay(dp);
         ra[n % LA] = fetch(NS + n + LA);
-        if (kPer * n % 4 == 0) st[(kPer * n / 4 + 1) & 1] = kPer * n < 12 ? stat(0, kPer * n / 4 + 1) : stat(1, 0);
 #pragma unroll
-        for (int v = kPer * n; v < kPer * (n + 1); ++v) exponential(v, st[(v >> 2) & 1][v & 3]);
+        for (int v = kPer * n; v < kPer * (n + 1); ++v) exponential(v);
         if (n == NS - 1) rb[0] = shared_p(0);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -778,10 +801,9 @@ __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
         if (n % NH == 0) rb[(ks + 1) & 1] = ks < 3 ? shared_p(ks + 1) : shared_ds(0);
         dv[n % NH] = T::mfma32(ra[n % LA], rb[ks & 1], dv[n % NH]);
         ra[n % LA] = fetch(2 * NS + n + LA);
-        if (kPer * n % 4 == 0 && kPer * n < 12) st[(kPer * n / 4 + 1) & 1] = stat(1, kPer * n / 4 + 1);
 #pragma unroll
-        for (int v = kPer * n; v < kPer * (n + 1); v += 2) finish(v, st[(v >> 2) & 1][v & 3], st[(v >> 2) & 1][(v & 3) + 1]);
-        if (kPer * (n + 1) % 8 == 0) share_ds(ds_now ^ 1u, kPer * (n + 1) / 8 - 1);
+        for (int v = kPer * n; v < kPer * (n + 1); v += 2) finish(v);
+        if (kPer * (n + 1) % 4 == 0) share_ds(ds_now ^ 1u, kPer * (n + 1) / 4 - 1);
         __builtin_amdgcn_sched_barrier(0);
       }
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // every wave has read this step's P
@@ -802,6 +824,7 @@ __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
       }
       ds_now ^= 1u;
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (what was asked for past the end has landed too)
     }
 
     const float by_k = kScaled ? g.scale / (ds_scale * __builtin_ldexpf(1.0f, (int)kShiftP<T>)) : g.scale;
@@ -934,15 +957,19 @@ GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, in
   p.units = (long long)B * Hkv;
   p.row_tiles = (group * Sq + kTileRows - 1) / kTileRows;
   p.key_tiles = (Sk + kGradKeys - 1) / kGradKeys;
-  // steps of 64 tokens of an ordinary key tile (an estimate), of which a worker has at least four
-  long long steps = window > 0 ? ((long long)window + kGradKeys + 62) / 64 + 1 : head_steps;
-  steps = (steps < head_steps ? steps : head_steps) * group * p.units * p.key_tiles;
-  p.workers = 256;  // one per CU
-  if (steps / 4 < p.workers) p.workers = (steps / 4 + 7) / 8 * 8;
-  if (p.workers < 8) p.workers = 8;
   p.sink_tiles = window > 0 ? ((long long)sinks + kGradKeys - 1) / kGradKeys : 0;
   if (p.sink_tiles > p.key_tiles) p.sink_tiles = p.key_tiles;
   const long long lines = p.units % 8 == 0 ? 8 : 1, plain = p.units / lines * (p.key_tiles - p.sink_tiles);
+  // steps of 64 tokens of an ordinary key tile (an estimate), and of all tiles together
+  long long steps = window > 0 ? ((long long)window + kGradKeys + 62) / 64 + 1 : head_steps;
+  steps = (steps < head_steps ? steps : head_steps) * group;
+  const long long all = steps * lines * plain + head_steps * group * p.units * p.sink_tiles;
+  // One worker per CU.  Where there are fewer tiles than that, a worker per tile saves the second tile of a worker's piece
+  // and the sums of parts (some 14 us, as much as 14 steps of D = 64 or 7 of 128), and splitting them saves steps.
+  p.workers = 256;
+  if (lines * plain < p.workers && steps - all / p.workers < (D == 64 ? 14 : 7)) p.workers = lines * plain;
+  if (all / 2 < p.workers) p.workers = all / 2 / lines * lines;
+  if (p.workers < lines) p.workers = lines;
   p.split = p.units * p.sink_tiles + lines * (plain % (p.workers / lines));
   p.rows = (size_t)B * (size_t)Hq * (size_t)Sq;
   const auto up = [](size_t n) { return (n + 15) & ~(size_t)15; };

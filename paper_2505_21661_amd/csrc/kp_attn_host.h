@@ -92,8 +92,9 @@ inline Plan plan_of(long long seqs, long long rows, long long most_keys, int Hkv
   const long long per_tile = p.few ? 16 : 128;
   p.tiles = even ? (rows / seqs + per_tile - 1) / per_tile * seqs : rows / per_tile + seqs;
   p.units = p.tiles * Hkv;
-  // as many workgroups as the chip holds at a time, as long as a run has 256 keys
-  const long long want = p.few ? 1024 : 512, runs = (most_keys + 255) / 256;
+  // As many workgroups as the chip holds at a time.  Joining the parts takes 6 us more, in which a workgroup gets through
+  // some 1000 keys: fewer than 1536 are not split, and a run has 512.
+  const long long want = p.few ? 1024 : 512, runs = most_keys < 1536 ? 1 : most_keys / 512;
   p.splits = p.units * 2 > want ? 1 : want / p.units;
   if (p.splits > runs) p.splits = runs;
   if (p.splits < 1) p.splits = 1;

@@ -506,18 +506,34 @@ __global__ __launch_bounds__(kThreads) void kp_attn_join(Args g) {
   const uint32_t flat = tl.first + r;
   if (flat >= tl.rows) return;
   const size_t rows = (size_t)g.tiles * g.hkv * ROWS, row = part_row<ROWS>(g, tile_id, h, r);
-  float m = kNoKey;
-  for (uint32_t s = 0; s < g.splits; ++s) m = fmaxf(m, g.part[2 * (s * rows + row)]);
-  float l = 0.f;
+  float m = kNoKey, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (uint32_t s = 0; s < g.splits; ++s) {
-    const f32x2 ml = *reinterpret_cast<const f32x2*>(g.part + 2 * (s * rows + row));
-    if (ml.y == 0.f) continue;
-    const float w = __builtin_amdgcn_exp2f(ml.x - m);
-    l = __builtin_fmaf(ml.y, w, l);
-    const f32x4 part = *reinterpret_cast<const f32x4*>(g.part + 2 * g.splits * rows + (s * rows + row) * D + 4u * c);
+  constexpr uint32_t kAtOnce = 8;  // parts whose loads are in flight together
+  for (uint32_t s0 = 0; s0 < g.splits; s0 += kAtOnce) {
+    f32x2 ml[kAtOnce];
+    f32x4 part[kAtOnce];
+    float top = m;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(part[i], w, o[i]);
+    for (uint32_t i = 0; i < kAtOnce; ++i) {
+      const size_t at = (s0 + i < g.splits ? s0 + i : g.splits - 1u) * rows + row;
+      ml[i] = *reinterpret_cast<const f32x2*>(g.part + 2 * at);
+      part[i] = *reinterpret_cast<const f32x4*>(g.part + 2 * g.splits * rows + at * D + 4u * c);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kAtOnce; ++i) top = fmaxf(top, ml[i].x);
+    const float before = __builtin_amdgcn_exp2f(m - top);
+    l *= before;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= before;
+    m = top;
+#pragma unroll
+    for (uint32_t i = 0; i < kAtOnce; ++i) {
+      if ((s0 + i >= g.splits) | (ml[i].y == 0.f)) continue;
+      const float w = __builtin_amdgcn_exp2f(ml[i].x - m);
+      l = __builtin_fmaf(ml[i].y, w, l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(part[i][e], w, o[e]);
+    }
   }
   const RowPlace at = place_of(flat, g.group);
   const uint32_t head = h * g.group + at.in_group, seq = PAGED ? 0u : tl.seq;
