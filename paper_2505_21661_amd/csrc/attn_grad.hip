@@ -344,13 +344,15 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
         }
         __builtin_amdgcn_s_setprio(0);
         if (masked) {
-          const int32_t base = (int32_t)(start + 4u * h32), hi = (p < (int32_t)limit ? p : (int32_t)limit - 1) - base;
-          const int32_t lo = g.window != 0u ? p - (int32_t)g.window + 1 - base : -base, sk = (int32_t)g.sinks - base;
+          const RowMask m(p, limit, (int32_t)(start + 4u * h32), g.window, g.sinks);
+          if ((g.window != 0u) & (start < g.sinks)) {
+            asm volatile("");  // (branches: no selects where nothing is masked)
 #pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const int32_t c = 32 * tk + 8 * (v >> 2) + (v & 3);
-            const bool seen = (c <= hi) & ((c >= lo) | (c < sk));
-            sacc[v] = seen ? sacc[v] : -INFINITY;
+            for (int v = 0; v < 16; ++v) sacc[v] = m.sees_mixed(32 * tk + 8 * (v >> 2) + (v & 3)) ? sacc[v] : -INFINITY;
+          } else {
+            asm volatile("");
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sacc[v] = m.sees(32 * tk + 8 * (v >> 2) + (v & 3)) ? sacc[v] : -INFINITY;
           }
         }
         u32x4 ds[2];
@@ -684,27 +686,20 @@ __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
     auto hide = [&]() __attribute__((always_inline)) {
       const int32_t first = (int32_t)(start + 32u * hf), last = first + 31, k0 = (int32_t)j0, k1 = k0 + 31;
       if ((last >= (int32_t)tok.to) | (off + first < k1) | ((g.window != 0u) & (k1 >= (int32_t)g.sinks) & (off + last - k0 >= (int32_t)g.window))) {
-        asm volatile("");  // (a branch, not 16 selects every time)
-        // key of element c: base + c; visible: from hi - count to hi (unsigned: c - from <= count), and below sk
-        const int32_t token = first + (int32_t)l32, p = token < (int32_t)tok.to ? off + token : -1, base = k0 + 4 * (int32_t)h32;
-        const int32_t hi = p - base, lo = (g.window != 0u ? p - (int32_t)g.window + 1 : 0) - base;
-        const uint32_t from = hi < lo ? 64u : (uint32_t)lo, count = hi < lo ? 0u : (uint32_t)(hi - lo);
+        const int32_t token = first + (int32_t)l32;
+        const RowMask m(token < (int32_t)tok.to ? off + token : -1, g.n_k, k0 + 4 * (int32_t)h32, g.window, g.sinks);
         if ((g.window == 0u) | (k0 >= (int32_t)g.sinks)) {
+          asm volatile("");  // (branches: no selects where nothing is masked)
 #pragma unroll
-          for (int v = 0; v < 16; ++v) sacc[v] = (uint32_t)(8 * (v >> 2) + (v & 3)) - from <= count ? sacc[v] : -INFINITY;
+          for (int v = 0; v < 16; ++v) sacc[v] = m.sees(8 * (v >> 2) + (v & 3)) ? sacc[v] : -INFINITY;
+        } else if (off + first - k1 >= (int32_t)g.window) {  // sinks alone are left
+          asm volatile("");
+#pragma unroll
+          for (int v = 0; v < 16; ++v) sacc[v] = 8 * (v >> 2) + (v & 3) <= m.sink ? sacc[v] : -INFINITY;
         } else {
-          const int32_t sk = (hi < (int32_t)g.sinks - 1 - base ? hi : (int32_t)g.sinks - 1 - base);
-          if (off + first - k1 >= (int32_t)g.window) {  // sinks alone are left
+          asm volatile("");
 #pragma unroll
-            for (int v = 0; v < 16; ++v) sacc[v] = 8 * (v >> 2) + (v & 3) <= sk ? sacc[v] : -INFINITY;
-          } else {
-            asm volatile("");
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-              const int32_t c = 8 * (v >> 2) + (v & 3);
-              sacc[v] = (((uint32_t)c - from <= count) | (c <= sk)) ? sacc[v] : -INFINITY;
-            }
-          }
+          for (int v = 0; v < 16; ++v) sacc[v] = m.sees_mixed(8 * (v >> 2) + (v & 3)) ? sacc[v] : -INFINITY;
         }
       }
     };
@@ -967,8 +962,8 @@ GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, in
   // One worker per CU.  Where there are fewer tiles than that, a worker per tile saves the second tile of a worker's piece
   // and the sums of parts (some 14 us, as much as 14 steps of D = 64 or 7 of 128), and splitting them saves steps.
   p.workers = 256;
-  if (lines * plain < p.workers && steps - all / p.workers < (D == 64 ? 14 : 7)) p.workers = lines * plain;
-  if (all / 2 < p.workers) p.workers = all / 2 / lines * lines;
+  if (plain > 0 && lines * plain < p.workers && steps - all / p.workers < (D == 64 ? 14 : 7)) p.workers = lines * plain;
+  if (all < p.workers) p.workers = all / lines * lines;
   if (p.workers < lines) p.workers = lines;
   p.split = p.units * p.sink_tiles + lines * (plain % (p.workers / lines));
   p.rows = (size_t)B * (size_t)Hq * (size_t)Sq;

@@ -164,6 +164,23 @@ __device__ __forceinline__ Span span_of(int32_t p_first, int32_t p_last, uint32_
   return s;
 }
 
+// Which of a row's scores against a run of keys are visible: element c, the key first + c, is if c - from <= count
+// (unsigned) or, where the run holds sinks (mixed), if c <= sink.  One subtraction and one comparison per score.
+struct RowMask {
+  uint32_t from, count;
+  int32_t sink;
+  // the row stands at p and sees nothing from `limit` on
+  __device__ __forceinline__ RowMask(int32_t p, uint32_t limit, int32_t first, uint32_t window, uint32_t sinks) {
+    const int32_t hi = (p < (int32_t)limit ? p : (int32_t)limit - 1) - first, lo = (window != 0u ? p - (int32_t)window + 1 : 0) - first;
+    const int32_t sk = (int32_t)sinks - 1 - first;
+    from = hi < lo ? 1u << 30 : (uint32_t)lo;
+    count = hi < lo ? 0u : (uint32_t)(hi - lo);
+    sink = sk < hi ? sk : hi;
+  }
+  __device__ __forceinline__ bool sees(int c) const { return (uint32_t)c - from <= count; }
+  __device__ __forceinline__ bool sees_mixed(int c) const { return ((uint32_t)c - from <= count) | (c <= sink); }
+};
+
 // Keys and values of one kv head of one sequence.
 template <int D, int SRC>
 struct Source {

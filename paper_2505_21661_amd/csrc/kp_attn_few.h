@@ -203,16 +203,15 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_few(Args g) {
       if (g.window != 0u) masked = masked || (p_max - (int32_t)start >= (int32_t)g.window && end > (int32_t)g.sinks);
       if constexpr (SRC != kPlain) masked = masked || valid != ~0ull;
       if (masked) {
-        const int32_t base = (int32_t)(start + 4u * g4), hi = (p < (int32_t)limit ? p : (int32_t)limit - 1) - base;
-        const int32_t lo = g.window != 0u ? p - (int32_t)g.window + 1 - base : -base, sk = (int32_t)g.sinks - base;
-        const uint32_t there = SRC != kPlain ? (uint32_t)valid >> (4u * g4) : 0u;
+        const RowMask m(p, limit, (int32_t)(start + 4u * g4), g.window, g.sinks);
+        const uint32_t there = SRC != kPlain ? (uint32_t)valid >> (4u * g4) : ~0u;  // keys whose page exists
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int32_t c = 16 * n + i;
-            bool seen = (c <= hi) & ((c >= lo) | (c < sk));  // (no short cuts: they become branches)
-            if constexpr (SRC != kPlain) seen = seen & (((there >> c) & 1u) != 0u);
+            const int c = 16 * n + i;
+            // (& and |: short cuts become branches)
+            const bool seen = (m.sees(c) | ((g.window != 0u) & (c <= m.sink))) & (((there >> c) & 1u) != 0u);
             sacc[n][i] = seen ? sacc[n][i] : -INFINITY;
           }
       }

@@ -296,16 +296,22 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
       u32x4 pw[4];  // P, in accumulator order: one entry per MFMA step of V^T P^T (16 keys)
       auto mask = [&](int tk) __attribute__((always_inline)) {
         if (!masked) return;
-        // key of element c: start + 4 h32 + c
-        const int32_t base = (int32_t)(start + 4u * h32), hi = (p < (int32_t)limit ? p : (int32_t)limit - 1) - base;
-        const int32_t lo = g.window != 0u ? p - (int32_t)g.window + 1 - base : -base, sk = (int32_t)g.sinks - base;
-        const uint64_t there = SRC != kPlain ? valid >> (4u * h32) : 0ull;
+        const RowMask m(p, limit, (int32_t)(start + 4u * h32), g.window, g.sinks);
+        if ((g.window != 0u) & (start < g.sinks)) {
+          asm volatile("");  // (branches: no selects where nothing is masked)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int32_t c = 32 * tk + 8 * (v >> 2) + (v & 3);
-          bool seen = (c <= hi) & ((c >= lo) | (c < sk));  // (no short cuts: they become branches)
-          if constexpr (SRC != kPlain) seen = seen & (((there >> c) & 1ull) != 0ull);
-          sacc[tk][v] = seen ? sacc[tk][v] : -INFINITY;
+          for (int v = 0; v < 16; ++v) sacc[tk][v] = m.sees_mixed(32 * tk + 8 * (v >> 2) + (v & 3)) ? sacc[tk][v] : -INFINITY;
+        } else {
+          asm volatile("");
+#pragma unroll
+          for (int v = 0; v < 16; ++v) sacc[tk][v] = m.sees(32 * tk + 8 * (v >> 2) + (v & 3)) ? sacc[tk][v] : -INFINITY;
+        }
+        if constexpr (SRC != kPlain) {
+          if (valid != ~0ull) {  // pages that are not there
+            const uint64_t there = valid >> (4u * h32);
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sacc[tk][v] = (there >> (32 * tk + 8 * (v >> 2) + (v & 3))) & 1ull ? sacc[tk][v] : -INFINITY;
+          }
         }
       };
       auto exps = [&](int pair) __attribute__((always_inline)) {

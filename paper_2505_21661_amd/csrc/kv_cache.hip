@@ -19,46 +19,57 @@ struct WriteArgs {
   uint64_t n_slots;
 };
 
-// D / 8 lanes to a row, 16 bytes to a lane; blockIdx.y: keys or values.
+// D / 8 lanes to a row, 16 bytes to a lane, kWriteRows rows one after the other, all of whose loads are in flight together;
+// blockIdx.y: keys or values.
+constexpr uint32_t kWriteRows = 4;
 template <class T, int D, bool E4M3>
 __global__ __launch_bounds__(kThreads) void kp_cache_write_rows(WriteArgs g) {
-  constexpr uint32_t kLanes = D / 8;
-  const uint32_t r = blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes, c = threadIdx.x % kLanes;
-  if (r >= g.rows) return;
-  const uint32_t token = r / g.hkv, head = r - token * g.hkv;
+  constexpr uint32_t kLanes = D / 8, kStep = kThreads / kLanes;
+  const uint32_t r0 = blockIdx.x * (kStep * kWriteRows) + threadIdx.x / kLanes, c = threadIdx.x % kLanes;
   const Heads src = blockIdx.y ? g.v : g.k;
   uint8_t* const cache = blockIdx.y ? g.v_cache : g.k_cache;
-  const int64_t slot = g.slots[token];
-  const u32x4 raw = *reinterpret_cast<const u32x4*>(src.at + src.token * (int64_t)token + src.head * (int64_t)head + 8u * c);
-  if (slot < 0 || (uint64_t)slot >= g.n_slots) return;
-  const uint32_t page = (uint32_t)((uint64_t)slot >> g.page_log2), in = (uint32_t)slot & ((1u << g.page_log2) - 1u);
-  const uint32_t row = ((page * g.hkv + head) << g.page_log2) + in;
-  if constexpr (!E4M3) {
-    *reinterpret_cast<u32x4*>(cache + (size_t)row * (2 * D) + 16u * c) = raw;
-  } else {
-    float x[8], top = 0.f;
+  int64_t slot[kWriteRows];
+  uint32_t head[kWriteRows];
+  u32x4 raw[kWriteRows];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      x[i] = T::to_float((raw[i >> 1] >> (16 * (i & 1))) & 0xFFFFu);
-      const bool finite = __builtin_fabsf(x[i]) < INFINITY;
-      top = fmaxf(top, finite ? __builtin_fabsf(x[i]) : 0.f);
-      x[i] = finite ? x[i] : __builtin_nanf("");
+  for (uint32_t i = 0; i < kWriteRows; ++i) {
+    const uint32_t r = r0 + kStep * i, row = r < g.rows ? r : g.rows - 1u, token = row / g.hkv;
+    head[i] = row - token * g.hkv;
+    slot[i] = r < g.rows ? g.slots[token] : -1;
+    raw[i] = *reinterpret_cast<const u32x4*>(src.at + src.token * (int64_t)token + src.head * (int64_t)head[i] + 8u * c);
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < kWriteRows; ++i) {
+    if (slot[i] < 0 || (uint64_t)slot[i] >= g.n_slots) continue;  // (the same for all lanes of a row)
+    const uint32_t page = (uint32_t)((uint64_t)slot[i] >> g.page_log2), in = (uint32_t)slot[i] & ((1u << g.page_log2) - 1u);
+    const uint32_t row = ((page * g.hkv + head[i]) << g.page_log2) + in;
+    if constexpr (!E4M3) {
+      *reinterpret_cast<u32x4*>(cache + (size_t)row * (2 * D) + 16u * c) = raw[i];
+    } else {
+      float x[8], top = 0.f;
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        x[n] = T::to_float((raw[i][n >> 1] >> (16 * (n & 1))) & 0xFFFFu);
+        const bool finite = __builtin_fabsf(x[n]) < INFINITY;
+        top = fmaxf(top, finite ? __builtin_fabsf(x[n]) : 0.f);
+        x[n] = finite ? x[n] : __builtin_nanf("");
+      }
+#pragma unroll
+      for (int d = 1; d < (int)kLanes; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+      const uint32_t bits = __builtin_bit_cast(uint32_t, top);
+      int e = (int)(bits >> 23) - ((bits & 0x7FFFFFu) <= 0x600000u ? 135 : 134);
+      e = top == 0.f ? 0 : (e < -126 ? -126 : e);
+      const float scale = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
+      u32x2 codes;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        int p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w] * scale, x[4 * w + 1] * scale, 0, false);
+        p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w + 2] * scale, x[4 * w + 3] * scale, p, true);
+        codes[w] = (uint32_t)p;
+      }
+      *reinterpret_cast<u32x2*>(cache + (size_t)row * D + 8u * c) = codes;
+      if (c == 0) (blockIdx.y ? g.v_exp : g.k_exp)[row] = (uint8_t)(e + 127);
     }
-#pragma unroll
-    for (int d = 1; d < (int)kLanes; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-    const uint32_t bits = __builtin_bit_cast(uint32_t, top);
-    int e = (int)(bits >> 23) - ((bits & 0x7FFFFFu) <= 0x600000u ? 135 : 134);
-    e = top == 0.f ? 0 : (e < -126 ? -126 : e);
-    const float scale = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
-    u32x2 codes;
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      int p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w] * scale, x[4 * w + 1] * scale, 0, false);
-      p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w + 2] * scale, x[4 * w + 3] * scale, p, true);
-      codes[w] = (uint32_t)p;
-    }
-    *reinterpret_cast<u32x2*>(cache + (size_t)row * D + 8u * c) = codes;
-    if (c == 0) (blockIdx.y ? g.v_exp : g.k_exp)[row] = (uint8_t)(e + 127);
   }
 }
 
@@ -107,6 +118,7 @@ __global__ __launch_bounds__(kThreads) void kp_cache_read_rows(ReadArgs g) {
   const uint8_t* const cache = blockIdx.y ? g.v_cache : g.k_cache;
   const uint8_t* const exps = blockIdx.y ? g.v_exp : g.k_exp;
   const uint32_t c = threadIdx.x % kLanes;
+#pragma unroll 4
   for (uint32_t i = threadIdx.x / kLanes; i < kReadTokens * g.hkv; i += kThreads / kLanes) {
     const uint32_t tl = i / g.hkv, head = i - tl * g.hkv, how = state[tl];
     if (how == 0) continue;
@@ -149,7 +161,7 @@ extern "C" kp_status kp_cache_write(const kp_heads* k, const kp_heads* v, const 
   g.k_exp = cache->k_exp; g.v_exp = cache->v_exp;
   g.rows = (uint32_t)T * (uint32_t)cache->Hkv; g.hkv = (uint32_t)cache->Hkv; g.page_log2 = log2_of(cache->page);
   g.n_slots = (uint64_t)cache->n_pages * (uint64_t)cache->page;
-  const uint32_t per = kThreads / (cache->D / 8);
+  const uint32_t per = kThreads / (cache->D / 8) * kWriteRows;
   const dim3 grid((g.rows + per - 1) / per, 2);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool e4m3 = cache->cache_type == KP_CACHE_E4M3, fp16 = cache->type == KP_FP16;
