@@ -451,11 +451,20 @@ typedef struct {
 /*
  * o = softmax(scale q k^T, visible keys) v for B sequences of Sq query tokens over Sk keys (any lengths from
  * 1 on, Sq > Sk included); lse [B, Hq, Sq].
+ * region_mask, trace_buf, trace_cap: as for the other targets (region_mask 0: the uninstrumented kernel, trace_buf may
+ * be NULL), through the generic record sites; the LDS ring has 16 KiB.  4 waves, n_wg workgroups (kp_attn_window_launch_shape)
+ * and three regions, per tile of 64 keys (per step of 32 where there are few rows, each wave for itself):
+ *   0 K Q^T, 1 mask and softmax, 2 V^T P^T; the requests of the next keys and values stand in 0 (values of few rows in 2).
+ * A workgroup records 6 times per wave and tile that its rows see any key of; where there are few workgroups the keys of
+ * the rows are split, so that a workgroup is a run of tiles, and a further, unrecorded kernel joins them.
  */
 size_t kp_attn_window_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks);
 kp_status kp_attn_window(const kp_heads* q, const kp_heads* k, const kp_heads* v, const kp_heads* o, float* lse,
                          int B, int Hq, int Hkv, int Sq, int Sk, int D, int type, int window, int sinks,
-                         float scale, void* workspace, size_t workspace_bytes, void* stream);
+                         float scale, void* workspace, size_t workspace_bytes, uint32_t region_mask, void* trace_buf,
+                         size_t trace_cap, void* stream);
+kp_status kp_attn_window_launch_shape(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks,
+                                      int* n_wg, int* waves_per_wg, int* n_regions);
 
 /*
  * Gradients of kp_attn_window: from its o and lse and the gradient d_o of o, with
@@ -519,7 +528,9 @@ size_t kp_attn_paged_bytes(int T, int n_seqs, int Hq, int Hkv, int D, int table_
 kp_status kp_attn_paged(const kp_heads* q, const kp_cache* cache, const int32_t* block_table, int table_width,
                         const int32_t* lens, const int32_t* starts, const kp_heads* o, float* lse, int T, int n_seqs,
                         int Hq, int window, int sinks, float scale, void* workspace, size_t workspace_bytes,
-                        void* stream);
+                        uint32_t region_mask, void* trace_buf, size_t trace_cap, void* stream);
+kp_status kp_attn_paged_launch_shape(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int window,
+                                     int sinks, int* n_wg, int* waves_per_wg, int* n_regions);
 
 /*
  * Timer calibration (Sec. 5.4 "Cycle-level Overhead": cost of one record; Sec. 4.3: that

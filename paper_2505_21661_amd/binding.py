@@ -126,11 +126,13 @@ def _optional(L):
     ip = ctypes.POINTER(ctypes.c_int)
     hp, cp = ctypes.POINTER(kp_heads), ctypes.POINTER(kp_cache)
     sigs = {
-        "kp_attn_window": [hp, hp, hp, hp, vp, ci, ci, ci, ci, ci, ci, ci, ci, ci, fl, vp, sz, vp],
+        "kp_attn_window": [hp, hp, hp, hp, vp, ci, ci, ci, ci, ci, ci, ci, ci, ci, fl, vp, sz, u32, vp, sz, vp],
+        "kp_attn_window_launch_shape": [ci] * 8 + [ip] * 3,
+        "kp_attn_paged_launch_shape": [ci] * 9 + [ip] * 3,
         "kp_attn_window_grad": [hp, hp, hp, hp, vp, hp, hp, hp, hp, ci, ci, ci, ci, ci, ci, ci, ci, ci, fl, vp, sz, vp],
         "kp_cache_write": [hp, hp, vp, ci, cp, vp],
         "kp_cache_read": [cp, vp, ci, vp, ci, ci, hp, hp, vp],
-        "kp_attn_paged": [hp, cp, vp, ci, vp, vp, hp, vp, ci, ci, ci, ci, ci, fl, vp, sz, vp],
+        "kp_attn_paged": [hp, cp, vp, ci, vp, vp, hp, vp, ci, ci, ci, ci, ci, fl, vp, sz, u32, vp, sz, vp],
         "kp_gemm_launch_shape": [ci, ci, ci, ip, ip, ip],
         "kp_gemm_instrumented": [vp, vp, vp, ci, ci, ci, u32, vp, sz, vp],
         "kp_attn_launch_shape": [ci, ci, ci, ci, ip, ip, ip],
@@ -440,7 +442,19 @@ def kp_attn_window_bytes(q, k, window: int, sinks: int) -> int:
     return int(lib().kp_attn_window_bytes(*_window_sizes(q, k), window, sinks))
 
 
-def kp_attn_window(q, k, v, o, lse, window: int, sinks: int, scale: float, workspace=None, stream=None) -> None:
+def _shape_of(call, *sizes) -> tuple[int, int, int]:
+    a, b, c = ctypes.c_int(), ctypes.c_int(), ctypes.c_int()
+    _check(call(*sizes, ctypes.byref(a), ctypes.byref(b), ctypes.byref(c)))
+    return a.value, b.value, c.value
+
+
+def kp_attn_window_launch_shape(q, k, window: int, sinks: int) -> tuple[int, int, int]:
+    """Workgroups, waves per workgroup and regions of a recording of kp_attn_window."""
+    return _shape_of(lib().kp_attn_window_launch_shape, *_window_sizes(q, k), window, sinks)
+
+
+def kp_attn_window(q, k, v, o, lse, window: int, sinks: int, scale: float, workspace=None, region_mask: int = 0,
+                   trace_buf=None, trace_cap: int = 0, stream=None) -> None:
     """o = softmax(scale q k^T over the visible keys) v; q, o [B, Hq, Sq, D], k, v [B, Hkv, Sk, D] (any strides with D
     innermost), lse [B, Hq, Sq] float32 or None.  A token at position p = Sk - Sq + i sees keys j <= p with p - j < window
     (window 0: all) or j < sinks."""
@@ -450,7 +464,8 @@ def kp_attn_window(q, k, v, o, lse, window: int, sinks: int, scale: float, works
     _check(lib().kp_attn_window(
         _heads("q", q, q.shape, dtype), _heads("k", k, (B, Hkv, Sk, D), dtype), _heads("v", v, kv, dtype),
         _heads("o", o, q.shape, dtype), 0 if lse is None else _flat("lse", lse, _dtype("float32"), (B, Hq, Sq)),
-        B, Hq, Hkv, Sq, Sk, D, _type_code(dtype), window, sinks, scale, ws, n, _stream(stream)))
+        B, Hq, Hkv, Sq, Sk, D, _type_code(dtype), window, sinks, scale, ws, n, region_mask & 0xFFFFFFFF, _ptr(trace_buf),
+        trace_cap, _stream(stream)))
 
 
 def kp_attn_window_grad_bytes(q, k, window: int, sinks: int) -> int:
@@ -509,8 +524,16 @@ def kp_attn_paged_bytes(q, k_cache, block_table, window: int, sinks: int) -> int
     return int(lib().kp_attn_paged_bytes(T, n, Hq, k_cache.shape[1], D, width, k_cache.shape[2], window, sinks))
 
 
+def kp_attn_paged_launch_shape(q, k_cache, block_table, window: int, sinks: int) -> tuple[int, int, int]:
+    """Workgroups, waves per workgroup and regions of a recording of kp_attn_paged."""
+    T, Hq, D = q.shape
+    n, width = block_table.shape
+    return _shape_of(lib().kp_attn_paged_launch_shape, T, n, Hq, k_cache.shape[1], D, width, k_cache.shape[2], window, sinks)
+
+
 def kp_attn_paged(q, k_cache, v_cache, k_exp, v_exp, block_table, lens, starts, o, lse, window: int, sinks: int,
-                  scale: float, workspace=None, stream=None) -> None:
+                  scale: float, workspace=None, region_mask: int = 0, trace_buf=None, trace_cap: int = 0,
+                  stream=None) -> None:
     """Attention of new tokens q [T, Hq, D] over a cache that holds them: sequence s has the tokens starts[s] ..
     starts[s + 1] - 1 and lens[s] keys, found through block_table [n, width] int32; o [T, Hq, D], lse [Hq, T] or None."""
     T, Hq, D = q.shape
@@ -523,7 +546,7 @@ def kp_attn_paged(q, k_cache, v_cache, k_exp, v_exp, block_table, lens, starts, 
         _flat("block_table", block_table, _dtype("int32")), width, _flat("lens", lens, _dtype("int32"), (n,)),
         _flat("starts", starts, _dtype("int32"), (n + 1,)), _heads("o", o, q.shape, q.dtype),
         0 if lse is None else _flat("lse", lse, _dtype("float32"), (Hq, T)), T, n, Hq, window, sinks, scale, ws, nbytes,
-        _stream(stream)))
+        region_mask & 0xFFFFFFFF, _ptr(trace_buf), trace_cap, _stream(stream)))
 
 
 # ---- views of the statistics block (layout documented in include/kperf.h) ------------------------

@@ -14,9 +14,18 @@ extern "C" size_t kp_attn_paged_bytes(int T, int n_seqs, int Hq, int Hkv, int D,
   return plan_paged(T, n_seqs, Hq, Hkv, D, (long long)table_width * page, window, sinks).bytes;
 }
 
+extern "C" kp_status kp_attn_paged_launch_shape(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int window,
+                                                int sinks, int* n_wg, int* waves_per_wg, int* n_regions) {
+  kp::clear_error();
+  if (kp_status s = check_common(Hq, Hkv, D, KP_BF16, window, sinks, 1.f)) return s;
+  if (T < 1 || n_seqs < 1 || table_width < 0 || page < 1) return kp::fail(KP_ERR_INVALID_ARG, "T, n_seqs and page must be positive, table_width not negative");
+  return launch_shape(plan_paged(T, n_seqs, Hq, Hkv, D, (long long)table_width * page, window, sinks), n_wg, waves_per_wg, n_regions);
+}
+
 extern "C" kp_status kp_attn_paged(const kp_heads* q, const kp_cache* cache, const int32_t* block_table, int table_width,
                                    const int32_t* lens, const int32_t* starts, const kp_heads* o, float* lse, int T, int n_seqs,
-                                   int Hq, int window, int sinks, float scale, void* workspace, size_t workspace_bytes, void* stream) {
+                                   int Hq, int window, int sinks, float scale, void* workspace, size_t workspace_bytes, uint32_t region_mask, void* trace_buf,
+                                    size_t trace_cap, void* stream) {
   kp::clear_error();
   if (kp_status s = check_cache(cache)) return s;
   const int Hkv = cache->Hkv, D = cache->D;
@@ -44,8 +53,8 @@ extern "C" kp_status kp_attn_paged(const kp_heads* q, const kp_cache* cache, con
   g.part = static_cast<float*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool e4m3 = cache->cache_type == KP_CACHE_E4M3;
-#define KP_PICK(T) (D == 64 ? (e4m3 ? launch<T, 64, kPagedE4m3>(g, plan, st) : launch<T, 64, kPaged>(g, plan, st)) \
-                            : (e4m3 ? launch<T, 128, kPagedE4m3>(g, plan, st) : launch<T, 128, kPaged>(g, plan, st)))
+#define KP_PICK(T) (D == 64 ? (e4m3 ? launch<T, 64, kPagedE4m3>(g, plan, region_mask, trace_buf, trace_cap, st) : launch<T, 64, kPaged>(g, plan, region_mask, trace_buf, trace_cap, st)) \
+                            : (e4m3 ? launch<T, 128, kPagedE4m3>(g, plan, region_mask, trace_buf, trace_cap, st) : launch<T, 128, kPaged>(g, plan, region_mask, trace_buf, trace_cap, st)))
   return cache->type == KP_FP16 ? KP_PICK(Fp16) : KP_PICK(Bf16);
 #undef KP_PICK
 }

@@ -23,9 +23,18 @@ extern "C" size_t kp_attn_window_bytes(int B, int Hq, int Hkv, int Sq, int Sk, i
   return plan_window(B, Hq, Hkv, Sq, Sk, D, window, sinks).bytes;
 }
 
+extern "C" kp_status kp_attn_window_launch_shape(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks, int* n_wg,
+                                                 int* waves_per_wg, int* n_regions) {
+  kp::clear_error();
+  if (kp_status s = check_common(Hq, Hkv, D, KP_BF16, window, sinks, 1.f)) return s;
+  if (kp_status s = check_sizes(B, Hq, Hkv, Sq, Sk, D)) return s;
+  return launch_shape(plan_window(B, Hq, Hkv, Sq, Sk, D, window, sinks), n_wg, waves_per_wg, n_regions);
+}
+
 extern "C" kp_status kp_attn_window(const kp_heads* q, const kp_heads* k, const kp_heads* v, const kp_heads* o, float* lse,
                                     int B, int Hq, int Hkv, int Sq, int Sk, int D, int type, int window, int sinks,
-                                    float scale, void* workspace, size_t workspace_bytes, void* stream) {
+                                    float scale, void* workspace, size_t workspace_bytes, uint32_t region_mask, void* trace_buf,
+                                    size_t trace_cap, void* stream) {
   kp::clear_error();
   if (kp_status s = check_common(Hq, Hkv, D, type, window, sinks, scale)) return s;
   if (kp_status s = check_sizes(B, Hq, Hkv, Sq, Sk, D)) return s;
@@ -44,6 +53,6 @@ extern "C" kp_status kp_attn_window(const kp_heads* q, const kp_heads* k, const 
   g.window = (uint32_t)window; g.sinks = (uint32_t)sinks; g.scale_log2 = scale * kLog2e;
   g.part = static_cast<float*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (type == KP_FP16) return D == 64 ? launch<Fp16, 64, kPlain>(g, plan, st) : launch<Fp16, 128, kPlain>(g, plan, st);
-  return D == 64 ? launch<Bf16, 64, kPlain>(g, plan, st) : launch<Bf16, 128, kPlain>(g, plan, st);
+  if (type == KP_FP16) return D == 64 ? launch<Fp16, 64, kPlain>(g, plan, region_mask, trace_buf, trace_cap, st) : launch<Fp16, 128, kPlain>(g, plan, region_mask, trace_buf, trace_cap, st);
+  return D == 64 ? launch<Bf16, 64, kPlain>(g, plan, region_mask, trace_buf, trace_cap, st) : launch<Bf16, 128, kPlain>(g, plan, region_mask, trace_buf, trace_cap, st);
 }

@@ -14,7 +14,9 @@ namespace attn {
 
 constexpr int kFewRows = 16, kFewKeys = 32;
 
-template <class T, int D, int SRC>
+// Recorded regions, per step of 32 keys: 0 K Q^T and the request of the next keys, 1 mask and softmax, 2 V to LDS, the
+// request of the next values, V^T P^T.
+template <class T, int D, int SRC, int INSTR>
 __global__ __launch_bounds__(kThreads, 2) void kp_attn_few(Args g) {
   constexpr bool E4M3 = SRC == kPagedE4m3;
   constexpr uint32_t kRow = 2u * D;
@@ -27,6 +29,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_few(Args g) {
   __shared__ __align__(16) unsigned char smem[4u * kWaveLds];
   __shared__ float join_m[4][kFewRows], join_l[4][kFewRows];
   __shared__ uint32_t again_rows;
+  extern __shared__ __align__(16) unsigned char ring_lds[];
 
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = wave_uniform(tid >> 6), r16 = lane & 15u, g4 = lane >> 4;
   // (splits of a tile next to one another: they share the tile's queries; heads are dealt to the XCDs as they come)
@@ -41,7 +44,14 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_few(Args g) {
     tile_id = seq * tiles_per + tile_id;
   }
   Tile tl;
-  if (!find_tile<kFewRows, SRC != kPlain>(g, tile_id, &tl)) return;
+  const bool there = find_tile<kFewRows, SRC != kPlain>(g, tile_id, &tl);
+  const uint32_t recorded = unit * (tiles_per * g.splits) + item;  // number of the workgroup in a trace
+  kp::Ring ring{};
+  if constexpr (INSTR != 0) ring = ring_of<INSTR>(g, ring_lds, smem, recorded);
+  if (!there) {
+    if constexpr (INSTR != 0) finish_ring<INSTR>(ring, g, recorded);
+    return;
+  }
   const Source<D, SRC> src(g, tl.seq, h);
   const uint32_t last_row = tl.rows - 1u, flat = tl.first + r16;
   const bool mine = flat <= last_row;
@@ -168,6 +178,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_few(Args g) {
     load_k();
     load_v(row_no);
     valid = valid_next;
+    KP_BOUNDARY(ring, kp::kNoRegion, 0);
     for (uint32_t t = t_first; t < t_end; t += 4u) {
       const bool more = t + 4u < t_end;
       uint32_t limit;
@@ -199,6 +210,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_few(Args g) {
         locate(t + 4u);
         load_k();
       }
+      KP_BOUNDARY(ring, 0, 1);
       bool masked = end > (int32_t)limit || end - 1 > p_min;
       if (g.window != 0u) masked = masked || (p_max - (int32_t)start >= (int32_t)g.window && end > (int32_t)g.sinks);
       if constexpr (SRC != kPlain) masked = masked || valid != ~0ull;
@@ -240,6 +252,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_few(Args g) {
         pw[2 * n] = T::pack(w[0], w[1]);
         pw[2 * n + 1] = T::pack(w[2], w[3]);
       }
+      KP_BOUNDARY(ring, 1, 2);
       // O^T += V^T P^T; the LDS accesses of one wave are in order, the fences keep the compiler to it
       store_v();
       asm volatile("" ::: "memory");
@@ -248,6 +261,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_few(Args g) {
       for (int dt = 0; dt < NT; ++dt) oacc[dt] = T::mfma16(read_v(dt), pw, oacc[dt]);
       asm volatile("" ::: "memory");
       valid = valid_next;
+      if (more) KP_BOUNDARY(ring, 2, 0); else KP_BOUNDARY(ring, 2, kp::kNoRegion);
     }
   }
   float l_tot = l_run + __shfl_xor(l_run, 16, 64);
@@ -330,6 +344,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_few(Args g) {
                            g.lse ? g.lse + g.lse_seq * (int64_t)q_seq + g.lse_head * (int64_t)hd + tok : nullptr);
     }
   }
+  if constexpr (INSTR != 0) finish_ring<INSTR>(ring, g, recorded);
 }
 
 }  // namespace attn

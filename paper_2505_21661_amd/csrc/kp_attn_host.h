@@ -110,6 +110,15 @@ inline long long most_keys_of(long long n_k, long long tokens, int window, int s
   return window > 0 && w < n_k ? w : n_k;
 }
 
+// Workgroups, waves and regions that a recording of the planned call has.
+inline kp_status launch_shape(const Plan& plan, int* n_wg, int* waves_per_wg, int* n_regions) {
+  if (plan.units * plan.splits >= (1ll << 31)) return fail(KP_ERR_UNSUPPORTED_SHAPE, "2^31 or more workgroups");
+  if (n_wg) *n_wg = (int)(plan.units * plan.splits);
+  if (waves_per_wg) *waves_per_wg = 4;
+  if (n_regions) *n_regions = 3;
+  return KP_OK;
+}
+
 inline uint32_t log2_of(int pow2) { return (uint32_t)__builtin_ctz((unsigned)pow2); }
 
 }  // namespace attn

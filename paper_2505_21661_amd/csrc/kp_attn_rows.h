@@ -64,8 +64,25 @@ __device__ __forceinline__ size_t part_row(const Args& g, uint32_t tile, uint32_
   return ((size_t)tile * g.hkv + h) * ROWS + r;
 }
 
+// Recording (INSTR: 0 no record sites, 1 generic sites, 3 the same on the constant-rate clock).
+template <int INSTR>
+__device__ __forceinline__ kp::Ring ring_of(const Args& g, unsigned char* ring_lds, unsigned char* scratch, uint32_t wg) {
+  kp::Ring ring = kp::ring_init<true>(reinterpret_cast<uint32_t*>(ring_lds), reinterpret_cast<uint64_t*>(scratch), g.cap_lds, g.region_mask, g.flush,
+                                      g.cap_hbm, g.trace, g.n_wg, 4u >> g.group_log2, wg, g.group_log2);
+  ring.collab = g.collab;
+  if constexpr (INSTR == 3) kp::ring_use_realtime(ring);
+  return ring;
+}
+template <int INSTR>
+__device__ __forceinline__ void finish_ring(kp::Ring& ring, const Args& g, uint32_t wg) {
+  const kp::TraceGeom tg{g.n_wg, 4u >> g.group_log2, 3, g.cap_hbm, g.flags};
+  kp::ring_finish<INSTR == 3>(ring, g.cap_lds, g.trace, tg, wg, g.rec_cost);
+}
+
 #define KP_BOUNDARY(ring, end_r, start_r) do { if constexpr (INSTR != 0) kp::site<INSTR>(ring, end_r, start_r); } while (0)
 
+// Recorded regions, per tile of 64 keys: 0 K Q^T, with the request of the next keys and values and the lower half's mask and
+// maximum between its MFMAs, 1 the rest of the softmax, 2 V^T P^T up to the barrier behind it.
 template <class T, int D, int SRC, int INSTR>
 __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
   constexpr uint32_t kRow = 2u * D, kChunks = kRow / 16u, kTile = kTileKeys * kRow;
@@ -92,12 +109,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
   const bool there = find_tile<kTileRows, SRC != kPlain>(g, tile_id, &tl);
 
   kp::Ring ring{};
-  if constexpr (INSTR != 0) {
-    ring = kp::ring_init<true>(reinterpret_cast<uint32_t*>(smem + 3u * kTile), reinterpret_cast<uint64_t*>(smem), g.cap_lds, g.region_mask, g.flush,
-                               g.cap_hbm, g.trace, g.n_wg, 4u >> g.group_log2, unit * per + item, g.group_log2);
-    ring.collab = g.collab;
-    if constexpr (INSTR == 3) kp::ring_use_realtime(ring);
-  }
+  if constexpr (INSTR != 0) ring = ring_of<INSTR>(g, smem + 3u * kTile, smem, unit * per + item);
   if (there) {
     const Source<D, SRC> src(g, tl.seq, h);
     const uint32_t last_row = tl.rows - 1u;
@@ -495,10 +507,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
       }
     }
   }
-  if constexpr (INSTR != 0) {
-    kp::TraceGeom tg{g.n_wg, 4u >> g.group_log2, 3, g.cap_hbm, g.flags};
-    kp::ring_finish<INSTR == 3>(ring, g.cap_lds, g.trace, tg, unit * per + item, g.rec_cost);
-  }
+  if constexpr (INSTR != 0) finish_ring<INSTR>(ring, g, unit * per + item);
 }
 
 // Joins the partial results of a row: D / 4 lanes to a row, 4 elements to a lane.  ROWS: of a tile of the kernel that made them.

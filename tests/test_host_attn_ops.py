@@ -22,7 +22,7 @@ def cache(**change):
 
 def window(**change):
     a = dict(q=heads(), k=heads(), v=heads(), o=heads(), lse=A, B=2, Hq=4, Hkv=2, Sq=64, Sk=64, D=64, type=kp.KP_BF16, window=8, sinks=1,
-             scale=0.1, ws=A, n=1 << 30, stream=0)
+             scale=0.1, ws=A, n=1 << 30, mask=0, trace=0, cap=0, stream=0)
     a.update(change)
     return kp.lib().kp_attn_window(*a.values())
 
@@ -36,7 +36,7 @@ def grad(**change):
 
 def paged(**change):
     a = dict(q=heads(), cache=cache(), table=A, width=4, lens=A, starts=A, o=heads(), lse=A, T=64, n=2, Hq=4, window=8, sinks=1, scale=0.1,
-             ws=A, nb=1 << 30, stream=0)
+             ws=A, nb=1 << 30, mask=0, trace=0, cap=0, stream=0)
     a.update(change)
     return kp.lib().kp_attn_paged(*a.values())
 
@@ -66,6 +66,11 @@ SIZES = [
     (dict(Sk=0), INVALID, "positive"), (dict(Sk=1 << 30), UNSUPPORTED, "tokens"), (dict(k=heads(at=A + 2)), INVALID, "k must be"),
     (dict(v=None), INVALID, "v is NULL"),
 ]
+RECORD = [
+    (dict(mask=1), INVALID, "trace_buf is NULL"), (dict(mask=8, trace=A, cap=64), INVALID, "3 regions"), (dict(mask=1, trace=A + 8, cap=64), INVALID, "aligned"),
+    (dict(mask=1, trace=A, cap=66), kp.KP_ERR_TRACE_TOO_SMALL, "power of two"), (dict(mask=1, trace=A, cap=1 << 14), UNSUPPORTED, "16 KiB"),
+    (dict(mask=kp.KP_MASK_PHASES), INVALID, "PHASES"),
+]
 GRAD = [
     (dict(lse=None), INVALID, "lse"), (dict(dk=heads(token=0)), INVALID, "rows of dk overlap"), (dict(dv=None), INVALID, "dv"),
     (dict(ws=None), INVALID, "workspace is NULL"), (dict(ws=A + 4), INVALID, "workspace must be"), (dict(n=15), INVALID, "needed"),
@@ -83,7 +88,7 @@ PAGED = [
 READ = [(dict(starts=None), INVALID, "starts"), (dict(table=A + 1), INVALID, "block_table"), (dict(v=heads(token=0)), INVALID, "rows of v overlap"),
         (dict(width=-1), INVALID, "negative")]
 WRITE = [(dict(slots=None), INVALID, "slots"), (dict(slots=A + 4), INVALID, "slots"), (dict(k=heads(at=A + 4)), INVALID, "k must be"), (dict(T=1 << 30), UNSUPPORTED, "rows")]
-ALL = ([(window, *c) for c in COMMON + SIZES] + [(grad, *c) for c in COMMON + SIZES + GRAD if "o" not in c[0]] + [(paged, *c) for c in COMMON + CACHE + PAGED]
+ALL = ([(window, *c) for c in COMMON + SIZES + RECORD] + [(grad, *c) for c in COMMON + SIZES + GRAD if "o" not in c[0]] + [(paged, *c) for c in COMMON + CACHE + PAGED + RECORD]
        + [(read, *c) for c in CACHE + READ] + [(write, *c) for c in CACHE + WRITE])
 
 
