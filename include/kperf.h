@@ -436,8 +436,9 @@ kp_status kp_attn_instrumented(const void* Q, const void* K, const void* V, void
  *   lse         log of the sum of exp(score) per row, natural, fp32, contiguous; may be NULL
  *   workspace   device, 16-byte aligned, at least the bytes that the operator's _bytes call names for the
  *               same sizes (which may be 0: then workspace may be NULL); its contents need not be kept
- * KP_ERR_UNSUPPORTED_SHAPE: D, strides of 2^24 elements or more between tokens, 2^30 or more tokens,
- * more workgroups than a launch takes.  All calls are asynchronous on `stream` and can be captured.
+ * Outputs must not overlap inputs or one another.  KP_ERR_UNSUPPORTED_SHAPE: D, strides of 2^24 elements or more between
+ * tokens, 2^30 or more tokens, more workgroups than a launch takes.  All calls are asynchronous on `stream` and can be
+ * captured; a workspace belongs to one call at a time.
  */
 enum { KP_BF16 = 0, KP_FP16 = 1 };
 
@@ -522,7 +523,9 @@ kp_status kp_cache_read(const kp_cache* cache, const int32_t* block_table, int t
  * Attention of T new tokens over a cache that already holds them: sequence s has the query tokens starts[s] ..
  * starts[s + 1] - 1 (device, n_seqs + 1 non-decreasing numbers from 0 to T; none, one or many per sequence) and lens[s] keys
  * (device, the new ones included; at most table_width * page count).  q, o: kp_heads with seq ignored; lse [Hq, T].  Keys whose
- * block_table entry names no page of the cache are not visible; table entries past a sequence's keys are not read.
+ * block_table entry names no page of the cache are not visible; table entries past a sequence's keys are not read, nor are the
+ * cache's rows behind them.  Tokens that belong to no sequence are left as they are.  Recording as for kp_attn_window
+ * (kp_attn_paged_launch_shape; workgroups that find no rows record nothing).
  */
 size_t kp_attn_paged_bytes(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int window, int sinks);
 kp_status kp_attn_paged(const kp_heads* q, const kp_cache* cache, const int32_t* block_table, int table_width,

@@ -948,21 +948,25 @@ struct GradPlan {
 };
 GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks) {
   GradPlan p{};
+  window = window_of(window);
+  sinks = sinks_of(sinks);
   const long long group = Hq / Hkv, head_steps = (Sq + 63) / 64;
   p.units = (long long)B * Hkv;
   p.row_tiles = (group * Sq + kTileRows - 1) / kTileRows;
   p.key_tiles = (Sk + kGradKeys - 1) / kGradKeys;
-  p.sink_tiles = window > 0 ? ((long long)sinks + kGradKeys - 1) / kGradKeys : 0;
-  if (p.sink_tiles > p.key_tiles) p.sink_tiles = p.key_tiles;
-  const long long lines = p.units % 8 == 0 ? 8 : 1, plain = p.units / lines * (p.key_tiles - p.sink_tiles);
-  // steps of 64 tokens of an ordinary key tile (an estimate), and of all tiles together
+  // steps of 64 tokens of an ordinary key tile (an estimate)
   long long steps = window > 0 ? ((long long)window + kGradKeys + 62) / 64 + 1 : head_steps;
   steps = (steps < head_steps ? steps : head_steps) * group;
+  const long long saves = D == 64 ? 14 : 7;  // steps that a worker has to save for its tile to be split
+  // tiles with sinks: where their steps are not many more, they are as the others
+  p.sink_tiles = window > 0 && head_steps * group - steps >= saves ? ((long long)sinks + kGradKeys - 1) / kGradKeys : 0;
+  if (p.sink_tiles > p.key_tiles) p.sink_tiles = p.key_tiles;
+  const long long lines = p.units % 8 == 0 ? 8 : 1, plain = p.units / lines * (p.key_tiles - p.sink_tiles);
   const long long all = steps * lines * plain + head_steps * group * p.units * p.sink_tiles;
   // One worker per CU.  Where there are fewer tiles than that, a worker per tile saves the second tile of a worker's piece
-  // and the sums of parts (some 14 us, as much as 14 steps of D = 64 or 7 of 128), and splitting them saves steps.
+  // and the sums of parts (some 14 us, as much as 14 steps of D = 64 or 7 of 128); splitting them saves steps.
   p.workers = 256;
-  if (plain > 0 && lines * plain < p.workers && steps - all / p.workers < (D == 64 ? 14 : 7)) p.workers = lines * plain;
+  if (plain > 0 && lines * plain < p.workers && steps - all / p.workers < saves) p.workers = lines * plain;
   if (all < p.workers) p.workers = all / lines * lines;
   if (p.workers < lines) p.workers = lines;
   p.split = p.units * p.sink_tiles + lines * (plain % (p.workers / lines));
@@ -1024,7 +1028,7 @@ extern "C" kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, c
     if (kp_status s = check_heads(a.name, a.t, B, a.query ? Hq : Hkv, a.query ? Sq : Sk, D, a.written)) return s;
   if (!lse || ((uintptr_t)lse & 3u)) return kp::fail(KP_ERR_INVALID_ARG, "lse must be device memory, 4-byte aligned");
   const GradPlan p = plan_grad(B, Hq, Hkv, Sq, Sk, D, window, sinks);
-  if (p.units * p.row_tiles >= (1ll << 31) || p.units * p.key_tiles * (kGradKeys / kJoinRows) >= (1ll << 31)) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^31 or more workgroups");
+  if (p.units * p.row_tiles >= kMostGroups || p.split * (kGradKeys / kJoinRows) * 2 >= kMostGroups) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^23 or more workgroups");
   if (kp_status s = check_workspace(workspace, workspace_bytes, p.bytes)) return s;
   GradArgs g{};
   g.q = heads_of(q, B, Hq, Sq); g.o = heads_of(o, B, Hq, Sq); g.d_o = heads_of(d_o, B, Hq, Sq); g.dq = heads_of(dq, B, Hq, Sq);
@@ -1035,7 +1039,7 @@ extern "C" kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, c
   g.most = reinterpret_cast<float*>(ws + p.most_at); g.part = reinterpret_cast<float*>(ws + p.part_at);
   g.row_tiles = (uint32_t)p.row_tiles; g.key_tiles = (uint32_t)p.key_tiles; g.sink_tiles = (uint32_t)p.sink_tiles; g.workers = (uint32_t)p.workers;
   g.seqs = (uint32_t)B; g.hkv = (uint32_t)Hkv; g.group = (uint32_t)(Hq / Hkv); g.n_q = (uint32_t)Sq; g.n_k = (uint32_t)Sk;
-  g.window = (uint32_t)window; g.sinks = (uint32_t)sinks; g.scale = scale; g.scale_log2 = scale * kLog2e;
+  g.window = (uint32_t)window_of(window); g.sinks = (uint32_t)sinks_of(sinks); g.scale = scale; g.scale_log2 = scale * kLog2e;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (type == KP_FP16) return D == 64 ? launch_grad<Fp16, 64>(g, p, st) : launch_grad<Fp16, 128>(g, p, st);
   return D == 64 ? launch_grad<Bf16, 64>(g, p, st) : launch_grad<Bf16, 128>(g, p, st);

@@ -5,6 +5,8 @@
 using namespace kp::attn;
 
 static Plan plan_paged(int T, int n_seqs, int Hq, int Hkv, int D, long long most, int window, int sinks) {
+  window = window_of(window);
+  sinks = sinks_of(sinks);
   const long long rows = (long long)(Hq / Hkv) * T, tokens = T < kTileRows ? T : kTileRows;
   return plan_of(n_seqs, rows, most_keys_of(most, tokens, window, sinks), Hkv, D, false);
 }
@@ -49,7 +51,7 @@ extern "C" kp_status kp_attn_paged(const kp_heads* q, const kp_cache* cache, con
   g.table = block_table; g.lens = lens; g.starts = starts;
   g.table_width = (uint32_t)table_width; g.page_log2 = log2_of(cache->page); g.n_pages = (uint32_t)cache->n_pages;
   g.seqs = (uint32_t)n_seqs; g.hkv = (uint32_t)Hkv; g.group = (uint32_t)(Hq / Hkv); g.n_q = (uint32_t)T; g.n_k = (uint32_t)(table_width * cache->page);
-  g.window = (uint32_t)window; g.sinks = (uint32_t)sinks; g.scale_log2 = scale * kLog2e;
+  g.window = (uint32_t)window_of(window); g.sinks = (uint32_t)sinks_of(sinks); g.scale_log2 = scale * kLog2e;
   g.part = static_cast<float*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool e4m3 = cache->cache_type == KP_CACHE_E4M3;

@@ -15,6 +15,8 @@ kp_status check_sizes(int B, int Hq, int Hkv, int Sq, int Sk, int D) {
 
 static Plan plan_window(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks) {
   const long long rows = (long long)(Hq / Hkv) * Sq;
+  window = window_of(window);
+  sinks = sinks_of(sinks);
   return plan_of(B, rows * B, most_keys_of(Sk, Sq < kTileRows ? Sq : kTileRows, window, sinks), Hkv, D, true);
 }
 
@@ -50,7 +52,7 @@ extern "C" kp_status kp_attn_window(const kp_heads* q, const kp_heads* k, const 
   g.k = heads_of(k, B, Hkv, Sk); g.v = heads_of(v, B, Hkv, Sk);
   g.lse = lse; g.lse_seq = (int64_t)Hq * Sq; g.lse_head = Sq;
   g.seqs = (uint32_t)B; g.hkv = (uint32_t)Hkv; g.group = (uint32_t)(Hq / Hkv); g.n_q = (uint32_t)Sq; g.n_k = (uint32_t)Sk;
-  g.window = (uint32_t)window; g.sinks = (uint32_t)sinks; g.scale_log2 = scale * kLog2e;
+  g.window = (uint32_t)window_of(window); g.sinks = (uint32_t)sinks_of(sinks); g.scale_log2 = scale * kLog2e;
   g.part = static_cast<float*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (type == KP_FP16) return D == 64 ? launch<Fp16, 64, kPlain>(g, plan, region_mask, trace_buf, trace_cap, st) : launch<Fp16, 128, kPlain>(g, plan, region_mask, trace_buf, trace_cap, st);

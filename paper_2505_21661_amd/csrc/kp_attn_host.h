@@ -6,6 +6,7 @@ namespace kp {
 namespace attn {
 
 constexpr int64_t kMostTokens = 1 << 30, kMostStep = 1 << 24;
+constexpr int64_t kMostGroups = 1 << 23;  // workgroups of a launch: its threads are counted in 32 bits
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0u; }
 
@@ -55,6 +56,10 @@ inline kp_status check_common(int Hq, int Hkv, int D, int type, int window, int 
   if (Hq / Hkv > (1 << 16)) return fail(KP_ERR_UNSUPPORTED_SHAPE, "more than 2^16 query heads per head of keys");
   return KP_OK;
 }
+
+// There are fewer than 2^30 tokens: a window of as many hides nothing, and more sinks are no more.
+inline int window_of(int window) { return window >= kMostTokens ? 0 : window; }
+inline int sinks_of(int sinks) { return sinks < kMostTokens ? sinks : (int)kMostTokens; }
 
 inline kp_status check_workspace(const void* workspace, size_t have, size_t need) {
   if (need == 0) return KP_OK;
@@ -112,7 +117,7 @@ inline long long most_keys_of(long long n_k, long long tokens, int window, int s
 
 // Workgroups, waves and regions that a recording of the planned call has.
 inline kp_status launch_shape(const Plan& plan, int* n_wg, int* waves_per_wg, int* n_regions) {
-  if (plan.units * plan.splits >= (1ll << 31)) return fail(KP_ERR_UNSUPPORTED_SHAPE, "2^31 or more workgroups");
+  if (plan.units * plan.splits >= kMostGroups) return fail(KP_ERR_UNSUPPORTED_SHAPE, "2^23 or more workgroups");
   if (n_wg) *n_wg = (int)(plan.units * plan.splits);
   if (waves_per_wg) *waves_per_wg = 4;
   if (n_regions) *n_regions = 3;

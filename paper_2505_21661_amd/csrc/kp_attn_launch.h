@@ -44,7 +44,7 @@ kp_status launch_as(const Args& g, const Plan& plan, size_t ring_bytes, hipStrea
 template <class T, int D, int SRC>
 kp_status launch(Args& g, const Plan& plan, uint32_t region_mask, void* trace_buf, size_t trace_cap, hipStream_t st) {
   constexpr long long kJoinRows = kThreads / (D / 4);
-  if (plan.units * plan.splits >= (1ll << 31) || plan.units * (kTileRows / kJoinRows) >= (1ll << 31)) return fail(KP_ERR_UNSUPPORTED_SHAPE, "2^31 or more workgroups");
+  if (plan.units * plan.splits >= kMostGroups) return fail(KP_ERR_UNSUPPORTED_SHAPE, "2^23 or more workgroups");
   g.tiles = (uint32_t)plan.tiles;
   g.splits = (uint32_t)plan.splits;
   size_t ring_bytes = 0;

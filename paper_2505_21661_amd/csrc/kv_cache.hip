@@ -153,7 +153,7 @@ extern "C" kp_status kp_cache_write(const kp_heads* k, const kp_heads* v, const 
   if (!slots || ((uintptr_t)slots & 7u)) return kp::fail(KP_ERR_INVALID_ARG, "slots must be device memory, 8-byte aligned");
   if (kp_status s = check_heads("k", k, 1, cache->Hkv, T, cache->D, false)) return s;
   if (kp_status s = check_heads("v", v, 1, cache->Hkv, T, cache->D, false)) return s;
-  if (T >= kMostTokens || (long long)T * cache->Hkv >= (1ll << 31)) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^31 or more rows in one call");
+  if (T >= kMostTokens || (long long)T * cache->Hkv >= (1ll << 28)) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^28 or more rows in one call");
   WriteArgs g{};
   g.k = heads_of(k, 1, cache->Hkv, T); g.v = heads_of(v, 1, cache->Hkv, T);
   g.slots = slots;
@@ -184,7 +184,7 @@ extern "C" kp_status kp_cache_read(const kp_cache* cache, const int32_t* block_t
   if (table_width > 0 && (!block_table || ((uintptr_t)block_table & 3u))) return kp::fail(KP_ERR_INVALID_ARG, "block_table must be device memory, 4-byte aligned");
   if (kp_status s = check_heads("k", k, 1, cache->Hkv, T, cache->D, true)) return s;
   if (kp_status s = check_heads("v", v, 1, cache->Hkv, T, cache->D, true)) return s;
-  if (T >= kMostTokens || n_seqs >= kMostTokens || (long long)T * cache->Hkv >= (1ll << 31)) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^31 or more rows in one call");
+  if (T >= kMostTokens || n_seqs >= kMostTokens || (T + kReadTokens - 1) / kReadTokens >= kMostGroups || (long long)T * cache->Hkv >= (1ll << 31)) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^27 or more tokens or 2^31 rows in one call");
   ReadArgs g{};
   g.k = heads_of(k, 1, cache->Hkv, T); g.v = heads_of(v, 1, cache->Hkv, T);
   g.k_cache = static_cast<const uint8_t*>(cache->k); g.v_cache = static_cast<const uint8_t*>(cache->v);

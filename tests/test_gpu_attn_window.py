@@ -186,9 +186,52 @@ def test_offsets_past_32_bits(kp):
         assert torch.equal(o, o2) and torch.equal(lse, lse2)
 
 
-def test_same_inputs_same_bits_on_any_stream_and_in_a_graph(kp):
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_key_tiles(kp, d):
+    """More key tiles than there are workers: whole tiles in several rounds, sinks and the rest split."""
+    gen = torch.Generator(device="cuda").manual_seed(14)
+    b, hq, hkv, n, dtype = 8, 4, 4, 2100, torch.bfloat16
+    q, k, v, d_o = (heads(gen, b, h, n, d, dtype, "bshd") for h in (hq, hkv, hkv, hq))
+    for window, sinks in ((100, 2), (0, 0)):
+        o, lse = attend(kp, q, k, v, window, sinks, 0.1)
+        got = grads(kp, q, k, v, o, lse, d_o, window, sinks, 0.1)
+        for i in (0, 3, 7):  # a sequence at a time
+            at = slice(i, i + 1)
+            p, want, _ = forward(q[at], k[at], v[at], window, sinks, 0.1)
+            assert_within(o[at], want, o_bound(p, v[at], dtype), "o")
+            for name, x, (want, bound) in zip(("dq", "dk", "dv"), got, gradients(q[at], k[at], v[at], d_o[at], window, sinks, 0.1, dtype)):
+                assert_within(x[at], want, bound, name)
+
+
+def test_windows_that_hide_nothing(kp):
+    """A window as long as the keys, or of the largest number there is, is none; so are as many sinks."""
+    gen = torch.Generator(device="cuda").manual_seed(15)
+    q, k, v, d_o = (heads(gen, 1, h, 200, 64, torch.bfloat16) for h in (2, 1, 1, 2))
+    want = attend(kp, q, k, v, 0, 0, 0.125)
+    want_grads = grads(kp, q, k, v, *want, d_o, 0, 0, 0.125)
+    for window, sinks in ((200, 0), (2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (1 << 30, 5), (10, 2 ** 31 - 1)):
+        got = attend(kp, q, k, v, window, sinks, 0.125)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), (window, sinks)
+        for a, (b, bound) in zip(grads(kp, q, k, v, *got, d_o, window, sinks, 0.125), gradients(q, k, v, d_o, 0, 0, 0.125, torch.bfloat16)):
+            assert_within(a, b, bound)
+    assert len(want_grads) == 3
+
+
+def test_without_lse(kp):
+    gen = torch.Generator(device="cuda").manual_seed(16)
+    for n_q, n_k in ((1, 3000), (150, 150)):
+        q, k, v = (heads(gen, 1, h, n, 64, torch.bfloat16) for h, n in ((4, n_q), (2, n_k), (2, n_k)))
+        want, _ = attend(kp, q, k, v, 0, 0, 0.125)
+        o = torch.zeros_like(q)
+        n = kp.kp_attn_window_bytes(q, k, 0, 0)
+        kp.kp_attn_window(q, k, v, o, None, 0, 0, 0.125, torch.empty(n, dtype=torch.uint8, device="cuda") if n else None)
+        assert torch.equal(o, want)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_same_inputs_same_bits_on_any_stream_and_in_a_graph(kp, d):
     gen = torch.Generator(device="cuda").manual_seed(11)
-    q, k, v, d_o = (heads(gen, 2, h, 333, 64, torch.float16) for h in (6, 2, 2, 6))
+    q, k, v, d_o = (heads(gen, 2, h, 333, d, torch.float16) for h in (6, 2, 2, 6))
     window, sinks, scale = 70, 5, 0.125
     o, lse = attend(kp, q, k, v, window, sinks, scale)
     first = [o, lse, *grads(kp, q, k, v, o, lse, d_o, window, sinks, scale)]
@@ -208,7 +251,7 @@ def test_same_inputs_same_bits_on_any_stream_and_in_a_graph(kp):
         kp.kp_attn_window(q, k, v, out[0], out[1], window, sinks, scale, ws)
         kp.kp_attn_window_grad(q, k, v, out[0], out[1], d_o, *out[2:], window, sinks, scale, ws)
     for step in range(4):
-        q.copy_(heads(gen, 2, 6, 333, 64, torch.float16))
+        q.copy_(heads(gen, 2, 6, 333, d, torch.float16))
         graph.replay()
         torch.cuda.synchronize()
         o, lse = attend(kp, q, k, v, window, sinks, scale)
