@@ -437,15 +437,15 @@ __device__ __forceinline__ Tokens tokens_of(const GradArgs& g, uint32_t kt) {
 // (and their L2s) evenly, each XCD's workers have heads of their own (a line).  Of a line's tiles every worker takes as many
 // whole as there are for all, side by side, so that the rows that neighbouring tiles share are in L2 when they are asked
 // for (with a run of tiles of its own for every worker 80 % of the requests missed it, this way 50 %), forwards and backwards in turn, since without a window the first are the longest.  What is left over, and the tiles that
-// hold sinks, which all later tokens see, stand in a line step by step (64 tokens of one query head), of which the workers
-// take equal pieces: a tile that does not lie whole in one of them leaves a partial sum for every worker that has a part,
-// first or last in its piece, and kp_grad_join adds them up in order.
+// hold sinks, which all later tokens see, stand in a line step by step (64 tokens of one query head), of which every worker
+// takes a piece that makes up for what its whole tiles are short of the others': a tile that does not lie whole in one piece
+// leaves a partial sum for every worker that has a part, first or last in its piece, and kp_grad_join adds them up in order.
+constexpr uint32_t kMostWorkers = 256, kTileCost = 4;  // kTileCost: steps' worth of time that a tile takes besides its steps
 struct Line {
   uint32_t lines, number, units, workers;  // lines, this one, its heads and workers
   uint32_t sink_tiles, per_unit;           // of a head: tiles with sinks, the others
   uint32_t whole, rest;                    // tiles that are taken whole, tiles that are split
-  uint64_t total;                          // steps of the latter
-  __device__ __forceinline__ uint64_t piece(uint32_t worker) const { return total * worker / workers; }
+  uint32_t total;                          // steps of the latter
   // the n-th of the tiles that are not sinks'; the n-th that is split
   __device__ __forceinline__ void plain_tile(uint32_t n, uint32_t* unit, uint32_t* kt) const {
     const uint32_t u = n / per_unit;
@@ -471,15 +471,26 @@ __device__ __forceinline__ uint32_t split_steps(const GradArgs& g, const Line& l
   l.split_tile(n, &unit, &kt);
   return steps_of(g, kt);
 }
+__device__ __forceinline__ uint32_t sum_over_wave(uint32_t x) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) x += (uint32_t)__shfl_xor((int)x, d, 64);
+  return kp::wave_uniform(x);
+}
+__device__ __forceinline__ uint32_t sum_up_to_lane(uint32_t x) {
+  const uint32_t lane = threadIdx.x & 63u;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t up = __shfl_up(x, d, 64);
+    if (lane >= (uint32_t)d) x += up;
+  }
+  return x;
+}
 // Steps of the split tiles before number n, by a wave.
-__device__ __forceinline__ uint64_t steps_before(const GradArgs& g, const Line& l, uint32_t n) {
-  uint64_t sum = 0;
+__device__ __forceinline__ uint32_t steps_before(const GradArgs& g, const Line& l, uint32_t n) {
+  uint32_t sum = 0;
   for (uint32_t t0 = 0; t0 < n; t0 += 64u) {
     const uint32_t t = t0 + (threadIdx.x & 63u);
-    uint32_t here = t < n ? split_steps(g, l, t) : 0u;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) here += (uint32_t)__shfl_xor((int)here, d, 64);
-    sum += kp::wave_uniform(here);
+    sum += sum_over_wave(t < n ? split_steps(g, l, t) : 0u);
   }
   return sum;
 }
@@ -494,26 +505,53 @@ __device__ __forceinline__ Line line_of(const GradArgs& g, uint32_t number, uint
   l.total = steps_before(g, l, l.rest);
   return l;
 }
-// The split tile that step number x of the line belongs to, and the step's number in it.
-__device__ __forceinline__ void split_at(const GradArgs& g, const Line& line, uint64_t x, uint32_t* n, uint32_t* in) {
+// The n-th whole tile of a worker.
+__device__ __forceinline__ uint32_t whole_tile(const Line& l, uint32_t worker, uint32_t n) {
+  return n * l.workers + ((n & 1u) ? l.workers - 1u - worker : worker);
+}
+// What a worker's whole tiles cost, in steps.
+__device__ __forceinline__ uint32_t whole_cost(const GradArgs& g, const Line& l, uint32_t worker) {
+  uint32_t sum = 0;
+  for (uint32_t n = 0; n * l.workers < l.whole; ++n) {
+    uint32_t unit, kt;
+    l.plain_tile(whole_tile(l, worker, n), &unit, &kt);
+    sum += steps_of(g, kt) + kTileCost;
+  }
+  return sum;
+}
+// Calls f(worker, first step of its piece, one past its last) for 64 workers at a time, one to a lane of the wave.
+template <class F>
+__device__ __forceinline__ void for_pieces(const GradArgs& g, const Line& l, F f) {
   const uint32_t lane = threadIdx.x & 63u;
-  uint64_t before = 0;
-  for (uint32_t t0 = 0; t0 < line.rest; t0 += 64u) {
-    const uint32_t steps = t0 + lane < line.rest ? split_steps(g, line, t0 + lane) : 0u;
-    uint32_t sum = steps;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t up = __shfl_up(sum, d, 64);
-      if (lane >= (uint32_t)d) sum += up;
+  uint32_t all = l.total;
+  for (uint32_t w0 = 0; w0 < l.workers; w0 += 64u) all += sum_over_wave(w0 + lane < l.workers ? whole_cost(g, l, w0 + lane) : 0u);
+  const uint32_t each = (all + l.workers - 1u) / l.workers;  // (what all are short of it is the line's total or more)
+  uint32_t before = 0;
+  for (uint32_t w0 = 0; w0 < l.workers; w0 += 64u) {
+    uint32_t short_of = 0;
+    if (w0 + lane < l.workers) {
+      const uint32_t has = whole_cost(g, l, w0 + lane);
+      short_of = has < each ? each - has : 0u;
     }
-    const uint64_t past = __builtin_amdgcn_ballot_w64(before + sum > x);
+    const uint32_t up_to = before + sum_up_to_lane(short_of), from = up_to - short_of;
+    f(w0 + lane, from < l.total ? from : l.total, up_to < l.total ? up_to : l.total);
+    before = __builtin_amdgcn_readlane(up_to, 63);
+  }
+}
+// The split tile that step number x of the line belongs to, and the step's number in it.
+__device__ __forceinline__ void split_at(const GradArgs& g, const Line& line, uint32_t x, uint32_t* n, uint32_t* in) {
+  const uint32_t lane = threadIdx.x & 63u;
+  uint32_t before = 0;
+  for (uint32_t t0 = 0; t0 < line.rest; t0 += 64u) {
+    const uint32_t steps = t0 + lane < line.rest ? split_steps(g, line, t0 + lane) : 0u, sum = before + sum_up_to_lane(steps);
+    const uint64_t past = __builtin_amdgcn_ballot_w64(sum > x);
     if (past != 0ull) {
       const int l = __builtin_ctzll(past);
       *n = t0 + (uint32_t)l;
-      *in = (uint32_t)(x - before) - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(steps, l));
+      *in = x - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(steps, l));
       return;
     }
-    before += __builtin_amdgcn_readlane(sum, 63);
+    before = __builtin_amdgcn_readlane(sum, 63);
   }
   *n = line.rest;  // (not reached: x is a step of the line)
   *in = 0u;
@@ -545,8 +583,14 @@ __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
   const uint32_t worker = blockIdx.x / line.lines;
   const int32_t off = (int32_t)g.n_k - (int32_t)g.n_q;
   const uint32_t j_last = g.n_k - 1u;
-  uint64_t at = line.piece(worker);
-  const uint64_t to = line.piece(worker + 1u);
+  uint32_t at = 0u, to = 0u;  // its piece of the line
+  for_pieces(g, line, [&](uint32_t w, uint32_t from, uint32_t end) __attribute__((always_inline)) {
+    const uint64_t mine = __builtin_amdgcn_ballot_w64(w == worker);
+    if (mine != 0ull) {
+      at = __builtin_amdgcn_readlane(from, __builtin_ctzll(mine));
+      to = __builtin_amdgcn_readlane(end, __builtin_ctzll(mine));
+    }
+  });
   uint32_t round = 0u, split_no = 0u, s_from = 0u;
   if (at < to) split_at(g, line, at, &split_no, &s_from);
   bool first_piece = true;
@@ -566,12 +610,12 @@ __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
   while (round * line.workers < line.whole || at < to) {
     uint32_t unit, key_tile;
     const bool rounds = round * line.workers < line.whole;  // first the whole tiles
-    if (rounds) line.plain_tile(round * line.workers + ((round & 1u) ? line.workers - 1u - worker : worker), &unit, &key_tile);
+    if (rounds) line.plain_tile(whole_tile(line, worker, round), &unit, &key_tile);
     else line.split_tile(split_no, &unit, &key_tile);
     const uint32_t seq = unit / g.hkv, hk = unit - seq * g.hkv;
     const Tokens tok = tokens_of(g, key_tile);
     const uint32_t steps_per_head = (tok.to - tok.from + 63u) / 64u, steps = steps_per_head * g.group;
-    const uint32_t s_begin = rounds ? 0u : s_from, s_end = rounds || (uint64_t)(steps - s_begin) <= to - at ? steps : s_begin + (uint32_t)(to - at);
+    const uint32_t s_begin = rounds ? 0u : s_from, s_end = rounds || steps - s_begin <= to - at ? steps : s_begin + (to - at);
     const uint32_t slot = first_piece && s_begin != 0u ? 0u : 1u;
     if (rounds) {
       ++round;
@@ -890,21 +934,35 @@ constexpr int kJoinRows = 32;
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) void kp_grad_join(GradArgs g) {
   constexpr uint32_t kLanes = D / 4, kPer = kThreads / kLanes, kBlocks = kGradKeys / kJoinRows;
-  __shared__ const float* from[kThreads];  // where the tile's parts are, kThreads at a time
+  __shared__ const float* from[kMostWorkers];  // where the tile's parts are
+  __shared__ uint32_t edge[kMostWorkers + 64u], ends[2];  // where the workers' pieces begin; the first and the last that have a part
   const uint32_t lines = lines_of(g), tile = blockIdx.x / kBlocks;
   const Line line = line_of(g, tile % lines, lines);
   uint32_t unit, kt;
   line.split_tile(tile / lines, &unit, &kt);
   const uint32_t n = steps_of(g, kt);
-  const uint64_t begin = steps_before(g, line, tile / lines), end = begin + n;
-  uint32_t worker = 0u, parts = 0u;  // the first worker that has a step of the tile, and how many from there on
+  const uint32_t begin = steps_before(g, line, tile / lines), end = begin + n;
+  if (threadIdx.x < 64u)
+    for_pieces(g, line, [&](uint32_t w, uint32_t first, uint32_t last) __attribute__((always_inline)) {
+      edge[w] = first;
+      if (w + 1u == line.workers) edge[line.workers] = last;
+    });
+  __syncthreads();
+  uint32_t parts = 0u;
   if (n != 0u) {
-    worker = (uint32_t)(begin * line.workers / line.total);
-    while (line.piece(worker + 1u) <= begin) ++worker;
-    if (line.piece(worker + 1u) >= end) return;  // it has all of them
-    parts = (uint32_t)((end - 1u) * line.workers / line.total);
-    while (line.piece(parts + 1u) < end) ++parts;
-    parts += 1u - worker;
+    if (threadIdx.x < line.workers) {
+      if (edge[threadIdx.x] <= begin && begin < edge[threadIdx.x + 1u]) ends[0] = threadIdx.x;
+      if (edge[threadIdx.x] < end && end <= edge[threadIdx.x + 1u]) ends[1] = threadIdx.x;
+    }
+    __syncthreads();
+    if (ends[0] == ends[1]) return;  // one worker has all of it
+    parts = ends[1] - ends[0] + 1u;
+    if (threadIdx.x < parts) {
+      const uint32_t w = ends[0] + threadIdx.x;
+      const size_t slot = 2u * (size_t)(w * line.lines + line.number) + (edge[w] > begin ? 0u : 1u);
+      from[threadIdx.x] = edge[w] == edge[w + 1u] ? nullptr : g.part + slot * (2u * kGradKeys * D) + (size_t)blockIdx.y * (kGradKeys * D);
+    }
+    __syncthreads();
   }
   const uint32_t seq = unit / g.hkv, hk = unit - seq * g.hkv;
   const uint32_t c = threadIdx.x % kLanes, r0 = (blockIdx.x % kBlocks) * kJoinRows + threadIdx.x / kLanes;
@@ -912,24 +970,15 @@ __global__ __launch_bounds__(kThreads) void kp_grad_join(GradArgs g) {
   f32x4 sum[kRows];
 #pragma unroll
   for (int i = 0; i < kRows; ++i) sum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (uint32_t p0 = 0; p0 < parts; p0 += kThreads) {
-    const uint32_t w = worker + p0 + threadIdx.x, left = parts - p0, here = left < (uint32_t)kThreads ? left : (uint32_t)kThreads;
-    __syncthreads();
-    if (threadIdx.x < here) {
-      const uint64_t mine = line.piece(w);
-      const size_t slot = 2u * (size_t)(w * line.lines + line.number) + (mine > begin ? 0u : 1u);
-      from[threadIdx.x] = line.piece(w + 1u) == mine ? nullptr : g.part + slot * (2u * kGradKeys * D) + (size_t)blockIdx.y * (kGradKeys * D);
-    }
-    __syncthreads();
-    for (uint32_t i = 0; i < here; ++i) {
-      const float* const part = from[i];
-      if (part == nullptr) continue;
+#pragma unroll 4
+  for (uint32_t i = 0; i < parts; ++i) {
+    const float* const part = from[i];
+    if (part == nullptr) continue;
 #pragma unroll
-      for (int k = 0; k < kRows; ++k) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(part + (size_t)(r0 + kPer * (uint32_t)k) * D + 4u * c);
+    for (int k = 0; k < kRows; ++k) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(part + (size_t)(r0 + kPer * (uint32_t)k) * D + 4u * c);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[k][e] += x[e];
-      }
+      for (int e = 0; e < 4; ++e) sum[k][e] += x[e];
     }
   }
   const Heads& out = blockIdx.y ? g.dv : g.dk;
@@ -943,6 +992,7 @@ __global__ __launch_bounds__(kThreads) void kp_grad_join(GradArgs g) {
 
 // Tiles of a call, its workers and its workspace.
 struct GradPlan {
+  bool too_many;  // the steps of a line are counted in 32 bits
   long long units, row_tiles, key_tiles, sink_tiles, workers, split;  // split: key tiles that kp_grad_join looks at
   size_t rows, most_at, part_at, bytes;  // rows: query rows; byte offsets into the workspace
 };
@@ -963,9 +1013,10 @@ GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, in
   if (p.sink_tiles > p.key_tiles) p.sink_tiles = p.key_tiles;
   const long long lines = p.units % 8 == 0 ? 8 : 1, plain = p.units / lines * (p.key_tiles - p.sink_tiles);
   const long long all = steps * lines * plain + head_steps * group * p.units * p.sink_tiles;
+  p.too_many = all / lines >= (1ll << 30);
   // One worker per CU.  Where there are fewer tiles than that, a worker per tile saves the second tile of a worker's piece
   // and the sums of parts (some 14 us, as much as 14 steps of D = 64 or 7 of 128); splitting them saves steps.
-  p.workers = 256;
+  p.workers = kMostWorkers;
   if (plain > 0 && lines * plain < p.workers && steps - all / p.workers < saves) p.workers = lines * plain;
   if (all < p.workers) p.workers = all / lines * lines;
   if (p.workers < lines) p.workers = lines;
@@ -1028,7 +1079,7 @@ extern "C" kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, c
     if (kp_status s = check_heads(a.name, a.t, B, a.query ? Hq : Hkv, a.query ? Sq : Sk, D, a.written)) return s;
   if (!lse || ((uintptr_t)lse & 3u)) return kp::fail(KP_ERR_INVALID_ARG, "lse must be device memory, 4-byte aligned");
   const GradPlan p = plan_grad(B, Hq, Hkv, Sq, Sk, D, window, sinks);
-  if (p.units * p.row_tiles >= kMostGroups || p.split * (kGradKeys / kJoinRows) * 2 >= kMostGroups) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^23 or more workgroups");
+  if (p.too_many || p.units * p.row_tiles >= kMostGroups || p.split * (kGradKeys / kJoinRows) * 2 >= kMostGroups) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^23 or more workgroups, or 2^30 or more steps");
   if (kp_status s = check_workspace(workspace, workspace_bytes, p.bytes)) return s;
   GradArgs g{};
   g.q = heads_of(q, B, Hq, Sq); g.o = heads_of(o, B, Hq, Sq); g.d_o = heads_of(d_o, B, Hq, Sq); g.dq = heads_of(dq, B, Hq, Sq);

@@ -208,13 +208,11 @@ def test_windows_that_hide_nothing(kp):
     gen = torch.Generator(device="cuda").manual_seed(15)
     q, k, v, d_o = (heads(gen, 1, h, 200, 64, torch.bfloat16) for h in (2, 1, 1, 2))
     want = attend(kp, q, k, v, 0, 0, 0.125)
-    want_grads = grads(kp, q, k, v, *want, d_o, 0, 0, 0.125)
     for window, sinks in ((200, 0), (2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (1 << 30, 5), (10, 2 ** 31 - 1)):
         got = attend(kp, q, k, v, window, sinks, 0.125)
         assert all(torch.equal(a, b) for a, b in zip(got, want)), (window, sinks)
         for a, (b, bound) in zip(grads(kp, q, k, v, *got, d_o, window, sinks, 0.125), gradients(q, k, v, d_o, 0, 0, 0.125, torch.bfloat16)):
             assert_within(a, b, bound)
-    assert len(want_grads) == 3
 
 
 def test_without_lse(kp):
