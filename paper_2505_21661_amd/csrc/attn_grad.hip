@@ -31,6 +31,7 @@ struct GradArgs {
   uint32_t seqs, hkv, group, n_q, n_k, window, sinks;
   uint32_t row_tiles, key_tiles, sink_tiles;  // of one head of keys; sink_tiles: key tiles that all later tokens see, for their sinks
   uint32_t workers;               // workgroups of kp_grad_keys; a multiple of 8 where B Hkv is one
+  uint32_t whole;                 // tiles of a line that are taken whole
   float scale, scale_log2;
 };
 
@@ -500,7 +501,7 @@ __device__ __forceinline__ Line line_of(const GradArgs& g, uint32_t number, uint
   l.units = g.seqs * g.hkv / lines; l.workers = g.workers / lines;
   l.sink_tiles = g.sink_tiles; l.per_unit = g.key_tiles - g.sink_tiles;
   const uint32_t plain = l.units * l.per_unit;
-  l.whole = plain / l.workers * l.workers;
+  l.whole = g.whole;
   l.rest = l.units * l.sink_tiles + (plain - l.whole);
   l.total = steps_before(g, l, l.rest);
   return l;
@@ -513,8 +514,10 @@ __device__ __forceinline__ uint32_t whole_tile(const Line& l, uint32_t worker, u
 __device__ __forceinline__ uint32_t whole_cost(const GradArgs& g, const Line& l, uint32_t worker) {
   uint32_t sum = 0;
   for (uint32_t n = 0; n * l.workers < l.whole; ++n) {
+    const uint32_t tile = whole_tile(l, worker, n);
+    if (tile >= l.whole) continue;  // (the last round may not be full)
     uint32_t unit, kt;
-    l.plain_tile(whole_tile(l, worker, n), &unit, &kt);
+    l.plain_tile(tile, &unit, &kt);
     sum += steps_of(g, kt) + kTileCost;
   }
   return sum;
@@ -610,6 +613,10 @@ __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
   while (round * line.workers < line.whole || at < to) {
     uint32_t unit, key_tile;
     const bool rounds = round * line.workers < line.whole;  // first the whole tiles
+    if (rounds && whole_tile(line, worker, round) >= line.whole) {
+      ++round;
+      continue;
+    }
     if (rounds) line.plain_tile(whole_tile(line, worker, round), &unit, &key_tile);
     else line.split_tile(split_no, &unit, &key_tile);
     const uint32_t seq = unit / g.hkv, hk = unit - seq * g.hkv;
@@ -929,13 +936,14 @@ __global__ __launch_bounds__(kKeysThreads, 2) void kp_grad_keys(GradArgs g) {
   }
 }
 
-// Adds up the parts of the split key tiles that do not lie whole in one worker's piece: 32 rows to a workgroup; blockIdx.y: dk or dv.
-constexpr int kJoinRows = 32;
+// Adds up the parts of the split key tiles that do not lie whole in one worker's piece: D / 4 lanes to a row, a row to a lane;
+// blockIdx.y: dk or dv.
+template <int D> constexpr int kJoinRows = kThreads / (D / 4);
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) void kp_grad_join(GradArgs g) {
-  constexpr uint32_t kLanes = D / 4, kPer = kThreads / kLanes, kBlocks = kGradKeys / kJoinRows;
+  constexpr uint32_t kLanes = D / 4, kBlocks = kGradKeys / kJoinRows<D>;
   __shared__ const float* from[kMostWorkers];  // where the tile's parts are
-  __shared__ uint32_t edge[kMostWorkers + 64u], ends[2];  // where the workers' pieces begin; the first and the last that have a part
+  __shared__ uint32_t edge[kMostWorkers + 64u], ends[2], counts[4];  // where the workers' pieces begin; the first and the last that have a part
   const uint32_t lines = lines_of(g), tile = blockIdx.x / kBlocks;
   const Line line = line_of(g, tile % lines, lines);
   uint32_t unit, kt;
@@ -956,44 +964,38 @@ __global__ __launch_bounds__(kThreads) void kp_grad_join(GradArgs g) {
     }
     __syncthreads();
     if (ends[0] == ends[1]) return;  // one worker has all of it
-    parts = ends[1] - ends[0] + 1u;
-    if (threadIdx.x < parts) {
-      const uint32_t w = ends[0] + threadIdx.x;
+    // their places, in the order of the workers, without those whose piece is empty
+    const uint32_t w = ends[0] + threadIdx.x;
+    const bool has = w <= ends[1] && edge[w] < edge[w + 1u];
+    const uint64_t all = __builtin_amdgcn_ballot_w64(has);
+    if ((threadIdx.x & 63u) == 0u) counts[threadIdx.x >> 6] = (uint32_t)__builtin_popcountll(all);
+    __syncthreads();
+    uint32_t before = __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0u));
+    for (uint32_t i = 0; i < (threadIdx.x >> 6); ++i) before += counts[i];
+    parts = counts[0] + counts[1] + counts[2] + counts[3];
+    if (has) {
       const size_t slot = 2u * (size_t)(w * line.lines + line.number) + (edge[w] > begin ? 0u : 1u);
-      from[threadIdx.x] = edge[w] == edge[w + 1u] ? nullptr : g.part + slot * (2u * kGradKeys * D) + (size_t)blockIdx.y * (kGradKeys * D);
+      from[before] = g.part + slot * (2u * kGradKeys * D) + (size_t)blockIdx.y * (kGradKeys * D);
     }
     __syncthreads();
   }
   const uint32_t seq = unit / g.hkv, hk = unit - seq * g.hkv;
-  const uint32_t c = threadIdx.x % kLanes, r0 = (blockIdx.x % kBlocks) * kJoinRows + threadIdx.x / kLanes;
-  constexpr int kRows = kJoinRows / (int)kPer;  // of a thread
-  f32x4 sum[kRows];
-#pragma unroll
-  for (int i = 0; i < kRows; ++i) sum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+  const uint32_t c = threadIdx.x % kLanes, row = (blockIdx.x % kBlocks) * kJoinRows<D> + threadIdx.x / kLanes, j = kt * kGradKeys + row;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
   for (uint32_t i = 0; i < parts; ++i) {
-    const float* const part = from[i];
-    if (part == nullptr) continue;
+    const f32x4 x = *reinterpret_cast<const f32x4*>(from[i] + row * D + 4u * c);
 #pragma unroll
-    for (int k = 0; k < kRows; ++k) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(part + (size_t)(r0 + kPer * (uint32_t)k) * D + 4u * c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[k][e] += x[e];
-    }
+    for (int e = 0; e < 4; ++e) sum[e] += x[e];
   }
   const Heads& out = blockIdx.y ? g.dv : g.dk;
-#pragma unroll
-  for (int k = 0; k < kRows; ++k) {
-    const uint32_t j = kt * kGradKeys + r0 + kPer * (uint32_t)k;
-    if (j < g.n_k)
-      *reinterpret_cast<u32x2*>(const_cast<uint16_t*>(row_at(out, seq, hk, j)) + 4u * c) = u32x2{T::pack(sum[k][0], sum[k][1]), T::pack(sum[k][2], sum[k][3])};
-  }
+  if (j < g.n_k) *reinterpret_cast<u32x2*>(const_cast<uint16_t*>(row_at(out, seq, hk, j)) + 4u * c) = u32x2{T::pack(sum[0], sum[1]), T::pack(sum[2], sum[3])};
 }
 
 // Tiles of a call, its workers and its workspace.
 struct GradPlan {
   bool too_many;  // the steps of a line are counted in 32 bits
-  long long units, row_tiles, key_tiles, sink_tiles, workers, split;  // split: key tiles that kp_grad_join looks at
+  long long units, row_tiles, key_tiles, sink_tiles, workers, whole, split;  // split: key tiles that kp_grad_join looks at
   size_t rows, most_at, part_at, bytes;  // rows: query rows; byte offsets into the workspace
 };
 GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks) {
@@ -1020,7 +1022,10 @@ GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, in
   if (plain > 0 && lines * plain < p.workers && steps - all / p.workers < saves) p.workers = lines * plain;
   if (all < p.workers) p.workers = all / lines * lines;
   if (p.workers < lines) p.workers = lines;
-  p.split = p.units * p.sink_tiles + lines * (plain % (p.workers / lines));
+  // Whole rounds, and one that is not full if what it lacks can be made up for by the tiles with sinks, or is little.
+  const long long places = p.workers / lines, lacks = (places - plain % places) % places;
+  p.whole = lacks * steps <= head_steps * group * (p.units / lines) * p.sink_tiles + places * steps / 16 ? plain : plain / places * places;
+  p.split = p.units * p.sink_tiles + lines * (plain - p.whole);
   p.rows = (size_t)B * (size_t)Hq * (size_t)Sq;
   const auto up = [](size_t n) { return (n + 15) & ~(size_t)15; };
   p.most_at = up(8 * p.rows);
@@ -1046,7 +1051,7 @@ kp_status launch_grad(GradArgs& g, const GradPlan& p, hipStream_t st) {
   hipLaunchKernelGGL((kp_grad_keys<T, D>), dim3((uint32_t)p.workers), dim3(kKeysThreads), kKeysLds, st, g);
   KP_HIP_TRY(hipGetLastError());
   if (p.split > 0) {
-    hipLaunchKernelGGL((kp_grad_join<T, D>), dim3((uint32_t)(p.split * (kGradKeys / kJoinRows)), 2), dim3(kThreads), 0, st, g);
+    hipLaunchKernelGGL((kp_grad_join<T, D>), dim3((uint32_t)(p.split * (kGradKeys / kJoinRows<D>)), 2), dim3(kThreads), 0, st, g);
     KP_HIP_TRY(hipGetLastError());
   }
   return KP_OK;
@@ -1079,7 +1084,7 @@ extern "C" kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, c
     if (kp_status s = check_heads(a.name, a.t, B, a.query ? Hq : Hkv, a.query ? Sq : Sk, D, a.written)) return s;
   if (!lse || ((uintptr_t)lse & 3u)) return kp::fail(KP_ERR_INVALID_ARG, "lse must be device memory, 4-byte aligned");
   const GradPlan p = plan_grad(B, Hq, Hkv, Sq, Sk, D, window, sinks);
-  if (p.too_many || p.units * p.row_tiles >= kMostGroups || p.split * (kGradKeys / kJoinRows) * 2 >= kMostGroups) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^23 or more workgroups, or 2^30 or more steps");
+  if (p.too_many || p.units * p.row_tiles >= kMostGroups || p.split * 32 >= kMostGroups) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^23 or more workgroups, or 2^30 or more steps");
   if (kp_status s = check_workspace(workspace, workspace_bytes, p.bytes)) return s;
   GradArgs g{};
   g.q = heads_of(q, B, Hq, Sq); g.o = heads_of(o, B, Hq, Sq); g.d_o = heads_of(d_o, B, Hq, Sq); g.dq = heads_of(dq, B, Hq, Sq);
@@ -1088,7 +1093,7 @@ extern "C" kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, c
   char* const ws = static_cast<char*>(workspace);
   g.neg = reinterpret_cast<float*>(ws); g.delta = g.neg + p.rows;
   g.most = reinterpret_cast<float*>(ws + p.most_at); g.part = reinterpret_cast<float*>(ws + p.part_at);
-  g.row_tiles = (uint32_t)p.row_tiles; g.key_tiles = (uint32_t)p.key_tiles; g.sink_tiles = (uint32_t)p.sink_tiles; g.workers = (uint32_t)p.workers;
+  g.row_tiles = (uint32_t)p.row_tiles; g.key_tiles = (uint32_t)p.key_tiles; g.sink_tiles = (uint32_t)p.sink_tiles; g.workers = (uint32_t)p.workers; g.whole = (uint32_t)p.whole;
   g.seqs = (uint32_t)B; g.hkv = (uint32_t)Hkv; g.group = (uint32_t)(Hq / Hkv); g.n_q = (uint32_t)Sq; g.n_k = (uint32_t)Sk;
   g.window = (uint32_t)window_of(window); g.sinks = (uint32_t)sinks_of(sinks); g.scale = scale; g.scale_log2 = scale * kLog2e;
   hipStream_t st = static_cast<hipStream_t>(stream);
