@@ -488,13 +488,15 @@ def kp_attn_window_grad(q, k, v, o, lse, d_o, dq, dk, dv, window: int, sinks: in
 def _cache_of(k_cache, v_cache, k_exp, v_exp, dtype):
     """kp_cache of two halves [n_pages, Hkv, page, D]: of `dtype`, or float8_e4m3fn with exponent bytes."""
     n_pages, Hkv, page, D = k_cache.shape
-    kind, ke, ve = dtype, 0, 0
-    e4m3 = k_cache.dtype == _dtype("float8_e4m3fn")
+    kind, ke, ve = k_cache.dtype, 0, 0
+    e4m3 = kind is _dtype("float8_e4m3fn")
+    if (not e4m3 and kind is not dtype) or v_cache.dtype is not kind or v_cache.shape != k_cache.shape:
+        raise ValueError(f"the cache's halves must be alike and of {dtype} or float8_e4m3fn, not {list(k_cache.shape)} of {kind} "
+                         f"and {list(v_cache.shape)} of {v_cache.dtype}")
     if e4m3:
-        kind, rows = k_cache.dtype, (n_pages, Hkv, page)
+        rows = (n_pages, Hkv, page)
         ke, ve = _flat("k_exp", k_exp, _dtype("uint8"), rows), _flat("v_exp", v_exp, _dtype("uint8"), rows)
-    return kp_cache(_flat("k_cache", k_cache, kind), _flat("v_cache", v_cache, kind, k_cache.shape), ke, ve,
-                    n_pages, Hkv, page, D, _type_code(dtype), int(e4m3))
+    return kp_cache(_ptr(k_cache), _ptr(v_cache), ke, ve, n_pages, Hkv, page, D, _type_code(dtype), int(e4m3))
 
 
 def kp_cache_write(k, v, slots, k_cache, v_cache, k_exp=None, v_exp=None, stream=None) -> None:

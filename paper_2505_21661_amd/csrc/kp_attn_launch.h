@@ -53,8 +53,13 @@ kp_status launch(Args& g, const Plan& plan, uint32_t region_mask, void* trace_bu
                     : (region_mask & KP_MASK_REALTIME) ? launch_as<T, D, SRC, 3>(g, plan, ring_bytes, st) : launch_as<T, D, SRC, 1>(g, plan, ring_bytes, st))
     return s;
   if (plan.splits > 1) {
-    if (plan.few) hipLaunchKernelGGL((kp_attn_join<T, D, kFewRows, SRC != kPlain>), dim3((uint32_t)(plan.units * kFewRows / kJoinRows)), dim3(kThreads), 0, st, g);
-    else hipLaunchKernelGGL((kp_attn_join<T, D, kTileRows, SRC != kPlain>), dim3((uint32_t)(plan.units * kTileRows / kJoinRows)), dim3(kThreads), 0, st, g);
+    constexpr bool kPages = SRC != kPlain;
+    const bool wide = plan.splits > (long long)kJoinAtOnce;
+    const dim3 grid((uint32_t)(plan.units * (plan.few ? kFewRows : kTileRows) / (wide ? 1 : kJoinRows))), block(kThreads);
+    if (plan.few && wide) hipLaunchKernelGGL((kp_attn_join<T, D, kFewRows, kPages, true>), grid, block, 0, st, g);
+    else if (plan.few) hipLaunchKernelGGL((kp_attn_join<T, D, kFewRows, kPages, false>), grid, block, 0, st, g);
+    else if (wide) hipLaunchKernelGGL((kp_attn_join<T, D, kTileRows, kPages, true>), grid, block, 0, st, g);
+    else hipLaunchKernelGGL((kp_attn_join<T, D, kTileRows, kPages, false>), grid, block, 0, st, g);
     KP_HIP_TRY(hipGetLastError());
   }
   return KP_OK;

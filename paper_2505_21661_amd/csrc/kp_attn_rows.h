@@ -510,12 +510,15 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
   if constexpr (INSTR != 0) finish_ring<INSTR>(ring, g, unit * per + item);
 }
 
-// Joins the partial results of a row: D / 4 lanes to a row, 4 elements to a lane.  ROWS: of a tile of the kernel that made them.
-template <class T, int D, int ROWS, bool PAGED>
+// Joins the partial results of a row: D / 4 lanes to a row, 4 elements to a lane.  ROWS: of a tile of the kernel that made
+// them.  WIDE: the workgroup has one row, whose parts its groups of lanes share, eight at a time to a group.
+constexpr uint32_t kJoinAtOnce = 8;  // parts of a group whose loads are in flight together
+template <class T, int D, int ROWS, bool PAGED, bool WIDE>
 __global__ __launch_bounds__(kThreads) void kp_attn_join(Args g) {
-  constexpr uint32_t kLanes = D / 4, kPer = kThreads / kLanes;  // rows of a workgroup
+  constexpr uint32_t kLanes = D / 4, kGroups = kThreads / kLanes, kPer = WIDE ? 1u : kGroups;  // rows of a workgroup
   const uint32_t blocks = ROWS / kPer, unit = blockIdx.x / blocks, block = blockIdx.x - unit * blocks;
-  const uint32_t tile_id = unit / g.hkv, h = unit - tile_id * g.hkv, r = block * kPer + threadIdx.x / kLanes, c = threadIdx.x % kLanes;
+  const uint32_t group = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
+  const uint32_t tile_id = unit / g.hkv, h = unit - tile_id * g.hkv, r = WIDE ? block : block * kPer + group;
   Tile tl;
   if (!find_tile<ROWS, PAGED>(g, tile_id, &tl)) return;
   const uint32_t flat = tl.first + r;
@@ -523,8 +526,8 @@ __global__ __launch_bounds__(kThreads) void kp_attn_join(Args g) {
   const size_t rows = (size_t)g.tiles * g.hkv * ROWS, row = part_row<ROWS>(g, tile_id, h, r);
   float m = kNoKey, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  constexpr uint32_t kAtOnce = 8;  // parts whose loads are in flight together
-  for (uint32_t s0 = 0; s0 < g.splits; s0 += kAtOnce) {
+  constexpr uint32_t kAtOnce = kJoinAtOnce;
+  for (uint32_t s0 = WIDE ? group * kAtOnce : 0u; s0 < g.splits; s0 += WIDE ? kGroups * kAtOnce : kAtOnce) {
     f32x2 ml[kAtOnce];
     f32x4 part[kAtOnce];
     float top = m;
@@ -549,6 +552,27 @@ __global__ __launch_bounds__(kThreads) void kp_attn_join(Args g) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(part[i][e], w, o[e]);
     }
+  }
+  if constexpr (WIDE) {
+    __shared__ float group_m[kGroups], group_l[kGroups];
+    __shared__ f32x4 group_o[kGroups][kLanes];
+    if (c == 0) { group_m[group] = m; group_l[group] = l; }
+    group_o[group][c] = o;
+    __syncthreads();
+    if (group != 0u) return;
+    float top = m;
+    for (uint32_t i = 1; i < kGroups; ++i) top = fmaxf(top, group_m[i]);
+    l = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (uint32_t i = 0; i < kGroups; ++i) {
+      if (group_l[i] == 0.f) continue;
+      const float w = __builtin_amdgcn_exp2f(group_m[i] - top);
+      l = __builtin_fmaf(group_l[i], w, l);
+      const f32x4 part = group_o[i][c];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(part[e], w, o[e]);
+    }
+    m = top;
   }
   const RowPlace at = place_of(flat, g.group);
   const uint32_t head = h * g.group + at.in_group, seq = PAGED ? 0u : tl.seq;

@@ -168,6 +168,7 @@ PAGED = [
     ([2100], [1], 8, 8, 32, 0, 0), ([3000, 77], [1, 1], 4, 1, 16, 500, 4), ([1000, 900], [1, 1], 20, 1, 128, 100, 130),
     ([100, 37], [100, 20], 4, 2, 16, 0, 0), ([300, 200, 9], [33, 1, 9], 8, 2, 32, 50, 3), ([260, 0, 5], [0, 2, 5], 4, 4, 8, 0, 0),
     ([20, 600], [30, 130], 6, 2, 16, 0, 0), ([513], [257], 7, 1, 64, 64, 64), ([90, 91], [2, 3], 2, 2, 1, 20, 1), ([1500], [300], 8, 1, 256, 0, 0),
+    ([20000], [1], 3, 1, 64, 0, 0), ([9000, 31], [30, 2], 4, 1, 256, 0, 0),
     ([64] * 70, [1] * 70, 2, 1, 16, 0, 0), ([130] * 67, [i % 4 for i in range(67)], 4, 2, 32, 60, 2),
 ]
 
