@@ -203,6 +203,19 @@ def test_many_key_tiles(kp, d):
                 assert_within(x[at], want, bound, name)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_few_more_key_tiles_than_compute_units(kp, dtype):
+    """288 tiles: a worker for each, of which a few share a compute unit."""
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    q, k, v, d_o = (heads(gen, 8, 4, 1100, 64, dtype) for _ in range(4))
+    o, lse = attend(kp, q, k, v, 0, 0, 0.1)
+    got = grads(kp, q, k, v, o, lse, d_o, 0, 0, 0.1)
+    for i in range(8):
+        at = slice(i, i + 1)
+        for name, x, (want, bound) in zip(("dq", "dk", "dv"), got, gradients(q[at], k[at], v[at], d_o[at], 0, 0, 0.1, dtype)):
+            assert_within(x[at], want, bound, name)
+
+
 def test_windows_that_hide_nothing(kp):
     """A window as long as the keys, or of the largest number there is, is none; so are as many sinks."""
     gen = torch.Generator(device="cuda").manual_seed(15)
