@@ -31,8 +31,8 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
   const RowPlace at = place_of(mine ? flat : last_row, g.group);
   const uint32_t head = hk * g.group + at.in_group;
   const int32_t p = off + (int32_t)at.token, p_min = position(wave_first), p_max = position(wave_first + 31u);
-  const Span span = span_of(position(first), position(first + kTileRows - 1u), g.window, g.sinks);
-  const uint32_t sink_tiles = (span.sink_end + 63u) / 64u, tiles = sink_tiles + (span.end > span.lo ? (span.end - span.lo + 63u) / 64u : 0u);
+  const KeyTiles kt(span_of(position(first), position(first + kTileRows - 1u), g.window, g.sinks));
+  const uint32_t tiles = kt.all;
 
   u32x4 qf[NS], dof[NS];
   float delta = 0.f, most = 0.f;
@@ -79,16 +79,20 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
   const uint32_t lds0 = kp::wave_uniform((uint32_t)(uintptr_t)smem + 1024u * wave);
   const uint16_t *k_head = row_at(g.k, seq, hk, 0), *v_head = row_at(g.v, seq, hk, 0);
   uint32_t loaded_last = ~0u, into = 0u;  // `into`: LDS offset of the buffer that the next tiles go to
-  auto tile_start = [&](uint32_t t, uint32_t* limit) __attribute__((always_inline)) {
-    *limit = t < sink_tiles ? span.sink_end : span.end;
-    return t < sink_tiles ? t * 64u : span.lo + (t - sink_tiles) * 64u;
-  };
   auto request = [&](uint32_t t) __attribute__((always_inline)) {
     uint32_t limit;
-    const uint32_t start = tile_start(t, &limit), left = limit - 1u - start, last = left < 63u ? left : 63u;
+    const uint32_t start = kt.start(t, &limit), left = limit - 1u - start, last = left < 63u ? left : 63u;
     if (last != loaded_last) { loaded_last = last; lk.upto(last); lv.upto(last); }
     lk.load(k_head + g.k.token * (int64_t)start, lds0 + into);
     lv.load(v_head + g.v.token * (int64_t)start, lds0 + into + kTile);
+    into ^= 2u * kTile;
+  };
+  auto request_first = [&]() __attribute__((always_inline)) {
+    if (!kt.is_mixed(0u)) { request(0u); return; }
+    uint32_t limit;
+    const uint32_t start = kt.start(0u, &limit), left = limit - 1u - start;
+    lk.load_two(k_head, g.k.token, kt.mixed, start, left, lds0 + into);
+    lv.load_two(v_head, g.v.token, kt.mixed, start, left, lds0 + into + kTile);
     into ^= 2u * kTile;
   };
 
@@ -110,7 +114,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
   // Over all keys; CHECK: with the sum of dS.
   auto over_keys = [&](auto check_c) __attribute__((always_inline)) {
     constexpr bool CHECK = decltype(check_c)::value;
-    request(0u);
+    request_first();
     __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own count of outstanding loads)
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
@@ -118,10 +122,10 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
     for (uint32_t t = 0; t < tiles; ++t) {
       if (t + 1u < tiles) request(t + 1u);
       uint32_t limit;
-      const uint32_t start = tile_start(t, &limit);
+      const uint32_t start = kt.start(t, &limit), sinks = kt.sinks_at(t, start, g.sinks);
       const int32_t end = (int32_t)(start + 64u);
       bool masked = (end > (int32_t)limit) | (end - 1 > p_min);
-      masked = masked | ((g.window != 0u) & (p_max - (int32_t)start >= (int32_t)g.window) & (end > (int32_t)g.sinks));
+      masked = masked | ((g.window != 0u) & (p_max - (int32_t)start >= (int32_t)g.window) & (end > (int32_t)sinks));
 #pragma unroll
       for (int tk = 0; tk < 2; ++tk) {
         f32x16 sacc = f32x16{0}, dp = f32x16{0};
@@ -135,8 +139,8 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
         }
         __builtin_amdgcn_s_setprio(0);
         if (masked) {
-          const RowMask m(p, limit, (int32_t)(start + 4u * h32), g.window, g.sinks);
-          if ((g.window != 0u) & (start < g.sinks)) {
+          const RowMask m(p, limit, (int32_t)(start + 4u * h32), g.window, sinks);
+          if ((g.window != 0u) & (start < sinks)) {
             asm volatile("");  // (branches: no selects where nothing is masked)
 #pragma unroll
             for (int v = 0; v < 16; ++v) sacc[v] = m.sees_mixed(32 * tk + 8 * (v >> 2) + (v & 3)) ? sacc[v] : -INFINITY;

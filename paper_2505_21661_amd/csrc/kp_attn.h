@@ -164,6 +164,29 @@ __device__ __forceinline__ Span span_of(int32_t p_first, int32_t p_last, uint32_
   return s;
 }
 
+// The same keys, 64 at a time.  The last sinks, where there are not 64 of them, and the first keys of the window are one tile,
+// the first: a window of 512 with one sink takes a tile of 128 rows over 10 tiles of keys, 11 if sinks had their own.
+struct KeyTiles {
+  Span span;
+  uint32_t mixed, sink_tiles, all;  // sinks in the first tile (keys 0 .. mixed - 1), whole tiles of sinks (keys mixed on)
+  __device__ __forceinline__ KeyTiles(const Span& s) : span(s) {
+    mixed = s.sink_end & 63u;
+    sink_tiles = s.sink_end >> 6;
+    all = sink_tiles + (s.end > s.lo ? (s.end - s.lo + mixed + 63u) / 64u : 0u);
+  }
+  __device__ __forceinline__ bool is_mixed(uint32_t t) const { return t == 0u && mixed != 0u; }
+  // Number of tile t's first key and one past the last that there is.  Element c of the mixed tile is key start + c, but
+  // key c in front of `mixed`.  (Sinks that a window hides from some row of the tile end in front of its first key.)
+  __device__ __forceinline__ uint32_t start(uint32_t t, uint32_t* limit) const {
+    const uint32_t n = t - (mixed != 0u ? 1u : 0u);
+    const bool sinks = n < sink_tiles;
+    *limit = sinks ? span.sink_end : span.end;
+    return sinks ? mixed + 64u * n : span.lo - mixed + 64u * (t == 0u ? 0u : t - sink_tiles);
+  }
+  // what RowMask takes for the number of sinks there: its comparison is of start + c
+  __device__ __forceinline__ uint32_t sinks_at(uint32_t t, uint32_t start, uint32_t sinks) const { return is_mixed(t) ? start + mixed : sinks; }
+};
+
 // Which of a row's scores against a run of keys are visible: element c, the key first + c, is if c - from <= count
 // (unsigned) or, where the run holds sinks (mixed), if c <= sink.  One subtraction and one comparison per score.
 struct RowMask {

@@ -174,6 +174,17 @@ struct TileLoader {
                    : "=&s"(saved_m0) : "v"(ofs[i]), "s"(base), "s"(dst + 1024u * WAVES * (uint32_t)i) : "memory");
     }
   }
+  // Row r < mixed is token r, the others token start + r (up to r = left): further apart than 32 bits reach, perhaps.
+  __device__ __forceinline__ void load_two(const uint16_t* head, int64_t token_step, uint32_t mixed, uint32_t start, uint32_t left, uint32_t dst) const {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const uint32_t r = first_row() + (uint32_t)WAVES * kBlockRows * (uint32_t)i, token = r < mixed ? r : start + (r < left ? r : left);
+      const uint64_t from = (uint64_t)(uintptr_t)(head + token_step * (int64_t)token) + in;
+      uint32_t saved_m0;
+      asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
+                   : "=&s"(saved_m0) : "v"(from), "s"(dst + 1024u * WAVES * (uint32_t)i) : "memory");
+    }
+  }
 };
 
 // A wave's 32 rows of D accumulators (row l32, d = 32 dt + 8 j + 4 h32 + i), times `by`, through LDS and out as whole rows.

@@ -121,10 +121,8 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
     const RowPlace at = place_of(mine ? flat : last_row, g.group);
     const int32_t p = (int32_t)tl.n_k - (int32_t)tl.n_q + (int32_t)at.token;
     const int32_t p_min = position(wave_first), p_max = position(wave_first + 31u);
-    const Span span = span_of(position(tl.first), position(tl.first + kTileRows - 1u), g.window, g.sinks);
-    const uint32_t sink_tiles = (span.sink_end + kTileKeys - 1u) / kTileKeys;
-    const uint32_t all_tiles = sink_tiles + (span.end > span.lo ? (span.end - span.lo + kTileKeys - 1u) / kTileKeys : 0u);
-    const uint32_t t_begin = (uint32_t)((uint64_t)all_tiles * split / g.splits), t_end = (uint32_t)((uint64_t)all_tiles * (split + 1u) / g.splits);
+    const KeyTiles kt(span_of(position(tl.first), position(tl.first + kTileRows - 1u), g.window, g.sinks));
+    const uint32_t t_begin = (uint32_t)((uint64_t)kt.all * split / g.splits), t_end = (uint32_t)((uint64_t)kt.all * (split + 1u) / g.splits);
 
     const uint32_t q_seq = SRC == kPlain ? tl.seq : 0u, head = h * g.group + at.in_group;
     const int64_t token = (int64_t)tl.q0 + at.token;
@@ -152,23 +150,25 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
     float ke[E4M3 ? D / 64 : 1], ve[E4M3 ? D / 64 : 1];
     uint32_t v_into = kTile;              // LDS offset of the V buffer that the next tile goes to
 
-    auto tile_start = [&](uint32_t t, uint32_t* limit) __attribute__((always_inline)) {
-      *limit = t < sink_tiles ? span.sink_end : span.end;
-      return t < sink_tiles ? t * kTileKeys : span.lo + (t - sink_tiles) * kTileKeys;
+    // the key that tile t's row r is (past the last one that again); FIRST: it may be the first tile
+    auto key_of = [&](uint32_t t, uint32_t start, uint32_t r, uint32_t last, auto first_c) __attribute__((always_inline)) {
+      uint32_t key = start + (r < last ? r : last);
+      if constexpr (decltype(first_c)::value) key = kt.is_mixed(t) && r < kt.mixed ? r : key;
+      return key;
     };
-    auto load_page_ids = [&](uint32_t t) __attribute__((always_inline)) {
+    auto load_page_ids = [&](uint32_t t, auto first_c) __attribute__((always_inline)) {
       if constexpr (SRC != kPlain) {
         if (t < t_end) {
           uint32_t limit;
-          const uint32_t start = tile_start(t, &limit), last = limit - 1u - start;
-          page_id = src.table[(start + (lane < last ? lane : last)) >> src.page_log2];
+          const uint32_t start = kt.start(t, &limit);
+          page_id = src.table[key_of(t, start, lane, limit - 1u - start, first_c) >> src.page_log2];
         }
       }
     };
     // Where tile t's rows are; its page ids have been asked for before.
-    auto locate = [&](uint32_t t) __attribute__((always_inline)) {
+    auto locate = [&](uint32_t t, auto first_c) __attribute__((always_inline)) {
       uint32_t limit;
-      const uint32_t start = tile_start(t, &limit), left = limit - 1u - start, last = left < kTileKeys - 1u ? left : kTileKeys - 1u;
+      const uint32_t start = kt.start(t, &limit), left = limit - 1u - start, last = left < kTileKeys - 1u ? left : kTileKeys - 1u;
       if constexpr (SRC == kPlain) {
         k_base = src.k + src.k_step * (int64_t)start;
         v_base = src.v + src.v_step * (int64_t)start;
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
           }
         }
       } else {
-        uint32_t row_no = src.row_of_page(page_id, start + (lane < last ? lane : last));
+        uint32_t row_no = src.row_of_page(page_id, key_of(t, start, lane, last, first_c));
         valid_next = __builtin_amdgcn_ballot_w64(row_no != ~0u);
         if (row_no == ~0u) row_no = 0u;  // (some row of the cache: its scores are masked)
         if constexpr (!E4M3) {
@@ -203,7 +203,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
             ve[i] = power_of(src.v_exp[r]);
           }
         }
-        load_page_ids(t + 1u);
+        load_page_ids(t + 1u, std::false_type{});
       }
     };
     // One load straight to LDS: M0 (the LDS base) is put back afterwards.  From inline assembly because the compiler would
@@ -297,10 +297,10 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
     auto tile = [&](uint32_t t, auto more_c) __attribute__((always_inline)) {
       constexpr bool MORE = decltype(more_c)::value;
       uint32_t limit;
-      const uint32_t start = tile_start(t, &limit);
+      const uint32_t start = kt.start(t, &limit), sinks = kt.sinks_at(t, start, g.sinks);
       const int32_t end = (int32_t)(start + kTileKeys);  // one past the tile's last key
       bool masked = end > (int32_t)limit || end - 1 > p_min;
-      if (g.window != 0u) masked = masked || (p_max - (int32_t)start >= (int32_t)g.window && end > (int32_t)g.sinks);
+      if (g.window != 0u) masked = masked || (p_max - (int32_t)start >= (int32_t)g.window && end > (int32_t)sinks);
       if constexpr (SRC != kPlain) masked = masked || valid != ~0ull;
       f32x16 sacc[2];
       sacc[0] = f32x16{0}; sacc[1] = f32x16{0};
@@ -308,8 +308,8 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
       u32x4 pw[4];  // P, in accumulator order: one entry per MFMA step of V^T P^T (16 keys)
       auto mask = [&](int tk) __attribute__((always_inline)) {
         if (!masked) return;
-        const RowMask m(p, limit, (int32_t)(start + 4u * h32), g.window, g.sinks);
-        if ((g.window != 0u) & (start < g.sinks)) {
+        const RowMask m(p, limit, (int32_t)(start + 4u * h32), g.window, sinks);
+        if ((g.window != 0u) & (start < sinks)) {
           asm volatile("");  // (branches: no selects where nothing is masked)
 #pragma unroll
           for (int v = 0; v < 16; ++v) sacc[tk][v] = m.sees_mixed(32 * tk + 8 * (v >> 2) + (v & 3)) ? sacc[tk][v] : -INFINITY;
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
       };
 
       // ---- region 0: S^T = K Q^T ------------------------------------------------------------------------------
-      if constexpr (MORE) locate(t + 1u);
+      if constexpr (MORE) locate(t + 1u, std::false_type{});
       __builtin_amdgcn_s_setprio(2);
       constexpr int kBarrier = NS + 1, kLoads = NS == 8 ? 11 : 6;
 #pragma unroll
@@ -410,11 +410,27 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
       if constexpr (MORE) KP_BOUNDARY(ring, 2, 0); else KP_BOUNDARY(ring, 2, kp::kNoRegion);
     };
     if (t_begin < t_end) {
-      load_page_ids(t_begin);
+      load_page_ids(t_begin, std::true_type{});
       ofs_last = ~0u;
-      locate(t_begin);
+      bool loaded = false;
+      if constexpr (SRC == kPlain) {
+        if (kt.is_mixed(t_begin)) {  // (the distance between its keys may take more than 32 bits)
+          uint32_t limit;
+          const uint32_t start = kt.start(t_begin, &limit), last = limit - 1u - start;
 #pragma unroll
-      for (int i = 0; i < NL; ++i) { load_k(i); load_v(i); }
+          for (int i = 0; i < NL; ++i) {
+            const int64_t key = (int64_t)key_of(t_begin, start, ld_row + 4u * kBlockRows * (uint32_t)i, last, std::true_type{});
+            load_at((uint64_t)(uintptr_t)(src.k + src.k_step * key) + k_in, lds0 + 4096u * (uint32_t)i);
+            load_at((uint64_t)(uintptr_t)(src.v + src.v_step * key) + v_in, lds0 + v_into + 4096u * (uint32_t)i);
+          }
+          loaded = true;
+        }
+      }
+      if (!loaded) {
+        locate(t_begin, std::true_type{});
+#pragma unroll
+        for (int i = 0; i < NL; ++i) { load_k(i); load_v(i); }
+      }
       store_codes(true);
       store_codes(false);
       requested();
@@ -492,8 +508,10 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
         Row<D / 64> row;
         for (uint32_t t = t_begin; t < t_end; ++t) {
           uint32_t limit;
-          const uint32_t start = tile_start(t, &limit), to = start + kTileKeys;
-          row_over_keys<T, D, SRC>(row, q, src, (int32_t)tl.n_k - (int32_t)tl.n_q + (int32_t)a.token, g.window, g.sinks, g.scale_log2, start, to < limit ? to : limit);
+          const int32_t at = (int32_t)tl.n_k - (int32_t)tl.n_q + (int32_t)a.token;
+          const uint32_t start = kt.start(t, &limit), to = start + kTileKeys, mixed = kt.is_mixed(t) ? kt.mixed : 0u;
+          if (mixed != 0u) row_over_keys<T, D, SRC>(row, q, src, at, g.window, g.sinks, g.scale_log2, 0u, mixed);
+          row_over_keys<T, D, SRC>(row, q, src, at, g.window, g.sinks, g.scale_log2, start + mixed, to < limit ? to : limit);
         }
         if (g.splits > 1u) {
           const size_t to = split * part_rows + part_row<kTileRows>(g, tile_id, h, 32u * wave + r);
