@@ -30,7 +30,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
   auto position = [&](uint32_t f) __attribute__((always_inline)) { return off + (int32_t)place_of(f < last_row ? f : last_row, g.group).token; };
   const RowPlace at = place_of(mine ? flat : last_row, g.group);
   const uint32_t head = hk * g.group + at.in_group;
-  const int32_t p = off + (int32_t)at.token, p_min = position(wave_first), p_max = position(wave_first + 31u);
+  const int32_t p = off + (int32_t)at.token, p_min = (int32_t)kp::wave_uniform((uint32_t)position(wave_first)), p_max = (int32_t)kp::wave_uniform((uint32_t)position(wave_first + 31u));
   const KeyTiles kt(span_of(position(first), position(first + kTileRows - 1u), g.window, g.sinks));
   const uint32_t tiles = kt.all;
 
@@ -79,20 +79,24 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
   const uint32_t lds0 = kp::wave_uniform((uint32_t)(uintptr_t)smem + 1024u * wave);
   const uint16_t *k_head = row_at(g.k, seq, hk, 0), *v_head = row_at(g.v, seq, hk, 0);
   uint32_t loaded_last = ~0u, into = 0u;  // `into`: LDS offset of the buffer that the next tiles go to
-  auto request = [&](uint32_t t) __attribute__((always_inline)) {
-    uint32_t limit;
-    const uint32_t start = kt.start(t, &limit), left = limit - 1u - start, last = left < 63u ? left : 63u;
+  uint32_t next_start = 0, next_limit = 0, next_sinks = g.sinks;  // of the tile that is requested
+  auto request_at = [&](uint32_t start, uint32_t limit) __attribute__((always_inline)) {
+    const uint32_t left = limit - 1u - start, last = left < 63u ? left : 63u;
     if (last != loaded_last) { loaded_last = last; lk.upto(last); lv.upto(last); }
     lk.load(k_head + g.k.token * (int64_t)start, lds0 + into);
     lv.load(v_head + g.v.token * (int64_t)start, lds0 + into + kTile);
     into ^= 2u * kTile;
   };
+  auto request = [&](uint32_t t) __attribute__((always_inline)) {
+    next_start = kt.start(t, &next_limit);
+    request_at(next_start, next_limit);
+  };
   auto request_first = [&]() __attribute__((always_inline)) {
-    if (!kt.is_mixed(0u)) { request(0u); return; }
-    uint32_t limit;
-    const uint32_t start = kt.start(0u, &limit), left = limit - 1u - start;
-    lk.load_two(k_head, g.k.token, kt.mixed, start, left, lds0 + into);
-    lv.load_two(v_head, g.v.token, kt.mixed, start, left, lds0 + into + kTile);
+    next_start = kt.start_of(0u, &next_limit, &next_sinks);
+    if (!kt.is_mixed(0u)) { request_at(next_start, next_limit); return; }
+    const uint32_t left = next_limit - 1u - next_start;
+    lk.load_two(k_head, g.k.token, kt.mixed, next_start, left, lds0 + into);
+    lv.load_two(v_head, g.v.token, kt.mixed, next_start, left, lds0 + into + kTile);
     into ^= 2u * kTile;
   };
 
@@ -120,9 +124,9 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
 #pragma unroll
     for (int n = 0; n < LA; ++n) ra[n] = fetch(n, 0);
     for (uint32_t t = 0; t < tiles; ++t) {
+      const uint32_t start = next_start, limit = next_limit, sinks = next_sinks;
+      next_sinks = g.sinks;
       if (t + 1u < tiles) request(t + 1u);
-      uint32_t limit;
-      const uint32_t start = kt.start(t, &limit), sinks = kt.sinks_at(t, start, g.sinks);
       const int32_t end = (int32_t)(start + 64u);
       bool masked = (end > (int32_t)limit) | (end - 1 > p_min);
       masked = masked | ((g.window != 0u) & (p_max - (int32_t)start >= (int32_t)g.window) & (end > (int32_t)sinks));
@@ -139,13 +143,13 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
         }
         __builtin_amdgcn_s_setprio(0);
         if (masked) {
-          const RowMask m(p, limit, (int32_t)(start + 4u * h32), g.window, sinks);
+          RowMask m(p, limit, (int32_t)(start + 4u * h32), g.window, sinks);
           if ((g.window != 0u) & (start < sinks)) {
-            asm volatile("");  // (branches: no selects where nothing is masked)
+            m.apart();
 #pragma unroll
             for (int v = 0; v < 16; ++v) sacc[v] = m.sees_mixed(32 * tk + 8 * (v >> 2) + (v & 3)) ? sacc[v] : -INFINITY;
           } else {
-            asm volatile("");
+            m.apart();
 #pragma unroll
             for (int v = 0; v < 16; ++v) sacc[v] = m.sees(32 * tk + 8 * (v >> 2) + (v & 3)) ? sacc[v] : -INFINITY;
           }

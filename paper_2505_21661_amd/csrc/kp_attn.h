@@ -167,24 +167,35 @@ __device__ __forceinline__ Span span_of(int32_t p_first, int32_t p_last, uint32_
 // The same keys, 64 at a time.  The last sinks, where there are not 64 of them, and the first keys of the window are one tile,
 // the first: a window of 512 with one sink takes a tile of 128 rows over 10 tiles of keys, 11 if sinks had their own.
 struct KeyTiles {
-  Span span;
-  uint32_t mixed, sink_tiles, all;  // sinks in the first tile (keys 0 .. mixed - 1), whole tiles of sinks (keys mixed on)
-  __device__ __forceinline__ KeyTiles(const Span& s) : span(s) {
-    mixed = s.sink_end & 63u;
-    sink_tiles = s.sink_end >> 6;
-    all = sink_tiles + (s.end > s.lo ? (s.end - s.lo + mixed + 63u) / 64u : 0u);
+  uint32_t mixed;  // sinks in the first tile: keys 0 .. mixed - 1
+  uint32_t all;
+  __device__ __forceinline__ KeyTiles(const Span& s) : mixed(s.sink_end & 63u) {
+    const uint32_t whole = s.sink_end >> 6;  // tiles of sinks alone: keys mixed .. sink_end - 1
+    all = whole + (s.end > s.lo ? (s.end - s.lo + mixed + 63u) / 64u : 0u);
+    sink_end = s.sink_end; end = s.end;
+    past_sinks = whole + (mixed != 0u ? 1u : 0u);
+    sinks_from = mixed - (mixed != 0u ? 64u : 0u);
+    window_from = s.lo - mixed - 64u * whole;
+    first = past_sinks == 0u || mixed != 0u ? s.lo - mixed : 0u;
   }
   __device__ __forceinline__ bool is_mixed(uint32_t t) const { return t == 0u && mixed != 0u; }
-  // Number of tile t's first key and one past the last that there is.  Element c of the mixed tile is key start + c, but
-  // key c in front of `mixed`.  (Sinks that a window hides from some row of the tile end in front of its first key.)
+  // Number of the first key of tile t > 0, and one past the last key that there is for it.
   __device__ __forceinline__ uint32_t start(uint32_t t, uint32_t* limit) const {
-    const uint32_t n = t - (mixed != 0u ? 1u : 0u);
-    const bool sinks = n < sink_tiles;
-    *limit = sinks ? span.sink_end : span.end;
-    return sinks ? mixed + 64u * n : span.lo - mixed + 64u * (t == 0u ? 0u : t - sink_tiles);
+    const bool sinks = t < past_sinks;
+    *limit = sinks ? sink_end : end;
+    return 64u * t + (sinks ? sinks_from : window_from);
   }
-  // what RowMask takes for the number of sinks there: its comparison is of start + c
-  __device__ __forceinline__ uint32_t sinks_at(uint32_t t, uint32_t start, uint32_t sinks) const { return is_mixed(t) ? start + mixed : sinks; }
+  // Of any tile.  Element c of the mixed one is key start + c, but key c in front of `mixed`; there RowMask takes start +
+  // mixed for the number of sinks, since its comparison is of start + c.  (Where a window hides sinks from some row of the
+  // tile, they end in front of its first key.)
+  __device__ __forceinline__ uint32_t start_of(uint32_t t, uint32_t* limit, uint32_t* sinks) const {
+    const uint32_t from = start(t, limit);
+    if (is_mixed(t)) { *limit = end; *sinks = first + mixed; }
+    return t == 0u ? first : from;
+  }
+
+ private:
+  uint32_t sink_end, end, past_sinks, sinks_from, window_from, first;
 };
 
 // Which of a row's scores against a run of keys are visible: element c, the key first + c, is if c - from <= count
@@ -200,6 +211,9 @@ struct RowMask {
     count = hi < lo ? 0u : (uint32_t)(hi - lo);
     sink = sk < hi ? sk : hi;
   }
+  // For a branch of its own: the compiler would make the comparisons that two branches share in front of both, and keep the
+  // results in scalar registers that the loop has none left of (chunks over an e4m3 cache of 64: 77 us, 86 that way).
+  __device__ __forceinline__ void apart() { asm volatile("" : "+v"(from), "+v"(count), "+v"(sink)); }
   __device__ __forceinline__ bool sees(int c) const { return (uint32_t)c - from <= count; }
   __device__ __forceinline__ bool sees_mixed(int c) const { return ((uint32_t)c - from <= count) | (c <= sink); }
 };

@@ -120,7 +120,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
     const bool mine = flat <= last_row;
     const RowPlace at = place_of(mine ? flat : last_row, g.group);
     const int32_t p = (int32_t)tl.n_k - (int32_t)tl.n_q + (int32_t)at.token;
-    const int32_t p_min = position(wave_first), p_max = position(wave_first + 31u);
+    const int32_t p_min = (int32_t)wave_uniform((uint32_t)position(wave_first)), p_max = (int32_t)wave_uniform((uint32_t)position(wave_first + 31u));
     const KeyTiles kt(span_of(position(tl.first), position(tl.first + kTileRows - 1u), g.window, g.sinks));
     const uint32_t t_begin = (uint32_t)((uint64_t)kt.all * split / g.splits), t_end = (uint32_t)((uint64_t)kt.all * (split + 1u) / g.splits);
 
@@ -156,19 +156,23 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
       if constexpr (decltype(first_c)::value) key = kt.is_mixed(t) && r < kt.mixed ? r : key;
       return key;
     };
+    uint32_t next_start = 0, next_limit = 0, next_sinks = g.sinks;  // of the tile that is requested
+    auto begin_of = [&](uint32_t t, uint32_t* limit, auto first_c) __attribute__((always_inline)) {
+      if constexpr (decltype(first_c)::value) return kt.start_of(t, limit, &next_sinks);
+      else return kt.start(t, limit);
+    };
     auto load_page_ids = [&](uint32_t t, auto first_c) __attribute__((always_inline)) {
       if constexpr (SRC != kPlain) {
         if (t < t_end) {
           uint32_t limit;
-          const uint32_t start = kt.start(t, &limit);
+          const uint32_t start = begin_of(t, &limit, first_c);
           page_id = src.table[key_of(t, start, lane, limit - 1u - start, first_c) >> src.page_log2];
         }
       }
     };
     // Where tile t's rows are; its page ids have been asked for before.
     auto locate = [&](uint32_t t, auto first_c) __attribute__((always_inline)) {
-      uint32_t limit;
-      const uint32_t start = kt.start(t, &limit), left = limit - 1u - start, last = left < kTileKeys - 1u ? left : kTileKeys - 1u;
+      const uint32_t start = next_start = begin_of(t, &next_limit, first_c), left = next_limit - 1u - start, last = left < kTileKeys - 1u ? left : kTileKeys - 1u;
       if constexpr (SRC == kPlain) {
         k_base = src.k + src.k_step * (int64_t)start;
         v_base = src.v + src.v_step * (int64_t)start;
@@ -296,25 +300,25 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
     };
     auto tile = [&](uint32_t t, auto more_c) __attribute__((always_inline)) {
       constexpr bool MORE = decltype(more_c)::value;
-      uint32_t limit;
-      const uint32_t start = kt.start(t, &limit), sinks = kt.sinks_at(t, start, g.sinks);
+      const uint32_t start = next_start, limit = next_limit, sinks = next_sinks;
+      next_sinks = g.sinks;
       const int32_t end = (int32_t)(start + kTileKeys);  // one past the tile's last key
-      bool masked = end > (int32_t)limit || end - 1 > p_min;
-      if (g.window != 0u) masked = masked || (p_max - (int32_t)start >= (int32_t)g.window && end > (int32_t)sinks);
-      if constexpr (SRC != kPlain) masked = masked || valid != ~0ull;
+      bool masked = (end > (int32_t)limit) | (end - 1 > p_min);
+      masked = masked | ((g.window != 0u) & (p_max - (int32_t)start >= (int32_t)g.window) & (end > (int32_t)sinks));
+      if constexpr (SRC != kPlain) masked = masked | (valid != ~0ull);
       f32x16 sacc[2];
       sacc[0] = f32x16{0}; sacc[1] = f32x16{0};
       float mx = -INFINITY, psum = 0.f;
       u32x4 pw[4];  // P, in accumulator order: one entry per MFMA step of V^T P^T (16 keys)
       auto mask = [&](int tk) __attribute__((always_inline)) {
         if (!masked) return;
-        const RowMask m(p, limit, (int32_t)(start + 4u * h32), g.window, sinks);
+        RowMask m(p, limit, (int32_t)(start + 4u * h32), g.window, sinks);
         if ((g.window != 0u) & (start < sinks)) {
-          asm volatile("");  // (branches: no selects where nothing is masked)
+          m.apart();
 #pragma unroll
           for (int v = 0; v < 16; ++v) sacc[tk][v] = m.sees_mixed(32 * tk + 8 * (v >> 2) + (v & 3)) ? sacc[tk][v] : -INFINITY;
         } else {
-          asm volatile("");
+          m.apart();
 #pragma unroll
           for (int v = 0; v < 16; ++v) sacc[tk][v] = m.sees(32 * tk + 8 * (v >> 2) + (v & 3)) ? sacc[tk][v] : -INFINITY;
         }
@@ -415,11 +419,11 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
       bool loaded = false;
       if constexpr (SRC == kPlain) {
         if (kt.is_mixed(t_begin)) {  // (the distance between its keys may take more than 32 bits)
-          uint32_t limit;
-          const uint32_t start = kt.start(t_begin, &limit), last = limit - 1u - start;
+          next_start = begin_of(t_begin, &next_limit, std::true_type{});
+          const uint32_t last = next_limit - 1u - next_start;
 #pragma unroll
           for (int i = 0; i < NL; ++i) {
-            const int64_t key = (int64_t)key_of(t_begin, start, ld_row + 4u * kBlockRows * (uint32_t)i, last, std::true_type{});
+            const int64_t key = (int64_t)key_of(t_begin, next_start, ld_row + 4u * kBlockRows * (uint32_t)i, last, std::true_type{});
             load_at((uint64_t)(uintptr_t)(src.k + src.k_step * key) + k_in, lds0 + 4096u * (uint32_t)i);
             load_at((uint64_t)(uintptr_t)(src.v + src.v_step * key) + v_in, lds0 + v_into + 4096u * (uint32_t)i);
           }
@@ -507,9 +511,9 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
         row_elements<T, D / 64>(reinterpret_cast<const uint8_t*>(g.q.at + g.q.seq * (int64_t)q_seq + g.q.head * (int64_t)hd + g.q.token * tok), lane, q);
         Row<D / 64> row;
         for (uint32_t t = t_begin; t < t_end; ++t) {
-          uint32_t limit;
+          uint32_t limit, unused;
           const int32_t at = (int32_t)tl.n_k - (int32_t)tl.n_q + (int32_t)a.token;
-          const uint32_t start = kt.start(t, &limit), to = start + kTileKeys, mixed = kt.is_mixed(t) ? kt.mixed : 0u;
+          const uint32_t start = kt.start_of(t, &limit, &unused), to = start + kTileKeys, mixed = kt.is_mixed(t) ? kt.mixed : 0u;
           if (mixed != 0u) row_over_keys<T, D, SRC>(row, q, src, at, g.window, g.sinks, g.scale_log2, 0u, mixed);
           row_over_keys<T, D, SRC>(row, q, src, at, g.window, g.sinks, g.scale_log2, start + mixed, to < limit ? to : limit);
         }
