@@ -328,32 +328,52 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
     auto stay = [](auto& x) __attribute__((always_inline)) { asm volatile("" : "+v"(x)); };
     // operands in the order of their use: Q and dO rows of the next step (this wave's half), dO^T and then Q^T of this one
     // (first of this wave's rows, then of the other's); behind them the next step's
-    const uint32_t row_own = rd.row0 + 32u * hf * kRow, col_own = (rd.col0 ^ (64u * NH * hf)) + 32u * hf * kRow;
-    const uint32_t col_other = (rd.col0 ^ (64u * NH * hf)) + 32u * (hf ^ 1u) * kRow;
+    // LDS addresses of those in the buffers at hand: rows by operand, transposed pieces by half of the rows, dt, half of the keys
+    uint32_t row_at_lds[NS], col_at_lds[2][NH][2];
+#pragma unroll
+    for (int n = 0; n < NS; ++n) row_at_lds[n] = (rd.row0 + 32u * hf * kRow) ^ (32u * (uint32_t)n);
+#pragma unroll
+    for (int dt = 0; dt < NH; ++dt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        col_at_lds[e >> 1][dt][e & 1] = ((rd.col0 ^ (64u * NH * hf)) + 32u * (hf ^ (uint32_t)(e >> 1)) * kRow) ^ (64u * (uint32_t)dt + 32u * (uint32_t)(e & 1));
+    auto step_rows = [&]() __attribute__((always_inline)) {
+      const uint32_t by = next == 2u ? 0u - 2u * kBuffer : kBuffer;
+      next = after(next);
+#pragma unroll
+      for (int n = 0; n < NS; ++n) row_at_lds[n] += by;
+    };
+    auto step_cols = [&]() __attribute__((always_inline)) {
+      const uint32_t by = now == 2u ? 0u - 2u * kBuffer : kBuffer;
+      now = after(now);
+#pragma unroll
+      for (int dt = 0; dt < NH; ++dt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) col_at_lds[e >> 1][dt][e & 1] += by;
+    };
     auto fetch = [&](int n) __attribute__((always_inline)) -> u32x4 {
       if (n >= 4 * NS) n -= 4 * NS;
-      if (n < NS) return rd.rows_at((row_own ^ (32u * (uint32_t)n)) + next * kBuffer, 0u);
-      if (n < 2 * NS) return rd.rows_at((row_own ^ (32u * (uint32_t)(n - NS))) + next * kBuffer, 64u);
+      if (n < NS) return rd.rows_at(row_at_lds[n], 0u);
+      if (n < 2 * NS) return rd.rows_at(row_at_lds[n - NS], 64u);
       const int m = (n - 2 * NS) % NS, ks = m / NH, dt = m % NH;
-      const uint32_t c = ks < 2 ? col_own : col_other, from = (n < 3 * NS ? 64u : 0u) + 16u * (uint32_t)(ks & 1);
-      return rd.cols_at((c ^ (64u * (uint32_t)dt)) + now * kBuffer, (c ^ (64u * (uint32_t)dt + 32u)) + now * kBuffer, from);
+      return rd.cols_at(col_at_lds[ks / 2][dt][0], col_at_lds[ks / 2][dt][1], (n < 3 * NS ? 64u : 0u) + 16u * (uint32_t)(ks & 1));
     };
     // S of the wave's 32 rows of the step that starts at `start`: what is not visible becomes -inf
     auto hide = [&]() __attribute__((always_inline)) {
       const int32_t first = (int32_t)(start + 32u * hf), last = first + 31, k0 = (int32_t)j0, k1 = k0 + 31;
       if ((last >= (int32_t)tok.to) | (off + first < k1) | ((g.window != 0u) & (k1 >= (int32_t)g.sinks) & (off + last - k0 >= (int32_t)g.window))) {
         const int32_t token = first + (int32_t)l32;
-        const RowMask m(token < (int32_t)tok.to ? off + token : -1, g.n_k, k0 + 4 * (int32_t)h32, g.window, g.sinks);
+        RowMask m(token < (int32_t)tok.to ? off + token : -1, g.n_k, k0 + 4 * (int32_t)h32, g.window, g.sinks);
         if ((g.window == 0u) | (k0 >= (int32_t)g.sinks)) {
-          asm volatile("");  // (branches: no selects where nothing is masked)
+          m.apart();
 #pragma unroll
           for (int v = 0; v < 16; ++v) sacc[v] = m.sees(8 * (v >> 2) + (v & 3)) ? sacc[v] : -INFINITY;
         } else if (off + first - k1 >= (int32_t)g.window) {  // sinks alone are left
-          asm volatile("");
+          m.apart();
 #pragma unroll
           for (int v = 0; v < 16; ++v) sacc[v] = 8 * (v >> 2) + (v & 3) <= m.sink ? sacc[v] : -INFINITY;
         } else {
-          asm volatile("");
+          m.apart();
 #pragma unroll
           for (int v = 0; v < 16; ++v) sacc[v] = m.sees_mixed(8 * (v >> 2) + (v & 3)) ? sacc[v] : -INFINITY;
         }
@@ -413,7 +433,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
 #pragma unroll
     for (int i = 0; i < 4; ++i) share_ds(0u, i);
     wait_all();
-    next = 1u;
+    step_rows();
 #pragma unroll
     for (int n = 0; n < LA; ++n) ra[n] = fetch(n);
     for (uint32_t step = s_begin; step < s_end; ++step) {
@@ -466,8 +486,8 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
         // behind the last operand of this step: P and dS of the next are there, so are its successor's tiles
         if (n == NS - LA) {
           wait_all();
-          now = now == 2u ? 0u : now + 1u;
-          next = next == 2u ? 0u : next + 1u;
+          step_cols();
+          step_rows();
         }
         dk[n % NH] = T::mfma32(ra[n % LA], rb[ks & 1], dk[n % NH]);
         ra[n % LA] = fetch(3 * NS + n + LA);
