@@ -74,7 +74,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
   }
   const float neg_p = kScaled ? neg - kShiftP<T> : neg;
 
-  TileReader<D> rd((uint32_t)(uintptr_t)smem);
+  TileCursor<D> rd((uint32_t)(uintptr_t)smem, 2u * kTile);
   TileLoader<D, 4> lk(g.k.token), lv(g.v.token);
   const uint32_t lds0 = kp::wave_uniform((uint32_t)(uintptr_t)smem + 1024u * wave);
   const uint16_t *k_head = row_at(g.k, seq, hk, 0), *v_head = row_at(g.v, seq, hk, 0);
@@ -106,13 +106,12 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
   // The operands of the three products come out of LDS LA MFMAs ahead, in one set of registers.
   constexpr int LA = 4;
   u32x4 ra[LA];
-  uint32_t buffer = 0u;
   // operand n of the half tile tk: K rows, V rows, K^T; from 3 NS on the half after it
   auto fetch = [&](int n, int tk) __attribute__((always_inline)) {
     if (n >= 3 * NS) { n -= 3 * NS; tk ^= 1; }
-    if (n < NS) return rd.rows(n, 32u * (uint32_t)tk, buffer);
-    if (n < 2 * NS) return rd.rows(n - NS, 64u + 32u * (uint32_t)tk, buffer);
-    return rd.cols((n - 2 * NS) % ND, 32u * (uint32_t)tk + 16u * (uint32_t)((n - 2 * NS) / ND), buffer);
+    if (n < NS) return rd.rows(n, 32u * (uint32_t)tk);
+    if (n < 2 * NS) return rd.rows(n - NS, 64u + 32u * (uint32_t)tk);
+    return rd.cols((n - 2 * NS) % ND, 32u * (uint32_t)tk + 16u * (uint32_t)((n - 2 * NS) / ND));
   };
   float lacks = 0.f;
   // Over all keys; CHECK: with the sum of dS.
@@ -174,7 +173,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
           // behind the tile's last operand read: every wave has read these tiles, and the next ones have landed
           if (tk == 1 && s == NS - LA) {
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            buffer ^= 2u * kTile;
+            rd.to_other();
           }
           acc[s % ND] = T::mfma32(ra[n % LA], ds[s / ND], acc[s % ND]);
           ra[n % LA] = fetch(n + LA, tk);  // (behind the last tile: not used)

@@ -140,6 +140,32 @@ struct TileReader {
   }
 };
 
+// The same of tiles in two buffers: the addresses go from one buffer to the other (an addition per register and step, where
+// every read had one).
+template <int D>
+struct TileCursor {
+  uint32_t row[D / 16], col[D / 32][2], by;
+  __device__ __forceinline__ TileCursor(uint32_t base, uint32_t buffer_bytes) : by(buffer_bytes) {
+    const TileReader<D> rd(base);
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) row[s] = rd.row0 ^ (32u * (uint32_t)s);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) {
+      col[dt][0] = rd.col0 ^ (64u * (uint32_t)dt);
+      col[dt][1] = rd.col0 ^ (64u * (uint32_t)dt + 32u);
+    }
+  }
+  __device__ __forceinline__ u32x4 rows(int s, uint32_t from) const { return TileReader<D>::rows_at(row[s], from); }
+  __device__ __forceinline__ u32x4 cols(int dt, uint32_t from) const { return TileReader<D>::cols_at(col[dt][0], col[dt][1], from); }
+  __device__ __forceinline__ void to_other() {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) row[s] += by;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) { col[dt][0] += by; col[dt][1] += by; }
+    by = 0u - by;
+  }
+};
+
 // 64 rows from global memory straight to such a tile: 1 KiB to a load of one of WAVES waves.
 template <int D, int WAVES>
 struct TileLoader {

@@ -555,7 +555,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan 
   const int32_t off = (int32_t)g.n_k - (int32_t)g.n_q;
   const uint32_t j_last = g.n_k - 1u;
   KeyWork work(plan);
-  const TileReader<D> rd((uint32_t)(uintptr_t)smem);
+  TileCursor<D> rd((uint32_t)(uintptr_t)smem, kBuffer);
   TileLoader<D, 4> lq(g.q.token), ld(g.d_o.token);
   const uint32_t lds0 = kp::wave_uniform((uint32_t)(uintptr_t)smem + 1024u * wave);
   while (work.next(plan)) {
@@ -574,6 +574,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan 
     }
     const float ds_scale = kScaled ? ds_scale_of(g, unit) : 1.f;  // dS is rounded times this (and 2^kShiftP, which is in P)
     uint32_t loaded_last = ~0u, into = 0u;  // `into`: buffer that the next step goes to
+    if (rd.by != kBuffer) rd.to_other();    // (an odd number of steps before: back to the first)
     const uint32_t head_steps = steps_per_head == 0u ? 1u : steps_per_head;
     uint32_t ask_group = s_begin / head_steps, ask_start = tok.from + (s_begin - ask_group * head_steps) * 64u;
     uint32_t start = ask_start;  // first token of the step at hand
@@ -602,16 +603,15 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan 
       request();
       __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own count of outstanding loads)
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      uint32_t buffer = 0u;
+      uint32_t stats = kStats;
 #pragma unroll
-      for (int s = 0; s < NS; ++s) ra[s] = rd.rows(s, 0u, 0u);
+      for (int s = 0; s < NS; ++s) ra[s] = rd.rows(s, 0u);
       for (uint32_t step = s_begin; step < s_end; ++step) {
-        const uint32_t stats = kStats + (buffer != 0u ? 512u : 0u);
         if (step + 1u < s_end) request();
         auto next_buffer = [&]() __attribute__((always_inline)) {
           // every wave has read these tiles, and the next ones have landed
           asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-          buffer ^= kBuffer;
+          rd.to_other();
         };
 #pragma unroll
         for (int rt = 0; rt < 2; ++rt) {
@@ -623,14 +623,14 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan 
           if (none) {
             if (rt == 1) next_buffer();
 #pragma unroll
-            for (int s = 0; s < NS; ++s) ra[s] = rd.rows(s, rt == 0 ? 32u : 0u, buffer);
+            for (int s = 0; s < NS; ++s) ra[s] = rd.rows(s, rt == 0 ? 32u : 0u);
             continue;
           }
           f32x16 sacc = f32x16{0}, dp = f32x16{0};
 #pragma unroll
           for (int s = 0; s < NS; ++s) {
             sacc = T::mfma32(ra[s], kf[s], sacc);
-            ra[s] = rd.rows(s, 64u + 32u * (uint32_t)rt, buffer);  // dO
+            ra[s] = rd.rows(s, 64u + 32u * (uint32_t)rt);  // dO
             __builtin_amdgcn_sched_barrier(0);
           }
           f32x4 neg[4], delta[4];  // of rows 8 i + 4 h32 .. + 3
@@ -643,7 +643,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan 
 #pragma unroll
           for (int s = 0; s < NS; ++s) {
             dp = T::mfma32(ra[s], vf[s], dp);
-            ra[s] = rd.cols(s % ND, 64u + 32u * (uint32_t)rt + 16u * (uint32_t)(s / ND), buffer);  // dO^T
+            ra[s] = rd.cols(s % ND, 64u + 32u * (uint32_t)rt + 16u * (uint32_t)(s / ND));  // dO^T
             __builtin_amdgcn_sched_barrier(0);
           }
           if ((last >= (int32_t)tok.to) | (p0 < k1) | ((g.window != 0u) & (k1 >= (int32_t)g.sinks) & (p1 - k0 >= (int32_t)g.window))) {
@@ -673,17 +673,18 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan 
 #pragma unroll
           for (int s = 0; s < NS; ++s) {
             dv[s % ND] = T::mfma32(ra[s], pw[s / ND], dv[s % ND]);
-            ra[s] = rd.cols(s % ND, 32u * (uint32_t)rt + 16u * (uint32_t)(s / ND), buffer);  // Q^T
+            ra[s] = rd.cols(s % ND, 32u * (uint32_t)rt + 16u * (uint32_t)(s / ND));  // Q^T
             __builtin_amdgcn_sched_barrier(0);
           }
           if (rt == 1) next_buffer();
 #pragma unroll
           for (int s = 0; s < NS; ++s) {
             dk[s % ND] = T::mfma32(ra[s], ds[s / ND], dk[s % ND]);
-            ra[s] = rd.rows(s, rt == 0 ? 32u : 0u, buffer);  // Q: the other half, or the next step's (the last time: not used)
+            ra[s] = rd.rows(s, rt == 0 ? 32u : 0u);  // Q: the other half, or the next step's (the last time: not used)
             __builtin_amdgcn_sched_barrier(0);
           }
         }
+        stats ^= 512u;
         start += 64u;
         if (start >= tok.to) start = tok.from;
       }
