@@ -237,7 +237,7 @@ GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, in
   p.sink_tiles = window > 0 && head_steps * group - steps >= saves ? ((long long)sinks + kGradKeys - 1) / kGradKeys : 0;
   if (p.sink_tiles > p.key_tiles) p.sink_tiles = p.key_tiles;
   const long long lines = p.lines = p.units % 8 == 0 ? 8 : 1, plain = p.units / lines * (p.key_tiles - p.sink_tiles);
-  const long long all = steps * lines * plain + head_steps * group * p.units * p.sink_tiles;
+  const long long sink_steps = head_steps * group * (p.units / lines) * p.sink_tiles, all = lines * (steps * plain + sink_steps);
   p.too_many = all / lines >= (1ll << 30);
   // One worker per CU, or two (D = 64).  Where there are fewer tiles than that, a worker per tile saves the second tile of a
   // worker's piece and the sums of parts (some 14 us, as much as 14 steps of D = 64 or 7 of 128); splitting them saves steps.
@@ -245,12 +245,17 @@ GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, in
   // 8/8 x 4096, window 1024, saves 10: 70 split, 56 whole.)
   const long long chip = D == 64 ? kMostWorkers : kChip;
   p.workers = chip;
-  if (plain > 0 && lines * plain < p.workers && steps - all / chip < saves) p.workers = lines * plain;
+  // The tiles with sinks go to more workers, as many as they keep busy for as long (6/3 x 1489 x 128, window 20, 148 sinks:
+  // 63 us without, 40 with; 5 x 6/2 x 637 x 64, window 49, 4 sinks: 46 and 36).
+  if (plain > 0 && lines * plain < chip && steps - all / chip < saves) {
+    const long long more = plain + sink_steps / steps;
+    p.workers = lines * (more < chip / lines ? more : chip / lines);
+  }
   if (all < p.workers) p.workers = all / lines * lines;
   if (p.workers < lines) p.workers = lines;
   // Whole rounds, and one that is not full if what it lacks can be made up for by the tiles with sinks, or is little.
   const long long places = p.workers / lines, lacks = (places - plain % places) % places;
-  p.whole = lacks * steps <= head_steps * group * (p.units / lines) * p.sink_tiles + places * steps / 16 ? plain : plain / places * places;
+  p.whole = lacks * steps <= sink_steps + places * steps / 16 ? plain : plain / places * places;
   p.split = p.units * p.sink_tiles + lines * (plain - p.whole);
   p.rows = (size_t)B * (size_t)Hq * (size_t)Sq;
   const auto up = [](size_t n) { return (n + 15) & ~(size_t)15; };

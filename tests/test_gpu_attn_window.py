@@ -216,6 +216,22 @@ def test_a_few_more_key_tiles_than_compute_units(kp, dtype):
             assert_within(x[at], want, bound, name)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n, window, sinks", [(1100, 20, 148), (1100, 60, 64), (900, 33, 5), (2000, 1, 129)])
+def test_sinks_of_many_tokens(kp, n, window, sinks, d):
+    """Key tiles that hold sinks are gone over by all later tokens, the others by a few: workers of their own."""
+    gen = torch.Generator(device="cuda").manual_seed(18)
+    b, hq, hkv, dtype = 1, 6, 3, torch.bfloat16
+    q, k, v, d_o = (heads(gen, b, h, n, d, dtype, "bshd") for h in (hq, hkv, hkv, hq))
+    o, lse = attend(kp, q, k, v, window, sinks, 0.1)
+    p, want, want_lse = forward(q, k, v, window, sinks, 0.1)
+    assert_within(o, want, o_bound(p, v, dtype), "o")
+    assert_lse(lse, want_lse)
+    for name, got, (want, bound) in zip(("dq", "dk", "dv"), grads(kp, q, k, v, o, lse, d_o, window, sinks, 0.1),
+                                        gradients(q, k, v, d_o, window, sinks, 0.1, dtype)):
+        assert_within(got, want, bound, name)
+
+
 def test_windows_that_hide_nothing(kp):
     """A window as long as the keys, or of the largest number there is, is none; so are as many sinks."""
     gen = torch.Generator(device="cuda").manual_seed(15)
