@@ -6,6 +6,9 @@
 // join in kp_attn_join.  Products as in kp_attn_rows.h with the 16x16x32 shape: K goes from memory to the operand
 // registers as it lies (a lane reads 16-byte pieces of one key's row), V through 8 KiB of LDS per wave, which the
 // transposing read needs; both are asked for a step ahead.
+// Bound by memory: 64 tokens of 32/8 heads of 128 over up to 16384 keys of e4m3, 1409 MB, take 253 us with the join (5570
+// GB/s, 91 % of what reading alone reaches); 16 tokens of 16/2 heads over a window of 4096, 67 MB, 18 us (14.4 of them this
+// kernel); small calls by latency (4 tokens over up to 700 keys: 8 us; an empty kernel takes 3.8 a launch).
 #pragma once
 #include "kp_attn_rows.h"
 

@@ -81,6 +81,11 @@ __device__ __forceinline__ void finish_ring(kp::Ring& ring, const Args& g, uint3
 
 #define KP_BOUNDARY(ring, end_r, start_r) do { if constexpr (INSTR != 0) kp::site<INSTR>(ring, end_r, start_r); } while (0)
 
+// Per tile of 64 keys a wave has 32 MFMAs (1024 cycles), 33 exponentials (530) and some 160 other vector instructions (640),
+// which its partner on the SIMD hides in part: the matrix pipes are busy 48 % of the time at 1.9 GHz (32/8 x 8192 x 128,
+// window 1024: 155 us, 830 TFLOP/s of what rows see), 38 % where a tile of rows has 10 tiles of keys (2 x 16/16 x 4000, window
+// 512: 57 us, 550), since the first loads and the stores of a workgroup then weigh more; chunks of 512 tokens over up to 8192
+// keys in pages, window 2048: 113 us, 750.
 // Recorded regions, per tile of 64 keys: 0 K Q^T, with the request of the next keys and values and the lower half's mask and
 // maximum between its MFMAs, 1 the rest of the softmax, 2 V^T P^T up to the barrier behind it.
 template <class T, int D, int SRC, int INSTR>
@@ -532,6 +537,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
   if constexpr (INSTR != 0) finish_ring<INSTR>(ring, g, unit * per + item);
 }
 
+// Bound by latency: 3 to 6 us for up to 4 MB of parts.
 // Joins the partial results of a row: D / 4 lanes to a row, 4 elements to a lane.  ROWS: of a tile of the kernel that made
 // them.  WIDE: the workgroup has one row, whose parts its groups of lanes share, eight at a time to a group.
 constexpr uint32_t kJoinAtOnce = 8;  // parts of a group whose loads are in flight together
