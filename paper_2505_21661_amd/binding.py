@@ -176,7 +176,7 @@ def _stream_lookup():
     if raw is None:  # (not part of torch's public interface)
         return lambda: torch.cuda.current_stream().cuda_stream
     torch.cuda.init()
-    device = torch.cuda.current_device
+    device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (the latter looks for the former's state first)
     return lambda: raw(device())
 
 
@@ -392,17 +392,17 @@ def kp_calibrate(cycles, n_wg: int, waves: int, mode: int, trace_buf, trace_cap:
 _names = {}  # torch's types by the names below, filled in by the first call
 
 
-def _dtype(name: str):
+def _types() -> dict:
     if not _names:
         import torch
 
         _names.update({n: getattr(torch, n) for n in ("float32", "uint8", "int32", "int64", "float8_e4m3fn")})
         _names.update({torch.bfloat16: KP_BF16, torch.float16: KP_FP16})
-    return _names.get(name)
+    return _names
 
 
 def _type_code(dtype) -> int:
-    code = _dtype(dtype)
+    code = (_names or _types()).get(dtype)
     if code is None:
         raise ValueError(f"tensors must be bfloat16 or float16, not {dtype}")
     return code
@@ -431,7 +431,7 @@ def _flat(name: str, t, dtype, shape=None):
     """Device pointer of a contiguous tensor of a type and (where given) a shape."""
     if t.dtype is not dtype or (shape is not None and t.shape != shape):
         raise ValueError(f"{name} must be {'' if shape is None else str(list(shape)) + ' '}of {dtype}, not {list(t.shape)} of {t.dtype}")
-    return _ptr(t)
+    return t.data_ptr() if t.is_cuda and t.is_contiguous() else _ptr(t)
 
 
 def _workspace(workspace) -> tuple[int, int]:
@@ -469,7 +469,7 @@ def kp_attn_window(q, k, v, o, lse, window: int, sinks: int, scale: float, works
     ws, n = _workspace(workspace)
     _check(lib().kp_attn_window(
         _heads("q", q, q.shape, dtype), _heads("k", k, (B, Hkv, Sk, D), dtype), _heads("v", v, kv, dtype),
-        _heads("o", o, q.shape, dtype), 0 if lse is None else _flat("lse", lse, _dtype("float32"), (B, Hq, Sq)),
+        _heads("o", o, q.shape, dtype), 0 if lse is None else _flat("lse", lse, (_names or _types())["float32"], (B, Hq, Sq)),
         B, Hq, Hkv, Sq, Sk, D, _type_code(dtype), window, sinks, scale, ws, n, region_mask & 0xFFFFFFFF, _ptr(trace_buf),
         trace_cap, _stream(stream)))
 
@@ -486,7 +486,7 @@ def kp_attn_window_grad(q, k, v, o, lse, d_o, dq, dk, dv, window: int, sinks: in
     ws, n = _workspace(workspace)
     _check(lib().kp_attn_window_grad(
         _heads("q", q, qs, dtype), _heads("k", k, (B, Hkv, Sk, D), dtype), _heads("v", v, ks, dtype),
-        _heads("o", o, qs, dtype), _flat("lse", lse, _dtype("float32"), (B, Hq, Sq)), _heads("d_o", d_o, qs, dtype),
+        _heads("o", o, qs, dtype), _flat("lse", lse, (_names or _types())["float32"], (B, Hq, Sq)), _heads("d_o", d_o, qs, dtype),
         _heads("dq", dq, qs, dtype), _heads("dk", dk, ks, dtype), _heads("dv", dv, ks, dtype),
         B, Hq, Hkv, Sq, Sk, D, _type_code(dtype), window, sinks, scale, ws, n, _stream(stream)))
 
@@ -499,10 +499,12 @@ def _cache_of(k_cache, v_cache, k_exp, v_exp, dtype) -> bytes:
     if (not e4m3 and kind is not dtype) or v_cache.dtype is not kind or v_cache.shape != shape:
         raise ValueError(f"the cache's halves must be alike and of {dtype} or float8_e4m3fn, not {list(k_cache.shape)} of {kind} "
                          f"and {list(v_cache.shape)} of {v_cache.dtype}")
+    if not (k_cache.is_cuda and v_cache.is_cuda and k_cache.is_contiguous() and v_cache.is_contiguous()):
+        _ptr(k_cache), _ptr(v_cache)  # (one of them raises)
     if not e4m3:
-        return _pack_cache(_ptr(k_cache), _ptr(v_cache), 0, 0, n_pages, Hkv, page, D, code, 0)
+        return _pack_cache(k_cache.data_ptr(), v_cache.data_ptr(), 0, 0, n_pages, Hkv, page, D, code, 0)
     rows, byte = shape[:3], _names["uint8"]
-    return _pack_cache(_ptr(k_cache), _ptr(v_cache), _flat("k_exp", k_exp, byte, rows), _flat("v_exp", v_exp, byte, rows),
+    return _pack_cache(k_cache.data_ptr(), v_cache.data_ptr(), _flat("k_exp", k_exp, byte, rows), _flat("v_exp", v_exp, byte, rows),
                        n_pages, Hkv, page, D, code, 1)
 
 
@@ -511,7 +513,7 @@ def kp_cache_write(k, v, slots, k_cache, v_cache, k_exp=None, v_exp=None, stream
     or, into a float8_e4m3fn cache with exponents [n_pages, Hkv, page] uint8, quantised row by row."""
     T, (_, Hkv, _, D) = k.shape[0], k_cache.shape
     _check(lib().kp_cache_write(_heads("k", k, (T, Hkv, D), k.dtype), _heads("v", v, (T, Hkv, D), k.dtype),
-                                _flat("slots", slots, _dtype("int64"), (T,)), T,
+                                _flat("slots", slots, (_names or _types())["int64"], (T,)), T,
                                 _cache_of(k_cache, v_cache, k_exp, v_exp, k.dtype), _stream(stream)))
 
 
@@ -521,8 +523,8 @@ def kp_cache_read(k_cache, v_cache, k_exp, v_exp, block_table, starts, k, v, str
     T, (_, Hkv, _, D) = k.shape[0], k_cache.shape
     n, width = block_table.shape
     _check(lib().kp_cache_read(_cache_of(k_cache, v_cache, k_exp, v_exp, k.dtype),
-                               _flat("block_table", block_table, _dtype("int32")), width,
-                               _flat("starts", starts, _dtype("int32"), (n + 1,)), n, T,
+                               _flat("block_table", block_table, (_names or _types())["int32"]), width,
+                               _flat("starts", starts, (_names or _types())["int32"], (n + 1,)), n, T,
                                _heads("k", k, (T, Hkv, D), k.dtype), _heads("v", v, (T, Hkv, D), k.dtype), _stream(stream)))
 
 
@@ -552,9 +554,9 @@ def kp_attn_paged(q, k_cache, v_cache, k_exp, v_exp, block_table, lens, starts, 
     ws, nbytes = _workspace(workspace)
     _check(lib().kp_attn_paged(
         _heads("q", q, q.shape, q.dtype), _cache_of(k_cache, v_cache, k_exp, v_exp, q.dtype),
-        _flat("block_table", block_table, _dtype("int32")), width, _flat("lens", lens, _dtype("int32"), (n,)),
-        _flat("starts", starts, _dtype("int32"), (n + 1,)), _heads("o", o, q.shape, q.dtype),
-        0 if lse is None else _flat("lse", lse, _dtype("float32"), (Hq, T)), T, n, Hq, window, sinks, scale, ws, nbytes,
+        _flat("block_table", block_table, (_names or _types())["int32"]), width, _flat("lens", lens, (_names or _types())["int32"], (n,)),
+        _flat("starts", starts, (_names or _types())["int32"], (n + 1,)), _heads("o", o, q.shape, q.dtype),
+        0 if lse is None else _flat("lse", lse, (_names or _types())["float32"], (Hq, T)), T, n, Hq, window, sinks, scale, ws, nbytes,
         region_mask & 0xFFFFFFFF, _ptr(trace_buf), trace_cap, _stream(stream)))
 
 
