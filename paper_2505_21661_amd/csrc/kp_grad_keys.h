@@ -63,14 +63,14 @@ struct KeyPlan {
     return n * workers + ((n & 1u) ? workers - 1u - worker : worker);
   }
   __host__ void deal() {
-    uint32_t total = 0, before = 0;
+    uint32_t total = 0;
     for (uint32_t n = 0; n < rest; ++n) total += split_steps(n);
-    uint64_t all = total;
+    uint64_t all = total, before = 0;
     for (uint32_t w = 0; w < workers; ++w) all += edge[w] = cost(w);
     const uint32_t each = (uint32_t)((all + workers - 1u) / workers);  // (what all are short of it is the total or more)
     for (uint32_t w = 0; w < workers; ++w) {
       const uint32_t has = edge[w];
-      edge[w] = before < total ? before : total;
+      edge[w] = before < total ? (uint32_t)before : total;
       before += has < each ? each - has : 0u;
     }
     edge[workers] = total;
@@ -507,14 +507,16 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
     float* const part = g.part + work.part_at(plan) * (2u * kGradKeys * D) + (size_t)(32u * group_no) * D;
     __syncthreads();  // (the tiles' room is used below)
     if (!whole) {
+      if (j <= j_last) {  // (3 x 64/8 x 5 x 128: 26 us for both kernels and the join, 37 with the rows that are no keys)
 #pragma unroll
-      for (int dt = 0; dt < NH; ++dt)
+        for (int dt = 0; dt < NH; ++dt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float* const out = part + l32 * D + 32u * (NH * hf + (uint32_t)dt) + 8 * i + 4 * h32;
-          *reinterpret_cast<f32x4*>(out) = f32x4{dk[dt][4 * i] * by_k, dk[dt][4 * i + 1] * by_k, dk[dt][4 * i + 2] * by_k, dk[dt][4 * i + 3] * by_k};
-          *reinterpret_cast<f32x4*>(out + kGradKeys * D) = f32x4{dv[dt][4 * i] * by_v, dv[dt][4 * i + 1] * by_v, dv[dt][4 * i + 2] * by_v, dv[dt][4 * i + 3] * by_v};
-        }
+          for (int i = 0; i < 4; ++i) {
+            float* const out = part + l32 * D + 32u * (NH * hf + (uint32_t)dt) + 8 * i + 4 * h32;
+            *reinterpret_cast<f32x4*>(out) = f32x4{dk[dt][4 * i] * by_k, dk[dt][4 * i + 1] * by_k, dk[dt][4 * i + 2] * by_k, dk[dt][4 * i + 3] * by_k};
+            *reinterpret_cast<f32x4*>(out + kGradKeys * D) = f32x4{dv[dt][4 * i] * by_v, dv[dt][4 * i + 1] * by_v, dv[dt][4 * i + 2] * by_v, dv[dt][4 * i + 3] * by_v};
+          }
+      }
     } else {
       // Through LDS as in store_rows, the dk tile and behind it the dv tile: [128 keys][D]
       unsigned char* const to_lds = smem + 32u * group_no * kRow + l32 * kRow;
@@ -754,6 +756,7 @@ __global__ __launch_bounds__(kThreads) void kp_grad_join(GradArgs g, KeyPlan pla
   if (parts == 1u) return;  // one worker has all of it and has written it (none: no token sees the tile)
   const uint32_t seq = unit / g.hkv, hk = unit - seq * g.hkv;
   const uint32_t c = threadIdx.x % kLanes, row = (blockIdx.x % kBlocks) * kJoinRows<D> + threadIdx.x / kLanes, j = kt * kGradKeys + row;
+  if (j >= g.n_k) return;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
   for (uint32_t i = 0; i < parts; ++i) {
@@ -762,7 +765,7 @@ __global__ __launch_bounds__(kThreads) void kp_grad_join(GradArgs g, KeyPlan pla
     for (int e = 0; e < 4; ++e) sum[e] += x[e];
   }
   const Heads& out = blockIdx.y ? g.dv : g.dk;
-  if (j < g.n_k) *reinterpret_cast<u32x2*>(const_cast<uint16_t*>(row_at(out, seq, hk, j)) + 4u * c) = u32x2{T::pack(sum[0], sum[1]), T::pack(sum[2], sum[3])};
+  *reinterpret_cast<u32x2*>(const_cast<uint16_t*>(row_at(out, seq, hk, j)) + 4u * c) = u32x2{T::pack(sum[0], sum[1]), T::pack(sum[2], sum[3])};
 }
 
 }  // namespace attn
