@@ -99,7 +99,7 @@ inline Plan plan_of(long long seqs, long long rows, long long most_keys, int Hkv
   p.units = p.tiles * Hkv;
   // Joining the parts takes 6 us more, in which a workgroup gets through some 1000 keys: fewer than 1536 are not split, and
   // a run has 512.  Tiles of 128 rows are split to fill the chip (two workgroups per CU: 6 chunks of up to 512 tokens over
-  // 8192 keys, 588 workgroups, 125 us, split in two 149); few rows further, since the sequences differ in length (64 tokens
+  // 8192 keys, 672 workgroups, 125 us, split in two 149); few rows further, since the sequences differ in length (64 tokens
   // over up to 16384 keys, 1024 workgroups 277 us, 4096 261, 8192 267).
   const long long want = p.few ? 4096 : 512, runs = most_keys < 1536 ? 1 : most_keys / 512;
   p.splits = p.units * 2 > want ? 1 : want / p.units;
