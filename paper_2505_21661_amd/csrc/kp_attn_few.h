@@ -6,8 +6,8 @@
 // join in kp_attn_join.  Products as in kp_attn_rows.h with the 16x16x32 shape: K goes from memory to the operand
 // registers as it lies (a lane reads 16-byte pieces of one key's row), V through 8 KiB of LDS per wave, which the
 // transposing read needs; both are asked for a step ahead.
-// Bound by memory: 64 tokens of 32/8 heads of 128 over up to 16384 keys of e4m3, 1409 MB, take 253 us with the join (5570
-// GB/s, 91 % of what reading alone reaches); 16 tokens of 16/2 heads over a window of 4096, 67 MB, 18 us (14.4 of them this
+// Bound by memory: 64 tokens of 32/8 heads of 128 over up to 16384 keys of e4m3, 1409 MB, take 238 us with the join (5920
+// GB/s, 96 % of what reading alone reaches); 16 tokens of 16/2 heads over a window of 4096, 67 MB, 17.7 us (14 of them this
 // kernel); small calls by latency (4 tokens over up to 700 keys: 8 us; an empty kernel takes 3.8 a launch).
 #pragma once
 #include "kp_attn_rows.h"
@@ -120,11 +120,13 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_few(Args g) {
       if constexpr (E4M3) k_e[n] = src.k_exp[r];
     }
   };
+  // Values are read once, whole lines at a time, and go past the caches; of a line of keys a load takes half, and the other
+  // half is to be there for the next (64 tokens over up to 16384 keys: 238 us, all through the caches 261, nothing 247).
   auto load_v = [&](uint32_t rows) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < VL; ++i) {
       const uint32_t r = __shfl(rows, (int)((64u / kVPer) * i + lane / kVPer), 64);
-      vr[i] = *reinterpret_cast<const u32x4*>(src.v_at(r) + 16u * (lane % kVPer));
+      vr[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src.v_at(r) + 16u * (lane % kVPer)));
       if constexpr (E4M3) v_e[i] = src.v_exp[r];
     }
   };
