@@ -176,7 +176,7 @@ def _stream_lookup():
     if raw is None:  # (not part of torch's public interface)
         return lambda: torch.cuda.current_stream().cuda_stream
     torch.cuda.init()
-    device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (the latter looks for the former's state first)
+    device = torch.cuda.current_device
     return lambda: raw(device())
 
 
