@@ -743,7 +743,7 @@ __global__ __launch_bounds__(kThreads) void kp_grad_join(GradArgs g, KeyPlan pla
     for (uint32_t t0 = 0; t0 < no; t0 += 64u) begin += __builtin_amdgcn_readlane(sum_up_to_lane(t0 + lane < no ? plan.split_steps(t0 + lane) : 0u), 63);
     for (uint32_t w0 = 0; w0 < plan.workers; w0 += 64u) {
       const uint32_t w = w0 + lane, a = w < plan.workers ? plan.edge[w] : 0u, b = w < plan.workers ? plan.edge[w + 1u] : 0u;
-      const bool has = (a < b) & (a < begin + n) & (b > begin);
+      const bool has = (n != 0u) & (a < b) & (a < begin + n) & (b > begin);  // (a piece may go on past a tile without steps)
       const uint64_t all = __builtin_amdgcn_ballot_w64(has);
       const uint32_t at = parts + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0u));
       if (has) from[at] = g.part + (2u * (size_t)(w * plan.lines + line) + (a > begin ? 0u : 1u)) * (2u * kGradKeys * D) + (size_t)blockIdx.y * (kGradKeys * D);

@@ -232,6 +232,26 @@ def test_sinks_of_many_tokens(kp, n, window, sinks, d):
         assert_within(got, want, bound, name)
 
 
+# (B, Hq, Hkv, Sq, Sk, window, sinks): tokens at the end of a longer run of keys, whose first key tiles no token sees.  Tiles of
+# several heads are dealt out in one line, so that such tiles lie at the ends of workers' pieces, and inside them.
+UNSEEN = [(1, 6, 2, 1000, 2000, 250, 4), (2, 3, 1, 600, 2000, 250, 0), (3, 6, 2, 300, 700, 250, 0), (2, 6, 2, 300, 1300, 60, 4), (3, 3, 1, 1000, 2000, 250, 4)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", UNSEEN)
+def test_keys_that_no_token_sees(kp, size, d):
+    b, hq, hkv, n_q, n_k, window, sinks = size
+    gen = torch.Generator(device="cuda").manual_seed(19)
+    dtype = torch.bfloat16
+    q, k, v, d_o = (heads(gen, b, h, n, d, dtype) for h, n in ((hq, n_q), (hkv, n_k), (hkv, n_k), (hq, n_q)))
+    o, lse = attend(kp, q, k, v, window, sinks, 0.1)
+    _, dk, dv = grads(kp, q, k, v, o, lse, d_o, window, sinks, 0.1)
+    unseen = slice(sinks, n_k - n_q - window + 1)
+    assert not dk[:, :, unseen].any() and not dv[:, :, unseen].any()
+    for name, got, (want, bound) in zip(("dk", "dv"), (dk, dv), gradients(q, k, v, d_o, window, sinks, 0.1, dtype)[1:]):
+        assert_within(got, want, bound, name)
+
+
 def test_windows_that_hide_nothing(kp):
     """A window as long as the keys, or of the largest number there is, is none; so are as many sinks."""
     gen = torch.Generator(device="cuda").manual_seed(15)
