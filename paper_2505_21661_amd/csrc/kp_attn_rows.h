@@ -20,7 +20,13 @@ namespace attn {
 
 constexpr int kThreads = 256;
 constexpr int kTileRows = 128, kTileKeys = 64;
-constexpr float kSlack = 8.0f;  // log2 of how far a score may exceed the softmax's reference before that moves
+// The reference that a row's exponentials are taken against only has to keep them in range: it moves when some score exceeds
+// it by more than 2^kSlack, to 2^kBelow under that score.  fp16 holds little below 2^-14: its reference stands so far below
+// that the largest weight P lies between 2^11 and 2^15, and a weight 2^-25 of the largest still has ten bits (a first key that
+// takes most of the weight, with a small value, over a long even tail: 32768 keys of 2^-25.3 are 7 % off without).  bf16 has the
+// exponents of fp32 and needs none of it.
+template <class T> constexpr float kBelow = std::is_same<T, Fp16>::value ? 11.f : 0.f;
+template <class T> constexpr float kSlack = std::is_same<T, Fp16>::value ? 15.f : 8.f;
 
 template <int D>
 constexpr uint32_t tile_lds_bytes() { return 3u * kTileKeys * 2u * D; }
@@ -374,11 +380,10 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
 #pragma unroll
       for (int v = 0; v < 16; v += 2) mx = fmaxf(fmaxf(mx, sacc[1][v]), sacc[1][v + 1]);
       mx = either_half_max(mx);
-      // The reference of the exponentials only has to keep them in range: it moves (and O and l are rescaled) when some
-      // row of the wave exceeds it by more than 2^kSlack.
+      // O and l are rescaled when some row's reference has to move
       const float mx_s = mx * g.scale_log2;
-      if (__builtin_amdgcn_ballot_w64(mx_s > m_run + kSlack) != 0ull) {
-        const float m_new = fmaxf(m_run, mx_s);
+      if (__builtin_amdgcn_ballot_w64(mx_s > m_run + kSlack<T>) != 0ull) {
+        const float m_new = fmaxf(m_run, mx_s - kBelow<T>);
         const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
         l_run *= alpha;
 #pragma unroll

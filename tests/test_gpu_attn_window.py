@@ -96,6 +96,29 @@ def test_peaked_scores(kp):
             assert bool(((lse.double() - want_lse).abs() <= 2.0 ** -18 * float(s)).all())
 
 
+# units (sequences x heads) so many that the keys are not split, or one
+@pytest.mark.parametrize("units", [(1, 1), (34, 64), (6, 64)], ids=["split", "few rows whole", "tiles whole"])
+@pytest.mark.parametrize("first", [0.01, 0.0])
+@pytest.mark.parametrize("n_k, below", [(4096, 24.2), (32768, 25.3)])
+def test_a_long_tail_of_small_weights_in_fp16(kp, units, first, n_k, below):
+    """One key takes most of the weight, with a small value, and many keys far below it make up the result.  Weights are held
+    to 2^-25 where the row's largest is 2^11 or more: each is off by 2^-36 of the largest, besides its relative rounding."""
+    gen = torch.Generator(device="cuda").manual_seed(20)
+    b, h = units
+    n_q, d = (40 if b == 6 else 1), 64
+    q, k = torch.zeros(1, 1, n_q, d, device="cuda"), torch.zeros(1, 1, n_k, d, device="cuda")
+    q[..., 0], k[:, :, 0, 0] = 4.0, below * math.log(2) / 4.0
+    v = 1 + torch.randn(1, 1, n_k, d, device="cuda", generator=gen).abs()
+    v[:, :, 0] = first
+    q, k, v = (x.half() for x in (q, k, v))
+    o, lse = attend(kp, *(x.expand(b, h, *x.shape[2:]) for x in (q, k, v)), 0, 0, 1.0, torch.empty(b, h, n_q, d, dtype=torch.float16, device="cuda"))
+    p, want, want_lse = forward(q, k, v, 0, 0, 1.0)
+    bound = o_bound(p, v, torch.float16) + 2.0 ** -36 * p.amax(-1, keepdim=True) * v.double().abs().sum(2, keepdim=True)
+    for i in (0, b - 1):
+        assert_within(o[i:i + 1, -1:], want, bound)
+        assert_lse(lse[i:i + 1, -1:], want_lse)
+
+
 def test_gradient_against_differences(kp):
     """The gradient along random directions against central differences of the definition in 64 bits."""
     gen = torch.Generator(device="cuda").manual_seed(7)
