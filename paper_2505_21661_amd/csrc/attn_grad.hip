@@ -65,14 +65,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
   if constexpr (kScaled) {
     most = either_half_max(most);
     row_scale = __builtin_ldexpf(1.0f, kShiftS) / power_of_two_in(most);
-    float all = mine ? most : 0.f;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) all = fmaxf(all, __shfl_xor(all, d, 64));
-    float* const most_of = reinterpret_cast<float*>(smem);
-    if (lane == 0) most_of[wave] = all;
-    __syncthreads();
-    if (threadIdx.x == 0) g.most[(size_t)unit * g.row_tiles + (g.row_tiles - 1u - item)] = fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3]));
-    __syncthreads();  // (the tiles go there)
+    if (mine && h32 == 0) g.most[row_no] = most;
   }
   const float neg_p = kScaled ? neg - kShiftP<T> : neg;
 
@@ -262,7 +255,7 @@ GradPlan plan_grad(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, in
   p.rows = (size_t)B * (size_t)Hq * (size_t)Sq;
   const auto up = [](size_t n) { return (n + 15) & ~(size_t)15; };
   p.most_at = up(8 * p.rows);
-  p.part_at = up(p.most_at + 4 * (size_t)(p.units * p.row_tiles));
+  p.part_at = up(p.most_at + 4 * p.rows);
   p.bytes = p.part_at + (size_t)p.workers * (2u * 2u * kGradKeys * 4u) * (size_t)D;
   return p;
 }
@@ -279,7 +272,7 @@ kp_status launch_grad(GradArgs& g, const GradPlan& p, hipStream_t st) {
   plan.whole = (uint32_t)p.whole; plan.rest = (uint32_t)(p.split / p.lines);
   plan.deal();
   if constexpr (D == 64) {
-    hipLaunchKernelGGL((kp_grad_keys<T, D>), dim3((uint32_t)p.workers), dim3(kThreads), 4u * kTile + 1024u, st, g, plan);
+    hipLaunchKernelGGL((kp_grad_keys<T, D>), dim3((uint32_t)p.workers), dim3(kThreads), 4u * kTile + 2u * kStatBytes, st, g, plan);
   } else {
     static thread_local int attr_dev = -1;  // the attribute is kept per device
     int dev = 0;

@@ -9,8 +9,8 @@ constexpr int kGradKeys = 128;   // keys of a workgroup of the dk, dv kernel
 
 // fp16 holds little below 2^-14, and P and dS are often smaller: they are rounded to it times a power of two that their
 // factors leave room for.  P <= 1 times 2^kShiftP; dS, of the order of |d_o|, times 2^kShiftS over the power of two of the
-// largest |d_o| of the row (dq) or of all rows of the key's heads (dk).  What overflows all the same is not finite and is
-// taken again in fp32.  bf16 has the exponents of fp32 and needs none of it.
+// largest |d_o| of the row (dq) or of the rows that it is summed with in one step (dk: RowsScale).  What overflows all the
+// same is not finite and is taken again in fp32.  bf16 has the exponents of fp32 and needs none of it.
 template <class T> constexpr float kShiftP = 0.f;
 template <> constexpr float kShiftP<Fp16> = 14.f;
 constexpr int kShiftS = 5;
@@ -19,7 +19,7 @@ struct GradArgs {
   Heads q, k, v, o, d_o, dq, dk, dv;
   const float* lse;
   float *neg, *delta;  // workspace, [B, Hq, Sq]: kShiftP - lse log2(e), and d_o . o
-  float* most;         // fp16: largest finite |d_o| of every row tile, [B, Hkv, row tiles]
+  float* most;         // workspace, fp16: largest finite |d_o| of every row, [B, Hq, Sq]
   float* part;         // partial dk, dv: [worker][first, last tile][dk, dv][kGradKeys][D]
   uint32_t seqs, hkv, group, n_q, n_k, window, sinks;
   uint32_t row_tiles;  // of one head of keys
@@ -92,6 +92,36 @@ __device__ __forceinline__ void key_row(const GradArgs& g, uint32_t seq, uint32_
     }
   }
 }
+
+__device__ __forceinline__ float power_of_two_in(float x) {  // the largest power of two <= x (1 for 0), as a number
+  const uint32_t e = __builtin_bit_cast(uint32_t, x) >> 23;
+  return x == 0.f ? 1.f : __builtin_bit_cast(float, (e < 1u ? 1u : e) << 23);
+}
+
+// fp16: what dS of the 64 tokens of a step is multiplied by before it is rounded (besides 2^kShiftP, which is in P).  Their
+// largest |d_o| sets it, so that a token decides about the precision of those that share a step with it and of nobody else:
+// with one scale for all rows of a head and one token 2^20 times the others, 31 % of dk's values are outside the bounds of its
+// other roundings (2 x 2100 x 64, the first token).  It moves, and dk with it, where that largest is twice as large or a
+// sixteenth, so seldom (no time is lost).  dS is off by at most 2^-26 of the largest |d_o| of its step, besides its relative
+// rounding.
+struct RowsScale {
+  uint32_t top = 127u << 23;  // bits of a power of two (scalar): |d_o| < 2 top
+  __device__ __forceinline__ float by() const { return __builtin_bit_cast(float, ((uint32_t)(254 + kShiftS - 14) << 23) - top); }
+  // most: of row `lane` of the step, 0 if none of the wave's keys sees it.  What dk has to be multiplied by.
+  __device__ __forceinline__ float moved(float most) {
+    const float least = __builtin_bit_cast(float, top - (4u << 23));
+    if (__builtin_amdgcn_ballot_w64(most >= __builtin_bit_cast(float, top + (1u << 23))) == 0ull &&
+        (__builtin_amdgcn_ballot_w64(most >= least) != 0ull || __builtin_amdgcn_ballot_w64(most != 0.f) == 0ull)) return 1.f;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+    const uint32_t before = top;
+    top = kp::wave_uniform(__builtin_bit_cast(uint32_t, power_of_two_in(most)));
+    return __builtin_bit_cast(float, (127u << 23) + before - top);
+  }
+};
+static_assert(kShiftP<Fp16> == 14.f, "RowsScale::by is 2^(kShiftS - kShiftP) / top");
+// Bytes of the statistics of a step's 64 rows in LDS: neg, delta, largest |d_o|.
+constexpr uint32_t kStatBytes = 1024u;
 
 // ---- tiles of 64 rows in LDS that are read both ways ---------------------------------------------------------------
 // A row's 16-byte chunk c lies at position c ^ swizzle(row).  Read as it lies (32 rows x 16 bytes to a half wave) the 16
@@ -244,10 +274,6 @@ __device__ __forceinline__ float odd_of(const f32x16 (&acc)[N]) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) odd = __builtin_fmaf(acc[n][v], 0.f, odd);
   return odd;
-}
-__device__ __forceinline__ float power_of_two_in(float x) {  // the largest power of two <= x (1 for 0), as a number
-  const uint32_t e = __builtin_bit_cast(uint32_t, x) >> 23;
-  return x == 0.f ? 1.f : __builtin_bit_cast(float, (e < 1u ? 1u : e) << 23);
 }
 
 }  // namespace attn

@@ -169,13 +169,12 @@ struct KeyWork {
   bool first;
 };
 
-// What dS of a head of keys is multiplied by before it is rounded to fp16, besides 2^kShiftP.
-__device__ __forceinline__ float ds_scale_of(const GradArgs& g, uint32_t unit) {
-  float most = 0.f;
-  for (uint32_t i = threadIdx.x & 63u; i < g.row_tiles; i += 64u) most = fmaxf(most, g.most[(size_t)unit * g.row_tiles + i]);
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
-  return __builtin_ldexpf(1.0f, kShiftS - (int)kShiftP<Fp16>) / power_of_two_in(most);
+// Largest |d_o| (at `most`) of row `lane` of the step that starts at `start`, 0 if it sees none of the keys k0 .. k1.
+__device__ __forceinline__ float most_of_row(const GradArgs& g, const Tokens& tok, uint32_t start, int32_t k0, int32_t k1, const float* most) {
+  const uint32_t token = start + (threadIdx.x & 63u);
+  const int32_t p = (int32_t)g.n_k - (int32_t)g.n_q + (int32_t)token;
+  const bool sees_some = (token < tok.to) & (p >= k0) & ((g.window == 0u) | (k0 < (int32_t)g.sinks) | (p - k1 < (int32_t)g.window));
+  return sees_some ? most[threadIdx.x & 63u] : 0.f;
 }
 
 // The keys of a wave's 32 (from j0 on) whose sums are not finite, taken again over the same steps, in fp32.
@@ -217,7 +216,7 @@ __device__ __forceinline__ void keys_again(const GradArgs& g, const KeyWork& wor
 // 32/8 x 8192 x 128, window 1024: 360 us, 715 TFLOP/s of four products, the matrix pipes busy 47 % of the time at 1.6 GHz, the
 // lowest clock of these kernels: it is bound by power as much as by the vector and scalar instructions between its MFMAs.
 constexpr int kPairThreads = 512;
-template <int D> constexpr uint32_t pairs_lds_bytes() { return 3u * (4u * 64u * D + 512u) + 24u * 2048u; }
+template <int D> constexpr uint32_t pairs_lds_bytes() { return 3u * (4u * 64u * D + kStatBytes) + 24u * 2048u; }
 template <class T, int D>
 __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g, KeyPlan plan) {
   constexpr uint32_t kRow = 2u * D, kTile = 64u * kRow, kBuffer = 2u * kTile;
@@ -225,7 +224,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
   constexpr int LA = 4;                    // operands come out of LDS this many MFMAs ahead
   constexpr bool kScaled = std::is_same<T, Fp16>::value;
   extern __shared__ __align__(16) unsigned char smem[];
-  // [three buffers of Q tile, dO tile][P of every wave: 2 KiB][dS, twice][three times neg, delta of 64 rows]
+  // [three buffers of Q tile, dO tile][P of every wave: 2 KiB][dS, twice][three times neg, delta, largest |d_o| of 64 rows]
   constexpr uint32_t kShared = 3u * kBuffer, kSharedDs = kShared + 8u * 2048u, kStats = kSharedDs + 16u * 2048u;
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = kp::wave_uniform(tid >> 6), h32 = lane >> 5, l32 = lane & 31u;
   const uint32_t group_no = wave & 3u, hf = wave >> 2;  // of 32 keys; the wave's half of the rows and of d
@@ -259,7 +258,8 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
         vf[s] = *reinterpret_cast<const u32x4*>(v + 16 * s + 8 * h32);
       }
     }
-    const float ds_scale = kScaled ? ds_scale_of(g, unit) : 1.f;  // dS is rounded times this (and 2^kShiftP, which is in P)
+    RowsScale scale;     // fp16: of dS that is formed
+    float dk_by = 1.f;   // what takes dk to that scale
 
     // ---- requests: the next step's head, first token, place ---------------------------------------------------------
     uint32_t loaded_last = ~0u, into = 0u;  // `into`: buffer that it goes to
@@ -274,7 +274,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
       const uint32_t head = hk * g.group + ask_group;
       ask_q = row_at(g.q, seq, head, ask_start);
       ask_do = row_at(g.d_o, seq, head, ask_start);
-      ask_stat = (wave == 0u ? g.neg : g.delta) + ((size_t)seq * g.hkv * g.group + head) * g.n_q + ask_start;
+      ask_stat = (wave == 0u ? g.neg : wave == 1u ? g.delta : g.most) + ((size_t)seq * g.hkv * g.group + head) * g.n_q + ask_start;
     };
     ask_at();
     constexpr int NL = TileLoader<D, 8>::NL, kAsks = 2 * NL + 2;
@@ -290,8 +290,8 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
       } else if (part < 2 * NL) {
         ld.load_one(part - NL, ask_do, lds0 + into * kBuffer + kTile);
       } else if (part == 2 * NL) {
-        if (wave < 2u) {  // the rows' neg (wave 0) and delta (wave 1): 4 bytes to a lane
-          const uint32_t ofs = 4u * (lane < loaded_last ? lane : loaded_last), dst = kp::wave_uniform((uint32_t)(uintptr_t)smem + kStats + into * 512u + 256u * wave);
+        if (wave < (kScaled ? 3u : 2u)) {  // the rows' neg (wave 0), delta (wave 1), largest |d_o| (wave 2): 4 bytes to a lane
+          const uint32_t ofs = 4u * (lane < loaded_last ? lane : loaded_last), dst = kp::wave_uniform((uint32_t)(uintptr_t)smem + kStats + into * kStatBytes + 256u * wave);
           uint32_t saved_m0;
           asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0"
                        : "=&s"(saved_m0) : "v"(ofs), "s"(ask_stat), "s"(dst) : "memory");
@@ -323,6 +323,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
     u32x4 ra[LA];
     f32x16 sacc, dp;
     float w[16], neg, delta;  // of the wave's 32 rows of the next step, row l32
+    float most = 0.f;         // fp16: of all its 64, row `lane`
     u32x2 pw[4], ds[4];  // P and dS: keys 8 i + 4 h32 .. + 3 of row l32
     uint32_t ds_now = 0u;  // which of the two dS in LDS is this step's
     uint32_t now = 0u, next = 0u;  // buffers of the step at hand and of the one whose S and dP are formed
@@ -382,9 +383,10 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
       }
     };
     auto load_stats = [&]() __attribute__((always_inline)) {
-      const float* const st = reinterpret_cast<const float*>(smem + kStats + next * 512u + 128u * hf) + l32;
+      const float* const st = reinterpret_cast<const float*>(smem + kStats + next * kStatBytes + 128u * hf) + l32;
       neg = st[0];
       delta = st[64];
+      if constexpr (kScaled) most = most_of_row(g, tok, start, (int32_t)j0, (int32_t)j0 + 31, reinterpret_cast<const float*>(smem + kStats + next * kStatBytes + 512u));
     };
     auto exponential = [&](int v) __attribute__((always_inline)) {
       w[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[v], g.scale_log2, neg));
@@ -392,7 +394,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
     };
     auto finish = [&](int v) __attribute__((always_inline)) {  // elements v, v + 1
       float x0 = w[v] * (dp[v] - delta), x1 = w[v + 1] * (dp[v + 1] - delta);
-      if constexpr (kScaled) { x0 *= ds_scale; x1 *= ds_scale; }
+      if constexpr (kScaled) { x0 *= scale.by(); x1 *= scale.by(); }
       pw[v >> 2][(v >> 1) & 1] = T::pack(w[v], w[v + 1]);
       ds[v >> 2][(v >> 1) & 1] = T::pack(x0, x1);
     };
@@ -427,6 +429,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
     }
     hide();
     load_stats();
+    if constexpr (kScaled) scale.moved(most);  // (dk is 0)
 #pragma unroll
     for (int v = 0; v < 16; ++v) exponential(v);
 #pragma unroll
@@ -458,6 +461,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
         __builtin_amdgcn_sched_barrier(0);
       }
       hide();
+      if constexpr (kScaled) dk_by = scale.moved(most);
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
         dp = T::mfma32(vf[n], ra[n % LA], dp);
@@ -496,11 +500,19 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
         __builtin_amdgcn_sched_barrier(0);
       }
       ds_now ^= 1u;
+      if constexpr (kScaled) {
+        if (dk_by != 1.f) {
+#pragma unroll
+          for (int dt = 0; dt < NH; ++dt)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) dk[dt][v] *= dk_by;
+        }
+      }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (what was asked for past the end has landed too)
     }
 
-    const float by_k = kScaled ? g.scale / (ds_scale * __builtin_ldexpf(1.0f, (int)kShiftP<T>)) : g.scale;
+    const float by_k = kScaled ? g.scale / (scale.by() * __builtin_ldexpf(1.0f, (int)kShiftP<T>)) : g.scale;
     const float by_v = kScaled ? __builtin_ldexpf(1.0f, -(int)kShiftP<T>) : 1.f;
     uint64_t again = __builtin_amdgcn_ballot_w64((odd_of<NH>(dk) != 0.f || odd_of<NH>(dv) != 0.f) && j <= j_last);
     again = (again | again >> 32) & 0xFFFFFFFFull;
@@ -555,7 +567,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan 
   constexpr uint32_t kTile = 64u * 2u * D, kBuffer = 2u * kTile;
   constexpr int NS = D / 16, ND = D / 32;
   constexpr bool kScaled = std::is_same<T, Fp16>::value;
-  extern __shared__ __align__(16) unsigned char smem[];  // two buffers of [Q tile][dO tile], then two of [neg][delta] of 64 rows
+  extern __shared__ __align__(16) unsigned char smem[];  // two buffers of [Q tile][dO tile], then two of [neg][delta][largest |d_o|] of 64 rows
   constexpr uint32_t kStats = 2u * kBuffer;
   const uint32_t lane = threadIdx.x & 63u, wave = kp::wave_uniform(threadIdx.x >> 6), h32 = lane >> 5, l32 = lane & 31u;
   const int32_t off = (int32_t)g.n_k - (int32_t)g.n_q;
@@ -578,7 +590,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan 
         vf[s] = *reinterpret_cast<const u32x4*>(v + 16 * s + 8 * h32);
       }
     }
-    const float ds_scale = kScaled ? ds_scale_of(g, unit) : 1.f;  // dS is rounded times this (and 2^kShiftP, which is in P)
+    RowsScale scale;  // fp16: of dS and dk
     uint32_t loaded_last = ~0u, into = 0u;  // `into`: buffer that the next step goes to
     if (rd.by != kBuffer) rd.to_other();    // (an odd number of steps before: back to the first)
     const uint32_t head_steps = steps_per_head == 0u ? 1u : steps_per_head;
@@ -589,9 +601,9 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan 
       if (last != loaded_last) { loaded_last = last; lq.upto(last); ld.upto(last); }
       lq.load(row_at(g.q, seq, head, ask_start), lds0 + into);
       ld.load(row_at(g.d_o, seq, head, ask_start), lds0 + into + kTile);
-      if (wave < 2u) {  // the rows' neg (wave 0) and delta (wave 1): 4 bytes to a lane
-        const float* from = (wave == 0u ? g.neg : g.delta) + ((size_t)seq * g.hkv * g.group + head) * g.n_q + ask_start;
-        const uint32_t ofs = 4u * (lane < last ? lane : last), dst = kp::wave_uniform((uint32_t)(uintptr_t)smem + kStats + (into != 0u ? 512u : 0u) + 256u * wave);
+      if (wave < (kScaled ? 3u : 2u)) {  // the rows' neg (wave 0), delta (wave 1), largest |d_o| (wave 2): 4 bytes to a lane
+        const float* from = (wave == 0u ? g.neg : wave == 1u ? g.delta : g.most) + ((size_t)seq * g.hkv * g.group + head) * g.n_q + ask_start;
+        const uint32_t ofs = 4u * (lane < last ? lane : last), dst = kp::wave_uniform((uint32_t)(uintptr_t)smem + kStats + (into != 0u ? kStatBytes : 0u) + 256u * wave);
         uint32_t saved_m0;
         asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0"
                      : "=&s"(saved_m0) : "v"(ofs), "s"(from), "s"(dst) : "memory");
@@ -613,7 +625,18 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan 
 #pragma unroll
       for (int s = 0; s < NS; ++s) ra[s] = rd.rows(s, 0u);
       for (uint32_t step = s_begin; step < s_end; ++step) {
+        float most = 0.f;
+        if constexpr (kScaled) most = most_of_row(g, tok, start, (int32_t)j0, (int32_t)j0 + 31, reinterpret_cast<const float*>(smem + stats + 512u));
         if (step + 1u < s_end) request();
+        if constexpr (kScaled) {
+          const float by = scale.moved(most);
+          if (by != 1.f) {
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+              for (int v = 0; v < 16; ++v) dk[dt][v] *= by;
+          }
+        }
         auto next_buffer = [&]() __attribute__((always_inline)) {
           // every wave has read these tiles, and the next ones have landed
           asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -671,7 +694,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan 
             for (int e = 0; e < 2; ++e) {
               w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[v + e], g.scale_log2, neg[v >> 2][(v & 3) + e]));
               x[e] = w[e] * (dp[v + e] - delta[v >> 2][(v & 3) + e]);
-              if constexpr (kScaled) x[e] *= ds_scale;
+              if constexpr (kScaled) x[e] *= scale.by();
             }
             pw[v >> 3][(v >> 1) & 3] = T::pack(w[0], w[1]);
             ds[v >> 3][(v >> 1) & 3] = T::pack(x[0], x[1]);
@@ -690,13 +713,13 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan 
             __builtin_amdgcn_sched_barrier(0);
           }
         }
-        stats ^= 512u;
+        stats ^= kStatBytes;
         start += 64u;
         if (start >= tok.to) start = tok.from;
       }
     }
 
-    const float by_k = kScaled ? g.scale / (ds_scale * __builtin_ldexpf(1.0f, (int)kShiftP<T>)) : g.scale;
+    const float by_k = kScaled ? g.scale / (scale.by() * __builtin_ldexpf(1.0f, (int)kShiftP<T>)) : g.scale;
     const float by_v = kScaled ? __builtin_ldexpf(1.0f, -(int)kShiftP<T>) : 1.f;
     const bool mine = j <= j_last;
     uint64_t again = __builtin_amdgcn_ballot_w64(mine && (odd_of<ND>(dk) != 0.f || odd_of<ND>(dv) != 0.f));

@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from tests.attn_util import assert_lse, assert_within, forward, gradients, o_bound
+from tests.attn_util import assert_lse, assert_within, forward, gradients, o_bound, visible
 
 pytestmark = pytest.mark.gpu
 TYPES = [torch.bfloat16, torch.float16]
@@ -94,6 +94,26 @@ def test_peaked_scores(kp):
             bound = o_bound(p, v, torch.bfloat16) + 2 * float(s) * 2.0 ** -20 * torch.matmul(p, v.double().abs())
             assert_within(o, want, bound)
             assert bool(((lse.double() - want_lse).abs() <= 2.0 ** -18 * float(s)).all())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n, window, at, ratio", [(4096, 2048, 4000, 16), (4096, 2048, 4000, 20), (2100, 0, 0, 14), (2100, 0, 0, 20), (1500, 300, 700, 20), (300, 0, 299, 18)])
+def test_gradients_of_one_token_much_larger_than_the_others(kp, n, window, at, ratio, d):
+    """In fp16, a token's dS is held to 2^-26 of the largest |d_o| of the 64 tokens of its step (at most 63 tokens away), and to
+    its own relative rounding: keys that other tokens see lose nothing."""
+    gen = torch.Generator(device="cuda").manual_seed(21)
+    dtype, scale = torch.float16, 1 / math.sqrt(d)
+    q, k, v, d_o = (heads(gen, 1, h, n, d, dtype) for h in (2, 1, 1, 2))
+    d_o = d_o.float() * 2.0 ** -8
+    d_o[:, :, at] *= 2.0 ** ratio
+    d_o = d_o.half()
+    o, lse = attend(kp, q, k, v, window, 3, scale)
+    near = torch.nn.functional.max_pool1d(d_o.float().abs().amax(-1), 127, 1, 63).double()  # [1, 2, n]
+    see = visible(n, n, window, 3, "cuda").double()
+    step = 2.0 ** -26 * scale * torch.matmul(see.t(), near[..., None] * q.double().abs()).sum(1, keepdim=True)
+    got = grads(kp, q, k, v, o, lse, d_o, window, 3, scale)
+    for name, x, (want, bound) in zip(("dq", "dk", "dv"), got, gradients(q, k, v, d_o, window, 3, scale, dtype)):
+        assert_within(x, want, bound + step if name == "dk" else bound, name)
 
 
 # units (sequences x heads) so many that the keys are not split, or one
