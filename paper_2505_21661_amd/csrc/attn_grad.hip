@@ -203,9 +203,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_query(GradArgs g) {
     for (; again != 0ull; again &= again - 1ull) {
       const int r = __builtin_ctzll(again);
       const RowPlace a = place_of(wave_first + (uint32_t)r, g.group);
-      float out[D / 64];
-      query_row<T, D>(g, seq, hk * g.group + a.in_group, a.token, __shfl(neg, r, 64), __shfl(delta, r, 64), out);
-      put_row<T, D / 64>(const_cast<uint16_t*>(row_at(g.dq, seq, hk * g.group + a.in_group, a.token)), out, g.scale);
+      query_row<T, D>(g, seq, hk * g.group + a.in_group, a.token, __shfl(neg, r, 64), __shfl(delta, r, 64), const_cast<uint16_t*>(row_at(g.dq, seq, hk * g.group + a.in_group, a.token)));
     }
   }
 }

@@ -260,80 +260,185 @@ struct Source {
   }
 };
 
-// Elements lane * E .. lane * E + E - 1 of a row of D = 64 E, in fp32.
-template <class T, int E>
-__device__ __forceinline__ void row_elements(const uint8_t* row, uint32_t lane, float (&out)[E]) {
-  if constexpr (E == 1) {
-    out[0] = T::to_float(reinterpret_cast<const uint16_t*>(row)[lane]);
-  } else {
-    const uint32_t w = reinterpret_cast<const uint32_t*>(row)[lane];
-    out[0] = T::to_float(w & 0xFFFFu);
-    out[1] = T::to_float(w >> 16);
-  }
-}
-template <int E>
-__device__ __forceinline__ void row_codes(const uint8_t* row, uint32_t lane, float scale, float (&out)[E]) {
-  uint32_t w = 0;
-  if constexpr (E == 1) w = row[lane]; else w = reinterpret_cast<const uint16_t*>(row)[lane];
-  out[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0) * scale;
-  if constexpr (E == 2) out[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1) * scale;
-}
+// ---- rows in fp32, one at a time by a whole wave ---------------------------------------------------------------------
+// A matrix instruction multiplies every value of a tile by some probability, 0 where the row does not see the key, and 0 times
+// an infinity or a NaN is a NaN; a row whose sums came out not finite is taken again in this way, where only what it sees is
+// touched.  64 of the rows that it meets at a time (Rows); what is a NaN for good is left.  It is the slow way, bound by
+// memory once the rows leave L2: 32/8 x 8192 x 128 without a window takes 0.5 ms forward, 33 with a NaN in one value that every
+// token sees; its gradient 2.2 ms, 110 with an infinity or a NaN in one token's d_o (3 with one in a key or a value).
+// (Pair by pair, with no end before the last, it was ten times that.)
 
 __device__ __forceinline__ float wave_sum(float x) {
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d, 64);
   return x;
 }
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
+  return x;
+}
 
-// The rows of the softmax, one at a time and in fp32 throughout: a lane owns E elements of D.  A matrix instruction
-// multiplies every value of a tile by some probability, 0 where the row does not see the key, and 0 times an infinity or
-// a NaN is a NaN; a row whose sums came out not finite is taken again here, where only what it sees is touched.
-template <int E>
-struct Row {
-  float m = kNoKey, l = 0.f, o[E] = {};
-};
-template <class T, int D, int SRC>
-__device__ __forceinline__ void row_over_keys(Row<D / 64>& r, const float (&q)[D / 64], const Source<D, SRC>& src, int32_t p,
-                                              uint32_t window, uint32_t sinks, float scale_log2, uint32_t from, uint32_t to) {
-  constexpr int E = D / 64;
-  const uint32_t lane = threadIdx.x & 63u;
-  if (p < 0) return;
-  if (to > (uint32_t)p + 1u) to = (uint32_t)p + 1u;
-  for (uint32_t j = from; j < to; ++j) {
-    if (window != 0u && (uint32_t)p - j >= window && j >= sinks) {
-      j = (uint32_t)p - window;  // (the next key is the window's first)
-      continue;
-    }
-    const uint32_t row = src.row_of(j);
-    if (SRC != kPlain && row == ~0u) continue;
-    float kk[E], vv[E], dot = 0.f;
-    if constexpr (SRC == kPagedE4m3) {
-      row_codes<E>(src.k_at(row), lane, power_of(src.k_exp[row]), kk);
-      row_codes<E>(src.v_at(row), lane, power_of(src.v_exp[row]), vv);
-    } else {
-      row_elements<T, E>(src.k_at(row), lane, kk);
-      row_elements<T, E>(src.v_at(row), lane, vv);
-    }
+// 64 rows of D in 16 bits or e4m3 codes.  kLanes lanes have 16 bytes each of a row, and a load brings kRows of them: whole lines
+// of memory.  What belongs to a row as a whole (its product with another, its weight) is in lane l for row number place(l).
+template <class T, int D, bool E4M3>
+struct Rows {
+  static constexpr uint32_t kLanes = (E4M3 ? D : 2 * D) / 16, kRows = 64u / kLanes;
+  static constexpr int kElements = E4M3 ? 16 : 8;  // of a row in a lane: those from kElements * (lane % kLanes) on
+  static __device__ __forceinline__ uint32_t place(uint32_t lane) { return lane % kLanes * kRows + lane / kLanes; }
+
+  static __device__ __forceinline__ void widen(const u32x4& raw, float (&x)[kElements]) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) dot = __builtin_fmaf(q[e], kk[e], dot);
-    const float s = wave_sum(dot) * scale_log2;
-    const float m = fmaxf(r.m, s), alpha = __builtin_amdgcn_exp2f(r.m - m), w = __builtin_amdgcn_exp2f(s - m);
-    r.m = m;
-    r.l = r.l * alpha + w;
-#pragma unroll
-    for (int e = 0; e < E; ++e) r.o[e] = __builtin_fmaf(w, vv[e], r.o[e] * alpha);
+    for (int w = 0; w < 4; ++w) {
+      if constexpr (E4M3) {
+        x[4 * w] = __builtin_amdgcn_cvt_f32_fp8((int)raw[w], 0);
+        x[4 * w + 1] = __builtin_amdgcn_cvt_f32_fp8((int)raw[w], 1);
+        x[4 * w + 2] = __builtin_amdgcn_cvt_f32_fp8((int)raw[w], 2);
+        x[4 * w + 3] = __builtin_amdgcn_cvt_f32_fp8((int)raw[w], 3);
+      } else {
+        x[2 * w] = T::to_float(raw[w] & 0xFFFFu);
+        x[2 * w + 1] = T::to_float(raw[w] >> 16);
+      }
+    }
   }
+  // A single row in 16 bits, laid out as the others.
+  static __device__ __forceinline__ void one(const uint16_t* row, float (&x)[kElements]) {
+    const uint16_t* const at = row + kElements * ((threadIdx.x & 63u) % kLanes);
+#pragma unroll
+    for (int n = 0; n < kElements; n += 8) {
+      const u32x4 raw = *reinterpret_cast<const u32x4*>(at + n);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        x[n + 2 * w] = T::to_float(raw[w] & 0xFFFFu);
+        x[n + 2 * w + 1] = T::to_float(raw[w] >> 16);
+      }
+    }
+  }
+  // Products of row x with the rows, of which number place(l) is at at(l), for any lane l.
+  template <class At>
+  static __device__ __forceinline__ float products(const float (&x)[kElements], At at) {
+    const uint32_t lane = threadIdx.x & 63u, c = lane % kLanes, group = lane / kLanes;
+    float mine = 0.f;
+#pragma unroll 4
+    for (uint32_t t = 0; t < kLanes; ++t) {
+      float y[kElements], s = 0.f;
+      widen(*reinterpret_cast<const u32x4*>(at(t + group * kLanes) + 16u * c), y);
+#pragma unroll
+      for (int e = 0; e < kElements; ++e) s = __builtin_fmaf(x[e], y[e], s);
+      s += moved<0xB1>(s);   // over kLanes lanes: from the next lane, the next two, the next four, the next eight
+      s += moved<0x4E>(s);
+      if constexpr (kLanes >= 8) s += moved<0x141>(s);
+      if constexpr (kLanes >= 16) s += moved<0x140>(s);
+      mine = c == t ? s : mine;
+    }
+    return mine;
+  }
+  // Adds the rows times `by`, those with `seen`; finish() adds up what the lanes have of an element.
+  template <class At>
+  static __device__ __forceinline__ void add(float (&sum)[kElements], float by, bool seen, At at) {
+    const uint32_t lane = threadIdx.x & 63u, c = lane % kLanes, group = lane / kLanes;
+    const float there = seen ? 1.f : 0.f;
+#pragma unroll 4
+    for (uint32_t t = 0; t < kLanes; ++t) {
+      const uint32_t from = t + group * kLanes;
+      u32x4 raw = *reinterpret_cast<const u32x4*>(at(from) + 16u * c);
+      const float counts = __shfl(there, (int)from, 64), weight_or_nan = __shfl(by, (int)from, 64), weight = counts != 0.f ? weight_or_nan : 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) raw[w] = counts != 0.f ? raw[w] : 0u;
+      float y[kElements];
+      widen(raw, y);
+#pragma unroll
+      for (int e = 0; e < kElements; ++e) sum[e] = __builtin_fmaf(weight, y[e], sum[e]);
+    }
+  }
+  static __device__ __forceinline__ void finish(float (&sum)[kElements]) {
+#pragma unroll
+    for (int e = 0; e < kElements; ++e)
+#pragma unroll
+      for (int d = (int)kLanes; d < 64; d <<= 1) sum[e] += __shfl_xor(sum[e], d, 64);
+  }
+  // A finished row, to where it belongs.
+  static __device__ __forceinline__ void put(const float (&x)[kElements], float by, uint16_t* row) {
+    const uint32_t lane = threadIdx.x & 63u;
+    if (lane >= kLanes) return;
+#pragma unroll
+    for (int n = 0; n < kElements; n += 8)
+      *reinterpret_cast<u32x4*>(row + kElements * lane + n) = u32x4{T::pack(x[n] * by, x[n + 1] * by), T::pack(x[n + 2] * by, x[n + 3] * by),
+                                                                    T::pack(x[n + 4] * by, x[n + 5] * by), T::pack(x[n + 6] * by, x[n + 7] * by)};
+  }
+  static __device__ __forceinline__ void put(const float (&x)[kElements], float by, float* row) {
+    const uint32_t lane = threadIdx.x & 63u;
+    if (lane >= kLanes) return;
+#pragma unroll
+    for (int n = 0; n < kElements; n += 4) *reinterpret_cast<f32x4*>(row + kElements * lane + n) = f32x4{x[n] * by, x[n + 1] * by, x[n + 2] * by, x[n + 3] * by};
+  }
+
+ private:
+  template <int CTRL>
+  static __device__ __forceinline__ float moved(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
+  }
+};
+
+// A NaN in every element of every lane?
+template <int K>
+__device__ __forceinline__ bool all_nan(const float (&x)[K]) {
+  bool nan = true;
+#pragma unroll
+  for (int e = 0; e < K; ++e) nan = nan & (x[e] != x[e]);
+  return __builtin_amdgcn_ballot_w64(nan) == ~0ull;
 }
 
-// A row's result, by a whole wave (lane: elements lane * E ..).
-template <class T, int E>
-__device__ __forceinline__ void store_row(const Row<E>& r, uint16_t* o, float* lse) {
-  const uint32_t lane = threadIdx.x & 63u;
-  const float inv = r.l == 0.f ? 0.f : 1.0f / r.l;
-  if constexpr (E == 1) o[lane] = (uint16_t)T::pack(r.o[0] * inv, 0.f);
-  else reinterpret_cast<uint32_t*>(o)[lane] = T::pack(r.o[0] * inv, r.o[1] * inv);
-  if (lse && lane == 0) *lse = r.l == 0.f ? -INFINITY : (r.m + __builtin_amdgcn_logf(r.l)) * kLn2;
-}
+// The softmax of one row.
+template <class T, int D, int SRC>
+struct Row {
+  using In = Rows<T, D, SRC == kPagedE4m3>;
+  float m = kNoKey, l = 0.f, o[In::kElements] = {};
+
+  // over the keys from .. to - 1 that the row sees, which stands at p
+  __device__ __forceinline__ void over_keys(const uint16_t* query, const Source<D, SRC>& src, int32_t p, uint32_t window, uint32_t sinks,
+                                            float scale_log2, uint32_t from, uint32_t to) {
+    if (p < 0) return;
+    if (to > (uint32_t)p + 1u) to = (uint32_t)p + 1u;
+    if (from >= to) return;
+    float q[In::kElements];
+    In::one(query, q);
+    for (uint32_t j0 = from; j0 < to; j0 += 64u) {
+      if (l != l) return;  // (a weight that is NaN: so is every value)
+      const uint32_t j = j0 + In::place(threadIdx.x & 63u);
+      bool seen = (j < to) & ((window == 0u) | ((uint32_t)p - j < window) | (j < sinks));
+      uint32_t row = ~0u;
+      if (seen) row = src.row_of(j);
+      if constexpr (SRC != kPlain) seen = seen & (row != ~0u);
+      const uint64_t all = __builtin_amdgcn_ballot_w64(seen);
+      if (all == 0ull) continue;
+      const uint32_t some = __builtin_amdgcn_readlane(row, __builtin_ctzll(all));
+      row = seen ? row : some;  // (a row that is seen)
+      float s = In::products(q, [&](uint32_t lane) __attribute__((always_inline)) { return src.k_at(__shfl(row, (int)lane, 64)); });
+      if constexpr (SRC == kPagedE4m3) s *= power_of(src.k_exp[row]);
+      s = seen ? s * scale_log2 : -INFINITY;
+      const float top = fmaxf(m, wave_max(s)), alpha = __builtin_amdgcn_exp2f(m - top);
+      float w = seen ? __builtin_amdgcn_exp2f(s - top) : 0.f;
+      m = top;
+      l = l * alpha + wave_sum(w);
+#pragma unroll
+      for (int e = 0; e < In::kElements; ++e) o[e] *= alpha;
+      if constexpr (SRC == kPagedE4m3) w *= power_of(src.v_exp[row]);
+      In::add(o, w, seen, [&](uint32_t lane) __attribute__((always_inline)) { return src.v_at(__shfl(row, (int)lane, 64)); });
+    }
+  }
+  __device__ __forceinline__ void store(uint16_t* to, float* lse) {
+    In::finish(o);
+    In::put(o, l == 0.f ? 0.f : 1.0f / l, to);
+    if (lse && (threadIdx.x & 63u) == 0u) *lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+  // a part of it, to be joined
+  __device__ __forceinline__ void store_part(float* values, float* max_and_sum) {
+    In::finish(o);
+    In::put(o, 1.f, values);
+    if ((threadIdx.x & 63u) == 0u) *reinterpret_cast<f32x2*>(max_and_sum) = f32x2{m, l};
+  }
+};
 
 }  // namespace attn
 }  // namespace kp

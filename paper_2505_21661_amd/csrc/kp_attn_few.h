@@ -331,22 +331,21 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_few(Args g) {
     const RowPlace a = place_of(tl.first + r, g.group);
     const uint32_t hd = h * g.group + a.in_group;
     const int64_t tok = (int64_t)tl.q0 + a.token;
-    float q[D / 64];
-    row_elements<T, D / 64>(reinterpret_cast<const uint8_t*>(g.q.at + g.q.seq * (int64_t)q_seq + g.q.head * (int64_t)hd + g.q.token * tok), lane, q);
-    Row<D / 64> rr;
-    for (uint32_t t = t_begin; t < t_end; ++t) {
+    const uint16_t* const q = g.q.at + g.q.seq * (int64_t)q_seq + g.q.head * (int64_t)hd + g.q.token * tok;
+    Row<T, D, SRC> rr;
+    for (int window = 0; window < 2; ++window) {  // the sinks of this split, then its other keys
+      const uint32_t from = window ? max(t_begin, sink_steps) : t_begin, to = window ? t_end : min(t_end, sink_steps);
+      if (from >= to) continue;
       uint32_t limit;
-      const uint32_t start = step_start(t, &limit), to = start + kFewKeys;
-      row_over_keys<T, D, SRC>(rr, q, src, p0 + (int32_t)a.token, g.window, g.sinks, g.scale_log2, start, to < limit ? to : limit);
+      const uint32_t start = step_start(from, &limit), end = start + (to - from) * kFewKeys;
+      rr.over_keys(q, src, p0 + (int32_t)a.token, g.window, g.sinks, g.scale_log2, start, end < limit ? end : limit);
     }
     if (g.splits > 1u) {
       const size_t to = split * part_rows + part_row<kFewRows>(g, tile_id, h, r);
-      if (lane == 0) *reinterpret_cast<f32x2*>(g.part + 2 * to) = f32x2{rr.m, rr.l};
-#pragma unroll
-      for (int e = 0; e < D / 64; ++e) g.part[2 * g.splits * part_rows + to * D + lane * (D / 64) + e] = rr.o[e];
+      rr.store_part(g.part + 2 * g.splits * part_rows + to * D, g.part + 2 * to);
     } else {
-      store_row<T, D / 64>(rr, const_cast<uint16_t*>(g.o.at) + g.o.seq * (int64_t)q_seq + g.o.head * (int64_t)hd + g.o.token * tok,
-                           g.lse ? g.lse + g.lse_seq * (int64_t)q_seq + g.lse_head * (int64_t)hd + tok : nullptr);
+      rr.store(const_cast<uint16_t*>(g.o.at) + g.o.seq * (int64_t)q_seq + g.o.head * (int64_t)hd + g.o.token * tok,
+               g.lse ? g.lse + g.lse_seq * (int64_t)q_seq + g.lse_head * (int64_t)hd + tok : nullptr);
     }
   }
   if constexpr (INSTR != 0) finish_ring<INSTR>(ring, g, recorded);

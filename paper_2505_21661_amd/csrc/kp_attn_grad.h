@@ -32,64 +32,60 @@ __device__ __forceinline__ const uint16_t* row_at(const Heads& t, uint32_t seq, 
 __device__ __forceinline__ bool sees(int32_t p, uint32_t j, uint32_t window, uint32_t sinks) {
   return ((int32_t)j <= p) & ((window == 0u) | ((uint32_t)p - j < window) | (j < sinks));
 }
-template <class T, int E>
-__device__ __forceinline__ void load_row(const uint16_t* at, float (&out)[E]) {
-  row_elements<T, E>(reinterpret_cast<const uint8_t*>(at), threadIdx.x & 63u, out);
-}
-template <int E>
-__device__ __forceinline__ float dot(const float (&a)[E], const float (&b)[E]) {
-  float s = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) s = __builtin_fmaf(a[e], b[e], s);
-  return wave_sum(s);
-}
-template <class T, int E>
-__device__ __forceinline__ void put_row(uint16_t* at, const float (&x)[E], float by) {
-  const uint32_t lane = threadIdx.x & 63u;
-  if constexpr (E == 1) at[lane] = (uint16_t)T::pack(x[0] * by, 0.f);
-  else reinterpret_cast<uint32_t*>(at)[lane] = T::pack(x[0] * by, x[1] * by);
-}
 
 // One query row's gradient in fp32, by a wave; only keys that the row sees are touched.  For rows whose sums on the matrix
-// instructions are not finite (as in kp_attn.h).
+// instructions are not finite (see Rows).
 template <class T, int D>
-__device__ __forceinline__ void query_row(const GradArgs& g, uint32_t seq, uint32_t head, uint32_t token, float neg, float delta, float (&dq)[D / 64]) {
-  constexpr int E = D / 64;
+__device__ __forceinline__ void query_row(const GradArgs& g, uint32_t seq, uint32_t head, uint32_t token, float neg, float delta, uint16_t* out) {
+  using R = Rows<T, D, false>;
   const uint32_t hk = head / g.group;
-  float q[E], d_o[E];
-  load_row<T, E>(row_at(g.q, seq, head, token), q);
-  load_row<T, E>(row_at(g.d_o, seq, head, token), d_o);
-#pragma unroll
-  for (int e = 0; e < E; ++e) dq[e] = 0.f;
   const int32_t p = (int32_t)g.n_k - (int32_t)g.n_q + (int32_t)token;
-  for (int32_t j = 0; j <= p; ++j) {
-    if (!sees(p, (uint32_t)j, g.window, g.sinks)) { j = p - (int32_t)g.window; continue; }
-    float k[E], v[E];
-    load_row<T, E>(row_at(g.k, seq, hk, (uint32_t)j), k);
-    load_row<T, E>(row_at(g.v, seq, hk, (uint32_t)j), v);
-    const float w = __builtin_amdgcn_exp2f(dot<E>(q, k) * g.scale_log2 + (neg - kShiftP<T>)), ds = w * (dot<E>(d_o, v) - delta);
-#pragma unroll
-    for (int e = 0; e < E; ++e) dq[e] = __builtin_fmaf(ds, k[e], dq[e]);
+  const Span span = span_of(p, p, g.window, g.sinks);
+  float q[R::kElements], d_o[R::kElements], dq[R::kElements] = {};
+  R::one(row_at(g.q, seq, head, token), q);
+  R::one(row_at(g.d_o, seq, head, token), d_o);
+  bool nan = false;
+  for (int window = 0; window < 2; ++window) {  // the sinks, then the other keys
+    const uint32_t to = window ? span.end : span.sink_end;
+    for (uint32_t j0 = window ? span.lo : 0u; j0 < to && !nan; j0 += 64u) {
+      const uint32_t n = to - j0;
+      const bool seen = R::place(threadIdx.x & 63u) < n;
+      const auto key = [&](uint32_t lane) __attribute__((always_inline)) { return j0 + (R::place(lane) < n ? R::place(lane) : n - 1u); };
+      const auto k = [&](uint32_t lane) __attribute__((always_inline)) { return reinterpret_cast<const uint8_t*>(row_at(g.k, seq, hk, key(lane))); };
+      const auto v = [&](uint32_t lane) __attribute__((always_inline)) { return reinterpret_cast<const uint8_t*>(row_at(g.v, seq, hk, key(lane))); };
+      const float w = __builtin_amdgcn_exp2f(R::products(q, k) * g.scale_log2 + (neg - kShiftP<T>)), ds = w * (R::products(d_o, v) - delta);
+      R::add(dq, ds, seen, k);
+      nan = __builtin_amdgcn_ballot_w64(seen && ds != ds) != 0ull || all_nan(dq);  // (so will be all of dq)
+    }
   }
+  R::finish(dq);
+  R::put(dq, g.scale, out);
 }
 
-// Adds one key's gradients from the query tokens from .. to - 1 of one head.
+// Adds one key's gradients from the query tokens from .. to - 1, at most 64, of one head, those wanted: of what is NaN for
+// good no more is.
 template <class T, int D>
 __device__ __forceinline__ void key_row(const GradArgs& g, uint32_t seq, uint32_t head, uint32_t j, uint32_t from, uint32_t to,
-                                        const float (&k)[D / 64], const float (&v)[D / 64], float (&dk)[D / 64], float (&dv)[D / 64]) {
-  constexpr int E = D / 64;
-  for (uint32_t i = from; i < to; ++i) {
-    if (!sees((int32_t)g.n_k - (int32_t)g.n_q + (int32_t)i, j, g.window, g.sinks)) continue;
-    float q[E], d_o[E];
-    load_row<T, E>(row_at(g.q, seq, head, i), q);
-    load_row<T, E>(row_at(g.d_o, seq, head, i), d_o);
-    const size_t at = ((size_t)seq * g.hkv * g.group + head) * g.n_q + i;
-    const float w = __builtin_amdgcn_exp2f(dot<E>(q, k) * g.scale_log2 + (g.neg[at] - kShiftP<T>)), ds = w * (dot<E>(d_o, v) - g.delta[at]);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      dk[e] = __builtin_fmaf(ds, q[e], dk[e]);
-      dv[e] = __builtin_fmaf(w, d_o[e], dv[e]);
-    }
+                                        const float (&k)[8], const float (&v)[8], bool* want_k, bool* want_v, float (&dk)[8], float (&dv)[8]) {
+  using R = Rows<T, D, false>;
+  uint32_t i = from + R::place(threadIdx.x & 63u);
+  const bool seen = i < to && sees((int32_t)g.n_k - (int32_t)g.n_q + (int32_t)i, j, g.window, g.sinks);
+  const uint64_t all = __builtin_amdgcn_ballot_w64(seen);
+  if (all == 0ull) return;
+  const uint32_t some = __builtin_amdgcn_readlane(i, __builtin_ctzll(all));
+  i = seen ? i : some;  // (a token that sees it)
+  const auto q = [&](uint32_t lane) __attribute__((always_inline)) { return reinterpret_cast<const uint8_t*>(row_at(g.q, seq, head, __shfl(i, (int)lane, 64))); };
+  const auto d_o = [&](uint32_t lane) __attribute__((always_inline)) { return reinterpret_cast<const uint8_t*>(row_at(g.d_o, seq, head, __shfl(i, (int)lane, 64))); };
+  const size_t stat = ((size_t)seq * g.hkv * g.group + head) * g.n_q + i;
+  const float w = __builtin_amdgcn_exp2f(R::products(k, q) * g.scale_log2 + (g.neg[stat] - kShiftP<T>));
+  if (*want_k) {
+    const float ds = w * (R::products(v, d_o) - g.delta[stat]);
+    R::add(dk, ds, seen, q);
+    *want_k = __builtin_amdgcn_ballot_w64(seen && ds != ds) == 0ull && !all_nan(dk);
+  }
+  if (*want_v) {
+    R::add(dv, w, seen, d_o);
+    *want_v = __builtin_amdgcn_ballot_w64(seen && w != w) == 0ull && !all_nan(dv);
   }
 }
 

@@ -517,24 +517,21 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
         const RowPlace a = place_of(wave_first + r, g.group);
         const uint32_t hd = h * g.group + a.in_group;
         const int64_t tok = (int64_t)tl.q0 + a.token;
-        float q[D / 64];
-        row_elements<T, D / 64>(reinterpret_cast<const uint8_t*>(g.q.at + g.q.seq * (int64_t)q_seq + g.q.head * (int64_t)hd + g.q.token * tok), lane, q);
-        Row<D / 64> row;
+        const uint16_t* const q = g.q.at + g.q.seq * (int64_t)q_seq + g.q.head * (int64_t)hd + g.q.token * tok;
+        Row<T, D, SRC> row;
         for (uint32_t t = t_begin; t < t_end; ++t) {
           uint32_t limit, unused;
           const int32_t at = (int32_t)tl.n_k - (int32_t)tl.n_q + (int32_t)a.token;
           const uint32_t start = kt.start_of(t, &limit, &unused), to = start + kTileKeys, mixed = kt.is_mixed(t) ? kt.mixed : 0u;
-          if (mixed != 0u) row_over_keys<T, D, SRC>(row, q, src, at, g.window, g.sinks, g.scale_log2, 0u, mixed);
-          row_over_keys<T, D, SRC>(row, q, src, at, g.window, g.sinks, g.scale_log2, start + mixed, to < limit ? to : limit);
+          if (mixed != 0u) row.over_keys(q, src, at, g.window, g.sinks, g.scale_log2, 0u, mixed);
+          row.over_keys(q, src, at, g.window, g.sinks, g.scale_log2, start + mixed, to < limit ? to : limit);
         }
         if (g.splits > 1u) {
           const size_t to = split * part_rows + part_row<kTileRows>(g, tile_id, h, 32u * wave + r);
-          if (lane == 0) *reinterpret_cast<f32x2*>(part_ml + 2 * to) = f32x2{row.m, row.l};
-#pragma unroll
-          for (int e = 0; e < D / 64; ++e) g.part[2 * g.splits * part_rows + to * D + lane * (D / 64) + e] = row.o[e];
+          row.store_part(g.part + 2 * g.splits * part_rows + to * D, part_ml + 2 * to);
         } else {
-          store_row<T, D / 64>(row, const_cast<uint16_t*>(g.o.at) + g.o.seq * (int64_t)q_seq + g.o.head * (int64_t)hd + g.o.token * tok,
-                               g.lse ? g.lse + g.lse_seq * (int64_t)q_seq + g.lse_head * (int64_t)hd + tok : nullptr);
+          row.store(const_cast<uint16_t*>(g.o.at) + g.o.seq * (int64_t)q_seq + g.o.head * (int64_t)hd + g.o.token * tok,
+                    g.lse ? g.lse + g.lse_seq * (int64_t)q_seq + g.lse_head * (int64_t)hd + tok : nullptr);
         }
       }
     }

@@ -177,31 +177,37 @@ __device__ __forceinline__ float most_of_row(const GradArgs& g, const Tokens& to
   return sees_some ? most[threadIdx.x & 63u] : 0.f;
 }
 
-// The keys of a wave's 32 (from j0 on) whose sums are not finite, taken again over the same steps, in fp32.
+// The keys of 32 (from j0 on) whose dk or dv are not finite, those taken again over the same steps, in fp32; `mine`: of which
+// keys this wave does so.
 template <class T, int D>
-__device__ __forceinline__ void keys_again(const GradArgs& g, const KeyWork& work, uint32_t seq, uint32_t hk, uint32_t j0, uint64_t again, float* part) {
-  constexpr int E = D / 64;
-  const uint32_t lane = threadIdx.x & 63u;
-  for (; again != 0ull; again &= again - 1ull) {
-    const uint32_t r = (uint32_t)__builtin_ctzll(again), key = j0 + r;
-    float k[E], v[E], out_k[E] = {}, out_v[E] = {};
-    load_row<T, E>(row_at(g.k, seq, hk, key), k);
-    load_row<T, E>(row_at(g.v, seq, hk, key), v);
-    for (uint32_t step = work.s_begin; step < work.s_end; ++step) {
+__device__ __forceinline__ void keys_again(const GradArgs& g, const KeyWork& work, uint32_t seq, uint32_t hk, uint32_t j0, uint32_t again_k, uint32_t again_v, uint32_t mine, float* part) {
+  using R = Rows<T, D, false>;
+  for (uint32_t again = (again_k | again_v) & mine; again != 0u; again &= again - 1u) {
+    const uint32_t r = (uint32_t)__builtin_ctz(again), key = j0 + r;
+    const bool need_k = ((again_k >> r) & 1u) != 0u, need_v = ((again_v >> r) & 1u) != 0u;
+    float k[8], v[8], dk[8] = {}, dv[8] = {};
+    R::one(row_at(g.k, seq, hk, key), k);
+    R::one(row_at(g.v, seq, hk, key), v);
+    bool want_k = need_k, want_v = need_v;
+    for (uint32_t step = work.s_begin; step < work.s_end && (want_k || want_v); ++step) {
       const uint32_t in_group = step / work.steps_per_head, first = work.tok.from + (step - in_group * work.steps_per_head) * 64u;
-      key_row<T, D>(g, seq, hk * g.group + in_group, key, first, first + 64u < work.tok.to ? first + 64u : work.tok.to, k, v, out_k, out_v);
+      key_row<T, D>(g, seq, hk * g.group + in_group, key, first, first + 64u < work.tok.to ? first + 64u : work.tok.to, k, v, &want_k, &want_v, dk, dv);
     }
+    R::finish(dk);
+    R::finish(dv);
     if (work.whole) {
-      put_row<T, E>(const_cast<uint16_t*>(row_at(g.dk, seq, hk, key)), out_k, g.scale);
-      put_row<T, E>(const_cast<uint16_t*>(row_at(g.dv, seq, hk, key)), out_v, 1.f);
+      if (need_k) R::put(dk, g.scale, const_cast<uint16_t*>(row_at(g.dk, seq, hk, key)));
+      if (need_v) R::put(dv, 1.f, const_cast<uint16_t*>(row_at(g.dv, seq, hk, key)));
     } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        part[r * D + lane * E + e] = out_k[e] * g.scale;
-        part[kGradKeys * D + r * D + lane * E + e] = out_v[e];
-      }
+      if (need_k) R::put(dk, g.scale, part + r * D);
+      if (need_v) R::put(dv, 1.f, part + kGradKeys * D + r * D);
     }
   }
+}
+// Keys (rows l32 of the wave) for which some lane's `odd` is not 0.
+__device__ __forceinline__ uint32_t odd_keys(float odd, bool mine) {
+  const uint64_t lanes = __builtin_amdgcn_ballot_w64(mine && odd != 0.f);
+  return (uint32_t)(lanes | lanes >> 32);
 }
 
 // dk and dv of 128 keys from a run of the query rows that see them.  A step is 64 tokens of one query head, whose Q and dO
@@ -514,10 +520,13 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
 
     const float by_k = kScaled ? g.scale / (scale.by() * __builtin_ldexpf(1.0f, (int)kShiftP<T>)) : g.scale;
     const float by_v = kScaled ? __builtin_ldexpf(1.0f, -(int)kShiftP<T>) : 1.f;
-    uint64_t again = __builtin_amdgcn_ballot_w64((odd_of<NH>(dk) != 0.f || odd_of<NH>(dv) != 0.f) && j <= j_last);
-    again = (again | again >> 32) & 0xFFFFFFFFull;
+    // what both waves of a group, each with half of d, have to take again, of which each takes every other key
+    uint32_t* const again = reinterpret_cast<uint32_t*>(smem + kStats + 768u);  // (behind a step's statistics)
+    const uint32_t odd_k = odd_keys(odd_of<NH>(dk), j <= j_last), odd_v = odd_keys(odd_of<NH>(dv), j <= j_last);
+    if (lane == 0u) { again[2u * wave] = odd_k; again[2u * wave + 1u] = odd_v; }
     float* const part = g.part + work.part_at(plan) * (2u * kGradKeys * D) + (size_t)(32u * group_no) * D;
     __syncthreads();  // (the tiles' room is used below)
+    const uint32_t again_k = kp::wave_uniform(odd_k | again[2u * (wave ^ 4u)]), again_v = kp::wave_uniform(odd_v | again[2u * (wave ^ 4u) + 1u]);
     if (!whole) {
       if (j <= j_last) {  // (3 x 64/8 x 5 x 128: 26 us for both kernels and the join, 37 with the rows that are no keys)
 #pragma unroll
@@ -553,7 +562,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the results have left, before some are put right
     __syncthreads();  // (and the next tile's rows go to the same room)
-    keys_again<T, D>(g, work, seq, hk, j0, again, part);
+    keys_again<T, D>(g, work, seq, hk, j0, again_k, again_v, hf == 0u ? 0x55555555u : 0xAAAAAAAAu, part);
   }
 }
 
@@ -722,8 +731,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan 
     const float by_k = kScaled ? g.scale / (scale.by() * __builtin_ldexpf(1.0f, (int)kShiftP<T>)) : g.scale;
     const float by_v = kScaled ? __builtin_ldexpf(1.0f, -(int)kShiftP<T>) : 1.f;
     const bool mine = j <= j_last;
-    uint64_t again = __builtin_amdgcn_ballot_w64(mine && (odd_of<ND>(dk) != 0.f || odd_of<ND>(dv) != 0.f));
-    again = (again | again >> 32) & 0xFFFFFFFFull;
+    const uint32_t again_k = odd_keys(odd_of<ND>(dk), mine), again_v = odd_keys(odd_of<ND>(dv), mine);
     const uint64_t rows_out = __builtin_amdgcn_ballot_w64(mine) & 0xFFFFFFFFull;
     float* const part = g.part + work.part_at(plan) * (2u * kGradKeys * D) + (size_t)(32u * wave) * D;
     __syncthreads();  // (the tiles' room is used below)
@@ -740,9 +748,9 @@ __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan 
       store_rows<T, D>(dk, by_k, smem + 64u * D * wave, const_cast<uint16_t*>(g.dk.at), g.dk.seq * (int64_t)seq + g.dk.head * (int64_t)hk + g.dk.token * (int64_t)j_in, rows_out);
       store_rows<T, D>(dv, by_v, smem + 64u * D * wave, const_cast<uint16_t*>(g.dv.at), g.dv.seq * (int64_t)seq + g.dv.head * (int64_t)hk + g.dv.token * (int64_t)j_in, rows_out);
     }
-    if (again != 0ull) {
+    if ((again_k | again_v) != 0u) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // their first results have left
-      keys_again<T, D>(g, work, seq, hk, j0, again, part);
+      keys_again<T, D>(g, work, seq, hk, j0, again_k, again_v, ~0u, part);
     }
     __syncthreads();  // (the next tile's rows go to the same room)
   }
