@@ -193,6 +193,75 @@ def test_what_is_not_seen_has_no_influence(kp, bad):
         assert torch.equal(got, ref)
 
 
+# (B, Hq, Hkv, Sq, Sk, window, sinks) and a key that some rows see and others do not: whole tiles; split keys with sinks in the
+# first tile; few rows, whole and split; key tiles that are split over workers, and whole ones in several rounds
+HIDDEN = [((1, 4, 2, 200, 200, 40, 2), 70), ((1, 2, 1, 200, 4000, 1700, 5), 2120), ((1, 2, 1, 200, 4000, 1700, 70), 66),
+          ((2, 8, 2, 3, 700, 90, 4), 609), ((2, 8, 2, 3, 9000, 4000, 4), 4998), ((1, 6, 2, 700, 700, 250, 5), 333), ((8, 4, 4, 1100, 1100, 100, 0), 600)]
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size, at", HIDDEN)
+def test_values_that_are_not_finite_and_who_sees_them(kp, size, at, d, dtype, bad):
+    """As above at other sizes: rows and keys that share tiles with a value that is not finite, and do not see it, keep their
+    results; those that see it get what the definition gives."""
+    b, hq, hkv, n_q, n_k, window, sinks = size
+    group, scale, i = hq // hkv, 0.1, n_q // 2
+    gen = torch.Generator(device="cuda").manual_seed(22)
+    q, k, v, d_o = (heads(gen, b, h, n, d, dtype, "bshd") for h, n in ((hq, n_q), (hkv, n_k), (hkv, n_k), (hq, n_q)))
+    see = visible(n_q, n_k, window, sinks, "cuda")
+    hit = see[:, at]
+    clean = attend(kp, q, k, v, window, sinks, scale)
+    p, want, want_lse = forward(q, k, v, window, sinks, scale)
+    bounds = gradients(q, k, v, d_o, window, sinks, scale, dtype)
+    bound = o_bound(p, v, dtype)
+    k2, v2, d_o2 = k.clone(), v.clone(), d_o.clone()
+    k2[0, 0, at, 3], v2[0, 0, at, 5], d_o2[0, 0, i, 7] = bad, bad, bad
+
+    # a value: element 5 of the rows that see it
+    o, lse = attend(kp, q, k, v2, window, sinks, scale)
+    want2 = want.clone()
+    want2[0, :group, :, 5][:, hit] = bad
+    assert_within(o, want2, torch.where(torch.isfinite(want2), bound, math.inf), "o")
+    assert bool((o[0, :group, :, 5].float()[:, hit].isinf() == (bad == math.inf)).all())
+    assert_lse(lse, want_lse)
+    dq, dk, dv = grads(kp, q, k, v2, o, lse, d_o, window, sinks, scale)
+    far = torch.ones(b, hq, n_q, dtype=torch.bool, device="cuda")
+    far[0, :group] = ~hit
+    assert_within(dq[far], bounds[0][0][far], bounds[0][1][far], "dq")
+    assert not torch.isfinite(dq[~far]).any()
+    keys = torch.zeros(b, hkv, n_k, dtype=torch.bool, device="cuda")
+    keys[0, 0] = see[hit].any(0)
+    assert_within(dk[~keys], bounds[1][0][~keys], bounds[1][1][~keys], "dk")
+    assert not torch.isfinite(dk[keys]).any()
+    assert_within(dv, bounds[2][0], bounds[2][1], "dv")
+
+    # a key: all of a row that sees it, unless its score is -inf
+    o, lse = attend(kp, q, k2, v, window, sinks, scale)
+    p2, want2, want_lse2 = forward(q, k2, v, window, sinks, scale)
+    assert_within(o, want2, o_bound(torch.nan_to_num(p2), v, dtype), "o")
+    sure = ~torch.isnan(want_lse2) & (want_lse2 != math.inf)
+    assert_lse(lse[sure], want_lse2[sure])
+    dq, dk, dv = grads(kp, q, k2, v, o, lse, d_o, window, sinks, scale)
+    assert_within(dq[far], bounds[0][0][far], bounds[0][1][far], "dq")
+    for name, x, (w, off) in zip(("dk", "dv"), (dk, dv), bounds[1:]):
+        assert_within(x[~keys], w[~keys], off[~keys], name)
+
+    # a gradient: the row's dq, dk of the keys that it sees, element 7 of their dv
+    dq, dk, dv = grads(kp, q, k, v, *clean, d_o2, window, sinks, scale)
+    others = torch.ones(b, hq, n_q, dtype=torch.bool, device="cuda")
+    others[0, 0, i] = False
+    assert_within(dq[others], bounds[0][0][others], bounds[0][1][others], "dq")
+    keys = torch.zeros(b, hkv, n_k, dtype=torch.bool, device="cuda")
+    keys[0, 0] = see[i]
+    assert_within(dk[~keys], bounds[1][0][~keys], bounds[1][1][~keys], "dk")
+    assert not torch.isfinite(dq[~others]).any() and not torch.isfinite(dk[keys]).any()
+    want2 = bounds[2][0].clone()
+    want2[0, 0, :, 7][see[i]] = bad
+    assert_within(dv, want2, torch.where(torch.isfinite(want2), bounds[2][1], math.inf), "dv")
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_a_value_that_is_not_finite_does_not_stall_a_call(kp, d):
     """One NaN or infinity that every token of a head meets, in turn in a key, a value and a gradient: a call takes some
@@ -220,6 +289,21 @@ def test_a_value_that_is_not_finite_does_not_stall_a_call(kp, d):
         for args in ((k2, v, d_o), (k, v2, d_o), (k, v, d_o2), (k, v, d_o3)):
             forward_ms, grad_ms = both(*args)
             assert forward_ms < 15 and grad_ms < 22, (forward_ms, grad_ms)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_q, n_k, window", [(300, 300, 0), (1100, 1100, 100), (40, 900, 300)])
+def test_what_fp16_does_not_hold_on_the_way(kp, n_q, n_k, window, d):
+    """Large values make dS leave fp16's range where the gradients themselves do not."""
+    gen = torch.Generator(device="cuda").manual_seed(23)
+    dtype, scale = torch.float16, 1 / math.sqrt(d)
+    q, k, v, d_o = (heads(gen, 1, h, n, d, dtype) for h, n in ((4, n_q), (2, n_k), (2, n_k), (4, n_q)))
+    v = (v.float() * 500).half()
+    o, lse = attend(kp, q, k, v, window, 0, scale)
+    ds = gradients(q, k, v, d_o, window, 0, scale, dtype)
+    for name, x, (want, bound) in zip(("dq", "dk", "dv"), grads(kp, q, k, v, o, lse, d_o, window, 0, scale), ds):
+        assert torch.isfinite(want.half()).all() and torch.isfinite(x).all()
+        assert_within(x, want, bound, name)
 
 
 def test_strides(kp):
