@@ -21,9 +21,9 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// The reference that the exponentials of a row are taken against before it has seen a key: low enough that the
-// first key moves it, finite so that a masked score (-inf) against it is exp2(-inf) = 0 and never inf - inf.
-constexpr float kNoKey = -1e30f;
+// The reference that the exponentials of a row are taken against before it has seen a key: the lowest finite number, which any
+// finite score moves, and finite so that a masked score (-inf) against it is exp2(-inf) = 0 and never inf - inf.
+constexpr float kNoKey = -3.4028234663852886e38f;
 
 struct Bf16 {
   typedef __bf16 x2 __attribute__((ext_vector_type(2)));

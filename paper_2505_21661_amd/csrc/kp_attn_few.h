@@ -238,7 +238,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_few(Args g) {
       const float mx_s = mx * g.scale_log2;
       if (__builtin_amdgcn_ballot_w64(mx_s > m_run + kSlack<T>) != 0ull) {
         const float m_new = fmaxf(m_run, mx_s - kBelow<T>), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-        l_run *= alpha;
+        l_run = sum_unless_far(l_run * alpha, m_new, mx_s);
 #pragma unroll
         for (int dt = 0; dt < NT; ++dt)
 #pragma unroll

@@ -27,6 +27,13 @@ constexpr int kTileRows = 128, kTileKeys = 64;
 // exponents of fp32 and needs none of it.
 template <class T> constexpr float kBelow = std::is_same<T, Fp16>::value ? 11.f : 0.f;
 template <class T> constexpr float kSlack = std::is_same<T, Fp16>::value ? 15.f : 8.f;
+// A weight is exp2 of score times scale less the reference, in one rounding, and the reference, a rounded score, may be off by
+// half a step of its own: at 2^24 by 1, at 2^33 by 512, which leaves no weight at all.  The sum of a row's weights is made a
+// NaN where the reference goes that far, so that the row is taken again with scores and reference rounded alike.
+constexpr float kFar = 16777216.f;
+__device__ __forceinline__ float sum_unless_far(float l, float reference, float score) {
+  return (__builtin_fabsf(reference) > kFar) & (score > -INFINITY) ? __builtin_nanf("") : l;
+}
 
 template <int D>
 constexpr uint32_t tile_lds_bytes() { return 3u * kTileKeys * 2u * D; }
@@ -385,7 +392,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
       if (__builtin_amdgcn_ballot_w64(mx_s > m_run + kSlack<T>) != 0ull) {
         const float m_new = fmaxf(m_run, mx_s - kBelow<T>);
         const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-        l_run *= alpha;
+        l_run = sum_unless_far(l_run * alpha, m_new, mx_s);
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt)
 #pragma unroll

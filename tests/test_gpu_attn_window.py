@@ -139,6 +139,27 @@ def test_a_long_tail_of_small_weights_in_fp16(kp, units, first, n_k, below):
         assert_lse(lse[i:i + 1, -1:], want_lse)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("log2", [20, 26, 33, 40, 105, 125])
+@pytest.mark.parametrize("size", [(1, 4, 2, 200, 200, 40, 2), (2, 8, 2, 1, 3000, 0, 0), (1, 2, 1, 200, 4000, 0, 0), (1, 2, 1, 20, 300, 0, 0)])
+def test_scores_of_any_size(kp, size, log2, sign, dtype):
+    """Scores around 2^log2 in 32 steps: a row's result is the mean of the values of its largest scores."""
+    b, hq, hkv, n_q, n_k, window, sinks = size
+    gen = torch.Generator(device="cuda").manual_seed(25)
+    q, k, v = torch.zeros(b, hq, n_q, 64, device="cuda"), torch.zeros(b, hkv, n_k, 64, device="cuda"), heads(gen, b, hkv, n_k, 64, dtype)
+    q[..., 0] = 2.0 ** 13
+    k[..., 0] = sign * 2.0 ** 13 * (1 + torch.randint(0, 32, (b, hkv, n_k), device="cuda", generator=gen) / 64)
+    q, k = q.to(dtype), k.to(dtype)
+    scale = 2.0 ** (log2 - 26)
+    o, lse = attend(kp, q, k, v, window, sinks, scale)
+    _, _, want_lse = forward(q, k, v, window, sinks, scale)
+    s = torch.matmul(q.double(), k.double().repeat_interleave(hq // hkv, 1).transpose(2, 3)) * scale
+    p = torch.softmax(s.masked_fill(~visible(n_q, n_k, window, sinks, "cuda"), -math.inf), -1)  # (lse does not hold what ties add)
+    assert_within(o, torch.matmul(p, v.double().repeat_interleave(hq // hkv, 1)), o_bound(p, v, dtype), "o")
+    assert_lse(lse, want_lse)
+
+
 def test_gradient_against_differences(kp):
     """The gradient along random directions against central differences of the definition in 64 bits."""
     gen = torch.Generator(device="cuda").manual_seed(7)
