@@ -393,11 +393,13 @@ _names = {}  # torch's types by the names below, filled in by the first call
 
 
 def _types() -> dict:
+    global _names
     if not _names:
         import torch
 
-        _names.update({n: getattr(torch, n) for n in ("float32", "uint8", "int32", "int64", "float8_e4m3fn")})
-        _names.update({torch.bfloat16: KP_BF16, torch.float16: KP_FP16})
+        names = {n: getattr(torch, n) for n in ("float32", "uint8", "int32", "int64", "float8_e4m3fn")}
+        names.update({torch.bfloat16: KP_BF16, torch.float16: KP_FP16})
+        _names = names  # (whole: another thread may be looking)
     return _names
 
 

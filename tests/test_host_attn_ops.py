@@ -156,3 +156,29 @@ def test_the_binding_refuses_what_does_not_match():
                    dict(k_exp=FakeTensor((4, 1, 8), torch.uint8)), dict(v_cache=FakeTensor((4, 1, 16, 64), bf)), dict(k_cache=FakeTensor((4, 1, 16, 64), torch.float16))):
         with pytest.raises((ValueError, AttributeError)):
             binding.kp_cache_write(**{**good, **change})
+
+
+def test_the_first_call_of_a_thread_finds_all_types_or_none(monkeypatch):
+    """While one thread's first call fills in torch's types, another's sees none of them, or all."""
+    import sys
+
+    import torch
+
+    monkeypatch.setattr(binding, "_names", {})
+    seen = []
+
+    def trace(frame, event, arg):
+        if frame.f_code is binding._types.__code__:
+            seen.append(len(binding._names))
+            return trace
+        return None
+
+    before = sys.gettrace()
+    sys.settrace(trace)
+    try:
+        full = binding._types()
+    finally:
+        sys.settrace(before)
+    assert full[torch.bfloat16] == kp.KP_BF16 and full[torch.float16] == kp.KP_FP16 and full["uint8"] is torch.uint8
+    assert seen and set(seen) <= {0, len(full)}
+    assert binding._types() is full
