@@ -68,6 +68,27 @@ def test_forward_and_gradient(kp, size, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window, sinks", [(2, 0), (5, 2), (12, 4), (16, 0)])
+def test_dq_does_not_depend_on_the_group(kp, window, sinks, d, dtype):
+    """Heads that share keys, and the same heads with a copy of the keys each.  Where rows see few keys delta is exact but for
+    fp32, and dq is the same but for the order of its sums (2^-23 of a value), which moves a rounding to the type (2^-8, 2^-11)
+    for one value in thousands; 1 % are allowed.  (With more keys delta has the rounding of o, whose weights are rounded against
+    a reference that depends on the tile.)"""
+    gen = torch.Generator(device="cuda").manual_seed(26)
+    n = 300
+    q, k, v, d_o = (heads(gen, 1, h, n, d, dtype) for h in (4, 1, 1, 4))
+    got = []
+    for kk, vv in ((k, v), (k.repeat(1, 4, 1, 1), v.repeat(1, 4, 1, 1))):
+        o, lse = attend(kp, q, kk, vv, window, sinks, 0.125)
+        dq = grads(kp, q, kk, vv, o, lse, d_o, window, sinks, 0.125)[0]
+        want, bound = gradients(q, kk, vv, d_o, window, sinks, 0.125, dtype)[0]
+        assert_within(dq, want, bound)
+        got.append(dq)
+    assert float((got[0] != got[1]).double().mean()) <= 0.01
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("shift", [-14, -4, 6])
 def test_gradients_of_other_magnitudes(kp, dtype, shift):
     """Losses scaled by a power of two scale the gradients, down to what the type's own range leaves of them."""
