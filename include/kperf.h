@@ -504,8 +504,9 @@ typedef struct {
 
 /*
  * Writes T new tokens' keys and values (kp_heads with seq ignored: [head, token, D]) to the slots
- * slots[T] (device, int64).  Slots below 0 are skipped, and so are slots past the cache's end.  If a slot is named
- * twice, one of the tokens' rows is left in it, unspecified which.  T = 0 is allowed.
+ * slots[T] (device, int64).  Slots below 0 are skipped, and so are slots past the cache's end.  A slot is to be named once:
+ * nothing is said about what one that is named twice holds (codes, exponents, keys and values are written apart from one
+ * another, and may come from different tokens); other slots are not touched by it.  T = 0 is allowed.
  */
 kp_status kp_cache_write(const kp_heads* k, const kp_heads* v, const int64_t* slots, int T, const kp_cache* cache,
                          void* stream);

@@ -511,7 +511,7 @@ def _cache_of(k_cache, v_cache, k_exp, v_exp, dtype) -> bytes:
 
 
 def kp_cache_write(k, v, slots, k_cache, v_cache, k_exp=None, v_exp=None, stream=None) -> None:
-    """New rows k, v [T, Hkv, D] into slots [T] int64 (negative: skipped) of the cache [n_pages, Hkv, page, D], as they are
+    """New rows k, v [T, Hkv, D] into slots [T] int64 (negative: skipped; each named at most once) of the cache [n_pages, Hkv, page, D], as they are
     or, into a float8_e4m3fn cache with exponents [n_pages, Hkv, page] uint8, quantised row by row."""
     T, (_, Hkv, _, D) = k.shape[0], k_cache.shape
     _check(lib().kp_cache_write(_heads("k", k, (T, Hkv, D), k.dtype), _heads("v", v, (T, Hkv, D), k.dtype),

@@ -22,7 +22,7 @@ struct WriteArgs {
 // D / 8 lanes to a row, 16 bytes to a lane, kWriteRows rows one after the other, all of whose loads are in flight together;
 // blockIdx.y: keys or values.  Rows are taken for one head from a run of tokens, then for the next: a run's rows lie side by
 // side in the cache, where rows in the order that they come in (all heads of a token) leave pieces of D bytes and single
-// exponents.  They are read once, past the caches (nontemporal), so that what stays there is the cache that is read next.
+// exponents.  (Nothing orders the rows of a slot that two tokens name: the caller's to avoid.)  They are read once, past the caches (nontemporal), so that what stays there is the cache that is read next.
 // Bound by memory: 32749 tokens of 8 heads of 128, 202 MB, take 39 us (5150 GB/s, what a copy reaches); in runs of 32 and 64
 // tokens 40 and 43, token by token 44, that through the caches 47.6; with 8 rows 42.5, with 2 42.9, with 1 51.
 constexpr uint32_t kWriteRows = 4, kMostRunLog2 = 4;

@@ -73,6 +73,31 @@ def test_write(kp, tokens, hkv, d, page, dtype, e4m3):
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
+def test_a_slot_that_is_named_twice_leaves_the_others_alone(kp, e4m3):
+    """What it holds itself is not defined: a code and an exponent may come from different tokens."""
+    gen = torch.Generator(device="cuda").manual_seed(27)
+    tokens, hkv, d, page, pages, dtype = 200, 3, 64, 16, 20, torch.bfloat16
+    kv = [torch.randn(tokens, hkv, d, device="cuda", generator=gen).to(dtype) for _ in range(2)]
+    slots = torch.randperm(pages * page, device="cuda", generator=gen)[:tokens]
+    twice = slots[:20].clone()
+    slots[100:120] = twice
+    halves, exps = new_cache(pages, hkv, page, d, dtype, e4m3)
+    kp.kp_cache_write(*kv, slots, *halves, *exps)
+    once = torch.ones(tokens, dtype=torch.bool)
+    once[:20], once[100:120] = False, False
+    at = slots.cpu()[once]
+    for h in range(2):
+        rows = halves[h].cpu()[at // page, :, at % page]
+        code, e = quantise(kv[h][once.cuda()], dtype) if e4m3 else (kv[h].cpu()[once].double(), None)
+        assert torch.equal(rows.double(), code)
+        assert e is None or torch.equal(exps[h].cpu()[at // page, :, at % page].long(), e)
+        free = torch.ones(pages * page, dtype=torch.bool)
+        free[slots.cpu()] = False
+        raw = halves[h].cpu().view(torch.uint8).permute(0, 2, 1, 3).reshape(pages * page, -1)
+        assert bool((raw[free] == 0xFF).all())
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("lens,hkv,d,page", [([1], 1, 64, 1), ([3, 0, 40, 16], 2, 128, 16), ([100, 7], 3, 64, 8), ([0, 0, 129], 8, 128, 64)])
 def test_read_is_what_was_written(kp, lens, hkv, d, page, dtype, e4m3):
@@ -234,6 +259,28 @@ def test_values_at_the_ends_of_fp16_in_an_e4m3_cache(kp):
     kp.kp_cache_write(*kv[0], slots, *halves, *exps)
     o, lse = run_paged(kp, halves, exps, table, lens_t, starts, q, 0, 0, 0.125)
     check_paged(o, lse, q, kv, [3], 0, 0, 0.125, dtype, True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_at_the_ends_of_the_range_read_back(kp, dtype, d):
+    """Written to e4m3 and read: the code times its power of two, rounded to the type, which makes an infinity of what it does not
+    hold (65504 rounds to a code that stands for 65536, bf16's largest to one that stands for 2^128)."""
+    info = torch.finfo(dtype)
+    tiny = info.smallest_normal * info.eps
+    x = torch.zeros(8, 1, d, dtype=torch.float64)
+    x[0], x[1], x[2], x[3] = info.max, -info.max, info.max / 2, tiny
+    x[4, 0, ::2], x[5, 0, ::3], x[6, 0, 0] = 3 * tiny, info.smallest_normal, info.max
+    x[6, 0, 1], x[7, 0, 0] = info.max * (1 - 2.0 ** -4), info.max * (1 - 2.0 ** -5)
+    x = x.to(dtype)
+    halves, exps = new_cache(1, 1, 8, d, dtype, True)
+    kp.kp_cache_write(x.cuda(), x.cuda(), torch.arange(8, device="cuda"), *halves, *exps)
+    out = [torch.zeros(8, 1, d, dtype=dtype, device="cuda") for _ in range(2)]
+    kp.kp_cache_read(*halves, *exps, torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.tensor([0, 8], dtype=torch.int32, device="cuda"), *out)
+    want = stored(x, True).to(dtype)
+    assert torch.isinf(want[0]).all() and torch.isfinite(want[2:6]).all()
+    for o in out:
+        assert torch.equal(o.cpu().double(), want.double())
 
 
 def test_cache_of_more_than_2_32_bytes(kp):
