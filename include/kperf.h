@@ -418,14 +418,23 @@ kp_status kp_attn_instrumented(const void* Q, const void* K, const void* V, void
 
 /* ---- attention with windows, caches and gradients ----------------------------------------------
  *
- * The attentions that models train and serve with, as further targets.  Everywhere below, query token
- * i of n_q stands over n_k keys at position p = n_k - n_q + i and sees key j where
+ * The attentions that models train and serve with.  Window and paged attention are further targets, which can be
+ * recorded; the gradient and the cache calls cannot.  Everywhere below, query token i of n_q stands over n_k keys at
+ * position p = n_k - n_q + i and sees key j where
  *     j <= p  and  (window == 0  or  p - j < window  or  j < sinks)
  * (window 0: all keys up to p; sinks: first keys that stay visible).  With Hq query heads and Hkv heads
- * of keys and values, Hq a multiple of Hkv, query head h reads head h / (Hq / Hkv).  Softmax, its sums
- * and all accumulation are in fp32; results are rounded once, to the inputs' type.  A token that sees no
+ * of keys and values, Hq a multiple of Hkv, query head h reads head h / (Hq / Hkv).  A token that sees no
  * key (p < 0), or only scores of -inf, gives o = 0 and lse = -inf.  What a token does not see has no
  * influence on its result, not even as an infinity or a NaN.
+ *
+ * Precision.  Scores (one that fp32 does not hold is an infinity), softmax, its sums, lse and all accumulation are in fp32.
+ * Matrix instructions take 16-bit operands, so that, besides the results, the weights that multiply values are rounded to
+ * the type (not those that are summed up), and so are P and dS in the gradient: o and dv are off by up to two half steps of
+ * the type, relative to the sum of their terms' magnitudes, dq and dk by two of dS's and what a rounded o adds (below).
+ * fp16 does not hold small numbers: there a weight is off by up to 2^-36 of its row's largest besides, dS in dk by 2^-26 of
+ * the largest |d_o| of the 64 tokens that it is taken together with, dS in dq by 2^-30 of its own row's.
+ * Rows (gradients: and keys) whose sums are not finite are taken again in fp32 over what they see, one by one: a few of them
+ * cost little; a value that is not finite and that all tokens of a long sequence see can make a call take 50 times as long.
  *
  * kp_heads names a tensor [sequence, head, token, D] by its first element and three strides, in
  * elements; the D values of a row are contiguous and 16-byte aligned (so are all strides: multiples of 8).
@@ -473,6 +482,8 @@ kp_status kp_attn_window_launch_shape(int B, int Hq, int Hkv, int Sq, int Sk, in
  *   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij d_o_i,
  * the latter two summed over the query heads that read the head.  Sums are taken in a fixed order: the same
  * inputs give the same bits.  lse as kp_attn_window wrote it (not NULL).  All of dq, dk, dv are written.
+ * P stands on lse in fp32: it is off by |lse| 2^-24 or so.  o was rounded, and so is delta; for tokens that see up to 16 keys
+ * it is put right by the sum of their dS, which is 0 with the exact one.
  */
 size_t kp_attn_window_grad_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D, int window, int sinks);
 kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, const kp_heads* v, const kp_heads* o,
@@ -490,7 +501,8 @@ kp_status kp_attn_window_grad(const kp_heads* q, const kp_heads* k, const kp_hea
  *                  c 2^(E - 127).  A row is written with the least E for which its largest finite magnitude is
  *                  at most 448 2^(E - 127) (E = 127 for a row of zeros, never below 1), each value rounded to
  *                  nearest even; what is not finite becomes the code of NaN.  A power of two costs a
- *                  floating-point code no precision, and makes writing and reading back exact but for that rounding.
+ *                  floating-point code no precision, and makes writing and reading back exact but for that rounding
+ *                  (which can take the type's largest values past it: 65504 reads back in fp16 as an infinity).
  */
 enum { KP_CACHE_SAME = 0, KP_CACHE_E4M3 = 1 };
 
