@@ -384,6 +384,27 @@ def test_offsets_past_32_bits(kp):
         assert torch.equal(o, o2) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("n_q", [4200, 40])
+@pytest.mark.parametrize("dtype, d", [(torch.bfloat16, 64), (torch.float16, 128)])
+def test_gradients_of_offsets_past_32_bits(kp, dtype, d, n_q):
+    """Every tensor with tokens 2^20 elements apart: the gradient's loaders, its first tile with sinks, and its stores."""
+    gen = torch.Generator(device="cuda").manual_seed(28)
+    n, step, window, sinks = 4200, 1 << 20, 64, 4
+    room = torch.empty(n * step, dtype=dtype, device="cuda")
+    place = lambda i, m: room[i * d:].as_strided((1, 1, m, d), (0, 0, step, 1))  # noqa: E731
+    near = [heads(gen, 1, 1, m, d, dtype) for m in (n_q, n, n, n_q)]
+    q, k, v, d_o = (place(i, x.shape[2]).copy_(x) for i, x in enumerate(near))
+    o, lse = attend(kp, *near[:3], window, sinks, 0.125)
+    want = grads(kp, *near[:3], o, lse, near[3], window, sinks, 0.125)
+    far_o, far_lse = attend(kp, q, k, v, window, sinks, 0.125, place(4, n_q))
+    assert torch.equal(far_o, o) and torch.equal(far_lse, lse)
+    out = [place(5 + i, m) for i, m in enumerate((n_q, n, n))]
+    ws = torch.empty(kp.kp_attn_window_grad_bytes(q, k, window, sinks), dtype=torch.uint8, device="cuda")
+    kp.kp_attn_window_grad(q, k, v, far_o, far_lse, d_o, *out, window, sinks, 0.125, ws)
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
+    assert all(torch.equal(a, b) for a, b in zip((q, k, v, d_o), near))
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_many_key_tiles(kp, d):
     """More key tiles than there are workers: whole tiles in several rounds, sinks and the rest split."""

@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from tests.attn_util import assert_lse, assert_within, forward, half_step, o_bound, quantise
+from tests.attn_util import assert_lse, assert_within, forward, half_step, o_bound, quantise, visible
 
 pytestmark = pytest.mark.gpu
 TYPES = [torch.bfloat16, torch.float16]
@@ -232,6 +232,28 @@ def test_pages_that_are_not_there_are_not_seen(kp, n_q, e4m3):
         assert_within(o[at : at + n].transpose(0, 1)[None], torch.matmul(p, v), o_bound(p, v, dtype))
         assert_lse(lse[:, at : at + n][None], torch.logsumexp(sc, -1))
         at += n
+
+
+# lengths, new tokens and window: few rows, whole and over split keys; tiles of rows, whole and over split keys
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n, n_q, window", [(900, 5, 60), (20000, 3, 9000), (400, 150, 100), (6000, 150, 3000)])
+def test_values_that_are_not_finite_in_the_cache(kp, n, n_q, window, d, e4m3):
+    """A value that is not finite reaches the rows that see it, in its own element, and nobody else."""
+    hq, hkv, page, dtype, scale, sinks = 6, 2, 16, torch.bfloat16, 0.1, 3
+    halves, exps, table, lens, starts, q, kv = paged_case(kp, [n], [n_q], hq, hkv, d, page, dtype, e4m3, seed=5)
+    at = n - n_q - window + 1 + n_q // 2  # the first half of the rows sees it
+    kv[0][1][at, 0, 5] = math.nan
+    slots = table[0, torch.arange(n, device="cuda") // page].long() * page + torch.arange(n, device="cuda") % page
+    kp.kp_cache_write(*kv[0], slots, *halves, *exps)
+    o, lse = run_paged(kp, halves, exps, table, lens, starts, q, window, sinks, scale)
+    k, v = (torch.nan_to_num(stored(x, e4m3).to("cuda")).transpose(0, 1)[None] for x in kv[0])
+    p, want, want_lse = forward(q.transpose(0, 1)[None], k, v, window, sinks, scale)
+    hit = visible(n_q, n, window, sinks, "cuda")[:, at]
+    assert bool(hit.any()) and not bool(hit.all())
+    want[0, : hq // hkv, :, 5][:, hit] = math.nan
+    assert_within(o.transpose(0, 1)[None], want, o_bound(p, v, dtype))
+    assert_lse(lse[None], want_lse)
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
