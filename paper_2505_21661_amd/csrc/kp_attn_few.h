@@ -120,8 +120,10 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_few(Args g) {
       if constexpr (E4M3) k_e[n] = src.k_exp[r];
     }
   };
-  // Values are read once, whole lines at a time, and go past the caches; of a line of keys a load takes half, and the other
-  // half is to be there for the next (64 tokens over up to 16384 keys: 238 us, all through the caches 261, nothing 247).
+  // Values go past the caches, whole lines at a time; of a line of keys a load takes half, and the other half is to be there
+  // for the next (64 tokens over up to 16384 keys: 238 us, all through the caches 261, nothing 247).  That suits sequences of
+  // one tile with pages of their own, whose values are read once; those of a longer run of tokens in a batch of single ones,
+  // or of a shared page, come from memory for every tile that sees them.
   auto load_v = [&](uint32_t rows) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < VL; ++i) {

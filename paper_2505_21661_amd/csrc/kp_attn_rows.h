@@ -96,8 +96,8 @@ __device__ __forceinline__ void finish_ring(kp::Ring& ring, const Args& g, uint3
 
 // Per tile of 64 keys a wave has 32 MFMAs (1024 cycles), 33 exponentials (530) and some 160 other vector instructions (640),
 // which its partner on the SIMD hides in part: the matrix pipes are busy 48 % of the time at 1.9 GHz (32/8 x 8192 x 128,
-// window 1024: 155 us, 830 TFLOP/s of what rows see), 38 % where a tile of rows has 10 tiles of keys (2 x 16/16 x 4000, window
-// 512: 57 us, 550), since the first loads and the stores of a workgroup then weigh more; chunks of 512 tokens over up to 8192
+// window 1024: 146 us, 890 TFLOP/s of what rows see), 38 % where a tile of rows has 10 tiles of keys (2 x 16/16 x 4000, window
+// 512: 55 us, 575), since the first loads and the stores of a workgroup then weigh more; chunks of 512 tokens over up to 8192
 // keys in pages, window 2048: 113 us, 750.
 // Recorded regions, per tile of 64 keys: 0 K Q^T, with the request of the next keys and values and the lower half's mask and
 // maximum between its MFMAs, 1 the rest of the softmax, 2 V^T P^T up to the barrier behind it.
@@ -516,7 +516,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
         if (wave_first + r <= last_row) *reinterpret_cast<u32x4*>(o + to + 8u * chunk) = (r & 8u) ? u32x4{v.z, v.w, v.x, v.y} : v;
       }
     }
-    // Rows with a value that is not finite, taken again (see kp_attn.h).
+    // Rows with a value that is not finite, taken again (see Row).
     if (again != 0ull) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // their first results have left
       for (; again != 0ull; again &= again - 1ull) {

@@ -219,7 +219,7 @@ __device__ __forceinline__ uint32_t odd_keys(float odd, bool mine) {
 // [row][key] and are read transposed, for dv^T += dO^T P and dk^T += Q^T dS, which have a key to a lane.
 // S and dP are formed a step ahead: the exponentials stand between the MFMAs of dP, the rest of the vector work between
 // those of dv.
-// 32/8 x 8192 x 128, window 1024: 360 us, 715 TFLOP/s of four products, the matrix pipes busy 47 % of the time at 1.6 GHz, the
+// 32/8 x 8192 x 128, window 1024: 343 us, 755 TFLOP/s of four products, the matrix pipes busy 46 % of the time at 1.6 GHz, the
 // lowest clock of these kernels: it is bound by power as much as by the vector and scalar instructions between its MFMAs.
 constexpr int kPairThreads = 512;
 template <int D> constexpr uint32_t pairs_lds_bytes() { return 3u * (4u * 64u * D + kStatBytes) + 24u * 2048u; }
@@ -569,8 +569,8 @@ __global__ __launch_bounds__(kPairThreads, 2) void kp_grad_keys_pairs(GradArgs g
 // The same for D = 64, where a wave's 32 keys leave room for two waves on a SIMD: 4 waves, each with all rows of a step, two
 // workgroups on a CU that overlap one another.  S = Q K^T and dP = dO V^T have a key to a lane, as dv^T += dO^T P and
 // dk^T += Q^T dS need it.  (The kernel above takes 33 us where this one takes 22: 2 x 12/4 x 1153 x 64, window 250.)
-// There a worker has 3 or 4 steps, and the start of a workgroup, its first loads and its partial sums (45 MB in all) are most
-// of the time; 32/8 x 8192, no window, takes 1146 us with the kernel of the queries, 840 TFLOP/s.
+// There a worker has 3 or 4 steps, and the start of a workgroup, its first loads and its partial sums (39 MB in all) are most
+// of the time; 32/8 x 8192, no window, takes 1105 us with the kernel of the queries (fp16 1270), 870 TFLOP/s.
 template <class T, int D>
 __global__ __launch_bounds__(kThreads, 2) void kp_grad_keys(GradArgs g, KeyPlan plan) {
   constexpr uint32_t kTile = 64u * 2u * D, kBuffer = 2u * kTile;
