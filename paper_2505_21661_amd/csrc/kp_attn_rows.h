@@ -32,7 +32,7 @@ template <class T> constexpr float kSlack = std::is_same<T, Fp16>::value ? 15.f 
 // NaN where the reference goes that far, so that the row is taken again with scores and reference rounded alike.
 constexpr float kFar = 16777216.f;
 __device__ __forceinline__ float sum_unless_far(float l, float reference, float score) {
-  return (__builtin_fabsf(reference) > kFar) & (score > -INFINITY) ? __builtin_nanf("") : l;
+  return ((__builtin_fabsf(reference) > kFar) & (score > -INFINITY)) ? __builtin_nanf("") : l;
 }
 
 template <int D>
