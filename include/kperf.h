@@ -449,7 +449,7 @@ kp_status kp_attn_instrumented(const void* Q, const void* K, const void* V, void
  * tokens, 2^30 or more tokens, more workgroups than a launch takes.  All calls are asynchronous on `stream` and can be
  * captured; a workspace belongs to one call at a time.
  */
-enum { KP_BF16 = 0, KP_FP16 = 1 };
+enum { KP_BF16 = 0, KP_FP16 = 1, KP_FP32 = 2 /* norms' weights only */ };
 
 typedef struct {
   void* at;        /* device, element [0][0][0][0] */
@@ -547,6 +547,57 @@ kp_status kp_attn_paged(const kp_heads* q, const kp_cache* cache, const int32_t*
                         uint32_t region_mask, void* trace_buf, size_t trace_cap, void* stream);
 kp_status kp_attn_paged_launch_shape(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int window,
                                      int sinks, int* n_wg, int* waves_per_wg, int* n_regions);
+
+/* ---- what goes into them: queries and keys normed and turned ------------------------------------
+ *
+ * Of a head x of D values, with weights w:  r = 1 / sqrt(mean x^2 + eps),  u_n = x_n r w_n  (without weights u = x).  The first
+ * 2 pairs values of u are pairs, (u_m, u_{pairs + m}) or, adjacent, (u_{2m}, u_{2m + 1}), and pair m = (a, b) becomes
+ *     (a cos t - b sin t, a sin t + b cos t),   t = position of the token on the pair's axis * freq[m];
+ * the other values stay.  All is fp32 but the angle, which is taken in 64 bits (off by at most 2^-21 for any position, with
+ * |freq| up to 1); the result is rounded once.
+ */
+typedef struct {
+  const int32_t* at;    /* device: the position of token s of sequence b on axis a, of any sign, at [a axis_step + b seq_step + s] */
+  int64_t axis_step;    /* not negative; 0: shared */
+  int64_t seq_step;
+  const float* freq;    /* device, [pairs], finite */
+  const uint8_t* axis;  /* device, [pairs]: a pair's axis (one of `axes` or more: the pair stays as it is); NULL: axis 0 for all */
+  int pairs;            /* 0 to D / 2, a multiple of 8; 0: nothing is turned */
+  int axes;             /* 1 to 255 */
+  int adjacent;         /* 0 or 1 */
+} kp_turns;
+
+/*
+ * q [B, Hq, S, D] and k [B, Hk, S, D] to q_out and k_out.  Either number of heads may be 0 (the tensors may be NULL then), and so
+ * may B and S.  q_weight, k_weight: device, [D], 16-byte aligned, of weight_type: the type or KP_FP32; NULL: that tensor is not
+ * normed.  eps from 1e-30 to 1e30.  turns (host) may be NULL: nothing is turned.  q_out may be q and k_out k, with the same
+ * strides; apart from that outputs must not overlap inputs.  bf16 rows of any finite size are normed right, also where the
+ * squares pass the range of fp32.
+ */
+kp_status kp_norm_rotate(const kp_heads* q, const kp_heads* k, const void* q_weight, const void* k_weight, int weight_type,
+                         float eps, const kp_turns* turns, const kp_heads* q_out, const kp_heads* k_out, int B, int Hq, int Hk,
+                         int S, int D, int type, void* stream);
+
+/*
+ * Its gradient: from d_q_out and d_k_out, with g the gradient turned back and n = x r,
+ *   d_w_n = sum over all rows of g_n n_n (fp32),   d_x = r (w g - n mean(w g n))   (without weights d_x = g).
+ * q and k are the tensors that were normed, and may be NULL where their weights are; dq_weight, dk_weight [D] fp32, all of them
+ * written (zeros where there are no rows), NULL where there are no weights.  dq may be d_q_out or q, dk d_k_out or k, with the same strides.
+ * Sums are taken in a fixed order: the same inputs give the same bits.  workspace: as above, not needed without weights.
+ */
+size_t kp_norm_rotate_grad_bytes(int B, int Hq, int Hk, int S, int D);
+kp_status kp_norm_rotate_grad(const kp_heads* q, const kp_heads* k, const void* q_weight, const void* k_weight, int weight_type,
+                              float eps, const kp_turns* turns, const kp_heads* d_q_out, const kp_heads* d_k_out,
+                              const kp_heads* dq, const kp_heads* dk, float* dq_weight, float* dk_weight, int B, int Hq, int Hk,
+                              int S, int D, int type, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * kp_norm_rotate of T new tokens (kp_heads with seq ignored) and kp_cache_write of the keys that it gives and of the values v, in
+ * one call and to the same bits: q to q_out, k and v to slots[T] of the cache.
+ */
+kp_status kp_norm_rotate_write(const kp_heads* q, const kp_heads* k, const kp_heads* v, const void* q_weight, const void* k_weight,
+                               int weight_type, float eps, const kp_turns* turns, const kp_heads* q_out, const int64_t* slots, int T,
+                               int Hq, const kp_cache* cache, void* stream);
 
 /*
  * Timer calibration (Sec. 5.4 "Cycle-level Overhead": cost of one record; Sec. 4.3: that

@@ -30,7 +30,7 @@ KP_MASK_COLLAB = 1 << 27      # all lanes store a record; hardware ids of the wa
 KP_MASK_UNFENCED = 1 << 26    # with KP_MASK_PHASES and no region: the staged K step without scheduling fences
 KP_FLAG_REALTIME = 2
 KP_FLAG_HW_IDS = 4
-KP_BF16, KP_FP16 = 0, 1
+KP_BF16, KP_FP16, KP_FP32 = 0, 1, 2
 KP_CACHE_SAME, KP_CACHE_E4M3 = 0, 1
 
 
@@ -56,6 +56,11 @@ class kp_cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
                 ("n_pages", ctypes.c_int), ("Hkv", ctypes.c_int), ("page", ctypes.c_int), ("D", ctypes.c_int),
                 ("type", ctypes.c_int), ("cache_type", ctypes.c_int)]
+
+
+class kp_turns(ctypes.Structure):
+    _fields_ = [("at", ctypes.c_void_p), ("axis_step", ctypes.c_int64), ("seq_step", ctypes.c_int64), ("freq", ctypes.c_void_p),
+                ("axis", ctypes.c_void_p), ("pairs", ctypes.c_int), ("axes", ctypes.c_int), ("adjacent", ctypes.c_int)]
 
 
 _lib = None
@@ -125,7 +130,7 @@ def lib() -> ctypes.CDLL:
 def _optional(L):
     vp, sz, ci, u32, fl = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_uint32, ctypes.c_float
     ip = ctypes.POINTER(ctypes.c_int)
-    hp = cp = vp  # kp_heads and kp_cache: their bytes, or byref of a structure
+    hp = cp = tp = vp  # kp_heads, kp_cache and kp_turns: their bytes, or byref of a structure
     sigs = {
         "kp_attn_window": [hp, hp, hp, hp, vp, ci, ci, ci, ci, ci, ci, ci, ci, ci, fl, vp, sz, u32, vp, sz, vp],
         "kp_attn_window_launch_shape": [ci] * 8 + [ip] * 3,
@@ -134,6 +139,9 @@ def _optional(L):
         "kp_cache_write": [hp, hp, vp, ci, cp, vp],
         "kp_cache_read": [cp, vp, ci, vp, ci, ci, hp, hp, vp],
         "kp_attn_paged": [hp, cp, vp, ci, vp, vp, hp, vp, ci, ci, ci, ci, ci, fl, vp, sz, u32, vp, sz, vp],
+        "kp_norm_rotate": [hp, hp, vp, vp, ci, fl, tp, hp, hp, ci, ci, ci, ci, ci, ci, vp],
+        "kp_norm_rotate_grad": [hp, hp, vp, vp, ci, fl, tp, hp, hp, hp, hp, vp, vp, ci, ci, ci, ci, ci, ci, vp, sz, vp],
+        "kp_norm_rotate_write": [hp, hp, hp, vp, vp, ci, fl, tp, hp, vp, ci, ci, cp, vp],
         "kp_gemm_launch_shape": [ci, ci, ci, ip, ip, ip],
         "kp_gemm_instrumented": [vp, vp, vp, ci, ci, ci, u32, vp, sz, vp],
         "kp_attn_launch_shape": [ci, ci, ci, ci, ip, ip, ip],
@@ -145,7 +153,7 @@ def _optional(L):
             f = getattr(L, name)
             f.restype = ci
             f.argtypes = args
-    for name, n in (("kp_attn_window_bytes", 8), ("kp_attn_window_grad_bytes", 8), ("kp_attn_paged_bytes", 9)):
+    for name, n in (("kp_attn_window_bytes", 8), ("kp_attn_window_grad_bytes", 8), ("kp_attn_paged_bytes", 9), ("kp_norm_rotate_grad_bytes", 5)):
         if hasattr(L, name):
             getattr(L, name).restype = sz
             getattr(L, name).argtypes = [ci] * n
@@ -164,6 +172,14 @@ def _ptr(t) -> int:
     if not t.is_contiguous():
         raise ValueError("tensor must be contiguous")
     return t.data_ptr()
+
+
+def _here(t):
+    """Raises where a tensor is on another GPU than the current one, whose stream a call without one goes to."""
+    import torch
+
+    if t.is_cuda and t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"tensor on GPU {t.get_device()}, but the current one is {torch.cuda.current_device()}")
 
 
 _current_stream = None  # () -> hipStream_t of torch's current stream
@@ -560,6 +576,126 @@ def kp_attn_paged(q, k_cache, v_cache, k_exp, v_exp, block_table, lens, starts, 
         _flat("starts", starts, (_names or _types())["int32"], (n + 1,)), _heads("o", o, q.shape, q.dtype),
         0 if lse is None else _flat("lse", lse, (_names or _types())["float32"], (Hq, T)), T, n, Hq, window, sinks, scale, ws, nbytes,
         region_mask & 0xFFFFFFFF, _ptr(trace_buf), trace_cap, _stream(stream)))
+
+
+# ---- queries and keys normed and turned ----------------------------------------------------------------
+# positions: int32, of each token, [S] (or [T]) if all sequences share them, [B, S], or with an axis in front, [axes, S] for a
+# batch without a dimension of its own and [axes, B, S] for one with it; any strides with the last dimension contiguous.
+
+
+_pack_turns = struct.Struct("PqqPPiiixxxx").pack
+
+
+def _turns(positions, freq, axis, adjacent, batch, tokens):
+    """kp_turns of the tensors above; batch: number of sequences, or None for a batch without a dimension of its own."""
+    if freq is None:
+        return None
+    names = _names or _types()
+    pairs = freq.shape[0]
+    p, dims = positions, positions.dim()
+    if p.dtype is not names["int32"] or not p.is_cuda or p.shape[-1] != tokens or (tokens > 1 and p.stride(-1) != 1):
+        raise ValueError(f"positions must be int32 on the GPU, {tokens} for each sequence, contiguous, not {list(p.shape)} of {p.dtype}")
+    axes, axis_step, seq_step = 1, 0, 0
+    if batch is not None and dims >= 2:
+        if p.shape[-2] != batch:
+            raise ValueError(f"positions must be [S], [B, S] or [axes, B, S] with B = {batch}, not {list(p.shape)}")
+        seq_step = p.stride(-2)
+    front = 2 if batch is None else 3
+    if dims == front:
+        axes, axis_step = p.shape[0], p.stride(0)
+    elif dims == 0 or dims > front:
+        raise ValueError(f"positions have too many dimensions or none: {list(p.shape)}")
+    return _pack_turns(p.data_ptr(), axis_step, seq_step, _flat("freq", freq, names["float32"], (pairs,)),
+                       0 if axis is None else _flat("axis", axis, names["uint8"], (pairs,)), pairs, axes, 1 if adjacent else 0)
+
+
+def _norms(q_weight, k_weight, D, dtype):
+    """Device pointers of the norms' weights (0: none) and their type."""
+    code, kind = _type_code(dtype), None
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is None:
+            continue
+        if w.dtype not in (dtype, _names["float32"]) or (kind is not None and w.dtype is not kind):
+            raise ValueError(f"weights must both be float32 or both {dtype}, not {w.dtype}")
+        kind = w.dtype
+    at = [0 if w is None else _flat("weights", w, kind, (D,)) for w in (q_weight, k_weight)]
+    return at[0], at[1], code if kind is dtype or kind is None else KP_FP32
+
+
+def _two(q, k):
+    """Of queries and keys, either of which may be None: number of sequences (None: [T, H, D]), heads, tokens, D and type."""
+    some = q if q is not None else k
+    if some is None:
+        raise ValueError("queries or keys are needed")
+    if some.dim() == 4:
+        B, _, S, D = some.shape
+        return B, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], S, D, some.dtype
+    S, _, D = some.shape
+    return None, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], S, D, some.dtype
+
+
+def _maybe(name, t, like, dtype):
+    """kp_heads of t in the shape of `like`, which may be None."""
+    return None if like is None else _heads(name, t, like.shape, dtype)
+
+
+def _alike(q, k, D, batch, tokens):
+    want = (tokens, D) if batch is None else (batch, tokens, D)
+    for name, t in (("queries", q), ("keys", k)):
+        if t is not None and (t.dim() != len(want) + 1 or ((t.shape[0], t.shape[2]) if batch is None else (t.shape[0], t.shape[2], t.shape[3])) != want):
+            raise ValueError(f"{name} must have the sequences, tokens and D of the others, not {list(t.shape)}")
+
+
+def kp_norm_rotate(q, k, q_weight, k_weight, eps: float, positions, freq, axis, adjacent: bool, q_out, k_out, stream=None) -> None:
+    """Heads of q and k ([B, H, S, D], or [T, H, D] where there is no batch) normed by their root mean square with weights [D]
+    (None: not normed), their pairs turned by position * freq[pair]; freq float32 [pairs] (None: not turned), axis uint8
+    [pairs] or None.  q and q_out, or k and k_out, may be None; outputs may be the inputs."""
+    B, Hq, Hk, S, D, dtype = _two(q, k)
+    _here(k if q is None else q)
+    _alike(q, k, D, B, S)
+    qw, kw, kind = _norms(q_weight, k_weight, D, dtype)
+    _check(lib().kp_norm_rotate(
+        _maybe("q", q, q, dtype), _maybe("k", k, k, dtype), qw, kw, kind, eps, _turns(positions, freq, axis, adjacent, B, S),
+        _maybe("q_out", q_out, q, dtype), _maybe("k_out", k_out, k, dtype), 1 if B is None else B, Hq, Hk, S, D, _type_code(dtype),
+        _stream(stream)))
+
+
+def kp_norm_rotate_grad_bytes(q, k) -> int:
+    """Bytes of workspace that kp_norm_rotate_grad takes for q and k (either may be None)."""
+    B, Hq, Hk, S, D, _ = _two(q, k)
+    return int(lib().kp_norm_rotate_grad_bytes(1 if B is None else B, Hq, Hk, S, D))
+
+
+def kp_norm_rotate_grad(q, k, q_weight, k_weight, eps: float, positions, freq, axis, adjacent: bool, d_q_out, d_k_out, dq, dk,
+                        dq_weight=None, dk_weight=None, workspace=None, stream=None) -> None:
+    """Gradient of kp_norm_rotate: dq, dk from d_q_out, d_k_out and the q, k that were normed (not looked at without weights), and
+    dq_weight, dk_weight [D] float32 where there are weights."""
+    B, Hq, Hk, S, D, dtype = _two(d_q_out, d_k_out)
+    _here(d_k_out if d_q_out is None else d_q_out)
+    _alike(d_q_out, d_k_out, D, B, S)
+    qw, kw, kind = _norms(q_weight, k_weight, D, dtype)
+    f32 = _names["float32"]
+    ws, n = _workspace(workspace)
+    _check(lib().kp_norm_rotate_grad(
+        _maybe("q", q, d_q_out if qw else None, dtype), _maybe("k", k, d_k_out if kw else None, dtype), qw, kw, kind, eps,
+        _turns(positions, freq, axis, adjacent, B, S), _maybe("d_q_out", d_q_out, d_q_out, dtype), _maybe("d_k_out", d_k_out, d_k_out, dtype),
+        _maybe("dq", dq, d_q_out, dtype), _maybe("dk", dk, d_k_out, dtype),
+        _flat("dq_weight", dq_weight, f32, (D,)) if qw else 0, _flat("dk_weight", dk_weight, f32, (D,)) if kw else 0,
+        1 if B is None else B, Hq, Hk, S, D, _type_code(dtype), ws, n, _stream(stream)))
+
+
+def kp_norm_rotate_write(q, k, v, q_weight, k_weight, eps: float, positions, freq, axis, adjacent: bool, q_out, slots, k_cache, v_cache,
+                         k_exp=None, v_exp=None, stream=None) -> None:
+    """kp_norm_rotate of new tokens q [T, Hq, D] (or None) and k [T, Hkv, D], queries to q_out, keys and the values v to slots [T] of the
+    cache as kp_cache_write puts them there."""
+    T, (_, Hkv, _, D), dtype = k.shape[0], k_cache.shape, k.dtype
+    Hq = 0 if q is None else q.shape[1]
+    _here(k)
+    qw, kw, kind = _norms(q_weight, k_weight, D, dtype)
+    _check(lib().kp_norm_rotate_write(
+        None if q is None else _heads("q", q, (T, Hq, D), dtype), _heads("k", k, (T, Hkv, D), dtype), _heads("v", v, (T, Hkv, D), dtype), qw, kw,
+        kind, eps, _turns(positions, freq, axis, adjacent, None, T), _maybe("q_out", q_out, q, dtype),
+        _flat("slots", slots, _names["int64"], (T,)), T, Hq, _cache_of(k_cache, v_cache, k_exp, v_exp, dtype), _stream(stream)))
 
 
 # ---- views of the statistics block (layout documented in include/kperf.h) ------------------------

@@ -1,9 +1,5 @@
 // A paged cache of keys and values: new rows quantised (or copied) into their slots, whole sequences read back.
-//
-// A row of D values becomes D e4m3 codes and one exponent byte: top = its largest finite magnitude, e the least integer
-// with top <= 448 2^e, code = top-preserving round to nearest even of x 2^-e.  With top = 1.f 2^x, 448 = 1.75 2^8: e is
-// x - 8 where 1.f <= 1.75, x - 7 otherwise, read off the bits of top.  The scaling is exact, so the code carries one
-// rounding (at most 2^-4 of the value, 2^-10 2^e below 2^-6 2^e) and the row reads back exactly as the codes say.
+#include "kp_cache_row.h"
 #include "kp_attn_host.h"
 
 namespace {
@@ -46,35 +42,7 @@ __global__ __launch_bounds__(kThreads) void kp_cache_write_rows(WriteArgs g) {
 #pragma unroll
   for (uint32_t i = 0; i < kWriteRows; ++i) {
     if (slot[i] < 0 || (uint64_t)slot[i] >= g.n_slots) continue;  // (the same for all lanes of a row)
-    const uint32_t page = (uint32_t)((uint64_t)slot[i] >> g.page_log2), in = (uint32_t)slot[i] & ((1u << g.page_log2) - 1u);
-    const uint32_t row = ((page * g.hkv + head[i]) << g.page_log2) + in;
-    if constexpr (!E4M3) {
-      *reinterpret_cast<u32x4*>(cache + (size_t)row * (2 * D) + 16u * c) = raw[i];
-    } else {
-      float x[8], top = 0.f;
-#pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        x[n] = T::to_float((raw[i][n >> 1] >> (16 * (n & 1))) & 0xFFFFu);
-        const bool finite = __builtin_fabsf(x[n]) < INFINITY;
-        top = fmaxf(top, finite ? __builtin_fabsf(x[n]) : 0.f);
-        x[n] = finite ? x[n] : __builtin_nanf("");
-      }
-#pragma unroll
-      for (int d = 1; d < (int)kLanes; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-      const uint32_t bits = __builtin_bit_cast(uint32_t, top);
-      int e = (int)(bits >> 23) - ((bits & 0x7FFFFFu) <= 0x600000u ? 135 : 134);
-      e = top == 0.f ? 0 : (e < -126 ? -126 : e);
-      const float scale = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
-      u32x2 codes;
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        int p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w] * scale, x[4 * w + 1] * scale, 0, false);
-        p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w + 2] * scale, x[4 * w + 3] * scale, p, true);
-        codes[w] = (uint32_t)p;
-      }
-      *reinterpret_cast<u32x2*>(cache + (size_t)row * D + 8u * c) = codes;
-      if (c == 0) (blockIdx.y ? g.v_exp : g.k_exp)[row] = (uint8_t)(e + 127);
-    }
+    put_row<T, D, E4M3>(raw[i], cache, blockIdx.y ? g.v_exp : g.k_exp, row_of_slot((uint64_t)slot[i], head[i], g.hkv, g.page_log2), c);
   }
 }
 

@@ -1,0 +1,302 @@
+"""Queries and keys normed and turned, their gradient, and the same into a cache, against definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from tests import rotate_util as ref
+from tests.attn_util import assert_within
+from tests.test_gpu_kv_cache import new_cache
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.bfloat16, torch.float16]
+EPS = 1e-6
+
+
+@pytest.fixture(scope="module")
+def kp():
+    import paper_2505_21661_amd as kp
+
+    return kp
+
+
+def heads(gen, layout, b, h, s, d, dtype):
+    """[b, h, s, d] for each number of heads in h, rows of different size, by their order in memory."""
+    scale = lambda *size: torch.exp2(2 * torch.randn(*size, 1, device="cuda", generator=gen))  # noqa: E731
+    if layout == "bhsd":
+        return [(torch.randn(b, n, s, d, device="cuda", generator=gen) * scale(b, n, s)).to(dtype) for n in h]
+    x = (torch.randn(b, s, sum(h), d, device="cuda", generator=gen) * scale(b, s, sum(h))).to(dtype).transpose(1, 2)
+    return list(x.split(list(h), 1))
+
+
+def inputs(seed, layout, b, hq, hkv, s, d, dtype, pairs, axes, weight, far=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    q, k = heads(gen, layout, b, (hq, hkv), s, d, dtype)
+    kind = {"none": None, "same": dtype, "fp32": torch.float32}[weight]
+    w = [None if kind is None else torch.randn(d, device="cuda", generator=gen).to(kind) for _ in range(2)]
+    at = (torch.randint(-50, 5000, (axes, b, s), device="cuda", generator=gen) + far).to(torch.int32)
+    freq = (1e4 ** (-torch.arange(pairs, device="cuda").double() / max(1, pairs))).float() if pairs else None
+    axis = torch.randint(0, axes, (pairs,), device="cuda", generator=gen).to(torch.uint8) if axes > 1 and pairs else None
+    return gen, q, k, w, at, freq, axis
+
+
+# (layout, sequences, heads, tokens, D, pairs, adjacent, axes, weight, where the positions begin)
+SHAPES = [
+    ("bhsd", 1, 1, 1, 1, 64, 32, False, 1, "same", 0),
+    ("bshd", 1, 5, 1, 1, 128, 64, True, 1, "fp32", 2 ** 31 - 6000),
+    ("bshd", 2, 12, 4, 33, 64, 16, True, 2, "fp32", 100),
+    ("bhsd", 3, 7, 1, 17, 128, 24, False, 3, "same", -2 ** 31 + 60),
+    ("bshd", 1, 40, 3, 130, 128, 64, False, 1, "none", 1 << 20),
+    ("bhsd", 2, 3, 3, 257, 64, 8, False, 1, "same", 0),
+    ("bshd", 1, 6, 2, 700, 128, 0, False, 1, "fp32", 0),
+    ("bhsd", 5, 2, 1, 9, 64, 32, True, 1, "none", 0),
+    ("bshd", 2, 32, 8, 1031, 128, 64, False, 3, "same", 0),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_forward(kp, shape, dtype):
+    layout, b, hq, hkv, s, d, pairs, adjacent, axes, weight, far = shape
+    _, q, k, w, at, freq, axis = inputs(sum(map(ord, str(shape))), layout, b, hq, hkv, s, d, dtype, pairs, axes, weight, far)
+    out = [torch.empty_like(q), torch.empty_like(k)]
+    kp.kp_norm_rotate(q, k, *w, EPS, at, freq, axis, adjacent, *out)
+    theta = None if freq is None else ref.angles(at, freq, axis, b, s)
+    for x, weight, got in zip((q, k), w, out):
+        assert_within(got, *ref.forward(x, weight, EPS, theta, adjacent), what=shape)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_gradient(kp, shape, dtype):
+    layout, b, hq, hkv, s, d, pairs, adjacent, axes, weight, far = shape
+    gen, q, k, w, at, freq, axis = inputs(sum(map(ord, str(shape))) + 1, layout, b, hq, hkv, s, d, dtype, pairs, axes, weight, far)
+    dy = heads(gen, layout, b, (hq, hkv), s, d, dtype)
+    theta = None if freq is None else ref.angles(at, freq, axis, b, s)
+    results = []
+    for _ in range(2):
+        dx = [torch.full_like(x, 7.0) for x in (q, k)]
+        dw = [None if x is None else torch.full((d,), 7.0, device="cuda") for x in w]
+        n = kp.kp_norm_rotate_grad_bytes(q, k)
+        workspace = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+        kp.kp_norm_rotate_grad(q, k, *w, EPS, at, freq, axis, adjacent, *dy, *dx, *dw, workspace)
+        results.append(dx + [x for x in dw if x is not None])
+    assert all(torch.equal(a, b) for a, b in zip(*results)), "the same inputs, other bits"
+    for x, weight, d_out, got, got_w in zip((q, k), w, dy, dx, dw):
+        want, bound, want_w, bound_w = ref.gradient(x, weight, EPS, theta, adjacent, d_out)
+        assert_within(got, want, bound, what=shape)
+        if weight is not None:
+            assert_within(got_w, want_w, bound_w, what=("weights", shape))
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_gradient_against_differences(kp, adjacent):
+    """The loss sum(y c) along a direction, by differences of the forward's definition in 64 bits: their own error is h^2 times the third
+    derivative, 1e-6 or so of the loss's scale here; what the gradient's rounding to fp16 gives is counted from its terms."""
+    b, hq, s, d, pairs, dtype = 2, 3, 5, 64, 16, torch.float16
+    gen, q, _, (w, _), at, freq, _ = inputs(5, "bhsd", b, hq, 1, s, d, dtype, pairs, 1, "fp32")
+    c = heads(gen, "bhsd", b, (hq,), s, d, dtype)[0]
+    theta = ref.angles(at, freq, None, b, s)
+    dq, dw = torch.empty_like(q), torch.empty(d, device="cuda")
+    kp.kp_norm_rotate_grad(q, None, w, None, EPS, at, freq, None, adjacent, c, None, dq, None, dw, None,
+                           torch.empty(kp.kp_norm_rotate_grad_bytes(q, None), dtype=torch.uint8, device="cuda"))
+    along = [torch.randn(q.shape, device="cuda", dtype=torch.float64, generator=gen) * q.double().abs(), torch.randn(d, device="cuda", dtype=torch.float64, generator=gen)]
+
+    def loss(h):
+        x, weight = q.double() + h * along[0], w.double() + h * along[1]
+        u = x / torch.sqrt(x.square().mean(-1, keepdim=True) + EPS) * weight
+        return float((ref.turn(u, theta, adjacent) * c.double()).sum())
+
+    h = 1e-4
+    want = (loss(h) - loss(-h)) / (2 * h)
+    got = float((dq.double() * along[0]).sum() + (dw.double() * along[1]).sum())
+    size = float((dq.double() * along[0]).abs().sum() + (dw.double() * along[1]).abs().sum())
+    assert abs(got - want) <= (2.0 ** -11 + 1e-5) * size
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_values_that_are_hard(kp, dtype):
+    """Zeros, the type's largest and smallest values, infinities and NaN: the definition's results, and no other row's business."""
+    b, h, s, d, pairs = 1, 2, 12, 128, 32
+    _, q, _, (w, _), at, freq, _ = inputs(9, "bhsd", b, h, 1, s, d, dtype, pairs, 1, "same")
+    q[0, 0, 0] = 0
+    q[0, 0, 1] = torch.finfo(dtype).max
+    q[0, 0, 2] = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+    q[0, 0, 3, ::2] = torch.finfo(dtype).max
+    q[0, 0, 4, 5] = math.inf
+    q[0, 0, 5, 100] = -math.inf  # in no pair
+    q[0, 0, 6, 7] = math.nan
+    q[0, 0, 7] = torch.finfo(dtype).smallest_normal
+    q[0, 0, 8, 1:] = 0
+    q[0, 0, 8, 0] = torch.finfo(dtype).max
+    theta = ref.angles(at, freq, None, b, s)
+    for weight in (w, None):
+        out = torch.empty_like(q)
+        kp.kp_norm_rotate(q, None, weight, None, EPS, at, freq, None, False, out, None)
+        want, bound = ref.forward(q, weight, EPS, theta, False)
+        rows = [r for r in range(s) if r not in (4, 5, 6)]
+        finite = want.abs() < torch.finfo(dtype).max * (1 - ref.half_step(dtype))
+        for r in rows:  # (what passes the type's range may be its largest value or an infinity)
+            keep = finite[0, :, r]
+            assert_within(out[0, :, r][keep], want[0, :, r][keep], bound[0, :, r][keep], what=r)
+        for r in (4, 5, 6):
+            assert_within(out[0, 1, r], want[0, 1, r], bound[0, 1, r])
+            got, exact = out[0, 0, r].double(), want[0, 0, r]
+            assert torch.equal(torch.isfinite(got), torch.isfinite(exact)), r
+            assert torch.equal(torch.isnan(got), torch.isnan(exact)), r
+    # the gradient at the largest rows: they are 1 / |x| of the others'
+    dy = torch.ones_like(q)
+    dq, dw = torch.empty_like(q), torch.empty(d, device="cuda")
+    q[0, 0, 4:7] = 1
+    kp.kp_norm_rotate_grad(q, None, w, None, EPS, at, freq, None, False, dy, None, dq, None, dw, None,
+                           torch.empty(kp.kp_norm_rotate_grad_bytes(q, None), dtype=torch.uint8, device="cuda"))
+    want, bound, want_w, bound_w = ref.gradient(q, w, EPS, theta, False, dy)
+    assert_within(dq, want, bound)
+    assert_within(dw, want_w, bound_w)
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_in_place_and_within_larger_tensors(kp, adjacent):
+    b, hq, hkv, s, d, pairs, dtype = 2, 6, 2, 40, 64, 32, torch.bfloat16
+    _, q, k, w, at, freq, _ = inputs(11, "bshd", b, hq, hkv, s, d, dtype, pairs, 1, "fp32")
+    out = [torch.empty_like(q), torch.empty_like(k)]
+    kp.kp_norm_rotate(q, k, *w, EPS, at, freq, None, adjacent, *out)
+    room = torch.full((b, s + 3, hq + hkv + 1, d), 3.0, dtype=dtype, device="cuda")
+    inside = [room[:, 2:-1, :hq].transpose(1, 2), room[:, 2:-1, hq + 1:].transpose(1, 2)]
+    kp.kp_norm_rotate(q, k, *w, EPS, at, freq, None, adjacent, *inside)
+    assert torch.equal(inside[0], out[0]) and torch.equal(inside[1], out[1])
+    inside[0].fill_(3.0), inside[1].fill_(3.0)
+    assert bool((room == 3.0).all())
+    q2, k2 = q.clone(), k.clone()
+    kp.kp_norm_rotate(q2, k2, *w, EPS, at, freq, None, adjacent, q2, k2)
+    assert torch.equal(q2, out[0]) and torch.equal(k2, out[1])
+    # gradients, over d_y
+    dy = [torch.randn_like(x) for x in (q, k)]
+    results = []
+    for dx in ([torch.empty_like(x) for x in dy], dy):
+        dw = [torch.empty(d, device="cuda") for _ in range(2)]
+        kp.kp_norm_rotate_grad(q, k, *w, EPS, at, freq, None, adjacent, *dy, *dx, *dw, torch.empty(kp.kp_norm_rotate_grad_bytes(q, k), dtype=torch.uint8, device="cuda"))
+        results.append([x.clone() for x in dx] + dw)
+    assert all(torch.equal(x, y) for x, y in zip(*results))
+    # a gradient that is the same for all heads and tokens: strides of 0
+    one = torch.randn(b, 1, 1, d, device="cuda").to(dtype)
+    got = []
+    for dy in ([one.expand(b, n, s, d) for n in (hq, hkv)], [one.expand(b, n, s, d).contiguous() for n in (hq, hkv)]):
+        dx, dw = [torch.empty_like(q), torch.empty_like(k)], [torch.empty(d, device="cuda") for _ in range(2)]
+        kp.kp_norm_rotate_grad(q, k, *w, EPS, at, freq, None, adjacent, *dy, *dx, *dw, torch.empty(kp.kp_norm_rotate_grad_bytes(q, k), dtype=torch.uint8, device="cuda"))
+        got.append(dx + dw)
+    assert all(torch.equal(x, y) for x, y in zip(*got))
+
+
+def test_positions_in_their_forms(kp):
+    b, h, s, d, pairs, dtype = 3, 2, 21, 64, 24, torch.float16
+    gen, q, _, (w, _), at, freq, _ = inputs(13, "bhsd", b, h, 1, s, d, dtype, pairs, 3, "same")
+    run = lambda x, at, axis=None: (kp.kp_norm_rotate(x, None, w, None, EPS, at, freq, axis, False, out := torch.empty_like(x), None), out)[1]  # noqa: E731
+    shared = at[0, 0]
+    assert torch.equal(run(q, shared), run(q, shared.expand(b, s).contiguous()))
+    assert torch.equal(run(q, shared), run(q, shared.expand(b, s)))
+    assert torch.equal(run(q, at[0]), run(q, at, torch.zeros(pairs, dtype=torch.uint8, device="cuda")))
+    # a batch without a dimension of its own
+    flat = q[0].transpose(0, 1)
+    assert torch.equal(run(flat, at[:, 0], None), run(q[:1], at[:1, :1])[0].transpose(0, 1))
+    # an axis that is not there: its pairs stay
+    axis = torch.zeros(pairs, dtype=torch.uint8, device="cuda")
+    axis[5], axis[20] = 3, 255
+    theta = ref.angles(at, freq, axis, b, s)
+    assert float(theta[..., 5].abs().max()) == 0.0
+    assert_within(run(q, at, axis), *ref.forward(q, w, EPS, theta, False))
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,hq,hkv,d,page,pairs,adjacent,weight", [
+    (1, 1, 1, 64, 1, 32, False, "same"), (5, 9, 3, 128, 16, 64, True, "fp32"), (48, 32, 8, 128, 16, 64, False, "same"),
+    (333, 0, 2, 64, 64, 16, False, "fp32"), (1500, 6, 6, 128, 256, 0, False, "none"), (2100, 3, 1, 64, 8, 32, True, "same")])
+def test_write_is_the_two_calls(kp, tokens, hq, hkv, d, page, pairs, adjacent, weight, dtype, e4m3):
+    gen, q, k, w, at, freq, _ = inputs(tokens, "bshd", 1, max(1, hq), hkv, tokens, d, dtype, pairs, 1, weight)
+    q, k = (x[0].transpose(0, 1) for x in (q, k))
+    if hq == 0:
+        q = None
+    v = torch.randn(tokens, hkv, d, device="cuda", generator=gen).to(dtype)
+    v[0, 0, :4] = torch.tensor([math.inf, -math.inf, math.nan, 0.0], dtype=dtype)
+    pages = 2 * tokens // page + 2
+    slots = torch.randperm(pages * page, device="cuda", generator=gen)[:tokens]
+    slots[4::7] = -1
+    slots[5::11] = pages * page + 3
+    results = []
+    for fused in (True, False):
+        halves, exps = new_cache(pages, hkv, page, d, dtype, e4m3)
+        out = None if q is None else torch.full((tokens, hq, d), 7.0, dtype=dtype, device="cuda")
+        if fused:
+            kp.kp_norm_rotate_write(q, k, v, *w, EPS, at[0, 0], freq, None, adjacent, out, slots, *halves, *exps)
+        else:
+            turned = torch.empty(tokens, hkv, d, dtype=dtype, device="cuda")
+            kp.kp_norm_rotate(q, k, *w, EPS, at[0, 0], freq, None, adjacent, out, turned)
+            kp.kp_cache_write(turned, v, slots, *halves, *exps)
+        results.append([x.view(torch.uint8) for x in halves + exps if x is not None] + ([] if out is None else [out]))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def test_nothing_to_do(kp):
+    d, dtype = 64, torch.bfloat16
+    w = torch.ones(d, device="cuda")
+    freq = torch.ones(8, device="cuda")
+    empty = torch.empty(0, 3, d, dtype=dtype, device="cuda")
+    at = torch.empty(0, dtype=torch.int32, device="cuda")
+    kp.kp_norm_rotate(empty, empty, w, w, EPS, at, freq, None, False, empty, empty)
+    dw = [torch.full((d,), 7.0, device="cuda") for _ in range(2)]
+    kp.kp_norm_rotate_grad(empty, empty, w, w, EPS, at, freq, None, False, empty, empty, empty, empty, *dw)
+    assert float(dw[0].abs().sum() + dw[1].abs().sum()) == 0.0
+    # queries alone: the keys' weights get zeros
+    q = torch.randn(4, 3, d, device="cuda").to(dtype)
+    dw[1].fill_(7.0)
+    kp.kp_norm_rotate_grad(q, None, w, w, EPS, torch.arange(4, dtype=torch.int32, device="cuda"), freq, None, False, q, None, torch.empty_like(q), None, *dw,
+                           torch.empty(kp.kp_norm_rotate_grad_bytes(q, None), dtype=torch.uint8, device="cuda"))
+    assert float(dw[1].abs().sum()) == 0.0 and float(dw[0].abs().sum()) > 0.0
+
+
+def test_captured_and_on_another_stream(kp):
+    b, hq, hkv, s, d, pairs, dtype = 2, 8, 2, 300, 128, 64, torch.bfloat16
+    _, q, k, w, at, freq, _ = inputs(17, "bshd", b, hq, hkv, s, d, dtype, pairs, 1, "same")
+    dy = [torch.randn_like(x) for x in (q, k)]
+    workspace = torch.empty(kp.kp_norm_rotate_grad_bytes(q, k), dtype=torch.uint8, device="cuda")
+
+    def both():
+        out, dx, dw = [torch.empty_like(q), torch.empty_like(k)], [torch.empty_like(q), torch.empty_like(k)], [torch.empty(d, device="cuda") for _ in range(2)]
+        kp.kp_norm_rotate(q, k, *w, EPS, at, freq, None, False, *out)
+        kp.kp_norm_rotate_grad(q, k, *w, EPS, at, freq, None, False, *dy, *dx, *dw, workspace)
+        return out + dx + dw
+
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        recorded = both()
+    for n in range(3):
+        q.copy_(torch.randn_like(q))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(recorded, eager)), n
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out = torch.empty_like(q)
+    kp.kp_norm_rotate(q, None, w[0], None, EPS, at, freq, None, False, out, None, stream=side)
+    side.synchronize()
+    assert torch.equal(out, eager[0])
+
+
+def test_offsets_past_32_bits(kp):
+    d, s, dtype = 64, 3, torch.bfloat16
+    step = (1 << 32) + 64
+    room = torch.empty(step + (1 << 16), dtype=dtype, device="cuda")
+    far = room.as_strided((2, 2, s, d), (step, s * d, d, 1))
+    near = torch.randn(2, 2, s, d, device="cuda").to(dtype)
+    far.copy_(near)
+    w, freq = torch.randn(d, device="cuda"), torch.rand(32, device="cuda")
+    at = torch.arange(s, dtype=torch.int32, device="cuda")
+    out = torch.empty_like(near)
+    kp.kp_norm_rotate(near, None, w, None, EPS, at, freq, None, False, out, None)
+    kp.kp_norm_rotate(far, None, w, None, EPS, at, freq, None, False, far, None)
+    assert torch.equal(far, out)
