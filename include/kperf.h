@@ -533,6 +533,21 @@ kp_status kp_cache_read(const kp_cache* cache, const int32_t* block_table, int t
                         int n_seqs, int T, const kp_heads* k, const kp_heads* v, void* stream);
 
 /*
+ * Moves rows of the cache, of all heads, keys and values, as they are: what slot from[i] holds goes to slot to[i] (device, int64),
+ * for i < N.  A move that names no slot of the cache on either side is left out; a slot may be read from by several moves, and is
+ * to be written to by one at most (nothing is said about what it holds otherwise).
+ *   starts NULL      no slot is both read from and written to (a sequence is forked, a page copied)
+ *   starts [n_groups + 1]  (device, non-decreasing numbers from 0 to N) group g has the moves starts[g] .. starts[g + 1] - 1, in
+ *                    order, and nothing in common with other groups' slots.  Up to KP_MOVE_RUN moves: any, done as if all rows
+ *                    were read before one is written (accepted drafts, a permutation).  More: no move may read a slot that
+ *                    an earlier one of its group writes (a sequence that loses tokens and closes up, from its first row on).
+ * Moves that no group has are left out.
+ */
+#define KP_MOVE_RUN 128
+kp_status kp_cache_move(const int64_t* from, const int64_t* to, int N, const int32_t* starts, int n_groups, const kp_cache* cache,
+                        void* stream);
+
+/*
  * Attention of T new tokens over a cache that already holds them: sequence s has the query tokens starts[s] ..
  * starts[s + 1] - 1 (device, n_seqs + 1 non-decreasing numbers from 0 to T; none, one or many per sequence) and lens[s] keys
  * (device, the new ones included; at most table_width * page count).  q, o: kp_heads with seq ignored; lse [Hq, T].  Keys whose

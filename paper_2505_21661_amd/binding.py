@@ -32,6 +32,7 @@ KP_FLAG_REALTIME = 2
 KP_FLAG_HW_IDS = 4
 KP_BF16, KP_FP16, KP_FP32 = 0, 1, 2
 KP_CACHE_SAME, KP_CACHE_E4M3 = 0, 1
+KP_MOVE_RUN = 128  # moves of a group of kp_cache_move that may be any
 
 
 class KperfError(RuntimeError):
@@ -139,6 +140,7 @@ def _optional(L):
         "kp_cache_write": [hp, hp, vp, ci, cp, vp],
         "kp_cache_read": [cp, vp, ci, vp, ci, ci, hp, hp, vp],
         "kp_attn_paged": [hp, cp, vp, ci, vp, vp, hp, vp, ci, ci, ci, ci, ci, fl, vp, sz, u32, vp, sz, vp],
+        "kp_cache_move": [vp, vp, ci, vp, ci, cp, vp],
         "kp_norm_rotate": [hp, hp, vp, vp, ci, fl, tp, hp, hp, ci, ci, ci, ci, ci, ci, vp],
         "kp_norm_rotate_grad": [hp, hp, vp, vp, ci, fl, tp, hp, hp, hp, hp, vp, vp, ci, ci, ci, ci, ci, ci, vp, sz, vp],
         "kp_norm_rotate_write": [hp, hp, hp, vp, vp, ci, fl, tp, hp, vp, ci, ci, cp, vp],
@@ -413,7 +415,7 @@ def _types() -> dict:
     if not _names:
         import torch
 
-        names = {n: getattr(torch, n) for n in ("float32", "uint8", "int32", "int64", "float8_e4m3fn")}
+        names = {n: getattr(torch, n) for n in ("float32", "uint8", "int32", "int64", "float8_e4m3fn", "bfloat16")}
         names.update({torch.bfloat16: KP_BF16, torch.float16: KP_FP16})
         _names = names  # (whole: another thread may be looking)
     return _names
@@ -544,6 +546,19 @@ def kp_cache_read(k_cache, v_cache, k_exp, v_exp, block_table, starts, k, v, str
                                _flat("block_table", block_table, (_names or _types())["int32"]), width,
                                _flat("starts", starts, (_names or _types())["int32"], (n + 1,)), n, T,
                                _heads("k", k, (T, Hkv, D), k.dtype), _heads("v", v, (T, Hkv, D), k.dtype), _stream(stream)))
+
+
+def kp_cache_move(source, target, starts, k_cache, v_cache, k_exp=None, v_exp=None, stream=None) -> None:
+    """Rows of slots source [N] int64 to slots target [N] int64 of the cache, all heads, keys and values.  starts None: no slot is
+    in both; else int32 [n + 1]: groups of moves, each in order (see the header for what groups of more than KP_MOVE_RUN may
+    hold)."""
+    i64, N = (_names or _types())["int64"], source.shape[0]
+    _here(source)
+    # (what the codes of an e4m3 cache are read as does not matter here)
+    kind = k_cache.dtype if k_cache.dtype is not _names["float8_e4m3fn"] else _names["bfloat16"]
+    _check(lib().kp_cache_move(_flat("source", source, i64, (N,)), _flat("target", target, i64, (N,)), N,
+                               0 if starts is None else _flat("starts", starts, _names["int32"]), 0 if starts is None else starts.shape[0] - 1,
+                               _cache_of(k_cache, v_cache, k_exp, v_exp, kind), _stream(stream)))
 
 
 def kp_attn_paged_bytes(q, k_cache, block_table, window: int, sinks: int) -> int:
