@@ -418,7 +418,7 @@ kp_status kp_attn_instrumented(const void* Q, const void* K, const void* V, void
 
 /* ---- attention with windows, caches and gradients ----------------------------------------------
  *
- * The attentions that models train and serve with.  Window and paged attention are further targets, which can be
+ * The attentions that models train and serve with.  Window, paged and tree attention are further targets, which can be
  * recorded; the gradient and the cache calls cannot.  Everywhere below, query token i of n_q stands over n_k keys at
  * position p = n_k - n_q + i and sees key j where
  *     j <= p  and  (window == 0  or  p - j < window  or  j < sinks)
@@ -562,6 +562,24 @@ kp_status kp_attn_paged(const kp_heads* q, const kp_cache* cache, const int32_t*
                         uint32_t region_mask, void* trace_buf, size_t trace_cap, void* stream);
 kp_status kp_attn_paged_launch_shape(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int window,
                                      int sinks, int* n_wg, int* waves_per_wg, int* n_regions);
+
+/*
+ * Attention of T drafted tokens over a cache that holds them: as kp_attn_paged, but for what a token sees.  Sequence s has n_q =
+ * starts[s + 1] - starts[s] drafted tokens, which are the last n_q of its n_k = lens[s] keys: drafted token j is key c + j, c = n_k -
+ * n_q, whatever it follows.  Token i sees
+ *   the drafted keys whose bits are set: bit j % 64 of word j / 64 of seen [T, words] (device, row starts[s] + i; its own bit among
+ *   them, as a rule; bits from n_q on mean nothing, words that there are not, nothing),
+ *   and of the keys j < c, the context, those with window == 0 or p - j < window or j < sinks, where p = c + depth_i and depth [T]
+ *   (device) says how many drafted tokens it follows (below 0: 0; NULL: 0 for all).  A window does not hide drafted keys.
+ * words from 0 to 2^24; seen may be NULL with words = 0.  workspace, recording: as for kp_attn_paged.
+ */
+size_t kp_attn_tree_bytes(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int window, int sinks);
+kp_status kp_attn_tree(const kp_heads* q, const kp_cache* cache, const int32_t* block_table, int table_width, const int32_t* lens,
+                       const int32_t* starts, const int64_t* seen, int words, const int32_t* depth, const kp_heads* o, float* lse,
+                       int T, int n_seqs, int Hq, int window, int sinks, float scale, void* workspace, size_t workspace_bytes,
+                       uint32_t region_mask, void* trace_buf, size_t trace_cap, void* stream);
+kp_status kp_attn_tree_launch_shape(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int window, int sinks,
+                                    int* n_wg, int* waves_per_wg, int* n_regions);
 
 /* ---- what goes into them: queries and keys normed and turned ------------------------------------
  *

@@ -140,6 +140,8 @@ def _optional(L):
         "kp_cache_write": [hp, hp, vp, ci, cp, vp],
         "kp_cache_read": [cp, vp, ci, vp, ci, ci, hp, hp, vp],
         "kp_attn_paged": [hp, cp, vp, ci, vp, vp, hp, vp, ci, ci, ci, ci, ci, fl, vp, sz, u32, vp, sz, vp],
+        "kp_attn_tree": [hp, cp, vp, ci, vp, vp, vp, ci, vp, hp, vp, ci, ci, ci, ci, ci, fl, vp, sz, u32, vp, sz, vp],
+        "kp_attn_tree_launch_shape": [ci] * 9 + [ip] * 3,
         "kp_cache_move": [vp, vp, ci, vp, ci, cp, vp],
         "kp_norm_rotate": [hp, hp, vp, vp, ci, fl, tp, hp, hp, ci, ci, ci, ci, ci, ci, vp],
         "kp_norm_rotate_grad": [hp, hp, vp, vp, ci, fl, tp, hp, hp, hp, hp, vp, vp, ci, ci, ci, ci, ci, ci, vp, sz, vp],
@@ -155,7 +157,8 @@ def _optional(L):
             f = getattr(L, name)
             f.restype = ci
             f.argtypes = args
-    for name, n in (("kp_attn_window_bytes", 8), ("kp_attn_window_grad_bytes", 8), ("kp_attn_paged_bytes", 9), ("kp_norm_rotate_grad_bytes", 5)):
+    for name, n in (("kp_attn_window_bytes", 8), ("kp_attn_window_grad_bytes", 8), ("kp_attn_paged_bytes", 9), ("kp_attn_tree_bytes", 9),
+                    ("kp_norm_rotate_grad_bytes", 5)):
         if hasattr(L, name):
             getattr(L, name).restype = sz
             getattr(L, name).argtypes = [ci] * n
@@ -590,6 +593,42 @@ def kp_attn_paged(q, k_cache, v_cache, k_exp, v_exp, block_table, lens, starts, 
         _flat("block_table", block_table, (_names or _types())["int32"]), width, _flat("lens", lens, (_names or _types())["int32"], (n,)),
         _flat("starts", starts, (_names or _types())["int32"], (n + 1,)), _heads("o", o, q.shape, q.dtype),
         0 if lse is None else _flat("lse", lse, (_names or _types())["float32"], (Hq, T)), T, n, Hq, window, sinks, scale, ws, nbytes,
+        region_mask & 0xFFFFFFFF, _ptr(trace_buf), trace_cap, _stream(stream)))
+
+
+def kp_attn_tree_bytes(q, k_cache, block_table, window: int, sinks: int) -> int:
+    """Bytes of workspace that kp_attn_tree takes for q [T, Hq, D]."""
+    T, Hq, D = q.shape
+    n, width = block_table.shape
+    return int(lib().kp_attn_tree_bytes(T, n, Hq, k_cache.shape[1], D, width, k_cache.shape[2], window, sinks))
+
+
+def kp_attn_tree_launch_shape(q, k_cache, block_table, window: int, sinks: int) -> tuple[int, int, int]:
+    """Workgroups, waves per workgroup and regions of a recording of kp_attn_tree."""
+    T, Hq, D = q.shape
+    n, width = block_table.shape
+    return _shape_of(lib().kp_attn_tree_launch_shape, T, n, Hq, k_cache.shape[1], D, width, k_cache.shape[2], window, sinks)
+
+
+def kp_attn_tree(q, k_cache, v_cache, k_exp, v_exp, block_table, lens, starts, seen, depth, o, lse, window: int, sinks: int,
+                 scale: float, workspace=None, region_mask: int = 0, trace_buf=None, trace_cap: int = 0, stream=None) -> None:
+    """Attention of drafted tokens q [T, Hq, D] over a cache that holds them as the last of each sequence's keys: as kp_attn_paged, but
+    that a token sees the drafted ones that its bits seen [T, words] int64 name (bit j % 64 of word j / 64: drafted token j of its
+    sequence), and the context from position lens - drafted + depth; depth [T] int32 or None."""
+    T, Hq, D = q.shape
+    n, width = block_table.shape
+    if D != k_cache.shape[3]:
+        raise ValueError("q and the cache must have the same D")
+    _here(q)
+    names = _names or _types()
+    i32 = names["int32"]
+    ws, nbytes = _workspace(workspace)
+    words = seen.shape[1]
+    _check(lib().kp_attn_tree(
+        _heads("q", q, q.shape, q.dtype), _cache_of(k_cache, v_cache, k_exp, v_exp, q.dtype), _flat("block_table", block_table, i32), width,
+        _flat("lens", lens, i32, (n,)), _flat("starts", starts, i32, (n + 1,)), _flat("seen", seen, names["int64"], (T, words)), words,
+        0 if depth is None else _flat("depth", depth, i32, (T,)), _heads("o", o, q.shape, q.dtype),
+        0 if lse is None else _flat("lse", lse, names["float32"], (Hq, T)), T, n, Hq, window, sinks, scale, ws, nbytes,
         region_mask & 0xFFFFFFFF, _ptr(trace_buf), trace_cap, _stream(stream)))
 
 

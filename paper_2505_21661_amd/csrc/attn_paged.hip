@@ -29,31 +29,14 @@ extern "C" kp_status kp_attn_paged(const kp_heads* q, const kp_cache* cache, con
                                    int Hq, int window, int sinks, float scale, void* workspace, size_t workspace_bytes, uint32_t region_mask, void* trace_buf,
                                     size_t trace_cap, void* stream) {
   kp::clear_error();
-  if (kp_status s = check_cache(cache)) return s;
-  const int Hkv = cache->Hkv, D = cache->D;
-  if (kp_status s = check_common(Hq, Hkv, D, cache->type, window, sinks, scale)) return s;
-  if (T < 0 || n_seqs < 0 || table_width < 0) return kp::fail(KP_ERR_INVALID_ARG, "T, n_seqs and table_width must not be negative");
-  if (T == 0 || n_seqs == 0) return KP_OK;
-  if (T >= kMostTokens || n_seqs >= kMostTokens || (long long)Hq / Hkv * T >= (1ll << 31)) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "2^30 or more tokens, or 2^31 rows of one head");
-  if ((long long)table_width * cache->page >= kMostTokens) return kp::fail(KP_ERR_UNSUPPORTED_SHAPE, "a block table of 2^30 or more tokens");
-  if (!lens || !starts || ((uintptr_t)lens & 3u) || ((uintptr_t)starts & 3u)) return kp::fail(KP_ERR_INVALID_ARG, "lens and starts must be device memory, 4-byte aligned");
-  if (table_width > 0 && (!block_table || ((uintptr_t)block_table & 3u))) return kp::fail(KP_ERR_INVALID_ARG, "block_table must be device memory, 4-byte aligned");
-  if (kp_status s = check_heads("q", q, 1, Hq, T, D, false)) return s;
-  if (kp_status s = check_heads("o", o, 1, Hq, T, D, true)) return s;
-  if ((uintptr_t)lse & 3u) return kp::fail(KP_ERR_INVALID_ARG, "lse must be 4-byte aligned");
-  const Plan plan = plan_paged(T, n_seqs, Hq, Hkv, D, (long long)table_width * cache->page, window, sinks);
-  if (kp_status s = check_workspace(workspace, workspace_bytes, plan.bytes)) return s;
   Args g{};
-  g.q = heads_of(q, 1, Hq, T); g.o = heads_of(o, 1, Hq, T);
-  g.k.at = static_cast<const uint16_t*>(cache->k); g.v.at = static_cast<const uint16_t*>(cache->v);
-  g.k_exp = cache->k_exp; g.v_exp = cache->v_exp;
-  g.lse = lse; g.lse_head = T;
-  g.table = block_table; g.lens = lens; g.starts = starts;
-  g.table_width = (uint32_t)table_width; g.page_log2 = log2_of(cache->page); g.n_pages = (uint32_t)cache->n_pages;
-  g.seqs = (uint32_t)n_seqs; g.hkv = (uint32_t)Hkv; g.group = (uint32_t)(Hq / Hkv); g.n_q = (uint32_t)T; g.n_k = (uint32_t)(table_width * cache->page);
-  g.window = (uint32_t)window_of(window); g.sinks = (uint32_t)sinks_of(sinks); g.scale_log2 = scale * kLog2e;
+  if (kp_status s = check_paged(g, q, cache, block_table, table_width, lens, starts, o, lse, T, n_seqs, Hq, window, sinks, scale)) return s;
+  if (T == 0 || n_seqs == 0) return KP_OK;
+  const Plan plan = plan_paged(T, n_seqs, Hq, cache->Hkv, cache->D, (long long)table_width * cache->page, window, sinks);
+  if (kp_status s = check_workspace(workspace, workspace_bytes, plan.bytes)) return s;
   g.part = static_cast<float*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
+  const int D = cache->D;
   const bool e4m3 = cache->cache_type == KP_CACHE_E4M3;
 #define KP_PICK(T) (D == 64 ? (e4m3 ? launch<T, 64, kPagedE4m3>(g, plan, region_mask, trace_buf, trace_cap, st) : launch<T, 64, kPaged>(g, plan, region_mask, trace_buf, trace_cap, st)) \
                             : (e4m3 ? launch<T, 128, kPagedE4m3>(g, plan, region_mask, trace_buf, trace_cap, st) : launch<T, 128, kPaged>(g, plan, region_mask, trace_buf, trace_cap, st)))

@@ -77,7 +77,10 @@ struct Heads {
   int64_t seq, head, token;
 };
 
-enum { kPlain = 0, kPaged = 1, kPagedE4m3 = 2 };  // where the keys are: one piece per sequence, pages, pages of e4m3 codes
+// where the keys are: one piece per sequence, pages, pages of e4m3 codes; and pages of which drafted tokens see what their bits name
+enum { kPlain = 0, kPaged = 1, kPagedE4m3 = 2, kTree = 3, kTreeE4m3 = 4 };
+template <int SRC> constexpr bool kCodes = SRC == kPagedE4m3 || SRC == kTreeE4m3;
+template <int SRC> constexpr bool kDrafts = SRC == kTree || SRC == kTreeE4m3;
 
 struct Args {
   Heads q, o, k, v;          // o is written; paged: k, v .at is the cache, q and o have no sequence stride
@@ -95,6 +98,10 @@ struct Args {
   uint32_t region_mask;
   void* trace;
   uint32_t cap_lds, cap_hbm, flush, n_wg, rec_cost, group_log2, collab, flags;
+  // drafted tokens: [n_q][words] bits of 64, [n_q] how deep each stands (may be NULL)
+  const uint32_t* seen;
+  const int32_t* depth;
+  uint32_t words;
 };
 
 // One row tile: which sequence, and which of its rows.  Rows are numbered token by token, the query heads of a group
@@ -218,10 +225,35 @@ struct RowMask {
   __device__ __forceinline__ bool sees_mixed(int c) const { return ((uint32_t)c - from <= count) | (c <= sink); }
 };
 
+// Which keys a drafted token sees of its sequence's drafted ones, the last n_q of n_k: its bits, `words` of 64 of them.
+// Context, the keys in front, is seen as ever, from the position of the context's end and the token's depth.
+struct Drafts {
+  const uint32_t* bits;
+  uint32_t words, n_q;
+  int32_t first;  // the key that the first drafted token is (before the first key there is where n_q > n_k)
+
+  __device__ __forceinline__ Drafts(const Args& g, const Tile& t, uint32_t token)
+      : bits(g.seen + (size_t)(t.q0 + token) * (2u * g.words)), words(2u * g.words), n_q(t.n_q), first((int32_t)t.n_k - (int32_t)t.n_q) {}
+  // Keys start .. start + 31, a bit for each; context is none of them.
+  __device__ __forceinline__ uint32_t of(uint32_t start) const {
+    const int32_t from = (int32_t)start - first, word = from >> 5, left = (int32_t)n_q - from;
+    if ((from <= -32) | (left <= 0)) return 0u;
+    const uint32_t lo = word >= 0 && (uint32_t)word < words ? bits[word] : 0u, hi = (uint32_t)(word + 1) < words ? bits[word + 1] : 0u;
+    const uint32_t some = (uint32_t)(((uint64_t)hi << 32 | lo) >> (from & 31));
+    return left < 32 ? some & ((1u << left) - 1u) : some;
+  }
+  __device__ __forceinline__ bool sees(uint32_t key) const { return (of(key) & 1u) != 0u; }
+};
+// Where a drafted token stands: behind its context, as deep as it says (none where nothing says so).
+__device__ __forceinline__ int32_t draft_position(const Args& g, const Tile& t, uint32_t token) {
+  const int32_t deep = g.depth ? g.depth[t.q0 + token] : 0, most = 1 << 30;
+  return (int32_t)t.n_k - (int32_t)t.n_q + (deep < 0 ? 0 : (deep < most ? deep : most - 1));
+}
+
 // Keys and values of one kv head of one sequence.
 template <int D, int SRC>
 struct Source {
-  static constexpr uint32_t kBytes = SRC == kPagedE4m3 ? D : 2 * D;  // of a row
+  static constexpr uint32_t kBytes = kCodes<SRC> ? D : 2 * D;  // of a row
   const uint8_t *k, *v;
   int64_t k_step, v_step;  // bytes from key to key (kPlain)
   const uint8_t *k_exp, *v_exp;
@@ -392,14 +424,16 @@ __device__ __forceinline__ bool all_nan(const float (&x)[K]) {
 // The softmax of one row.
 template <class T, int D, int SRC>
 struct Row {
-  using In = Rows<T, D, SRC == kPagedE4m3>;
+  using In = Rows<T, D, kCodes<SRC>>;
   float m = kNoKey, l = 0.f, o[In::kElements] = {};
 
-  // over the keys from .. to - 1 that the row sees, which stands at p
+  // over the keys from .. to - 1 that the row sees, which stands at p (drafts: of a drafted token, what else it sees)
   __device__ __forceinline__ void over_keys(const uint16_t* query, const Source<D, SRC>& src, int32_t p, uint32_t window, uint32_t sinks,
-                                            float scale_log2, uint32_t from, uint32_t to) {
-    if (p < 0) return;
-    if (to > (uint32_t)p + 1u) to = (uint32_t)p + 1u;
+                                            float scale_log2, uint32_t from, uint32_t to, const Drafts* drafts = nullptr) {
+    if constexpr (!kDrafts<SRC>) {
+      if (p < 0) return;
+      if (to > (uint32_t)p + 1u) to = (uint32_t)p + 1u;
+    }
     if (from >= to) return;
     float q[In::kElements];
     In::one(query, q);
@@ -407,6 +441,7 @@ struct Row {
       if (l != l) return;  // (a weight that is NaN: so is every value)
       const uint32_t j = j0 + In::place(threadIdx.x & 63u);
       bool seen = (j < to) & ((window == 0u) | ((uint32_t)p - j < window) | (j < sinks));
+      if constexpr (kDrafts<SRC>) seen = (j < to) & ((int32_t)j < drafts->first ? seen : drafts->sees(j));
       uint32_t row = ~0u;
       if (seen) row = src.row_of(j);
       if constexpr (SRC != kPlain) seen = seen & (row != ~0u);
@@ -415,7 +450,7 @@ struct Row {
       const uint32_t some = __builtin_amdgcn_readlane(row, __builtin_ctzll(all));
       row = seen ? row : some;  // (a row that is seen)
       float s = In::products(q, [&](uint32_t lane) __attribute__((always_inline)) { return src.k_at(__shfl(row, (int)lane, 64)); });
-      if constexpr (SRC == kPagedE4m3) s *= power_of(src.k_exp[row]);
+      if constexpr (kCodes<SRC>) s *= power_of(src.k_exp[row]);
       s = seen ? s * scale_log2 : -INFINITY;
       const float top = fmaxf(m, wave_max(s)), alpha = __builtin_amdgcn_exp2f(m - top);
       float w = seen ? __builtin_amdgcn_exp2f(s - top) : 0.f;
@@ -423,7 +458,7 @@ struct Row {
       l = l * alpha + wave_sum(w);
 #pragma unroll
       for (int e = 0; e < In::kElements; ++e) o[e] *= alpha;
-      if constexpr (SRC == kPagedE4m3) w *= power_of(src.v_exp[row]);
+      if constexpr (kCodes<SRC>) w *= power_of(src.v_exp[row]);
       In::add(o, w, seen, [&](uint32_t lane) __attribute__((always_inline)) { return src.v_at(__shfl(row, (int)lane, 64)); });
     }
   }

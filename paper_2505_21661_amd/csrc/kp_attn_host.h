@@ -8,6 +8,7 @@ namespace attn {
 constexpr int64_t kMostTokens = 1 << 30, kMostStep = 1 << 24;
 constexpr int64_t kMostGroups = 1 << 23;  // workgroups of a launch: its threads are counted in 32 bits
 
+inline uint32_t log2_of(int pow2) { return (uint32_t)__builtin_ctz((unsigned)pow2); }
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0u; }
 
 // Strides and alignment of a tensor of heads; `written`: its rows must not overlap.  With one sequence, head or token
@@ -83,6 +84,32 @@ inline kp_status check_cache(const kp_cache* c) {
   return KP_OK;
 }
 
+// A call over a paged cache: its arguments checked and put into `g`, as far as there is anything to do.
+inline kp_status check_paged(Args& g, const kp_heads* q, const kp_cache* cache, const int32_t* block_table, int table_width, const int32_t* lens,
+                             const int32_t* starts, const kp_heads* o, float* lse, int T, int n_seqs, int Hq, int window, int sinks, float scale) {
+  if (kp_status s = check_cache(cache)) return s;
+  const int Hkv = cache->Hkv, D = cache->D;
+  if (kp_status s = check_common(Hq, Hkv, D, cache->type, window, sinks, scale)) return s;
+  if (T < 0 || n_seqs < 0 || table_width < 0) return fail(KP_ERR_INVALID_ARG, "T, n_seqs and table_width must not be negative");
+  if (T == 0 || n_seqs == 0) return KP_OK;
+  if (T >= kMostTokens || n_seqs >= kMostTokens || (long long)Hq / Hkv * T >= (1ll << 31)) return fail(KP_ERR_UNSUPPORTED_SHAPE, "2^30 or more tokens, or 2^31 rows of one head");
+  if ((long long)table_width * cache->page >= kMostTokens) return fail(KP_ERR_UNSUPPORTED_SHAPE, "a block table of 2^30 or more tokens");
+  if (!lens || !starts || ((uintptr_t)lens & 3u) || ((uintptr_t)starts & 3u)) return fail(KP_ERR_INVALID_ARG, "lens and starts must be device memory, 4-byte aligned");
+  if (table_width > 0 && (!block_table || ((uintptr_t)block_table & 3u))) return fail(KP_ERR_INVALID_ARG, "block_table must be device memory, 4-byte aligned");
+  if (kp_status s = check_heads("q", q, 1, Hq, T, D, false)) return s;
+  if (kp_status s = check_heads("o", o, 1, Hq, T, D, true)) return s;
+  if ((uintptr_t)lse & 3u) return fail(KP_ERR_INVALID_ARG, "lse must be 4-byte aligned");
+  g.q = heads_of(q, 1, Hq, T); g.o = heads_of(o, 1, Hq, T);
+  g.k.at = static_cast<const uint16_t*>(cache->k); g.v.at = static_cast<const uint16_t*>(cache->v);
+  g.k_exp = cache->k_exp; g.v_exp = cache->v_exp;
+  g.lse = lse; g.lse_head = T;
+  g.table = block_table; g.lens = lens; g.starts = starts;
+  g.table_width = (uint32_t)table_width; g.page_log2 = log2_of(cache->page); g.n_pages = (uint32_t)cache->n_pages;
+  g.seqs = (uint32_t)n_seqs; g.hkv = (uint32_t)Hkv; g.group = (uint32_t)(Hq / Hkv); g.n_q = (uint32_t)T; g.n_k = (uint32_t)(table_width * cache->page);
+  g.window = (uint32_t)window_of(window); g.sinks = (uint32_t)sinks_of(sinks); g.scale_log2 = scale * kLog2e;
+  return KP_OK;
+}
+
 // Which kernel takes a call, on how many row tiles, and into how many runs the keys of a tile are split.
 struct Plan {
   bool few;
@@ -91,9 +118,9 @@ struct Plan {
 };
 // rows: query rows of a head of keys, of all `seqs` sequences; most_keys: keys that a row tile may have to go over;
 // even: every sequence has rows / seqs of them.
-inline Plan plan_of(long long seqs, long long rows, long long most_keys, int Hkv, int D, bool even) {
+inline Plan plan_of(long long seqs, long long rows, long long most_keys, int Hkv, int D, bool even, bool may_be_few = true) {
   Plan p{};
-  p.few = rows <= 16 * seqs;
+  p.few = may_be_few && rows <= 16 * seqs;
   const long long per_tile = p.few ? 16 : 128;
   p.tiles = even ? (rows / seqs + per_tile - 1) / per_tile * seqs : rows / per_tile + seqs;
   p.units = p.tiles * Hkv;
@@ -123,8 +150,6 @@ inline kp_status launch_shape(const Plan& plan, int* n_wg, int* waves_per_wg, in
   if (n_regions) *n_regions = 3;
   return KP_OK;
 }
-
-inline uint32_t log2_of(int pow2) { return (uint32_t)__builtin_ctz((unsigned)pow2); }
 
 }  // namespace attn
 }  // namespace kp

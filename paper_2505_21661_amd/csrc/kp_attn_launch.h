@@ -35,8 +35,14 @@ inline kp_status recording(Args& g, const Plan& plan, uint32_t region_mask, void
 template <class T, int D, int SRC, int INSTR>
 kp_status launch_as(const Args& g, const Plan& plan, size_t ring_bytes, hipStream_t st) {
   const dim3 grid((uint32_t)(plan.units * plan.splits)), block(kThreads);
-  if (plan.few) hipLaunchKernelGGL((kp_attn_few<T, D, SRC, INSTR>), grid, block, ring_bytes, st, g);
-  else hipLaunchKernelGGL((kp_attn_tile<T, D, SRC, INSTR>), grid, block, tile_lds_bytes<D>() + ring_bytes, st, g);
+  if constexpr (!kDrafts<SRC>) {
+    if (plan.few) {
+      hipLaunchKernelGGL((kp_attn_few<T, D, SRC, INSTR>), grid, block, ring_bytes, st, g);
+      KP_HIP_TRY(hipGetLastError());
+      return KP_OK;
+    }
+  }
+  hipLaunchKernelGGL((kp_attn_tile<T, D, SRC, INSTR>), grid, block, tile_lds_bytes<D>() + ring_bytes, st, g);
   KP_HIP_TRY(hipGetLastError());
   return KP_OK;
 }

@@ -55,6 +55,16 @@ __device__ __forceinline__ float either_half_max(float x) {
   return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
 }
 
+// The largest of a wave's values.
+__device__ __forceinline__ int32_t last_of_wave(int32_t x) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int32_t other = __shfl_xor(x, d, 64);
+    x = x > other ? x : other;
+  }
+  return x;
+}
+
 // Workgroup `id` of units x per items: which unit (a head of keys, of one sequence or of all), which of its items.
 // Workgroups are dealt round-robin to the 8 XCDs, each with its own L2.  All items of a unit go to one XCD where the units
 // can be dealt out evenly; as many units as have places at a time (two workgroups per CU) are taken together, the first
@@ -106,7 +116,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
   constexpr uint32_t kRow = 2u * D, kChunks = kRow / 16u, kTile = kTileKeys * kRow;
   constexpr uint32_t kBlockRows = 1024u / kRow;  // rows of the 1 KiB that a wave's load fills
   constexpr int NS = D / 16, ND = D / 32, NL = (int)(kTile / 4096u);
-  constexpr bool E4M3 = SRC == kPagedE4m3;
+  constexpr bool E4M3 = kCodes<SRC>;
   extern __shared__ __align__(16) unsigned char smem[];  // [K tile][V tile, two buffers][ring]
 
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = wave_uniform(tid >> 6);
@@ -137,9 +147,13 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
     const uint32_t wave_first = tl.first + 32u * wave, flat = wave_first + l32;
     const bool mine = flat <= last_row;
     const RowPlace at = place_of(mine ? flat : last_row, g.group);
-    const int32_t p = (int32_t)tl.n_k - (int32_t)tl.n_q + (int32_t)at.token;
-    const int32_t p_min = (int32_t)wave_uniform((uint32_t)position(wave_first)), p_max = (int32_t)wave_uniform((uint32_t)position(wave_first + 31u));
-    const KeyTiles kt(span_of(position(tl.first), position(tl.first + kTileRows - 1u), g.window, g.sinks));
+    // drafted tokens: positions in the order of the tree, so that the first is the context's end, and any may be the last
+    const int32_t context = (int32_t)tl.n_k - (int32_t)tl.n_q;
+    const int32_t p = kDrafts<SRC> ? draft_position(g, tl, at.token) : context + (int32_t)at.token;
+    const int32_t p_min = kDrafts<SRC> ? context - 1 : (int32_t)wave_uniform((uint32_t)position(wave_first));
+    const int32_t p_max = (int32_t)wave_uniform((uint32_t)(kDrafts<SRC> ? last_of_wave(p) : position(wave_first + 31u)));
+    const KeyTiles kt(kDrafts<SRC> ? span_of(context, (int32_t)tl.n_k - 1, g.window, g.sinks)
+                                   : span_of(position(tl.first), position(tl.first + kTileRows - 1u), g.window, g.sinks));
     const uint32_t t_begin = (uint32_t)((uint64_t)kt.all * split / g.splits), t_end = (uint32_t)((uint64_t)kt.all * (split + 1u) / g.splits);
 
     const uint32_t q_seq = SRC == kPlain ? tl.seq : 0u, head = h * g.group + at.in_group;
@@ -330,8 +344,16 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
       u32x4 pw[4];  // P, in accumulator order: one entry per MFMA step of V^T P^T (16 keys)
       auto mask = [&](int tk) __attribute__((always_inline)) {
         if (!masked) return;
-        RowMask m(p, limit, (int32_t)(start + 4u * h32), g.window, sinks);
-        if ((g.window != 0u) & (start < sinks)) {
+        RowMask m(p, kDrafts<SRC> && context < (int32_t)limit ? (uint32_t)context : limit, (int32_t)(start + 4u * h32), g.window, sinks);
+        const bool mixed = (g.window != 0u) & (start < sinks);
+        if constexpr (kDrafts<SRC>) {
+          const uint32_t bits = end > context ? Drafts(g, tl, at.token).of(start + 32u * (uint32_t)tk) >> (4u * h32) : 0u;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int c = 8 * (v >> 2) + (v & 3);
+            sacc[tk][v] = (m.sees(32 * tk + c) | (mixed & (32 * tk + c <= m.sink)) | (((bits >> c) & 1u) != 0u)) ? sacc[tk][v] : -INFINITY;
+          }
+        } else if (mixed) {
           m.apart();
 #pragma unroll
           for (int v = 0; v < 16; ++v) sacc[tk][v] = m.sees_mixed(32 * tk + 8 * (v >> 2) + (v & 3)) ? sacc[tk][v] : -INFINITY;
@@ -528,10 +550,11 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
         Row<T, D, SRC> row;
         for (uint32_t t = t_begin; t < t_end; ++t) {
           uint32_t limit, unused;
-          const int32_t at = (int32_t)tl.n_k - (int32_t)tl.n_q + (int32_t)a.token;
+          const int32_t at = kDrafts<SRC> ? draft_position(g, tl, a.token) : context + (int32_t)a.token;
+          const Drafts drafts(g, tl, a.token);
           const uint32_t start = kt.start_of(t, &limit, &unused), to = start + kTileKeys, mixed = kt.is_mixed(t) ? kt.mixed : 0u;
-          if (mixed != 0u) row.over_keys(q, src, at, g.window, g.sinks, g.scale_log2, 0u, mixed);
-          row.over_keys(q, src, at, g.window, g.sinks, g.scale_log2, start + mixed, to < limit ? to : limit);
+          if (mixed != 0u) row.over_keys(q, src, at, g.window, g.sinks, g.scale_log2, 0u, mixed, &drafts);
+          row.over_keys(q, src, at, g.window, g.sinks, g.scale_log2, start + mixed, to < limit ? to : limit, &drafts);
         }
         if (g.splits > 1u) {
           const size_t to = split * part_rows + part_row<kTileRows>(g, tile_id, h, 32u * wave + r);
