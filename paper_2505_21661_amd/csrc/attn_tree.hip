@@ -6,7 +6,14 @@ using namespace kp::attn;
 
 static Plan plan_tree(int T, int n_seqs, int Hq, int Hkv, int D, long long most, int window, int sinks) {
   const long long rows = (long long)(Hq / Hkv) * T, tokens = T < kTileRows ? T : kTileRows;
-  return plan_of(n_seqs, rows, most_keys_of(most, tokens, window_of(window), sinks_of(sinks)), Hkv, D, false, false);
+  const long long most_keys = most_keys_of(most, tokens, window_of(window), sinks_of(sinks));
+  Plan p{};
+  p.few = rows <= 64ll * n_seqs;
+  const long long per_tile = p.few ? kDraftRows : kTileRows;
+  p.tiles = rows / per_tile + n_seqs;
+  p.units = p.tiles * Hkv;
+  split_keys(p, p.few ? 2048 : 512, most_keys, per_tile, D);
+  return p;
 }
 
 extern "C" size_t kp_attn_tree_bytes(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int window, int sinks) {

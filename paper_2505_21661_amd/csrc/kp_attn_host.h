@@ -116,11 +116,20 @@ struct Plan {
   long long tiles, splits, units;  // units: heads of keys (of all sequences where a tile belongs to one)
   size_t bytes;                    // workspace
 };
+// Into how many runs the keys go, for about `want` workgroups.
+inline void split_keys(Plan& p, long long want, long long most_keys, long long per_tile, int D) {
+  const long long runs = most_keys < 1536 ? 1 : most_keys / 512;
+  p.splits = p.units * 2 > want ? 1 : want / p.units;
+  if (p.splits > runs) p.splits = runs;
+  if (p.splits > 256) p.splits = 256;
+  if (p.splits < 1) p.splits = 1;
+  p.bytes = p.splits > 1 ? (size_t)p.splits * (size_t)(p.units * per_tile) * (size_t)(D + 2) * 4 : 0;
+}
 // rows: query rows of a head of keys, of all `seqs` sequences; most_keys: keys that a row tile may have to go over;
 // even: every sequence has rows / seqs of them.
-inline Plan plan_of(long long seqs, long long rows, long long most_keys, int Hkv, int D, bool even, bool may_be_few = true) {
+inline Plan plan_of(long long seqs, long long rows, long long most_keys, int Hkv, int D, bool even) {
   Plan p{};
-  p.few = may_be_few && rows <= 16 * seqs;
+  p.few = rows <= 16 * seqs;
   const long long per_tile = p.few ? 16 : 128;
   p.tiles = even ? (rows / seqs + per_tile - 1) / per_tile * seqs : rows / per_tile + seqs;
   p.units = p.tiles * Hkv;
@@ -128,12 +137,7 @@ inline Plan plan_of(long long seqs, long long rows, long long most_keys, int Hkv
   // a run has 512.  Tiles of 128 rows are split to fill the chip (two workgroups per CU: 6 chunks of up to 512 tokens over
   // 8192 keys, 672 workgroups, 125 us, split in two 149); few rows further, since the sequences differ in length (64 tokens
   // over up to 16384 keys, 1024 workgroups 277 us, 4096 261, 8192 267).
-  const long long want = p.few ? 4096 : 512, runs = most_keys < 1536 ? 1 : most_keys / 512;
-  p.splits = p.units * 2 > want ? 1 : want / p.units;
-  if (p.splits > runs) p.splits = runs;
-  if (p.splits > 256) p.splits = 256;
-  if (p.splits < 1) p.splits = 1;
-  p.bytes = p.splits > 1 ? (size_t)p.splits * (size_t)(p.units * per_tile) * (size_t)(D + 2) * 4 : 0;
+  split_keys(p, p.few ? 4096 : 512, most_keys, per_tile, D);
   return p;
 }
 // Keys that the rows of a tile may see: all there are, or the window of its tokens and the sinks.

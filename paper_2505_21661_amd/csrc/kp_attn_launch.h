@@ -1,5 +1,6 @@
 // Launches the attention kernels of a call that has been checked.
 #pragma once
+#include "kp_attn_drafts.h"
 #include "kp_attn_few.h"
 #include "kp_attn_host.h"
 #include "kp_attn_rows.h"
@@ -35,14 +36,10 @@ inline kp_status recording(Args& g, const Plan& plan, uint32_t region_mask, void
 template <class T, int D, int SRC, int INSTR>
 kp_status launch_as(const Args& g, const Plan& plan, size_t ring_bytes, hipStream_t st) {
   const dim3 grid((uint32_t)(plan.units * plan.splits)), block(kThreads);
-  if constexpr (!kDrafts<SRC>) {
-    if (plan.few) {
-      hipLaunchKernelGGL((kp_attn_few<T, D, SRC, INSTR>), grid, block, ring_bytes, st, g);
-      KP_HIP_TRY(hipGetLastError());
-      return KP_OK;
-    }
-  }
-  hipLaunchKernelGGL((kp_attn_tile<T, D, SRC, INSTR>), grid, block, tile_lds_bytes<D>() + ring_bytes, st, g);
+  if (plan.few) {
+    if constexpr (kDrafts<SRC>) hipLaunchKernelGGL((kp_attn_drafts<T, D, SRC, INSTR>), grid, block, ring_bytes, st, g);
+    else hipLaunchKernelGGL((kp_attn_few<T, D, SRC, INSTR>), grid, block, ring_bytes, st, g);
+  } else hipLaunchKernelGGL((kp_attn_tile<T, D, SRC, INSTR>), grid, block, tile_lds_bytes<D>() + ring_bytes, st, g);
   KP_HIP_TRY(hipGetLastError());
   return KP_OK;
 }
@@ -60,10 +57,11 @@ kp_status launch(Args& g, const Plan& plan, uint32_t region_mask, void* trace_bu
     return s;
   if (plan.splits > 1) {
     constexpr bool kPages = SRC != kPlain;
+    constexpr int kFew = kDrafts<SRC> ? kDraftRows : kFewRows;
     const bool wide = plan.splits > (long long)kJoinAtOnce;
-    const dim3 grid((uint32_t)(plan.units * (plan.few ? kFewRows : kTileRows) / (wide ? 1 : kJoinRows))), block(kThreads);
-    if (plan.few && wide) hipLaunchKernelGGL((kp_attn_join<T, D, kFewRows, kPages, true>), grid, block, 0, st, g);
-    else if (plan.few) hipLaunchKernelGGL((kp_attn_join<T, D, kFewRows, kPages, false>), grid, block, 0, st, g);
+    const dim3 grid((uint32_t)(plan.units * (plan.few ? kFew : kTileRows) / (wide ? 1 : kJoinRows))), block(kThreads);
+    if (plan.few && wide) hipLaunchKernelGGL((kp_attn_join<T, D, kFew, kPages, true>), grid, block, 0, st, g);
+    else if (plan.few) hipLaunchKernelGGL((kp_attn_join<T, D, kFew, kPages, false>), grid, block, 0, st, g);
     else if (wide) hipLaunchKernelGGL((kp_attn_join<T, D, kTileRows, kPages, true>), grid, block, 0, st, g);
     else hipLaunchKernelGGL((kp_attn_join<T, D, kTileRows, kPages, false>), grid, block, 0, st, g);
     KP_HIP_TRY(hipGetLastError());
