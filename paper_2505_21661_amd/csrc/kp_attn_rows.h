@@ -451,6 +451,7 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_tile(Args g) {
       if constexpr (MORE) { requested(); valid = valid_next; }
       __builtin_amdgcn_s_setprio(0);
       if constexpr (MORE) KP_BOUNDARY(ring, 2, 0); else KP_BOUNDARY(ring, 2, kp::kNoRegion);
+      if constexpr (!MORE && INSTR != 0) kp::sample_landed(ring);  // (registers are spilled between the loop and the trace's end)
     };
     if (t_begin < t_end) {
       load_page_ids(t_begin, std::true_type{});

@@ -225,6 +225,10 @@ __device__ __forceinline__ void boundary(Ring& r, uint32_t end_region, uint32_t 
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// Waits for the last site's sample, where the compiler may move or spill its registers before the next site (it takes them as
+// written at once: what it copied would be the old contents, and the sample would land on whatever they hold by then).
+__device__ __forceinline__ void sample_landed(Ring& r) { asm volatile("s_waitcnt lgkmcnt(0)" : "+s"(r.pend_t)); }
+
 // The same site for the case "every region enabled, circular strategy", without a branch (the calibration kernel
 // measures it next to the other two forms).
 // Every instruction here is paid once per wave and site (a wave issues roughly one instruction
