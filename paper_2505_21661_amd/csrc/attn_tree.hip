@@ -4,11 +4,11 @@
 
 using namespace kp::attn;
 
-static Plan plan_tree(int T, int n_seqs, int Hq, int Hkv, int D, long long most, int window, int sinks) {
+static Plan plan_tree(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int window, int sinks) {
   const long long rows = (long long)(Hq / Hkv) * T, tokens = T < kTileRows ? T : kTileRows;
-  const long long most_keys = most_keys_of(most, tokens, window_of(window), sinks_of(sinks));
+  const long long most_keys = most_keys_of((long long)table_width * page, tokens, window_of(window), sinks_of(sinks));
   Plan p{};
-  p.few = rows <= 64ll * n_seqs;
+  p.few = rows <= 64ll * n_seqs && page >= kDraftPage;
   const long long per_tile = p.few ? kDraftRows : kTileRows;
   p.tiles = rows / per_tile + n_seqs;
   p.units = p.tiles * Hkv;
@@ -18,7 +18,7 @@ static Plan plan_tree(int T, int n_seqs, int Hq, int Hkv, int D, long long most,
 
 extern "C" size_t kp_attn_tree_bytes(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int window, int sinks) {
   if (T < 1 || n_seqs < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv || (D != 64 && D != 128) || table_width < 0 || page < 1 || window < 0 || sinks < 0) return 0;
-  return plan_tree(T, n_seqs, Hq, Hkv, D, (long long)table_width * page, window, sinks).bytes;
+  return plan_tree(T, n_seqs, Hq, Hkv, D, table_width, page, window, sinks).bytes;
 }
 
 extern "C" kp_status kp_attn_tree_launch_shape(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int window,
@@ -26,7 +26,7 @@ extern "C" kp_status kp_attn_tree_launch_shape(int T, int n_seqs, int Hq, int Hk
   kp::clear_error();
   if (kp_status s = check_common(Hq, Hkv, D, KP_BF16, window, sinks, 1.f)) return s;
   if (T < 1 || n_seqs < 1 || table_width < 0 || page < 1) return kp::fail(KP_ERR_INVALID_ARG, "T, n_seqs and page must be positive, table_width not negative");
-  return launch_shape(plan_tree(T, n_seqs, Hq, Hkv, D, (long long)table_width * page, window, sinks), n_wg, waves_per_wg, n_regions);
+  return launch_shape(plan_tree(T, n_seqs, Hq, Hkv, D, table_width, page, window, sinks), n_wg, waves_per_wg, n_regions);
 }
 
 extern "C" kp_status kp_attn_tree(const kp_heads* q, const kp_cache* cache, const int32_t* block_table, int table_width,
@@ -41,7 +41,7 @@ extern "C" kp_status kp_attn_tree(const kp_heads* q, const kp_cache* cache, cons
   if (T == 0 || n_seqs == 0) return KP_OK;
   if ((words > 0 && !seen) || ((uintptr_t)seen & 7u)) return kp::fail(KP_ERR_INVALID_ARG, "seen must be device memory, 8-byte aligned");
   if ((uintptr_t)depth & 3u) return kp::fail(KP_ERR_INVALID_ARG, "depth must be device memory, 4-byte aligned");
-  const Plan plan = plan_tree(T, n_seqs, Hq, cache->Hkv, cache->D, (long long)table_width * cache->page, window, sinks);
+  const Plan plan = plan_tree(T, n_seqs, Hq, cache->Hkv, cache->D, table_width, cache->page, window, sinks);
   if (kp_status s = check_workspace(workspace, workspace_bytes, plan.bytes)) return s;
   g.part = static_cast<float*>(workspace);
   g.seen = reinterpret_cast<const uint32_t*>(seen); g.depth = depth; g.words = (uint32_t)words;
