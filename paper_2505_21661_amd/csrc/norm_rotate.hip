@@ -13,17 +13,17 @@
 namespace {
 using namespace kp::attn;
 
-constexpr uint32_t kThreads = 256, kAtOnce = 4;  // rows of a thread whose loads are in flight together
+constexpr uint32_t kThreads = 256;
 
 struct RotateArgs {
   Heads x[2], y[2];          // queries and keys (gradient: d_y and d_x); y is written
   Heads in[2];               // gradient: what was normed
   const void* weight[2];
   float* d_weight[2];
-  uint32_t heads[2], chunks[2];  // chunk of heads: what a workgroup takes
+  uint32_t heads[2], chunk;  // chunk: heads (of queries, keys and values, one behind the other) that a workgroup takes
   uint32_t tokens, per_seq;  // tokens of all sequences, and of one
   uint32_t tile_log2, tiles; // tokens side by side in a workgroup, and how many times as many there are
-  uint32_t per;              // heads that a thread goes over
+  uint32_t heads_first;      // neighbouring threads have neighbouring heads, not tokens
   float eps;
   uint32_t fp32_weights;
   const int32_t* at;
@@ -54,19 +54,19 @@ __device__ __forceinline__ float row_sum(float s) {
   return s;
 }
 
-// cos and sin of position * freq: the angle in turns in 64 bits, less whole quarters, and the Taylor series up to an eighth of
-// a turn (they end 2^-29 and 2^-32 from the functions).  With |freq| <= 1 off by at most 2^-22 for any position of 31 bits.
-__device__ __forceinline__ void turn_of(int32_t position, float freq, float* cos, float* sin) {
-  const double turns = (double)position * ((double)freq * 0.15915494309189535);
-  const double quarters = __builtin_rint(4.0 * turns);
-  const float z = (float)((turns - 0.25 * quarters) * 6.283185307179586);
-  const uint32_t q = (uint32_t)(int32_t)(quarters - 4.0 * __builtin_floor(0.25 * quarters));
-  const float z2 = z * z;
+// cos and sin of position * freq.  The angle in turns is taken in 64 bits, its fraction in 32 as a whole number (the low word of a
+// double whose last place is 2^-32 turns), of which the nearest quarter goes off; what is left, up to an eighth of a turn, goes into the
+// Taylor series (they end 2^-29 and 2^-32 from the functions).  With |freq| <= 1 off by at most 2^-21 for any position of 31 bits.
+__device__ __forceinline__ void turn_of(int32_t position, double freq_turns, float* cos, float* sin) {
+  const double at = (double)position, whole = __builtin_rint(at * freq_turns), part = __builtin_fma(at, freq_turns, -whole);
+  const uint32_t u = (uint32_t)__builtin_bit_cast(uint64_t, __builtin_fma(part, 4294967296.0, 6755399441055744.0));
+  const uint32_t q = (u + 0x20000000u) >> 30;
+  const float z = (float)(int32_t)(u - (q << 30)) * 1.4629180792671596e-09f, z2 = z * z;  // 2 pi / 2^32
   const float s = z * __builtin_fmaf(z2, __builtin_fmaf(z2, __builtin_fmaf(z2, __builtin_fmaf(z2, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), 1.f);
   const float c = __builtin_fmaf(z2, __builtin_fmaf(z2, __builtin_fmaf(z2, __builtin_fmaf(z2, __builtin_fmaf(z2, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
   const float a = (q & 1u) ? s : c, b = (q & 1u) ? c : s;
-  *cos = ((q + 1u) & 2u) ? -a : a;
-  *sin = (q & 2u) ? -b : b;
+  *cos = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, a) ^ (((q + 1u) & 2u) << 30));
+  *sin = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, b) ^ ((q & 2u) << 30));
 }
 
 template <class T>
@@ -115,7 +115,7 @@ struct Turn {
     for (int i = 0; i < (ADJACENT ? 4 : 8); ++i) {
       const uint32_t axis = g.axis ? g.axis[first + i] : 0u;
       float co = 1.f, si = 0.f;
-      if (axis < g.axes) turn_of(at[g.axis_step * (int64_t)axis], g.freq[first + i], &co, &si);
+      if (axis < g.axes) turn_of(at[g.axis_step * (int64_t)axis], (double)g.freq[first + i] * 0.15915494309189535, &co, &si);
       if constexpr (ADJACENT) { cos[2 * i] = cos[2 * i + 1] = co; sin[2 * i] = -si; sin[2 * i + 1] = si; }
       else { cos[i] = co; sin[i] = lower ? -si : si; }
     }
@@ -157,9 +157,9 @@ __device__ __forceinline__ float norm_of(float (&x)[8], float eps, float* factor
   return __builtin_amdgcn_rsqf(__builtin_fmaf(ss, 1.0f / D, eps));
 }
 
-// Which heads a thread has, of queries (0), keys (1) or values (2): head, head + step, .. before end.
+// Which rows of a workgroup's tokens and heads a thread has: token `token` of the tile, heads `head`, head + step, ..
 struct Mine {
-  uint32_t which, head, step, end, slot, c;
+  uint32_t token, head, slot, c;
 };
 template <int D>
 __device__ __forceinline__ Mine mine_of(const RotateArgs& g) {
@@ -167,162 +167,184 @@ __device__ __forceinline__ Mine mine_of(const RotateArgs& g) {
   Mine m;
   m.c = threadIdx.x % kLanes;
   m.slot = threadIdx.x / kLanes;
-  m.which = 0;
-  uint32_t chunk = blockIdx.y;
-  if (chunk >= g.chunks[0]) { chunk -= g.chunks[0]; m.which = 1; }
-  if (m.which == 1 && chunk >= g.chunks[1]) { chunk -= g.chunks[1]; m.which = 2; }
-  const uint32_t heads = g.heads[m.which == 0u ? 0u : 1u];
-  m.step = kSlots >> g.tile_log2;
-  const uint32_t first = chunk * m.step * g.per;
-  m.head = first + (m.slot >> g.tile_log2);
-  m.end = first + m.step * g.per < heads ? first + m.step * g.per : heads;
+  const uint32_t step_log2 = __builtin_ctz(kSlots) - g.tile_log2;
+  m.token = g.heads_first ? m.slot >> step_log2 : m.slot & ((1u << g.tile_log2) - 1u);
+  m.head = g.heads_first ? m.slot & ((1u << step_log2) - 1u) : m.slot >> g.tile_log2;
   return m;
 }
 
-// WRITE: 0 keys go to a tensor, 1 to a cache in 16 bits, 2 to one of e4m3 codes; so do values then.
-template <class T, int D, bool ADJACENT, int WRITE>
-__global__ __launch_bounds__(kThreads) void kp_norm_rotate_rows(RotateArgs g) {
-  const Mine m = mine_of<D>(g);
-  const uint32_t w = m.which & 1u;
-  const Heads src = m.which == 2u ? g.v : g.x[w], dst = g.y[w];
-  const bool cached = WRITE != 0 && m.which != 0u, turns = m.which != 2u, normed = turns && g.weight[w] != nullptr;
-  Turn<ADJACENT> turn(g, m.c);
-  float mine[8], others[8];
-  if (turns) {
-    weights_of<T>(g.weight[w], g.fp32_weights != 0u, 8u * m.c, mine);
-    weights_of<T>(g.weight[w], g.fp32_weights != 0u, 8u * turn.partner_of(m.c), others);
-  }
-  for (uint32_t t = blockIdx.x; t < g.tiles; t += gridDim.x) {
-    const uint32_t n = (t << g.tile_log2) + (m.slot & ((1u << g.tile_log2) - 1u)), at = n < g.tokens ? n : g.tokens - 1u;
-    const uint32_t seq = at / g.per_seq, token = at - seq * g.per_seq;
-    const uint16_t* const from = src.at + src.seq * (int64_t)seq + src.token * (int64_t)token + 8u * m.c;
-    uint16_t* const to = const_cast<uint16_t*>(dst.at) + dst.seq * (int64_t)seq + dst.token * (int64_t)token + 8u * m.c;
-    int64_t slot = 0;
-    if (cached) slot = g.slots[at];
-    const bool there = n < g.tokens && (!cached || (slot >= 0 && (uint64_t)slot < g.n_slots));
-    float a[8], b[8];
-    if (turns) {
-      turn.angles(g, m.c, seq, token);
+// Goes over heads first .. end - 1 of a tensor, `step` apart: load(i, head, there) of a few at a time, then work(i, head, there).
+template <uint32_t AT_ONCE, class Load, class Work>
+__device__ __forceinline__ void over_heads(uint32_t first, uint32_t end, uint32_t step, uint32_t mine, Load load, Work work) {
+  for (uint32_t h0 = first; h0 < end; h0 += step * AT_ONCE) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        a[e] = mine[e] * turn.cos[e];
-        b[e] = others[ADJACENT ? e ^ 1 : e] * turn.sin[e];
-      }
+    for (uint32_t i = 0; i < AT_ONCE; ++i) {
+      const uint32_t h = h0 + step * i + mine;
+      if (h0 + step * i < end) load(i, h < end ? h : end - 1u);
     }
-    for (uint32_t i0 = 0; i0 < g.per; i0 += kAtOnce) {
-      u32x4 raw[kAtOnce];
 #pragma unroll
-      for (uint32_t i = 0; i < kAtOnce; ++i) {
-        const uint32_t h = m.head + m.step * (i0 + i);
-        if (i0 + i < g.per) raw[i] = *reinterpret_cast<const u32x4*>(from + src.head * (int64_t)(h < m.end ? h : m.end - 1u));
-      }
-#pragma unroll
-      for (uint32_t i = 0; i < kAtOnce; ++i) {
-        if (i0 + i >= g.per) break;
-        const uint32_t h = m.head + m.step * (i0 + i);
-        u32x4 out = raw[i];
-        if (turns) {
-          float x[8], o[8], y[8], r = 1.f, factor = 1.f;
-          widen<T>(raw[i], x);
-          widen<T>(turn.partners(raw[i]), o);
-          if (normed) r = norm_of<T, D>(x, g.eps, &factor);
-          const float r_o = r * factor;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = __builtin_fmaf(r * x[e], a[e], (r_o * o[e]) * b[e]);
-          out = narrow<T>(y);
-        }
-        if (!there || h >= m.end) continue;
-        if (cached) {
-          const uint32_t row = row_of_slot((uint64_t)slot, h, g.heads[1], g.page_log2);
-          put_row<T, D, WRITE == 2>(out, m.which == 2u ? g.v_cache : g.k_cache, m.which == 2u ? g.v_exp : g.k_exp, row, m.c);
-        } else {
-          *reinterpret_cast<u32x4*>(to + dst.head * (int64_t)h) = out;
-        }
-      }
+    for (uint32_t i = 0; i < AT_ONCE; ++i) {
+      const uint32_t h = h0 + step * i + mine;
+      if (h0 + step * i < end) work(i, h < end ? h : end - 1u, h < end);
     }
   }
 }
 
-template <class T, int D, bool ADJACENT>
-__global__ __launch_bounds__(kThreads) void kp_norm_rotate_back(RotateArgs g) {
-  constexpr uint32_t kSlots = kThreads / (D / 8);
-  __shared__ float sums[kSlots][D];
+// Bound by memory.  In sequences of 8192 tokens with 32/8 heads of 128 of bf16 side by side, four of them on three axes, 671 MB take
+// 148 us (4530 GB/s; a copy 5120).  What counts is the order of the rows: neighbouring lanes take those that are neighbours in memory, heads
+// of a token here; with tokens in their place, 8 KB apart and so on few of the L2's channels, 173 us.  Eight rows of a thread in
+// flight 148, four 161 (into a cache, whose rows take more registers: four 39.7 us for 12001 tokens, eight 45).  Rows are read past
+// the caches, once: 161 us and 39.7, through them 163 and 44.
+// WRITE: 0 keys go to a tensor, 1 to a cache in 16 bits, 2 to one of e4m3 codes; so do values then.
+template <class T, int D, bool ADJACENT, int WRITE>
+__global__ __launch_bounds__(kThreads) void kp_norm_rotate_rows(RotateArgs g) {
+  constexpr uint32_t kSlots = kThreads / (D / 8), kAtOnce = WRITE == 0 ? 8 : 4;
   const Mine m = mine_of<D>(g);
-  const uint32_t w = m.which;
-  const Heads src = g.x[w], in = g.in[w], dst = g.y[w];
-  const bool normed = g.weight[w] != nullptr;
+  const uint32_t step = kSlots >> g.tile_log2;
+  const uint32_t begin = blockIdx.y * g.chunk, end = begin + g.chunk;  // of the heads of all tensors, one behind the other
   Turn<ADJACENT> turn(g, m.c);
-  float weight[8], dw[8];
-  weights_of<T>(g.weight[w], g.fp32_weights != 0u, 8u * m.c, weight);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) dw[e] = 0.f;
   for (uint32_t t = blockIdx.x; t < g.tiles; t += gridDim.x) {
-    const uint32_t n = (t << g.tile_log2) + (m.slot & ((1u << g.tile_log2) - 1u)), at = n < g.tokens ? n : g.tokens - 1u;
+    const uint32_t n = (t << g.tile_log2) + m.token, at = n < g.tokens ? n : g.tokens - 1u;
     const uint32_t seq = at / g.per_seq, token = at - seq * g.per_seq;
-    const uint16_t* const from = src.at + src.seq * (int64_t)seq + src.token * (int64_t)token + 8u * m.c;
-    const uint16_t* const from_x = normed ? in.at + in.seq * (int64_t)seq + in.token * (int64_t)token + 8u * m.c : from;
-    const int64_t x_head = normed ? in.head : src.head;
-    uint16_t* const to = const_cast<uint16_t*>(dst.at) + dst.seq * (int64_t)seq + dst.token * (int64_t)token + 8u * m.c;
+    int64_t slot = 0;
+    if constexpr (WRITE != 0) slot = g.slots[at];
     turn.angles(g, m.c, seq, token);
-    for (uint32_t i0 = 0; i0 < g.per; i0 += kAtOnce) {
-      u32x4 raw[kAtOnce], raw_x[kAtOnce];
+    uint32_t before = 0;  // heads of the tensors ahead
 #pragma unroll
-      for (uint32_t i = 0; i < kAtOnce; ++i) {
-        const uint32_t h = m.head + m.step * (i0 + i);
-        const int64_t there = h < m.end ? h : m.end - 1u;
-        if (i0 + i >= g.per) continue;
-        raw[i] = *reinterpret_cast<const u32x4*>(from + src.head * there);
-        if (normed) raw_x[i] = *reinterpret_cast<const u32x4*>(from_x + x_head * there);
+    for (int w = 0; w < (WRITE != 0 ? 3 : 2); ++w) {
+      const uint32_t heads = g.heads[w == 0 ? 0 : 1], first = begin > before ? begin - before : 0u, last = end > before ? min(end - before, heads) : 0u;
+      before += heads;
+      if (first >= last) continue;
+      const Heads src = w == 2 ? g.v : g.x[w & 1], dst = g.y[w & 1];
+      const uint16_t* const from = src.at + src.seq * (int64_t)seq + src.token * (int64_t)token + 8u * m.c;
+      uint16_t* const to = const_cast<uint16_t*>(dst.at) + dst.seq * (int64_t)seq + dst.token * (int64_t)token + 8u * m.c;
+      const bool cached = WRITE != 0 && w != 0, normed = w != 2 && g.weight[w & 1] != nullptr;
+      const bool there = n < g.tokens && (!cached || (slot >= 0 && (uint64_t)slot < g.n_slots));
+      float a[8], b[8];
+      if (w != 2) {
+        weights_of<T>(g.weight[w & 1], g.fp32_weights != 0u, 8u * m.c, a);
+        weights_of<T>(g.weight[w & 1], g.fp32_weights != 0u, 8u * turn.partner_of(m.c), b);
+        if constexpr (ADJACENT)
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) { const float x = b[e]; b[e] = b[e + 1]; b[e + 1] = x; }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { a[e] *= turn.cos[e]; b[e] *= turn.sin[e]; }
       }
+      u32x4 raw[kAtOnce];
+      over_heads<kAtOnce>(
+          first, last, step, m.head, [&](uint32_t i, uint32_t h) __attribute__((always_inline)) { raw[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from + src.head * (int64_t)h)); },
+          [&](uint32_t i, uint32_t h, bool is_head) __attribute__((always_inline)) {
+            u32x4 out = raw[i];
+            if (w != 2) {
+              float x[8], o[8], y[8], r = 1.f, factor = 1.f;
+              widen<T>(raw[i], x);
+              widen<T>(turn.partners(raw[i]), o);
+              if (normed) r = norm_of<T, D>(x, g.eps, &factor);
+              const float r_o = r * factor;
 #pragma unroll
-      for (uint32_t i = 0; i < kAtOnce; ++i) {
-        if (i0 + i >= g.per) break;
-        const uint32_t h = m.head + m.step * (i0 + i);
-        const bool there = n < g.tokens && h < m.end;
-        float d[8], o[8], y[8];
-        widen<T>(raw[i], d);
-        widen<T>(turn.partners(raw[i]), o);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = __builtin_fmaf(d[e], turn.cos[e], -o[e] * turn.sin[e]);
-        if (normed) {
-          float x[8], factor, dot = 0.f;
-          widen<T>(raw_x[i], x);
-          const float r = norm_of<T, D>(x, g.eps, &factor);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            x[e] *= r;
-            dw[e] = there ? __builtin_fmaf(y[e], x[e], dw[e]) : dw[e];
-            y[e] *= weight[e];
-            dot = __builtin_fmaf(y[e], x[e], dot);
-          }
-          dot = row_sum<D>(dot) * (1.0f / D);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = r * factor * __builtin_fmaf(-x[e], dot, y[e]);
-        }
-        if (there) *reinterpret_cast<u32x4*>(to + dst.head * (int64_t)h) = narrow<T>(y);
-      }
+              for (int e = 0; e < 8; ++e) y[e] = __builtin_fmaf(r * x[e], a[e], (r_o * o[e]) * b[e]);
+              out = narrow<T>(y);
+            }
+            if (!there || !is_head) return;
+            if (cached) {
+              const uint32_t row = row_of_slot((uint64_t)slot, h, g.heads[1], g.page_log2);
+              put_row<T, D, WRITE == 2>(out, w == 2 ? g.v_cache : g.k_cache, w == 2 ? g.v_exp : g.k_exp, row, m.c);
+            } else {
+              *reinterpret_cast<u32x4*>(to + dst.head * (int64_t)h) = out;
+            }
+          });
     }
   }
-  if (!normed) return;
+}
+
+// Bound by memory: 8192 tokens of 32/8 heads of 128, 252 MB, take 52 us with the join (4830 GB/s); before the join had eight loads in flight 59, with 512, 1024 and 256
+// workgroups instead of 768 67, 74 and 98.
+template <class T, int D, bool ADJACENT>
+__global__ __launch_bounds__(kThreads) void kp_norm_rotate_back(RotateArgs g) {
+  constexpr uint32_t kSlots = kThreads / (D / 8), kBackAtOnce = 4;
+  __shared__ float sums[kSlots][D];
+  const Mine m = mine_of<D>(g);
+  const uint32_t step = kSlots >> g.tile_log2;
+  const uint32_t begin = blockIdx.y * g.chunk, end = begin + g.chunk;
+  Turn<ADJACENT> turn(g, m.c);
+  float dw[2][8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sums[m.slot][8u * m.c + e] = dw[e];
-  __syncthreads();
-  if (threadIdx.x < (uint32_t)D) {
-    float s = 0.f;
-    for (uint32_t i = 0; i < kSlots; ++i) s += sums[i][threadIdx.x];
-    g.part[((size_t)blockIdx.y * gridDim.x + blockIdx.x) * D + threadIdx.x] = s;
+  for (int e = 0; e < 8; ++e) dw[0][e] = dw[1][e] = 0.f;
+  for (uint32_t t = blockIdx.x; t < g.tiles; t += gridDim.x) {
+    const uint32_t n = (t << g.tile_log2) + m.token, at = n < g.tokens ? n : g.tokens - 1u;
+    const uint32_t seq = at / g.per_seq, token = at - seq * g.per_seq;
+    turn.angles(g, m.c, seq, token);
+    uint32_t before = 0;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const uint32_t heads = g.heads[w], first = begin > before ? begin - before : 0u, last = end > before ? min(end - before, heads) : 0u;
+      before += heads;
+      if (first >= last) continue;
+      const Heads src = g.x[w], in = g.in[w], dst = g.y[w];
+      const bool normed = g.weight[w] != nullptr;
+      const uint16_t* const from = src.at + src.seq * (int64_t)seq + src.token * (int64_t)token + 8u * m.c;
+      const uint16_t* const from_x = normed ? in.at + in.seq * (int64_t)seq + in.token * (int64_t)token + 8u * m.c : from;
+      uint16_t* const to = const_cast<uint16_t*>(dst.at) + dst.seq * (int64_t)seq + dst.token * (int64_t)token + 8u * m.c;
+      float weight[8];
+      weights_of<T>(g.weight[w], g.fp32_weights != 0u, 8u * m.c, weight);
+      u32x4 raw[kBackAtOnce], raw_x[kBackAtOnce];
+      over_heads<kBackAtOnce>(
+          first, last, step, m.head,
+          [&](uint32_t i, uint32_t h) __attribute__((always_inline)) {
+            raw[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from + src.head * (int64_t)h));
+            if (normed) raw_x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from_x + in.head * (int64_t)h));
+          },
+          [&](uint32_t i, uint32_t h, bool is_head) __attribute__((always_inline)) {
+            const bool there = n < g.tokens && is_head;
+            float d[8], o[8], y[8];
+            widen<T>(raw[i], d);
+            widen<T>(turn.partners(raw[i]), o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = __builtin_fmaf(d[e], turn.cos[e], -o[e] * turn.sin[e]);
+            if (normed) {
+              float x[8], factor, dot = 0.f;
+              widen<T>(raw_x[i], x);
+              const float r = norm_of<T, D>(x, g.eps, &factor);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                x[e] *= r;
+                dw[w][e] = there ? __builtin_fmaf(y[e], x[e], dw[w][e]) : dw[w][e];
+                y[e] *= weight[e];
+                dot = __builtin_fmaf(y[e], x[e], dot);
+              }
+              dot = row_sum<D>(dot) * (1.0f / D);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) y[e] = r * factor * __builtin_fmaf(-x[e], dot, y[e]);
+            }
+            if (there) *reinterpret_cast<u32x4*>(to + dst.head * (int64_t)h) = narrow<T>(y);
+          });
+    }
+  }
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    if (!g.weight[w]) continue;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[m.slot][8u * m.c + e] = dw[w][e];
+    __syncthreads();
+    if (threadIdx.x < (uint32_t)D) {
+      float s = 0.f;
+      for (uint32_t i = 0; i < kSlots; ++i) s += sums[i][threadIdx.x];
+      g.part[((size_t)w * gridDim.x * gridDim.y + blockIdx.y * gridDim.x + blockIdx.x) * D + threadIdx.x] = s;
+    }
   }
 }
 
 // The workgroups' sums of d_w, added up: 32 values of a head to a workgroup, blockIdx.y: queries' or keys'.
 constexpr uint32_t kJoinRows = 32;
-__global__ __launch_bounds__(32 * kJoinRows) void kp_norm_rotate_join(RotateArgs g, uint32_t per_chunk, uint32_t D) {
+__global__ __launch_bounds__(32 * kJoinRows) void kp_norm_rotate_join(RotateArgs g, uint32_t rows, uint32_t D) {
   __shared__ float sums[kJoinRows][33];
   const uint32_t w = blockIdx.y, c = threadIdx.x & 31u, r = threadIdx.x >> 5;
   if (!g.weight[w]) return;
-  const uint32_t rows = g.chunks[w] * per_chunk, d = 32u * blockIdx.x + c;
-  const float* const part = g.part + (w ? (size_t)g.chunks[0] * per_chunk * D : 0) + d;
+  const uint32_t d = 32u * blockIdx.x + c;
+  const float* const part = g.part + (size_t)w * rows * D + d;
   float s = 0.f;
+#pragma unroll 8
   for (uint32_t i = r; i < rows; i += kJoinRows) s += part[(size_t)i * D];
   sums[r][c] = s;
   __syncthreads();
@@ -375,28 +397,42 @@ void set_turns(RotateArgs& g, const kp_turns* t) {
   g.freq = t->freq; g.axis = t->axis; g.pairs = (uint32_t)t->pairs; g.axes = (uint32_t)t->axes;
 }
 
-// Tokens and heads of a workgroup: as many tokens side by side as there are, up to a row of lanes for each, and up to 8 heads
-// to a thread, which share its angles, while that leaves four workgroups for each compute unit.
-constexpr uint32_t kWanted = 1024;
-void plan_rows(RotateArgs& g, int tokens, int per_seq, int Hq, int Hk, int Hv, int D) {
-  const uint32_t slots = kThreads / (uint32_t)(D / 8);
+// Tokens and heads of a workgroup.
+constexpr uint32_t kWanted = 1024, kBackWanted = 768, kMostTiles = 1u << 16;  // (a workgroup goes on with further tiles)
+struct RotatePlan {
+  uint32_t groups, chunks;  // of tokens, of heads
+};
+RotatePlan plan_rows(RotateArgs& g, int tokens, int per_seq, int Hq, int Hk, int Hv, int D, bool heads_first) {
+  const uint32_t slots = kThreads / (uint32_t)(D / 8), rows = slots / 4u;  // of a workgroup, of a wave
   g.tokens = (uint32_t)tokens; g.per_seq = (uint32_t)per_seq;
   g.heads[0] = (uint32_t)Hq; g.heads[1] = (uint32_t)Hk;
-  while ((1u << g.tile_log2) < slots && (1u << g.tile_log2) < g.tokens) ++g.tile_log2;
-  g.tiles = (g.tokens + (1u << g.tile_log2) - 1u) >> g.tile_log2;
-  for (g.per = 8u; ; g.per >>= 1) {
-    const uint32_t of = (slots >> g.tile_log2) * g.per;
-    g.chunks[0] = (g.heads[0] + of - 1u) / of;
-    g.chunks[1] = (g.heads[1] + of - 1u) / of;
-    if (g.per == 1u || (uint64_t)g.tiles * (g.chunks[0] + g.chunks[1] * (Hv ? 2u : 1u)) >= kWanted) break;
+  g.heads_first = heads_first;
+  uint32_t most = slots;
+  if (heads_first) {
+    uint32_t step = 1u;
+    while (step < rows && step < (uint32_t)(Hq > Hk ? Hq : Hk)) step *= 2u;
+    most = slots / step;
   }
+  while ((1u << g.tile_log2) < most && (1u << g.tile_log2) < g.tokens) ++g.tile_log2;
+  g.tiles = (g.tokens + (1u << g.tile_log2) - 1u) >> g.tile_log2;
+  const uint32_t all = (uint32_t)(Hq + Hk + Hv), step = slots >> g.tile_log2;
+  RotatePlan p;
+  g.chunk = (all + step - 1u) / step * step;
+  while (g.chunk > step && (uint64_t)g.tiles * ((all + g.chunk - 1u) / g.chunk) < kWanted) g.chunk = (g.chunk / step + 1u) / 2u * step;
+  p.chunks = (all + g.chunk - 1u) / g.chunk;
+  p.groups = g.tiles < kMostTiles ? g.tiles : kMostTiles;
+  return p;
+}
+
+// Do heads of a token lie closer together than tokens of a head?  As the first tensor has it.
+bool heads_first(const RotateArgs& g) {
+  const Heads& x = g.x[g.x[0].at ? 0 : 1];
+  return x.head < x.token;
 }
 
 #define KP_PICK_ADJACENT(T, D, ...) do { if (adjacent) KP_LAUNCH(T, D, true, ##__VA_ARGS__); else KP_LAUNCH(T, D, false, ##__VA_ARGS__); } while (0)
 #define KP_PICK_D(T, ...) do { if (D == 64) KP_PICK_ADJACENT(T, 64, ##__VA_ARGS__); else KP_PICK_ADJACENT(T, 128, ##__VA_ARGS__); } while (0)
 #define KP_PICK_TYPE(...) do { if (type == KP_FP16) KP_PICK_D(Fp16, ##__VA_ARGS__); else KP_PICK_D(Bf16, ##__VA_ARGS__); } while (0)
-
-constexpr uint32_t kMostTiles = 1u << 16;  // of a launch: a workgroup goes on with the next ones
 
 }  // namespace
 
@@ -420,9 +456,9 @@ extern "C" kp_status kp_norm_rotate(const kp_heads* q, const kp_heads* k, const 
   }
   g.weight[0] = q_weight; g.weight[1] = k_weight; g.fp32_weights = weight_type == KP_FP32; g.eps = eps;
   set_turns(g, turns);
-  plan_rows(g, B * S, S, Hq, Hk, 0, D);
+  const RotatePlan plan = plan_rows(g, B * S, S, Hq, Hk, 0, D, heads_first(g));
   const bool adjacent = g.pairs && turns->adjacent;
-  const dim3 grid(g.tiles < kMostTiles ? g.tiles : kMostTiles, g.chunks[0] + g.chunks[1]);
+  const dim3 grid(plan.groups, plan.chunks);
   hipStream_t st = static_cast<hipStream_t>(stream);
 #define KP_LAUNCH(T, D, A) hipLaunchKernelGGL((kp_norm_rotate_rows<T, D, A, 0>), grid, dim3(kThreads), 0, st, g)
   KP_PICK_TYPE();
@@ -457,9 +493,9 @@ extern "C" kp_status kp_norm_rotate_write(const kp_heads* q, const kp_heads* k, 
   g.k_cache = static_cast<uint8_t*>(cache->k); g.v_cache = static_cast<uint8_t*>(cache->v);
   g.k_exp = cache->k_exp; g.v_exp = cache->v_exp; g.page_log2 = log2_of(cache->page);
   g.n_slots = (uint64_t)cache->n_pages * (uint64_t)cache->page;
-  plan_rows(g, T, T, Hq, Hk, Hk, D);
+  const RotatePlan plan = plan_rows(g, T, T, Hq, Hk, Hk, D, heads_first(g));
   const bool adjacent = g.pairs && turns->adjacent;
-  const dim3 grid(g.tiles < kMostTiles ? g.tiles : kMostTiles, g.chunks[0] + 2u * g.chunks[1]);
+  const dim3 grid(plan.groups, plan.chunks);
   hipStream_t st = static_cast<hipStream_t>(stream);
 #define KP_LAUNCH(T, D, A, W) hipLaunchKernelGGL((kp_norm_rotate_rows<T, D, A, W>), grid, dim3(kThreads), 0, st, g)
   if (cache->cache_type == KP_CACHE_E4M3) KP_PICK_TYPE(2); else KP_PICK_TYPE(1);
@@ -468,17 +504,24 @@ extern "C" kp_status kp_norm_rotate_write(const kp_heads* q, const kp_heads* k, 
   return KP_OK;
 }
 
-// Workgroups of the gradient that share a chunk of heads: each leaves its sums of d_w.
-static uint32_t back_groups(const RotateArgs& g) {
-  const uint32_t chunks = g.chunks[0] + g.chunks[1], most = kWanted / (chunks ? chunks : 1u);
-  return g.tiles < most ? g.tiles : most ? most : 1u;
+// The gradient: each workgroup leaves its sums of d_w, so that there are fewer, each with more tiles.
+static RotatePlan plan_back(RotateArgs& g, int tokens, int per_seq, int Hq, int Hk, int D, bool heads_first) {
+  RotatePlan p = plan_rows(g, tokens, per_seq, Hq, Hk, 0, D, heads_first);
+  const uint32_t most = kBackWanted / p.chunks;
+  if (p.groups > most) p.groups = most > 1u ? most : 1u;
+  return p;
 }
 
 extern "C" size_t kp_norm_rotate_grad_bytes(int B, int Hq, int Hk, int S, int D) {
-  if (check_sizes(B, Hq, Hk, S, D, KP_BF16, KP_BF16, 1.f, true) || B == 0 || S == 0) return 0;
-  RotateArgs g{};
-  plan_rows(g, B * S, S, Hq, Hk, 0, D);
-  return (size_t)back_groups(g) * (g.chunks[0] + g.chunks[1]) * (size_t)D * sizeof(float);
+  if (check_sizes(B, Hq, Hk, S, D, KP_BF16, KP_BF16, 1.f, true) || B == 0 || S == 0 || (Hq == 0 && Hk == 0)) return 0;
+  size_t rows = 0;
+  for (int first = 0; first < 2; ++first) {
+    RotateArgs g{};
+    const RotatePlan p = plan_back(g, B * S, S, Hq, Hk, D, first != 0);
+    const size_t n = (size_t)p.groups * p.chunks;
+    rows = n > rows ? n : rows;
+  }
+  return 2 * rows * (size_t)D * sizeof(float);
 }
 
 extern "C" kp_status kp_norm_rotate_grad(const kp_heads* q, const kp_heads* k, const void* q_weight, const void* k_weight, int weight_type,
@@ -513,25 +556,25 @@ extern "C" kp_status kp_norm_rotate_grad(const kp_heads* q, const kp_heads* k, c
   }
   g.weight[0] = q_weight; g.weight[1] = k_weight; g.fp32_weights = weight_type == KP_FP32; g.eps = eps;
   g.d_weight[0] = dq_weight; g.d_weight[1] = dk_weight;
-  if (rows) {
+  RotatePlan plan{};
+  if (rows && (Hq > 0 || Hk > 0)) {
     set_turns(g, turns);
-    plan_rows(g, B * S, S, Hq, Hk, 0, D);
+    plan = plan_back(g, B * S, S, Hq, Hk, D, heads_first(g));
   }
-  const uint32_t chunks = g.chunks[0] + g.chunks[1], groups = rows && chunks ? back_groups(g) : 0u;
   if (q_weight || k_weight)
-    if (kp_status s = check_workspace(workspace, workspace_bytes, (size_t)groups * chunks * (size_t)D * sizeof(float))) return s;
+    if (kp_status s = check_workspace(workspace, workspace_bytes, kp_norm_rotate_grad_bytes(B, Hq, Hk, S, D))) return s;
   g.part = static_cast<float*>(workspace);
   const bool adjacent = g.pairs && turns->adjacent;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (groups) {
-    const dim3 grid(groups, chunks);
+  if (plan.groups) {
+    const dim3 grid(plan.groups, plan.chunks);
 #define KP_LAUNCH(T, D, A) hipLaunchKernelGGL((kp_norm_rotate_back<T, D, A>), grid, dim3(kThreads), 0, st, g)
     KP_PICK_TYPE();
 #undef KP_LAUNCH
     KP_HIP_TRY(hipGetLastError());
   }
   if (q_weight || k_weight) {
-    hipLaunchKernelGGL(kp_norm_rotate_join, dim3((uint32_t)D / 32u, 2), dim3(32 * kJoinRows), 0, st, g, groups, (uint32_t)D);
+    hipLaunchKernelGGL(kp_norm_rotate_join, dim3((uint32_t)D / 32u, 2), dim3(32 * kJoinRows), 0, st, g, plan.groups * plan.chunks, (uint32_t)D);
     KP_HIP_TRY(hipGetLastError());
   }
   return KP_OK;
