@@ -179,15 +179,8 @@ def _ptr(t) -> int:
     return t.data_ptr()
 
 
-def _here(t):
-    """Raises where a tensor is on another GPU than the current one, whose stream a call without one goes to."""
-    import torch
-
-    if t.is_cuda and t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"tensor on GPU {t.get_device()}, but the current one is {torch.cuda.current_device()}")
-
-
 _current_stream = None  # () -> hipStream_t of torch's current stream
+_raw_stream = None  # the same, of a GPU by its number (where torch offers it)
 
 
 def _stream_lookup():
@@ -197,8 +190,29 @@ def _stream_lookup():
     if raw is None:  # (not part of torch's public interface)
         return lambda: torch.cuda.current_stream().cuda_stream
     torch.cuda.init()
+    global _raw_stream
+    _raw_stream = raw
     device = torch.cuda.current_device
     return lambda: raw(device())
+
+
+_current_device = None  # torch.cuda.current_device
+
+
+def _stream_at(stream, t) -> int:
+    """The stream of a call on tensor t, which has to be on the current GPU."""
+    global _current_device
+    if _current_device is None:
+        import torch
+
+        torch.cuda.init()
+        _current_device = torch.cuda.current_device
+    device = _current_device()
+    if t.get_device() != device:
+        raise ValueError(f"tensor on {t.device}, but the current GPU is {device}")
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device)
+    return _stream(stream)
 
 
 def _stream(stream) -> int:
@@ -556,12 +570,11 @@ def kp_cache_move(source, target, starts, k_cache, v_cache, k_exp=None, v_exp=No
     in both; else int32 [n + 1]: groups of moves, each in order (see the header for what groups of more than KP_MOVE_RUN may
     hold)."""
     i64, N = (_names or _types())["int64"], source.shape[0]
-    _here(source)
     # (what the codes of an e4m3 cache are read as does not matter here)
     kind = k_cache.dtype if k_cache.dtype is not _names["float8_e4m3fn"] else _names["bfloat16"]
     _check(lib().kp_cache_move(_flat("source", source, i64, (N,)), _flat("target", target, i64, (N,)), N,
                                0 if starts is None else _flat("starts", starts, _names["int32"]), 0 if starts is None else starts.shape[0] - 1,
-                               _cache_of(k_cache, v_cache, k_exp, v_exp, kind), _stream(stream)))
+                               _cache_of(k_cache, v_cache, k_exp, v_exp, kind), _stream_at(stream, source)))
 
 
 def kp_attn_paged_bytes(q, k_cache, block_table, window: int, sinks: int) -> int:
@@ -619,7 +632,6 @@ def kp_attn_tree(q, k_cache, v_cache, k_exp, v_exp, block_table, lens, starts, s
     n, width = block_table.shape
     if D != k_cache.shape[3]:
         raise ValueError("q and the cache must have the same D")
-    _here(q)
     names = _names or _types()
     i32 = names["int32"]
     ws, nbytes = _workspace(workspace)
@@ -629,7 +641,7 @@ def kp_attn_tree(q, k_cache, v_cache, k_exp, v_exp, block_table, lens, starts, s
         _flat("lens", lens, i32, (n,)), _flat("starts", starts, i32, (n + 1,)), _flat("seen", seen, names["int64"], (T, words)), words,
         0 if depth is None else _flat("depth", depth, i32, (T,)), _heads("o", o, q.shape, q.dtype),
         0 if lse is None else _flat("lse", lse, names["float32"], (Hq, T)), T, n, Hq, window, sinks, scale, ws, nbytes,
-        region_mask & 0xFFFFFFFF, _ptr(trace_buf), trace_cap, _stream(stream)))
+        region_mask & 0xFFFFFFFF, _ptr(trace_buf), trace_cap, _stream_at(stream, q)))
 
 
 # ---- queries and keys normed and turned ----------------------------------------------------------------
@@ -645,59 +657,45 @@ def _turns(positions, freq, axis, adjacent, batch, tokens):
     if freq is None:
         return None
     names = _names or _types()
-    pairs = freq.shape[0]
-    p, dims = positions, positions.dim()
-    if p.dtype is not names["int32"] or not p.is_cuda or p.shape[-1] != tokens or (tokens > 1 and p.stride(-1) != 1):
-        raise ValueError(f"positions must be int32 on the GPU, {tokens} for each sequence, contiguous, not {list(p.shape)} of {p.dtype}")
-    axes, axis_step, seq_step = 1, 0, 0
-    if batch is not None and dims >= 2:
-        if p.shape[-2] != batch:
-            raise ValueError(f"positions must be [S], [B, S] or [axes, B, S] with B = {batch}, not {list(p.shape)}")
-        seq_step = p.stride(-2)
-    front = 2 if batch is None else 3
-    if dims == front:
-        axes, axis_step = p.shape[0], p.stride(0)
-    elif dims == 0 or dims > front:
-        raise ValueError(f"positions have too many dimensions or none: {list(p.shape)}")
-    return _pack_turns(p.data_ptr(), axis_step, seq_step, _flat("freq", freq, names["float32"], (pairs,)),
+    shape, steps, pairs = positions.shape, positions.stride(), freq.shape[0]
+    front = 2 if batch is None else 3  # dimensions, with that of the axes
+    n = len(shape)
+    if positions.dtype is not names["int32"] or not positions.is_cuda or not 0 < n <= front or shape[-1] != tokens or (tokens > 1 and steps[-1] != 1):
+        raise ValueError(f"positions must be int32 on the GPU, {tokens} for each sequence, contiguous, not {list(shape)} of {positions.dtype}")
+    if batch is not None and n >= 2 and shape[-2] != batch:
+        raise ValueError(f"positions must be [S], [B, S] or [axes, B, S] with B = {batch}, not {list(shape)}")
+    axes, axis_step = (shape[0], steps[0]) if n == front else (1, 0)
+    return _pack_turns(positions.data_ptr(), axis_step, steps[-2] if batch is not None and n >= 2 else 0, _flat("freq", freq, names["float32"], (pairs,)),
                        0 if axis is None else _flat("axis", axis, names["uint8"], (pairs,)), pairs, axes, 1 if adjacent else 0)
 
 
 def _norms(q_weight, k_weight, D, dtype):
     """Device pointers of the norms' weights (0: none) and their type."""
-    code, kind = _type_code(dtype), None
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is None:
-            continue
-        if w.dtype not in (dtype, _names["float32"]) or (kind is not None and w.dtype is not kind):
-            raise ValueError(f"weights must both be float32 or both {dtype}, not {w.dtype}")
-        kind = w.dtype
-    at = [0 if w is None else _flat("weights", w, kind, (D,)) for w in (q_weight, k_weight)]
-    return at[0], at[1], code if kind is dtype or kind is None else KP_FP32
+    code = _type_code(dtype)
+    if q_weight is None and k_weight is None:
+        return 0, 0, code
+    kind = (k_weight if q_weight is None else q_weight).dtype
+    if kind is not dtype:
+        if kind is not _names["float32"]:
+            raise ValueError(f"weights must both be float32 or both {dtype}, not {kind}")
+        code = KP_FP32
+    return 0 if q_weight is None else _flat("q_weight", q_weight, kind, (D,)), 0 if k_weight is None else _flat("k_weight", k_weight, kind, (D,)), code
 
 
 def _two(q, k):
     """Of queries and keys, either of which may be None: number of sequences (None: [T, H, D]), heads, tokens, D and type."""
-    some = q if q is not None else k
+    some = k if q is None else q
     if some is None:
         raise ValueError("queries or keys are needed")
-    if some.dim() == 4:
-        B, _, S, D = some.shape
-        return B, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], S, D, some.dtype
-    S, _, D = some.shape
-    return None, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], S, D, some.dtype
-
-
-def _maybe(name, t, like, dtype):
-    """kp_heads of t in the shape of `like`, which may be None."""
-    return None if like is None else _heads(name, t, like.shape, dtype)
-
-
-def _alike(q, k, D, batch, tokens):
-    want = (tokens, D) if batch is None else (batch, tokens, D)
-    for name, t in (("queries", q), ("keys", k)):
-        if t is not None and (t.dim() != len(want) + 1 or ((t.shape[0], t.shape[2]) if batch is None else (t.shape[0], t.shape[2], t.shape[3])) != want):
-            raise ValueError(f"{name} must have the sequences, tokens and D of the others, not {list(t.shape)}")
+    shape = some.shape
+    B = shape[0] if len(shape) == 4 else None
+    S, D = (shape[0], shape[2]) if B is None else (shape[2], shape[3])
+    if q is None or k is None:
+        return B, 0 if q is None else shape[1], 0 if k is None else shape[1], S, D, some.dtype
+    other = k.shape
+    if len(other) != len(shape) or other[0] != shape[0] or other[2:] != shape[2:]:
+        raise ValueError(f"keys must have the queries' sequences, tokens and D, not {list(other)} to {list(shape)}")
+    return B, shape[1], other[1], S, D, some.dtype
 
 
 def kp_norm_rotate(q, k, q_weight, k_weight, eps: float, positions, freq, axis, adjacent: bool, q_out, k_out, stream=None) -> None:
@@ -705,13 +703,12 @@ def kp_norm_rotate(q, k, q_weight, k_weight, eps: float, positions, freq, axis, 
     (None: not normed), their pairs turned by position * freq[pair]; freq float32 [pairs] (None: not turned), axis uint8
     [pairs] or None.  q and q_out, or k and k_out, may be None; outputs may be the inputs."""
     B, Hq, Hk, S, D, dtype = _two(q, k)
-    _here(k if q is None else q)
-    _alike(q, k, D, B, S)
     qw, kw, kind = _norms(q_weight, k_weight, D, dtype)
     _check(lib().kp_norm_rotate(
-        _maybe("q", q, q, dtype), _maybe("k", k, k, dtype), qw, kw, kind, eps, _turns(positions, freq, axis, adjacent, B, S),
-        _maybe("q_out", q_out, q, dtype), _maybe("k_out", k_out, k, dtype), 1 if B is None else B, Hq, Hk, S, D, _type_code(dtype),
-        _stream(stream)))
+        None if q is None else _heads("q", q, q.shape, dtype), None if k is None else _heads("k", k, k.shape, dtype), qw, kw, kind, eps,
+        _turns(positions, freq, axis, adjacent, B, S), None if q is None else _heads("q_out", q_out, q.shape, dtype),
+        None if k is None else _heads("k_out", k_out, k.shape, dtype), 1 if B is None else B, Hq, Hk, S, D, _names[dtype],
+        _stream_at(stream, k if q is None else q)))
 
 
 def kp_norm_rotate_grad_bytes(q, k) -> int:
@@ -725,17 +722,15 @@ def kp_norm_rotate_grad(q, k, q_weight, k_weight, eps: float, positions, freq, a
     """Gradient of kp_norm_rotate: dq, dk from d_q_out, d_k_out and the q, k that were normed (not looked at without weights), and
     dq_weight, dk_weight [D] float32 where there are weights."""
     B, Hq, Hk, S, D, dtype = _two(d_q_out, d_k_out)
-    _here(d_k_out if d_q_out is None else d_q_out)
-    _alike(d_q_out, d_k_out, D, B, S)
     qw, kw, kind = _norms(q_weight, k_weight, D, dtype)
     f32 = _names["float32"]
     ws, n = _workspace(workspace)
+    some = lambda name, t, like: None if like is None else _heads(name, t, like.shape, dtype)  # noqa: E731
     _check(lib().kp_norm_rotate_grad(
-        _maybe("q", q, d_q_out if qw else None, dtype), _maybe("k", k, d_k_out if kw else None, dtype), qw, kw, kind, eps,
-        _turns(positions, freq, axis, adjacent, B, S), _maybe("d_q_out", d_q_out, d_q_out, dtype), _maybe("d_k_out", d_k_out, d_k_out, dtype),
-        _maybe("dq", dq, d_q_out, dtype), _maybe("dk", dk, d_k_out, dtype),
+        some("q", q, d_q_out if qw else None), some("k", k, d_k_out if kw else None), qw, kw, kind, eps, _turns(positions, freq, axis, adjacent, B, S),
+        some("d_q_out", d_q_out, d_q_out), some("d_k_out", d_k_out, d_k_out), some("dq", dq, d_q_out), some("dk", dk, d_k_out),
         _flat("dq_weight", dq_weight, f32, (D,)) if qw else 0, _flat("dk_weight", dk_weight, f32, (D,)) if kw else 0,
-        1 if B is None else B, Hq, Hk, S, D, _type_code(dtype), ws, n, _stream(stream)))
+        1 if B is None else B, Hq, Hk, S, D, _names[dtype], ws, n, _stream_at(stream, d_k_out if d_q_out is None else d_q_out)))
 
 
 def kp_norm_rotate_write(q, k, v, q_weight, k_weight, eps: float, positions, freq, axis, adjacent: bool, q_out, slots, k_cache, v_cache,
@@ -744,12 +739,12 @@ def kp_norm_rotate_write(q, k, v, q_weight, k_weight, eps: float, positions, fre
     cache as kp_cache_write puts them there."""
     T, (_, Hkv, _, D), dtype = k.shape[0], k_cache.shape, k.dtype
     Hq = 0 if q is None else q.shape[1]
-    _here(k)
+    queries, keys = (T, Hq, D), (T, Hkv, D)
     qw, kw, kind = _norms(q_weight, k_weight, D, dtype)
     _check(lib().kp_norm_rotate_write(
-        None if q is None else _heads("q", q, (T, Hq, D), dtype), _heads("k", k, (T, Hkv, D), dtype), _heads("v", v, (T, Hkv, D), dtype), qw, kw,
-        kind, eps, _turns(positions, freq, axis, adjacent, None, T), _maybe("q_out", q_out, q, dtype),
-        _flat("slots", slots, _names["int64"], (T,)), T, Hq, _cache_of(k_cache, v_cache, k_exp, v_exp, dtype), _stream(stream)))
+        None if q is None else _heads("q", q, queries, dtype), _heads("k", k, keys, dtype), _heads("v", v, keys, dtype), qw, kw, kind, eps,
+        _turns(positions, freq, axis, adjacent, None, T), None if q is None else _heads("q_out", q_out, queries, dtype),
+        _flat("slots", slots, _names["int64"], (T,)), T, Hq, _cache_of(k_cache, v_cache, k_exp, v_exp, dtype), _stream_at(stream, k)))
 
 
 # ---- views of the statistics block (layout documented in include/kperf.h) ------------------------
