@@ -325,3 +325,42 @@ def test_a_step_with_drafts(kp):
                 for j in range(lens[s] + len(paths[s])):
                     at = slot(s, j)
                     assert torch.equal(a.view(torch.uint8)[at // page, :, at % page], b.view(torch.uint8)[at // page, :, at % page])
+
+
+@pytest.mark.parametrize("drafts", [1, 6, 70])
+def test_the_example_runs_with_drafts(drafts):
+    from examples import attention_layer
+
+    got = attention_layer.main(["--tokens", "150", "--new", "2", "--chunk", "64", "--window", "50", "--heads", "8", "--kv-heads", "2", "--dim", "64", "--drafts", str(drafts)])
+    kept = drafts - drafts // 2
+    assert got["lens"] == [152 + kept, 115 + kept, 78 + kept]
+    assert all(torch.isfinite(x.float()).all() for x in (got["tree"], *got["grads"])) and got["off"] <= 2.0 ** -4
+
+
+def test_a_layer_is_differentiated_as_a_whole(kp):
+    """Norm, rotation and attention, and back, against differences of the definition in 64 bits along a direction."""
+    from examples.attention_layer import Layer, train_step
+
+    from tests import rotate_util
+    from tests.attn_util import forward
+
+    gen = torch.Generator(device="cuda").manual_seed(21)
+    b, hq, hkv, s, d, window, sinks, dtype = 1, 4, 2, 70, 64, 20, 2, torch.float16
+    layer = Layer(d)
+    layer.weights = [0.5 + torch.rand(d, device="cuda", generator=gen) for _ in range(2)]
+    q, k, v, d_o = (torch.randn(b, h, s, d, device="cuda", generator=gen).to(dtype) for h in (hq, hkv, hkv, hq))
+    _, grads = train_step(layer, q, k, v, d_o, window, sinks)
+    along = [torch.randn(x.shape, device="cuda", generator=gen, dtype=torch.float64) for x in (q, k, v, *layer.weights)]
+    theta = rotate_util.angles(torch.arange(s, device="cuda"), layer.freq, None, b, s)
+
+    def loss(h):
+        x = [t.double() + h * a for t, a in zip((q, k, v, *layer.weights), along)]
+        turned = [rotate_util.turn(y / torch.sqrt(y.square().mean(-1, keepdim=True) + layer.eps) * w, theta, False) for y, w in zip(x[:2], x[3:])]
+        return float((forward(*turned, x[2], window, sinks, d ** -0.5)[1] * d_o.double()).sum())
+
+    h = 1e-5
+    want = (loss(h) - loss(-h)) / (2 * h)
+    got = sum(float((g.double() * a).sum()) for g, a in zip(grads, along))
+    # each gradient's value is off by a few half steps of fp16 of its terms (P, dS, the turned q and k, o): 32 of them of the sum's norm
+    size = math.sqrt(sum(float((g.double() * a).square().sum()) for g, a in zip(grads, along)))
+    assert abs(got - want) <= 32 * half_step(dtype) * size
