@@ -573,13 +573,13 @@ kp_status kp_attn_paged_launch_shape(int T, int n_seqs, int Hq, int Hkv, int D, 
  *   (device) says how many drafted tokens it follows (below 0: 0; NULL: 0 for all).  A window does not hide drafted keys.
  * words from 0 to 2^24; seen may be NULL with words = 0.  workspace, recording: as for kp_attn_paged.
  */
-size_t kp_attn_tree_bytes(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int window, int sinks);
+size_t kp_attn_tree_bytes(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int cache_type, int window, int sinks);
 kp_status kp_attn_tree(const kp_heads* q, const kp_cache* cache, const int32_t* block_table, int table_width, const int32_t* lens,
                        const int32_t* starts, const int64_t* seen, int words, const int32_t* depth, const kp_heads* o, float* lse,
                        int T, int n_seqs, int Hq, int window, int sinks, float scale, void* workspace, size_t workspace_bytes,
                        uint32_t region_mask, void* trace_buf, size_t trace_cap, void* stream);
-kp_status kp_attn_tree_launch_shape(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int window, int sinks,
-                                    int* n_wg, int* waves_per_wg, int* n_regions);
+kp_status kp_attn_tree_launch_shape(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int cache_type, int window,
+                                    int sinks, int* n_wg, int* waves_per_wg, int* n_regions);
 
 /* ---- what goes into them: queries and keys normed and turned ------------------------------------
  *

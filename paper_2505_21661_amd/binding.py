@@ -141,7 +141,7 @@ def _optional(L):
         "kp_cache_read": [cp, vp, ci, vp, ci, ci, hp, hp, vp],
         "kp_attn_paged": [hp, cp, vp, ci, vp, vp, hp, vp, ci, ci, ci, ci, ci, fl, vp, sz, u32, vp, sz, vp],
         "kp_attn_tree": [hp, cp, vp, ci, vp, vp, vp, ci, vp, hp, vp, ci, ci, ci, ci, ci, fl, vp, sz, u32, vp, sz, vp],
-        "kp_attn_tree_launch_shape": [ci] * 9 + [ip] * 3,
+        "kp_attn_tree_launch_shape": [ci] * 10 + [ip] * 3,
         "kp_cache_move": [vp, vp, ci, vp, ci, cp, vp],
         "kp_norm_rotate": [hp, hp, vp, vp, ci, fl, tp, hp, hp, ci, ci, ci, ci, ci, ci, vp],
         "kp_norm_rotate_grad": [hp, hp, vp, vp, ci, fl, tp, hp, hp, hp, hp, vp, vp, ci, ci, ci, ci, ci, ci, vp, sz, vp],
@@ -157,7 +157,7 @@ def _optional(L):
             f = getattr(L, name)
             f.restype = ci
             f.argtypes = args
-    for name, n in (("kp_attn_window_bytes", 8), ("kp_attn_window_grad_bytes", 8), ("kp_attn_paged_bytes", 9), ("kp_attn_tree_bytes", 9),
+    for name, n in (("kp_attn_window_bytes", 8), ("kp_attn_window_grad_bytes", 8), ("kp_attn_paged_bytes", 9), ("kp_attn_tree_bytes", 10),
                     ("kp_norm_rotate_grad_bytes", 5)):
         if hasattr(L, name):
             getattr(L, name).restype = sz
@@ -609,18 +609,22 @@ def kp_attn_paged(q, k_cache, v_cache, k_exp, v_exp, block_table, lens, starts, 
         region_mask & 0xFFFFFFFF, _ptr(trace_buf), trace_cap, _stream(stream)))
 
 
+def _cache_type(k_cache) -> int:
+    return KP_CACHE_E4M3 if k_cache.dtype is (_names or _types())["float8_e4m3fn"] else KP_CACHE_SAME
+
+
 def kp_attn_tree_bytes(q, k_cache, block_table, window: int, sinks: int) -> int:
     """Bytes of workspace that kp_attn_tree takes for q [T, Hq, D]."""
     T, Hq, D = q.shape
     n, width = block_table.shape
-    return int(lib().kp_attn_tree_bytes(T, n, Hq, k_cache.shape[1], D, width, k_cache.shape[2], window, sinks))
+    return int(lib().kp_attn_tree_bytes(T, n, Hq, k_cache.shape[1], D, width, k_cache.shape[2], _cache_type(k_cache), window, sinks))
 
 
 def kp_attn_tree_launch_shape(q, k_cache, block_table, window: int, sinks: int) -> tuple[int, int, int]:
     """Workgroups, waves per workgroup and regions of a recording of kp_attn_tree."""
     T, Hq, D = q.shape
     n, width = block_table.shape
-    return _shape_of(lib().kp_attn_tree_launch_shape, T, n, Hq, k_cache.shape[1], D, width, k_cache.shape[2], window, sinks)
+    return _shape_of(lib().kp_attn_tree_launch_shape, T, n, Hq, k_cache.shape[1], D, width, k_cache.shape[2], _cache_type(k_cache), window, sinks)
 
 
 def kp_attn_tree(q, k_cache, v_cache, k_exp, v_exp, block_table, lens, starts, seen, depth, o, lse, window: int, sinks: int,

@@ -116,10 +116,10 @@ struct Plan {
   long long tiles, splits, units;  // units: heads of keys (of all sequences where a tile belongs to one)
   size_t bytes;                    // workspace
 };
-// Into how many runs the keys go, for about `want` workgroups.
-inline void split_keys(Plan& p, long long want, long long most_keys, long long per_tile, int D) {
-  const long long runs = most_keys < 1536 ? 1 : most_keys / 512;
-  p.splits = p.units * 2 > want ? 1 : want / p.units;
+// Into how many runs the keys of `units` go, for about `want` workgroups, a run of `least` keys or more.
+inline void split_keys(Plan& p, long long units, long long want, long long most_keys, long long least, long long per_tile, int D) {
+  const long long runs = most_keys < 1536 ? 1 : most_keys / least;
+  p.splits = units * 2 > want ? 1 : want / units;
   if (p.splits > runs) p.splits = runs;
   if (p.splits > 256) p.splits = 256;
   if (p.splits < 1) p.splits = 1;
@@ -137,7 +137,7 @@ inline Plan plan_of(long long seqs, long long rows, long long most_keys, int Hkv
   // a run has 512.  Tiles of 128 rows are split to fill the chip (two workgroups per CU: 6 chunks of up to 512 tokens over
   // 8192 keys, 672 workgroups, 125 us, split in two 149); few rows further, since the sequences differ in length (64 tokens
   // over up to 16384 keys, 1024 workgroups 277 us, 4096 261, 8192 267).
-  split_keys(p, p.few ? 4096 : 512, most_keys, per_tile, D);
+  split_keys(p, p.units, p.few ? 4096 : 512, most_keys, 512, per_tile, D);
   return p;
 }
 // Keys that the rows of a tile may see: all there are, or the window of its tokens and the sinks.
