@@ -364,3 +364,51 @@ def test_a_layer_is_differentiated_as_a_whole(kp):
     # each gradient's value is off by a few half steps of fp16 of its terms (P, dS, the turned q and k, o): 32 of them of the sum's norm
     size = math.sqrt(sum(float((g.double() * a).square().sum()) for g, a in zip(grads, along)))
     assert abs(got - want) <= 32 * half_step(dtype) * size
+
+
+@pytest.mark.parametrize("most", [3, 60])
+def test_many_sequences(kp, most):
+    r = random.Random(most)
+    n_q = [r.choice([0, 1, 2, r.randint(1, most)]) for _ in range(150)]
+    n_k = [n + r.choice([0, 1, 5, r.randint(0, 300)]) for n in n_q]
+    case = Case(most, n_q, n_k, 4, 2, 64, 16, torch.bfloat16, True, 30, 3)
+    case.check(*case.run(kp))
+
+
+@pytest.mark.parametrize("n_q", [[9, 4], [90, 70]])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_a_cache_past_32_bits(kp, n_q, e4m3):
+    """The last pages of a cache of more than 2^32 bytes hold what the first ones of a small one do."""
+    case = Case(17, n_q, [300, 150], 4, 2, 128, 64, torch.bfloat16, e4m3, 0, 0)
+    o, lse = case.run(kp)
+    small, hkv, page, d = case.halves[0].shape
+    pages = (9 << 29) // (hkv * page * d * (1 if e4m3 else 2))
+    halves = [torch.empty(pages, hkv, page, d, dtype=x.dtype, device="cuda") for x in case.halves]
+    for big, x in zip(halves, case.halves):
+        big.view(torch.uint8)[-small:] = x.view(torch.uint8)
+    exps = [None if e is None else torch.empty(pages, hkv, page, dtype=torch.uint8, device="cuda") for e in case.exps]
+    for big, x in zip(exps, case.exps):
+        if x is not None:
+            big[-small:] = x
+    table, *rest = case.args
+    far = torch.where(table >= 0, table + (pages - small), table)
+    again, sums = torch.full_like(o, 7.0), torch.full_like(lse, 7.0)
+    kp.kp_attn_tree(case.q, *halves, *exps, far, *rest, again, sums, 0, 0, case.scale, case.workspace)
+    assert torch.equal(again, o) and torch.equal(sums, lse)
+
+
+def test_strides_and_tables_of_other_widths(kp):
+    """Queries and results inside larger tensors, heads before tokens; a table with room for far more keys."""
+    case = Case(19, [7, 30, 2], [400, 900, 64], 8, 2, 64, 32, torch.float16, False, 0, 0)
+    o, lse = case.run(kp)
+    T = sum(case.n_q)
+    room = torch.full((9, T + 5, 128), 5.0, dtype=case.dtype, device="cuda")
+    q, out = room[1:, 2 : T + 5, :64].transpose(0, 1), torch.full((8, T + 3, 64), 7.0, dtype=case.dtype, device="cuda").transpose(0, 1)
+    q.copy_(case.q)
+    wide = torch.full((3, 700), -1, dtype=torch.int32, device="cuda")
+    wide[:, : case.table.shape[1]] = case.table.cuda()
+    n = kp.kp_attn_tree_bytes(q, case.halves[0], wide, 0, 0)
+    sums = torch.empty_like(lse)
+    kp.kp_attn_tree(q, *case.halves, *case.exps, wide, *case.args[1:], out, sums, 0, 0, case.scale, torch.empty(max(16, n), dtype=torch.uint8, device="cuda"))
+    case.o = out
+    case.check(out, torch.where(torch.arange(T + 3, device="cuda") < T, sums, 7.0))

@@ -300,3 +300,49 @@ def test_offsets_past_32_bits(kp):
     kp.kp_norm_rotate(near, None, w, None, EPS, at, freq, None, False, out, None)
     kp.kp_norm_rotate(far, None, w, None, EPS, at, freq, None, False, far, None)
     assert torch.equal(far, out)
+
+
+@pytest.mark.parametrize("layout,d,hq,hk,s", [("bhsd", 64, 1, 0, 2_200_000), ("bshd", 128, 4, 1, 270_000), ("bshd", 64, 700, 3, 5), ("bhsd", 128, 70, 70, 40)])
+def test_many_tokens_and_many_heads(kp, layout, d, hq, hk, s):
+    """More tiles than a launch has workgroups, and more heads than a workgroup takes: the bits of calls on parts."""
+    gen = torch.Generator(device="cuda").manual_seed(s)
+    dtype, pairs = torch.bfloat16, d // 2
+    q, k = heads(gen, layout, 1, (hq, max(1, hk)), s, d, dtype)
+    k = k if hk else None
+    w = [torch.rand(d, device="cuda", generator=gen) for _ in range(2)]
+    at, freq = torch.arange(s, dtype=torch.int32, device="cuda"), torch.rand(pairs, device="cuda", generator=gen)
+    out, out_k = torch.empty_like(q), None if k is None else torch.empty_like(k)
+    kp.kp_norm_rotate(q, k, w[0], w[1], EPS, at, freq, None, False, out, out_k)
+    for a, b in ((0, s // 3), (s // 3, s - 1), (s - 1, s)):
+        for h0, h1 in ((0, 1), (hq // 2, hq)):
+            part = torch.empty_like(q[:, h0:h1, a:b])
+            kp.kp_norm_rotate(q[:, h0:h1, a:b], None, w[0], None, EPS, at[a:b], freq, None, False, part, None)
+            assert torch.equal(part, out[:, h0:h1, a:b]), (a, b, h0)
+        if k is not None:
+            part = torch.empty_like(k[:, :, a:b])
+            kp.kp_norm_rotate(None, k[:, :, a:b], None, w[1], EPS, at[a:b], freq, None, False, None, part)
+            assert torch.equal(part, out_k[:, :, a:b]), (a, b)
+    # the gradient of the input does not go over rows: parts again
+    dy, dx, dw = torch.randn_like(q), torch.empty_like(q), torch.empty(d, device="cuda")
+    kp.kp_norm_rotate_grad(q, None, w[0], None, EPS, at, freq, None, False, dy, None, dx, None, dw, None,
+                           torch.empty(kp.kp_norm_rotate_grad_bytes(q, None), dtype=torch.uint8, device="cuda"))
+    a, part, dw2 = s // 2, torch.empty_like(q[:, :, s // 2:]), torch.empty(d, device="cuda")
+    kp.kp_norm_rotate_grad(q[:, :, a:], None, w[0], None, EPS, at[a:], freq, None, False, dy[:, :, a:], None, part, None, dw2, None,
+                           torch.empty(kp.kp_norm_rotate_grad_bytes(q[:, :, a:], None), dtype=torch.uint8, device="cuda"))
+    assert torch.equal(part, dx[:, :, a:])
+
+
+def test_a_tensor_of_another_place_or_form_is_refused(kp):
+    d, dtype = 64, torch.bfloat16
+    q = torch.zeros(2, 3, 5, d, dtype=dtype, device="cuda")
+    w, freq, at = torch.ones(d, device="cuda"), torch.ones(8, device="cuda"), torch.zeros(5, dtype=torch.int32, device="cuda")
+    good = dict(q=q, k=q, q_weight=w, k_weight=w, eps=EPS, positions=at, freq=freq, axis=None, adjacent=False, q_out=q.clone(), k_out=q.clone())
+    kp.kp_norm_rotate(**good)
+    for bad in (dict(k=q[:, :, :4]), dict(k=q[:1]), dict(k=q[0]), dict(q_out=q[:, :2]), dict(q_weight=w.half()), dict(q_weight=w.to(dtype)), dict(q_weight=w[:32]),
+                dict(positions=at[:4]), dict(positions=at.long()), dict(positions=at.expand(3, 5)), dict(positions=at.expand(2, 2, 2, 5)), dict(positions=at.cpu()),
+                dict(freq=freq.double()), dict(axis=torch.zeros(7, dtype=torch.uint8, device="cuda")), dict(q=q.cpu()), dict(q=q.float()), dict(q=None, k=None),
+                dict(positions=torch.zeros(10, dtype=torch.int32, device="cuda")[::2])):
+        with pytest.raises(ValueError):
+            kp.kp_norm_rotate(**{**good, **bad})
+    with pytest.raises(kp.KperfError):
+        kp.kp_norm_rotate(**{**good, "freq": torch.ones(40, device="cuda")})
