@@ -451,11 +451,11 @@ _pack_heads, _pack_cache = struct.Struct("Pqqq").pack, struct.Struct("PPPPiiiiii
 
 
 def _heads(name: str, t, shape, dtype) -> bytes:
-    """kp_heads of a [B, H, S, D] or (three sizes in `shape`) [T, H, D] tensor."""
+    """kp_heads of a [B, H, S, D] or [T, H, D] tensor of a shape (None: its own is the one that counts)."""
     if not t.is_cuda:
         raise ValueError("libkperf takes device memory: tensor must be on the GPU")
-    if t.dtype is not dtype or t.shape != shape:
-        raise ValueError(f"{name} must be {list(shape)} of {dtype}, not {list(t.shape)} of {t.dtype}")
+    if t.dtype is not dtype or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} must be {'' if shape is None else str(list(shape)) + ' '}of {dtype}, not {list(t.shape)} of {t.dtype}")
     st = t.stride()
     if st[-1] != 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
@@ -687,37 +687,43 @@ def _norms(q_weight, k_weight, D, dtype):
 
 
 def _two(q, k):
-    """Of queries and keys, either of which may be None: number of sequences (None: [T, H, D]), heads, tokens, D and type."""
+    """Of queries and keys, either of which may be None: number of sequences (None: [T, H, D]), both shapes, heads, tokens, D and
+    type."""
     some = k if q is None else q
     if some is None:
         raise ValueError("queries or keys are needed")
     shape = some.shape
-    B = shape[0] if len(shape) == 4 else None
-    S, D = (shape[0], shape[2]) if B is None else (shape[2], shape[3])
-    if q is None or k is None:
-        return B, 0 if q is None else shape[1], 0 if k is None else shape[1], S, D, some.dtype
+    if len(shape) == 4:
+        B, H, S, D = shape
+    else:
+        S, H, D = shape
+        B = None
+    if q is None:
+        return B, None, shape, 0, H, S, D, some.dtype
+    if k is None:
+        return B, shape, None, H, 0, S, D, some.dtype
     other = k.shape
     if len(other) != len(shape) or other[0] != shape[0] or other[2:] != shape[2:]:
         raise ValueError(f"keys must have the queries' sequences, tokens and D, not {list(other)} to {list(shape)}")
-    return B, shape[1], other[1], S, D, some.dtype
+    return B, shape, other, H, other[1], S, D, some.dtype
 
 
 def kp_norm_rotate(q, k, q_weight, k_weight, eps: float, positions, freq, axis, adjacent: bool, q_out, k_out, stream=None) -> None:
     """Heads of q and k ([B, H, S, D], or [T, H, D] where there is no batch) normed by their root mean square with weights [D]
     (None: not normed), their pairs turned by position * freq[pair]; freq float32 [pairs] (None: not turned), axis uint8
     [pairs] or None.  q and q_out, or k and k_out, may be None; outputs may be the inputs."""
-    B, Hq, Hk, S, D, dtype = _two(q, k)
+    B, qs, ks, Hq, Hk, S, D, dtype = _two(q, k)
     qw, kw, kind = _norms(q_weight, k_weight, D, dtype)
     _check(lib().kp_norm_rotate(
-        None if q is None else _heads("q", q, q.shape, dtype), None if k is None else _heads("k", k, k.shape, dtype), qw, kw, kind, eps,
-        _turns(positions, freq, axis, adjacent, B, S), None if q is None else _heads("q_out", q_out, q.shape, dtype),
-        None if k is None else _heads("k_out", k_out, k.shape, dtype), 1 if B is None else B, Hq, Hk, S, D, _names[dtype],
+        None if q is None else _heads("q", q, None, dtype), None if k is None else _heads("k", k, None, dtype), qw, kw, kind, eps,
+        _turns(positions, freq, axis, adjacent, B, S), None if q is None else _heads("q_out", q_out, qs, dtype),
+        None if k is None else _heads("k_out", k_out, ks, dtype), 1 if B is None else B, Hq, Hk, S, D, _names[dtype],
         _stream_at(stream, k if q is None else q)))
 
 
 def kp_norm_rotate_grad_bytes(q, k) -> int:
     """Bytes of workspace that kp_norm_rotate_grad takes for q and k (either may be None)."""
-    B, Hq, Hk, S, D, _ = _two(q, k)
+    B, _, _, Hq, Hk, S, D, _ = _two(q, k)
     return int(lib().kp_norm_rotate_grad_bytes(1 if B is None else B, Hq, Hk, S, D))
 
 
@@ -725,14 +731,14 @@ def kp_norm_rotate_grad(q, k, q_weight, k_weight, eps: float, positions, freq, a
                         dq_weight=None, dk_weight=None, workspace=None, stream=None) -> None:
     """Gradient of kp_norm_rotate: dq, dk from d_q_out, d_k_out and the q, k that were normed (not looked at without weights), and
     dq_weight, dk_weight [D] float32 where there are weights."""
-    B, Hq, Hk, S, D, dtype = _two(d_q_out, d_k_out)
+    B, qs, ks, Hq, Hk, S, D, dtype = _two(d_q_out, d_k_out)
     qw, kw, kind = _norms(q_weight, k_weight, D, dtype)
     f32 = _names["float32"]
     ws, n = _workspace(workspace)
-    some = lambda name, t, like: None if like is None else _heads(name, t, like.shape, dtype)  # noqa: E731
+    some = lambda name, t, shape: None if shape is None else _heads(name, t, shape, dtype)  # noqa: E731
     _check(lib().kp_norm_rotate_grad(
-        some("q", q, d_q_out if qw else None), some("k", k, d_k_out if kw else None), qw, kw, kind, eps, _turns(positions, freq, axis, adjacent, B, S),
-        some("d_q_out", d_q_out, d_q_out), some("d_k_out", d_k_out, d_k_out), some("dq", dq, d_q_out), some("dk", dk, d_k_out),
+        some("q", q, qs if qw else None), some("k", k, ks if kw else None), qw, kw, kind, eps, _turns(positions, freq, axis, adjacent, B, S),
+        some("d_q_out", d_q_out, qs), some("d_k_out", d_k_out, ks), some("dq", dq, qs), some("dk", dk, ks),
         _flat("dq_weight", dq_weight, f32, (D,)) if qw else 0, _flat("dk_weight", dk_weight, f32, (D,)) if kw else 0,
         1 if B is None else B, Hq, Hk, S, D, _names[dtype], ws, n, _stream_at(stream, d_k_out if d_q_out is None else d_q_out)))
 

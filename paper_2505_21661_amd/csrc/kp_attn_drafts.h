@@ -85,13 +85,14 @@ __global__ __launch_bounds__(kThreads, 2) void kp_attn_drafts(Args g) {
     pages[1] = src.table[(key + 16u < last ? key + 16u : last) >> src.page_log2];
   };
   // The block that is requested: its first key, which of its keys' pages there are, and of either half the cache's row and which of
-  // 16 keys are read (what lies in front of the window or behind the last key is not: those of the other half or of the border are
-  // taken in its place).
+  // 16 keys are read (what lies between the sinks and the window or behind the last key is not: those of the other half or of the
+  // border are taken in its place).
   uint32_t next_key = 0, next_valid = 0, half_row[2], half_first[2], half_last[2];
   auto locate = [&](uint32_t t) __attribute__((always_inline)) {
     const uint32_t l = (t - t_first) / 4u;
     if ((l & 63u) == 0u) load_pages(t);
-    const uint32_t key = next_key = 32u * block_of(t), left = span.end - 1u - key, last = left < 31u ? left : 31u;
+    const uint32_t key = next_key = 32u * block_of(t), end = t < sink_blocks && span.lo > key + 31u ? span.sink_end : span.end;
+    const uint32_t left = end - 1u - key, last = left < 31u ? left : 31u;
     const int32_t ahead = (int32_t)span.lo - (int32_t)key;  // keys in front of the window
     const uint32_t first = t >= sink_blocks && ahead > 0 ? (uint32_t)ahead : 0u;
     next_valid = 0u;

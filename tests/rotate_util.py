@@ -1,8 +1,8 @@
 """Normed and turned heads by their definition in 64 bits, and the error that fp32 arithmetic and one rounding allow.
 
 Counted in roundings of fp32, e = 2^-24: the sum of D squares is 8 multiply-adds in a lane, 4 additions of lanes and one of eps,
-half of which the root leaves (6.5 e), the reciprocal root itself 2 e; x r w another 2 e; a cosine or sine 3 e (its argument, up to
-pi / 4, is rounded once; the series ends below e / 8; two roundings near 1); the multiply-add of a pair 1 e.  16 e = 2^-20 of the
+half of which the root leaves (6.5 e), the reciprocal root itself 2 e; x r w another 2 e; a cosine or sine 4 e (its argument, up to
+pi / 4, goes through three roundings, 2 e; the series ends below e / 8; two roundings near 1); the multiply-add of a pair 1 e.  16 e = 2^-20 of the
 magnitudes of both values of a pair covers a forward value.  Angles: positions times frequencies in doubles, three roundings
 of 2^-53 here and there: 2^-51 of the angle.
 """

@@ -412,3 +412,24 @@ def test_strides_and_tables_of_other_widths(kp):
     kp.kp_attn_tree(q, *case.halves, *case.exps, wide, *case.args[1:], out, sums, 0, 0, case.scale, torch.empty(max(16, n), dtype=torch.uint8, device="cuda"))
     case.o = out
     case.check(out, torch.where(torch.arange(T + 3, device="cuda") < T, sums, 7.0))
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("sinks", [0, 5, 20, 40])
+@pytest.mark.parametrize("n_q", [[6, 9], [80, 60]])
+def test_pages_between_sinks_and_window_are_gone(kp, n_q, sinks, e4m3):
+    """A server that frees what a window has left behind: the table names no page there, and the first rows of the cache are NaN."""
+    window, page, d = 100, 16, 64
+    case = Case(23, n_q, [700, 433], 4, 2, d, page, torch.bfloat16, e4m3, window, sinks)
+    for s in range(2):
+        c = case.n_k[s] - n_q[s]
+        lo = c - window + 1
+        case.table[s, -(-sinks // page) : lo // page] = -1
+    named = set(case.table[case.table >= 0].tolist())
+    for half, value in zip(case.halves, case.values):
+        for at in range(half.shape[0]):
+            if at not in named:
+                half[at] = torch.tensor(math.nan).to(half.dtype)
+                value[at] = 0.0
+    o, lse = case.run(kp)
+    case.check(o, lse)
