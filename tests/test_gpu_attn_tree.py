@@ -433,3 +433,30 @@ def test_pages_between_sinks_and_window_are_gone(kp, n_q, sinks, e4m3):
                 value[at] = 0.0
     o, lse = case.run(kp)
     case.check(o, lse)
+
+
+@pytest.mark.parametrize("n_q", [[5, 3], [24, 9], [100, 130]])
+def test_queries_that_are_not_finite_are_their_own_business(kp, n_q):
+    case = Case(25, n_q, [300, 1700], 4, 2, 64, 16, torch.bfloat16, False, 0, 0)
+    o, lse = case.run(kp)
+    bad = [(0, 1, math.nan), (1, 3, math.inf), (n_q[0], 0, -math.inf), (n_q[0] + n_q[1] - 1, 2, math.nan)]
+    clean = torch.ones(o.shape[:2], dtype=torch.bool, device="cuda")
+    for token, head, value in bad:
+        case.q[token, head, 7] = value
+        clean[token, head] = False
+    again, sums = case.run(kp)
+    assert torch.equal(again[clean], o[clean]) and torch.equal(sums.t()[clean], lse.t()[clean])
+    assert bool(torch.isnan(again[0, 1]).all()) and bool(torch.isnan(again[n_q[0] + n_q[1] - 1, 2]).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n_q", [[5, 3], [24, 9], [100, 130]])
+def test_scores_that_are_large(kp, n_q, dtype):
+    """Scores that fp32 holds exactly and that differ by 2^23 or not at all: the average over the largest ones' values."""
+    case = Case(27, n_q, [300, 1700], 4, 2, 64, 16, dtype, False, 0, 0)
+    case.scale = 1.0
+    whole = lambda x, by: torch.randint(-2, 3, x.shape, device="cuda", generator=case.gen).to(dtype) * by  # noqa: E731
+    case.q.copy_(whole(case.q, 2.0 ** 13))
+    case.halves[0].copy_(whole(case.halves[0], 2.0 ** 10))
+    case.values[0] = case.halves[0].double()
+    case.check(*case.run(kp))

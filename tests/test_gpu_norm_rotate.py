@@ -346,3 +346,22 @@ def test_a_tensor_of_another_place_or_form_is_refused(kp):
             kp.kp_norm_rotate(**{**good, **bad})
     with pytest.raises(kp.KperfError):
         kp.kp_norm_rotate(**{**good, "freq": torch.ones(40, device="cuda")})
+
+
+@pytest.mark.parametrize("normed", ["q", "k"])
+def test_one_of_the_two_is_normed(kp, normed):
+    gen, q, k, w, at, freq, _ = inputs(29, "bshd", 2, 6, 2, 90, 64, torch.bfloat16, 32, 1, "same")
+    weights = (w[0], None) if normed == "q" else (None, w[1])
+    out = [torch.empty_like(q), torch.empty_like(k)]
+    kp.kp_norm_rotate(q, k, *weights, EPS, at, freq, None, False, *out)
+    dy, dx = heads(gen, "bshd", 2, (6, 2), 90, 64, torch.bfloat16), [torch.empty_like(q), torch.empty_like(k)]
+    dw = [None if x is None else torch.empty(64, device="cuda") for x in weights]
+    kp.kp_norm_rotate_grad(q if normed == "q" else None, k if normed == "k" else None, *weights, EPS, at, freq, None, False, *dy, *dx, *dw,
+                           torch.empty(kp.kp_norm_rotate_grad_bytes(q, k), dtype=torch.uint8, device="cuda"))
+    theta = ref.angles(at, freq, None, 2, 90)
+    for x, weight, got, d_out, d_x, d_w in zip((q, k), weights, out, dy, dx, dw):
+        assert_within(got, *ref.forward(x, weight, EPS, theta, False))
+        want, bound, want_w, bound_w = ref.gradient(x, weight, EPS, theta, False, d_out)
+        assert_within(d_x, want, bound)
+        if weight is not None:
+            assert_within(d_w, want_w, bound_w)
