@@ -571,7 +571,7 @@ kp_status kp_attn_paged_launch_shape(int T, int n_seqs, int Hq, int Hkv, int D, 
  *   them, as a rule; bits from n_q on mean nothing, words that there are not, nothing),
  *   and of the keys j < c, the context, those with window == 0 or p - j < window or j < sinks, where p = c + depth_i and depth [T]
  *   (device) says how many drafted tokens it follows (below 0: 0; NULL: 0 for all).  A window does not hide drafted keys.
- * words from 0 to 2^24; seen may be NULL with words = 0.  workspace: as for kp_attn_paged; recording, too (up to 64 rows of a sequence on
+ * words from 0 to 2^24; seen may be NULL with words = 0.  workspace: as for kp_attn_paged (cache_type: of the cache); recording, too (up to 64 rows of a sequence on
  * average per block of 32 keys, with sites that wait for their sample: some 200 cycles of each region).
  */
 size_t kp_attn_tree_bytes(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int cache_type, int window, int sinks);
