@@ -134,8 +134,8 @@ struct Turn {
   }
 };
 
-// 1 / sqrt(mean x^2 + eps) of a row.  Squares of bf16 may pass the range of fp32: such a row is taken 2^-96 as large, which eps
-// does not show in; x becomes x times the factor.
+// 1 / sqrt(mean x^2 + eps) of a row.  Squares of bf16 may pass the range of fp32: such a row is taken 2^-96 as large, and eps 2^-192;
+// x becomes x times the factor.
 template <class T, int D>
 __device__ __forceinline__ float norm_of(float (&x)[8], float eps, float* factor) {
   float ss = 0.f;
@@ -151,7 +151,7 @@ __device__ __forceinline__ float norm_of(float (&x)[8], float eps, float* factor
 #pragma unroll
       for (int e = 0; e < 8; ++e) { x[e] *= by; small = __builtin_fmaf(x[e], x[e], small); }
       small = row_sum<D>(small);
-      if (far) { ss = small; eps = 0.f; *factor = by; }
+      if (far) { ss = small; eps = eps * 0x1p-96f * 0x1p-96f; *factor = by; }  // (one factor of 2^-192 would be 0)
     }
   }
   return __builtin_amdgcn_rsqf(__builtin_fmaf(ss, 1.0f / D, eps));

@@ -365,3 +365,23 @@ def test_one_of_the_two_is_normed(kp, normed):
         assert_within(d_x, want, bound)
         if weight is not None:
             assert_within(d_w, want_w, bound_w)
+
+
+@pytest.mark.parametrize("eps", [2.0 ** 70, 2.0 ** 86, 2.0 ** 99])
+@pytest.mark.parametrize("d", [64, 128])
+def test_eps_counts_beside_rows_of_any_size(kp, d, eps):
+    """bf16 rows from 2^40 to 2^120: their squares are of eps's size, far below it, and past the range of fp32."""
+    b, h, s, pairs, dtype = 1, 2, 81, 32, torch.bfloat16
+    gen, q, _, (w, _), at, freq, _ = inputs(31, "bhsd", b, h, 1, s, d, dtype, pairs, 1, "fp32")
+    q = (torch.randn(b, h, s, d, device="cuda", generator=gen) * torch.exp2(40.0 + torch.arange(s, device="cuda"))[:, None]).to(dtype)
+    theta = ref.angles(at, freq, None, b, s)
+    out = torch.empty_like(q)
+    kp.kp_norm_rotate(q, None, w, None, eps, at, freq, None, False, out, None)
+    assert_within(out, *ref.forward(q, w, eps, theta, False))
+    dy = torch.randn(q.shape, device="cuda", generator=gen).to(dtype)
+    dq, dw = torch.empty_like(q), torch.empty(d, device="cuda")
+    kp.kp_norm_rotate_grad(q, None, w, None, eps, at, freq, None, False, dy, None, dq, None, dw, None,
+                           torch.empty(kp.kp_norm_rotate_grad_bytes(q, None), dtype=torch.uint8, device="cuda"))
+    want, bound, want_w, bound_w = ref.gradient(q, w, eps, theta, False, dy)
+    assert_within(dq, want, bound)
+    assert_within(dw, want_w, bound_w)
