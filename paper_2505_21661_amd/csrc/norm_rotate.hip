@@ -95,32 +95,44 @@ __device__ __forceinline__ void weights_of(const void* weight, bool fp32, uint32
   }
 }
 
+// The sine of a value that is not turned, being in no pair or in one whose axis is not there: one that no angle gives (they are 0 or 2^-30 and
+// more).  Nothing of a partner may come to such a value, which an infinity or a NaN does through any factor.
+constexpr float kStays = 0x1p-149f;
+
 // What a lane needs for its values 8 c .. 8 c + 7 of a row, and how it meets their partners.
 template <bool ADJACENT>
 struct Turn {
   bool turned;    // its values belong to pairs
   bool lower;     // (not ADJACENT) they are the first of their pairs
   uint32_t far;   // (not ADJACENT) lanes from one half of the pairs to the other
+  bool some_stay; // a lane of the wave has a pair that is not turned
   float cos[8], sin[8];
 
   __device__ __forceinline__ Turn(const RotateArgs& g, uint32_t c) : turned(8u * c < 2u * g.pairs), lower(8u * c < g.pairs), far(g.pairs / 8u) {}
   __device__ __forceinline__ uint32_t partner_of(uint32_t x) const { return ADJACENT || !turned ? x : (lower ? x + far : x - far); }
   __device__ __forceinline__ void angles(const RotateArgs& g, uint32_t c, uint32_t seq, uint32_t token) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) { cos[e] = 1.f; sin[e] = 0.f; }
-    if (!turned) return;
+    for (int e = 0; e < 8; ++e) { cos[e] = 1.f; sin[e] = ADJACENT && !(e & 1) ? -kStays : kStays; }
+    bool stays = false;
+    if (turned) stays = pairs_of(g, c, seq, token);
+    some_stay = __builtin_amdgcn_ballot_w64(stays) != 0ull;
+  }
+  __device__ __forceinline__ bool pairs_of(const RotateArgs& g, uint32_t c, uint32_t seq, uint32_t token) {
+    bool stays = false;
     const uint32_t first = ADJACENT ? 4u * c : (lower ? 8u * c : 8u * c - g.pairs);
     const int32_t* at = g.at + g.seq_step * (int64_t)seq + token;
 #pragma unroll
     for (int i = 0; i < (ADJACENT ? 4 : 8); ++i) {
       const uint32_t axis = g.axis ? g.axis[first + i] : 0u;
-      float co = 1.f, si = 0.f;
-      if (axis < g.axes) turn_of(at[g.axis_step * (int64_t)axis], (double)g.freq[first + i] * 0.15915494309189535, &co, &si);
+      if (axis >= g.axes) { stays = true; continue; }
+      float co, si;
+      turn_of(at[g.axis_step * (int64_t)axis], (double)g.freq[first + i] * 0.15915494309189535, &co, &si);
       if constexpr (ADJACENT) { cos[2 * i] = cos[2 * i + 1] = co; sin[2 * i] = -si; sin[2 * i + 1] = si; }
       else { cos[i] = co; sin[i] = lower ? -si : si; }
     }
+    return stays;
   }
-  // The partners of a row's values, in the type; 0 where a value is in no pair.  y_e = u_e cos + u_partner sin.
+  // The partners of a row's values, in the type; 0 where a value stays.  y_e = u_e cos + u_partner sin.
   __device__ __forceinline__ u32x4 partners(const u32x4& raw) const {
     u32x4 other;
 #pragma unroll
@@ -129,6 +141,14 @@ struct Turn {
       if constexpr (ADJACENT) x = raw[w] << 16 | raw[w] >> 16;
       else x = (uint32_t)__shfl((int)raw[w], (int)partner_of(threadIdx.x & 63u), 64);
       other[w] = turned ? x : 0u;
+    }
+    if (some_stay) {
+#pragma unroll
+      for (int e = ADJACENT ? 1 : 0; e < 8; e += ADJACENT ? 2 : 1) {
+        float s = sin[e];
+        asm volatile("" : "+v"(s));  // (compared here, not ahead of the loop over heads: there are no registers to keep it in)
+        other[e >> 1] &= s != kStays ? ~0u : ADJACENT ? 0u : e & 1 ? 0xFFFFu : 0xFFFF0000u;
+      }
     }
     return other;
   }
@@ -228,7 +248,7 @@ __global__ __launch_bounds__(kThreads) void kp_norm_rotate_rows(RotateArgs g) {
 #pragma unroll
           for (int e = 0; e < 8; e += 2) { const float x = b[e]; b[e] = b[e + 1]; b[e + 1] = x; }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { a[e] *= turn.cos[e]; b[e] *= turn.sin[e]; }
+        for (int e = 0; e < 8; ++e) { a[e] *= turn.cos[e]; b[e] = __builtin_fabsf(turn.sin[e]) == kStays ? -0.f : b[e] * turn.sin[e]; }  // (-0: what it is added to keeps its sign)
       }
       u32x4 raw[kAtOnce];
       over_heads<kAtOnce>(

@@ -385,3 +385,47 @@ def test_eps_counts_beside_rows_of_any_size(kp, d, eps):
     want, bound, want_w, bound_w = ref.gradient(q, w, eps, theta, False, dy)
     assert_within(dq, want, bound)
     assert_within(dw, want_w, bound_w)
+
+
+@pytest.mark.parametrize("weight", ["none", "fp32"])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("d,pairs", [(64, 32), (128, 24)])
+def test_what_is_not_turned_stays(kp, d, pairs, adjacent, weight):
+    """Pairs whose axis is not there and values in no pair, next to infinities and NaN in their partners and in the weights."""
+    b, h, s, dtype = 1, 2, 9, torch.bfloat16
+    gen, q, _, (w, _), at, freq, _ = inputs(33, "bhsd", b, h, 1, s, d, dtype, pairs, 1, weight)
+    axis = torch.zeros(pairs, dtype=torch.uint8, device="cuda")
+    axis[3], axis[pairs - 1] = 1, 255
+    pair_of = lambda m: (2 * m, 2 * m + 1) if adjacent else (m, pairs + m)  # noqa: E731
+    alone = [n for m in (3, pairs - 1) for n in pair_of(m)] + list(range(2 * pairs, d))
+    dy = torch.randn(b, h, s, d, device="cuda", generator=gen).to(dtype)
+    if w is None:  # (a row that is normed has no finite value beside a NaN)
+        for x in (q, dy):
+            x[0, 0, 0, pair_of(3)[0]], x[0, 0, 1, pair_of(3)[1]], x[0, 1, 2, pair_of(pairs - 1)[0]] = math.inf, math.nan, -math.inf
+            x[0, 1, 3, pair_of(pairs - 1)[1]] = -0.0
+    else:
+        w[pair_of(3)[0]], w[pair_of(pairs - 1)[1]] = math.inf, -math.inf
+        if 2 * pairs < d:
+            w[2 * pairs + 1] = math.inf
+    x64 = q.double()
+    u = x64 if w is None else x64 / torch.sqrt(x64.square().mean(-1, keepdim=True) + EPS) * w.double()
+    out = torch.empty_like(q)
+    kp.kp_norm_rotate(q, None, w, None, EPS, at, freq, axis, adjacent, out, None)
+    got, want = out[..., alone].double(), u[..., alone]
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+    if w is None:
+        assert torch.equal(got.nan_to_num(), want.nan_to_num()) and torch.equal(torch.signbit(got), torch.signbit(want))
+        dq = torch.empty_like(q)
+        kp.kp_norm_rotate_grad(None, None, None, None, EPS, at, freq, axis, adjacent, dy, None, dq, None)
+        assert torch.equal(dq[..., alone].nan_to_num(), dy[..., alone].nan_to_num()) and torch.equal(torch.isnan(dq[..., alone]), torch.isnan(dy[..., alone]))
+        return
+    finite = torch.isfinite(want)
+    bound = (ref.half_step(dtype) + 2.0 ** -20) * want.abs() + ref.least(dtype)
+    assert_within(got[finite], want[finite], bound[finite])
+    # a gradient that is infinite at one value of such a pair stays in that column of the weights' gradient
+    bad = pair_of(3)[1]
+    dy[0, 0, 4, bad] = math.inf
+    dq, dw = torch.empty_like(q), torch.empty(d, device="cuda")
+    kp.kp_norm_rotate_grad(q, None, w, None, EPS, at, freq, axis, adjacent, dy, None, dq, None, dw, None,
+                           torch.empty(kp.kp_norm_rotate_grad_bytes(q, None), dtype=torch.uint8, device="cuda"))
+    assert [n for n in range(d) if not math.isfinite(dw[n])] == [bad]
