@@ -631,7 +631,7 @@ def kp_attn_tree(q, k_cache, v_cache, k_exp, v_exp, block_table, lens, starts, s
                  scale: float, workspace=None, region_mask: int = 0, trace_buf=None, trace_cap: int = 0, stream=None) -> None:
     """Attention of drafted tokens q [T, Hq, D] over a cache that holds them as the last of each sequence's keys: as kp_attn_paged, but
     that a token sees the drafted ones that its bits seen [T, words] int64 name (bit j % 64 of word j / 64: drafted token j of its
-    sequence), and the context from position lens - drafted + depth; depth [T] int32 or None."""
+    sequence; None: none), and the context from position lens - drafted + depth; depth [T] int32 or None."""
     T, Hq, D = q.shape
     n, width = block_table.shape
     if D != k_cache.shape[3]:
@@ -639,10 +639,10 @@ def kp_attn_tree(q, k_cache, v_cache, k_exp, v_exp, block_table, lens, starts, s
     names = _names or _types()
     i32 = names["int32"]
     ws, nbytes = _workspace(workspace)
-    words = seen.shape[1]
+    words = 0 if seen is None else seen.shape[1]
     _check(lib().kp_attn_tree(
         _heads("q", q, q.shape, q.dtype), _cache_of(k_cache, v_cache, k_exp, v_exp, q.dtype), _flat("block_table", block_table, i32), width,
-        _flat("lens", lens, i32, (n,)), _flat("starts", starts, i32, (n + 1,)), _flat("seen", seen, names["int64"], (T, words)), words,
+        _flat("lens", lens, i32, (n,)), _flat("starts", starts, i32, (n + 1,)), 0 if seen is None else _flat("seen", seen, names["int64"], (T, words)), words,
         0 if depth is None else _flat("depth", depth, i32, (T,)), _heads("o", o, q.shape, q.dtype),
         0 if lse is None else _flat("lse", lse, names["float32"], (Hq, T)), T, n, Hq, window, sinks, scale, ws, nbytes,
         region_mask & 0xFFFFFFFF, _ptr(trace_buf), trace_cap, _stream_at(stream, q)))

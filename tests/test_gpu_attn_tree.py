@@ -460,3 +460,14 @@ def test_scores_that_are_large(kp, n_q, dtype):
     case.halves[0].copy_(whole(case.halves[0], 2.0 ** 10))
     case.values[0] = case.halves[0].double()
     case.check(*case.run(kp))
+
+
+def test_without_bits(kp):
+    """No words: the context alone, with seen [T, 0] and without it."""
+    case = Case(35, [10, 40], [300, 80], 4, 2, 64, 16, torch.bfloat16, False, 0, 0, words=0)
+    o, lse = case.run(kp)
+    case.check(o, lse)
+    case.args[3] = None
+    again, sums = torch.full_like(o, 7.0), torch.full_like(lse, 7.0)
+    kp.kp_attn_tree(case.q, *case.halves, *case.exps, *case.args, again, sums, 0, 0, case.scale, case.workspace)
+    assert torch.equal(again, o) and torch.equal(sums, lse)
