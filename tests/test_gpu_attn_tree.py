@@ -471,3 +471,28 @@ def test_without_bits(kp):
     again, sums = torch.full_like(o, 7.0), torch.full_like(lse, 7.0)
     kp.kp_attn_tree(case.q, *case.halves, *case.exps, *case.args, again, sums, 0, 0, case.scale, case.workspace)
     assert torch.equal(again, o) and torch.equal(sums, lse)
+
+
+@pytest.mark.parametrize("n_q", [[6, 3], [150, 120]])
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_every_form_can_be_recorded(kp, d, dtype, e4m3, n_q):
+    """Both kernels, in each type, size and form of the cache: results that recording does not change, on either clock, and a trace whose
+    pairs are whole and in order, as many of each region."""
+    case = Case(37, n_q, [2500, 700], 4, 2, d, 32, dtype, e4m3, 1500, 3)
+    o, lse = case.run(kp)
+    n_wg, waves, regions = kp.kp_attn_tree_launch_shape(case.q, case.halves[0], case.args[0], 1500, 3)
+    counts = []
+    for mask in (0b111, 0b111 | kp.KP_MASK_REALTIME, 0b111 | kp.KP_MASK_WAVE_GROUP):
+        cap, streams = 512, waves if not mask & kp.KP_MASK_WAVE_GROUP else 1
+        trace = torch.zeros(kp.kp_trace_bytes(n_wg, streams, cap), dtype=torch.uint8, device="cuda")
+        again, sums = case.run(kp, record=(mask, trace, cap))
+        assert torch.equal(again, o) and torch.equal(sums, lse)
+        stats = torch.zeros(kp.kp_stats_bytes(n_wg, streams, regions), dtype=torch.uint8, device="cuda")
+        kp.kp_trace_reduce(trace, n_wg * cap, stats)
+        st = kp.parse_stats(stats)
+        assert st["n_invalid"] == 0 and st["n_disorder"] == 0
+        counts.append([int(st["cnt"][r]) for r in range(3)])
+        assert min(counts[-1]) > 0 and len(set(counts[-1])) == 1
+    assert counts[0] == counts[1]

@@ -429,3 +429,38 @@ def test_what_is_not_turned_stays(kp, d, pairs, adjacent, weight):
     kp.kp_norm_rotate_grad(q, None, w, None, EPS, at, freq, axis, adjacent, dy, None, dq, None, dw, None,
                            torch.empty(kp.kp_norm_rotate_grad_bytes(q, None), dtype=torch.uint8, device="cuda"))
     assert [n for n in range(d) if not math.isfinite(dw[n])] == [bad]
+
+
+@pytest.mark.parametrize("layout,d,hq,hk,s", [("bhsd", 64, 2, 0, 700_000), ("bshd", 128, 4, 2, 180_001), ("bshd", 64, 13, 1, 60_011), ("bshd", 64, 8, 0, 900_000)])
+def test_weights_gradient_of_many_tokens(kp, layout, d, hq, hk, s):
+    """Workgroups that each take many tiles.  768 of them have 256 / (D / 8) rows at a time, so that a thread has at most
+    n = rows / (512 * 256 / (D / 8)) + heads.  Its sum is off by n e of its terms' magnitudes, the sums of a workgroup and of workgroups by 32 + 56 e,
+    a term by 20 e.  With gradients of all tokens that is what the sums' rounding is held to; with those of one token in 1000, which
+    are then a thousandth of the sum each and not a millionth, a tile that is left out or counted twice shows."""
+    gen = torch.Generator(device="cuda").manual_seed(s)
+    dtype, pairs = torch.bfloat16, d // 2
+    n_heads = [n for n in (hq, hk) if n]
+    x, dense = (heads(gen, layout, 1, n_heads, s, d, dtype) for _ in range(2))
+    w = [torch.rand(d, device="cuda", generator=gen) for _ in n_heads]
+    at, freq = torch.arange(s, dtype=torch.int32, device="cuda"), torch.rand(pairs, device="cuda", generator=gen)
+    some = torch.arange(s, device="cuda") % 1000 == 7
+    some[-1] = True
+    pad = lambda v: list(v) + [None] * (2 - len(v))  # noqa: E731
+    thread = s * sum(n_heads) / (512 * 256 / (d // 8)) + max(n_heads)
+    for dy in (dense, [y * some[:, None].to(dtype) for y in dense]):
+        results = []
+        for _ in range(2):
+            dx, dw = [torch.empty_like(y) for y in x], [torch.full((d,), 7.0, device="cuda") for _ in x]
+            workspace = torch.full((kp.kp_norm_rotate_grad_bytes(*pad(x)),), 0xFF, dtype=torch.uint8, device="cuda")
+            kp.kp_norm_rotate_grad(*pad(x), *pad(w), EPS, at, freq, None, False, *pad(dy), *pad(dx), *pad(dw), workspace)
+            results.append(dw)
+        assert all(torch.equal(a, b) for a, b in zip(*results)), "the same inputs, other bits"
+        for n, (y, weight, got, d_out, got_w) in enumerate(zip(x, w, dx, dy, dw)):
+            total, allowed = torch.zeros(2, d, device="cuda", dtype=torch.float64)
+            for a in range(0, s, 40_000):
+                part = slice(a, min(a + 40_000, s))
+                theta = ref.angles(at[part], freq, None, 1, part.stop - a)
+                want, bound, want_w, bound_w = ref.gradient(y[:, :, part], weight, EPS, theta, False, d_out[:, :, part])
+                assert_within(got[:, :, part], want, bound, what=(n, a))
+                total, allowed = total + want_w, allowed + bound_w
+            assert_within(got_w, total, allowed * max(1.0, (thread + 32 + 56 + 20) / 384), what=("weights", n))
