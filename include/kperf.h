@@ -571,8 +571,10 @@ kp_status kp_attn_paged_launch_shape(int T, int n_seqs, int Hq, int Hkv, int D, 
  *   them, as a rule; bits from n_q on mean nothing, words that there are not, nothing),
  *   and of the keys j < c, the context, those with window == 0 or p - j < window or j < sinks, where p = c + depth_i and depth [T]
  *   (device) says how many drafted tokens it follows (below 0: 0; NULL: 0 for all).  A window does not hide drafted keys.
- * words from 0 to 2^24; seen may be NULL with words = 0.  workspace: as for kp_attn_paged (cache_type: of the cache); recording, too (up to 64 rows of a sequence on
- * average per block of 32 keys, with sites that wait for their sample: some 200 cycles of each region).
+ * words from 0 to 2^24; seen may be NULL with words = 0.  workspace: as for kp_attn_paged (cache_type: of the cache).
+ * Recording, too, per tile of 64 keys; or per block of 32, with sites that wait for their sample (some 200 cycles of each region),
+ * where pages have 16 tokens or more and either sequences have up to 64 rows on average (a row: a drafted token and a query head of the
+ * group; 40 in a 16-bit cache), or a row may see fewer than 1536 keys and there is work for no more than 128 workgroups of 128 rows.
  */
 size_t kp_attn_tree_bytes(int T, int n_seqs, int Hq, int Hkv, int D, int table_width, int page, int cache_type, int window, int sinks);
 kp_status kp_attn_tree(const kp_heads* q, const kp_cache* cache, const int32_t* block_table, int table_width, const int32_t* lens,

@@ -7,9 +7,14 @@
 // from memory to the operand registers as it lies and V through 8 KiB of LDS per wave; both are asked for a block ahead.
 // Blocks begin at multiples of 32 keys, and pages hold at least 16 (kp_attn_tile has the others): either half of a block lies in one
 // page, whose place is a scalar, and a load takes no more than the row's number in the half.
-// Per block a wave has 16 MFMAs (512 cycles) and some 240 other instructions (950); two waves to a SIMD take 2000 for both of theirs where they
-// have no others to wait for.  32 sequences of up to 16 tokens of 32/8 heads of 128 over up to 16384 keys of e4m3, 749 MB, take 187 us
-// and 10 for the join (3730 GB/s; 162 with up to 8 tokens, a tile for each, 4490), 3 of up to 7 over 700 keys 9.8, which is latency.
+// The weights that multiply values are rounded to the type, as the matrix instructions take them (those that are summed up are not): the one
+// rounding besides the result's, as in kp_attn_tile.
+// Per block a wave has 16 MFMAs (512 cycles) and some 240 other instructions (950).  64 sequences of one tile of 32 rows each, 32/8 heads of 128,
+// over 16384 keys of e4m3: with pages of their own 390 us, 2.16 GB, which is memory (5550 GB/s; 16 bits 741, 5800), with pages that they
+// share, out of the caches, 207: 1.6 us for a block of each of a SIMD's two waves (16 bits 305, 2.4).  With unequal lengths and more than a tile to a
+// sequence it is neither alone: 32 sequences of up to 16 tokens (1.8 tiles each) over up to 16384 keys of e4m3, 749 MB, take 187 us and
+// 10 for the join (3800 GB/s), of which the 162528 blocks out of the caches would be some 130, and the longest sequences' last
+// workgroups 20 % more than the mean.  3 sequences of up to 7 tokens over 700 keys take 9.8 us, which is latency.
 #pragma once
 #include "kp_attn_rows.h"
 

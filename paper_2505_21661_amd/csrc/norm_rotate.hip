@@ -211,10 +211,13 @@ __device__ __forceinline__ void over_heads(uint32_t first, uint32_t end, uint32_
 }
 
 // Bound by memory.  In sequences of 8192 tokens with 32/8 heads of 128 of bf16 side by side, four of them on three axes, 671 MB take
-// 148 us (4530 GB/s; a copy 5120).  What counts is the order of the rows: neighbouring lanes take those that are neighbours in memory, heads
+// 149.5 us (4490 GB/s; a copy 5120).  What counts is the order of the rows: neighbouring lanes take those that are neighbours in memory, heads
 // of a token here; with tokens in their place, 8 KB apart and so on few of the L2's channels, 173 us.  Eight rows of a thread in
 // flight 148, four 161 (into a cache, whose rows take more registers: four 39.7 us for 12001 tokens, eight 45).  Rows are read past
-// the caches, once: 161 us and 39.7, through them 163 and 44.
+// the caches, once: 161 us and 39.7, through them 163 and 44.  (Compared before pairs without an axis had their mark: 148 then.)
+// 12001 tokens of 16/8 heads of 128 into a cache: in 16 bits 40 to 42 us with neighbours for pairs and 54 with halves, however many are
+// turned, 197 MB; into e4m3 45 to 47 and 60, 172 MB.  Halves take registers for 8 sines and cosines, where neighbours share 4: three
+// workgroups to a compute unit and four rounds of them, four and three with neighbours.
 // WRITE: 0 keys go to a tensor, 1 to a cache in 16 bits, 2 to one of e4m3 codes; so do values then.
 template <class T, int D, bool ADJACENT, int WRITE>
 __global__ __launch_bounds__(kThreads) void kp_norm_rotate_rows(RotateArgs g) {
@@ -277,7 +280,7 @@ __global__ __launch_bounds__(kThreads) void kp_norm_rotate_rows(RotateArgs g) {
   }
 }
 
-// Bound by memory: 8192 tokens of 32/8 heads of 128, 252 MB, take 52 us with the join (4830 GB/s); before the join had eight loads in flight 59, with 512, 1024 and 256
+// Bound by memory: 8192 tokens of 32/8 heads of 128, 252 MB, take 52 us with the join (4810 GB/s; the kernel 48.6 of them); before the join had eight loads in flight 59, with 512, 1024 and 256
 // workgroups instead of 768 67, 74 and 98.
 template <class T, int D, bool ADJACENT>
 __global__ __launch_bounds__(kThreads) void kp_norm_rotate_back(RotateArgs g) {
