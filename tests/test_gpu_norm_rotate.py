@@ -464,3 +464,52 @@ def test_weights_gradient_of_many_tokens(kp, layout, d, hq, hk, s):
                 assert_within(got[:, :, part], want, bound, what=(n, a))
                 total, allowed = total + want_w, allowed + bound_w
             assert_within(got_w, total, allowed * max(1.0, (thread + 32 + 56 + 20) / 384), what=("weights", n))
+
+
+@pytest.mark.parametrize("layout", ["bhsd", "bshd"])
+def test_gradients_over_the_tensors_that_were_normed_and_queries_over_themselves(kp, layout):
+    """dq and dk where q and k are, and q_out of the write into a cache where q is."""
+    b, hq, hkv, s, d, pairs, dtype = 2, 6, 2, 333, 128, 64, torch.bfloat16
+    gen, q, k, w, at, freq, _ = inputs(37, layout, b, hq, hkv, s, d, dtype, pairs, 1, "fp32")
+    dy = heads(gen, layout, b, (hq, hkv), s, d, dtype)
+    results = []
+    for over in (False, True):
+        x = [t.clone(memory_format=torch.preserve_format) for t in (q, k)]
+        dx = x if over else [torch.empty_like(t) for t in x]
+        dw = [torch.empty(d, device="cuda") for _ in range(2)]
+        kp.kp_norm_rotate_grad(*x, *w, EPS, at, freq, None, False, *dy, *dx, *dw, torch.empty(kp.kp_norm_rotate_grad_bytes(*x), dtype=torch.uint8, device="cuda"))
+        results.append(dx + dw)
+    assert all(torch.equal(x, y) for x, y in zip(*results))
+    flat = [t[0].transpose(0, 1) for t in (q, k)]
+    slots = torch.randperm(512, device="cuda", generator=gen)[:s]
+    results = []
+    for over in (False, True):
+        halves, exps = new_cache(32, hkv, 16, d, dtype, True)
+        x = flat[0].clone(memory_format=torch.preserve_format)
+        out = x if over else torch.empty_like(x)
+        kp.kp_norm_rotate_write(x, flat[1], flat[1], *w, EPS, at[0, 0], freq, None, False, out, slots, *halves, *exps)
+        results.append([out] + [t.view(torch.uint8) for t in halves + exps])
+    assert all(torch.equal(x, y) for x, y in zip(*results))
+
+
+def test_two_calls_at_once(kp):
+    """On two streams, each with a workspace of its own: the bits of one after the other."""
+    sets = [inputs(seed, "bshd", 1, 16, 4, 3001, 128, torch.bfloat16, 64, 1, "same") for seed in (41, 43)]
+    dy = [[torch.randn_like(x) for x in s[1:3]] for s in sets]
+    workspaces = [torch.empty(kp.kp_norm_rotate_grad_bytes(*s[1:3]), dtype=torch.uint8, device="cuda") for s in sets]
+
+    def call(n, stream):
+        _, q, k, w, at, freq, _ = sets[n]
+        kp.kp_norm_rotate_grad(q, k, *w, EPS, at, freq, None, False, *dy[n], *results[-1][n][:2], *results[-1][n][2:], workspaces[n], stream=stream)
+
+    results, streams = [], [torch.cuda.Stream() for _ in range(2)]
+    for apart in (True, False):
+        results.append([[torch.empty_like(x) for x in s[1:3]] + [torch.empty(128, device="cuda") for _ in range(2)] for s in sets])
+        for stream in streams:
+            stream.wait_stream(torch.cuda.current_stream())
+        for n in (0, 1, 0, 1):
+            call(n, streams[n])
+            if apart:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for a, b in zip(*results) for x, y in zip(a, b))
